@@ -62,7 +62,8 @@ enum { SAEM_MAX_EXPERTS = 128 };         /* routed experts per layer */
 enum { SAEM_TEMP = -2 };                 /* slot argument of saem_cache_load: take a temporary slot */
 enum { SAEM_HOST_MAPPED = -3 };          /* slot reported by saem_cache_query for an expert bound by saem_cache_map_host */
 enum { SAEM_OUT_F32 = 0, SAEM_OUT_BF16 = 1 };
-enum { SAEM_FFN_AUTO = 0, SAEM_FFN_SCALAR = 1, SAEM_FFN_TENSOR = 2, SAEM_FFN_TENSOR_PAIRS = 3, SAEM_FFN_DECODE_FUSED = 4 };
+enum { SAEM_FFN_AUTO = 0, SAEM_FFN_SCALAR = 1, SAEM_FFN_TENSOR = 2, SAEM_FFN_TENSOR_PAIRS = 3, SAEM_FFN_DECODE_FUSED = 4, SAEM_FFN_MX = 5 };
+enum { SAEM_GATE_NONE = 0, SAEM_GATE_TOKEN = 1, SAEM_GATE_CHANNEL = 2, SAEM_GATE_FULL = 3 };  /* saem_block_norm */
 
 /*
  * Shape of one context.  d_model and d_ff must be multiples of 128, at most 16384; 1 <= top_k <= n_experts <=
@@ -84,6 +85,10 @@ enum { SAEM_FFN_AUTO = 0, SAEM_FFN_SCALAR = 1, SAEM_FFN_TENSOR = 2, SAEM_FFN_TEN
  * saem_moe_step takes its one-launch form (see there) for every batch it supports (up to 8 tokens, top_k
  * up to 8); AUTO takes it up to 4 tokens, and up to 8 on layers whose experts are at most 20 MB
  * (3 * d_model * d_ff * 2 bytes) and numerous enough (see saem_moe_step).
+ * SAEM_FFN_MX: the slots hold experts in the microscaled 4-bit format (see saem_mx_quantize): 3 * d_model * d_ff *
+ * 17/32 bytes per slot instead of 3 * d_model * d_ff * 2, packed by saem_mx_pack_expert (device) or
+ * saem_pack_expert_host (which then quantises); x stays bf16, the hidden activations are fp32 in the workspace.  All step
+ * and cache calls take such a context except saem_cache_map_host (UNSUPPORTED).
  * n_shared (0..16, n_experts + n_shared <= SAEM_MAX_EXPERTS): always-on shared experts of the same
  * width d_ff that run INSIDE the layer's grouped launch.  They are experts n_experts ..
  * n_experts + n_shared - 1 of every layer for the cache calls (outside the routed cache-ratio
@@ -112,7 +117,7 @@ typedef struct saem_config {
 int saem_version(void);
 const char* saem_status_string(int status);
 
-/* Bytes of one packed expert (= one slot): 3 * d_model * d_ff * 2.  0 on an invalid config. */
+/* Bytes of one packed expert (= one slot): 3 * d_model * d_ff * 2 (SAEM_FFN_MX: * 17/32).  0 on an invalid config. */
 size_t saem_slot_bytes(const saem_config* cfg);
 /* Bytes the slot region must have: (n_layers * slots_per_layer + temp_slots) * saem_slot_bytes. */
 size_t saem_slot_region_bytes(const saem_config* cfg);
@@ -138,7 +143,8 @@ void saem_destroy(saem_ctx* ctx);
  * (host memory, saem_slot_bytes): tiles of 128 weight rows x 64 reduction elements, each tile
  * 16 KB with its 16-byte chunks XOR-swizzled by (row mod 8) so that a tile can be bulk-copied
  * into shared memory and fed to the tensor cores as is; gate and up tiles of the same position
- * are adjacent.  A slot's content is opaque to the caller.
+ * are adjacent.  A slot's content is opaque to the caller.  With SAEM_FFN_MX the matrices are quantised to the microscaled
+ * 4-bit format on the way (the same codes and scales as saem_mx_quantize).
  */
 int saem_pack_expert_host(const saem_config* cfg, const void* gate, const void* up, const void* down,
                           void* packed_out);
@@ -255,7 +261,7 @@ int saem_moe_step_host_async(saem_ctx* ctx, saem_ctx* shared_ctx, int layer, con
 void* saem_step_buffer(saem_ctx* ctx, int which);
 
 /*
- * Expert cache.  saem_cache_load copies one packed expert (pinned host, saem_slot_bytes) into a
+ * Expert cache.  saem_cache_load copies one packed expert (pinned host or device memory, saem_slot_bytes) into a
  * slot with cudaMemcpyAsync on copy_stream and records a completion event; the residency map
  * changes at once on the host.  slot: 0..slots_per_layer-1 of `layer`, which must be empty
  * (SLOT_BUSY otherwise: evict first), or SAEM_TEMP: take the next temporary slot round-robin,
@@ -315,6 +321,77 @@ int saem_cache_wait(saem_ctx* ctx, int layer, int expert, void* consumer_stream)
 enum { SAEM_STATIC_SCRATCH_ELEMS = 1 << 20 };
 int saem_expert_ffn_static(const void* x_packed, const int32_t* offsets, int n_experts, int max_rows,
                            int d_model, int d_ff, const void* packed_experts, float* y_packed, void* stream);
+
+/*
+ * Microscaled 4-bit matrices (no counterpart in the paper: it fits more experts into the same region).
+ *
+ * Format: 32 consecutive elements of a row are a block with one scale 2^(s - 127) (a byte; 255: the block is NaN);
+ * elements are E2M1 codes (sign, then 0 .5 1 1.5 2 3 4 6), element 2i of a row in the low half of byte i.
+ *   codes  [rows][ceil(cols / 32) * 16] bytes, the last block padded with zeros        (saem_mx_codes_bytes)
+ *   scales [ceil(rows / 128)][ceil(cols / 128)][512] bytes: the scales of blocks 4c .. 4c + 3 of row r are the four
+ *          bytes at piece (r / 128, c), offset (r % 32) * 16 + (r / 32 % 4) * 4        (saem_mx_scales_bytes)
+ * Both must be 16-byte aligned.  The scales of rows beyond the last in a piece are unspecified.  The size queries return
+ * 0 for sizes that are not supported (rows < 0, cols < 1, more than 2^31 - 1 pieces of a row's 256 elements).
+ *
+ * saem_mx_quantize: s = max(floor(log2 max|x|) - 2, -127) + 127 and the code nearest to x * 2^-(s - 127), ties to the even
+ * mantissa, saturated at 6; a block with a NaN or an infinity gets s = 255.  x[rows, cols] fp32 or bf16 (dtype: SAEM_OUT_*),
+ * row r at r * row_stride elements, aligned to its elements (16-byte aligned rows and cols % 8 == 0 are faster).
+ * saem_mx_dequantize: the values back, out[rows, cols] fp32 or bf16 (both exact).
+ *
+ * saem_mx_matmul: out[m, n] = sum_k A[m, k] * W[n, k] of two such matrices (row r of out at r * out_stride), block-scaled
+ * tensor cores, fp32 sums, out fp32 or bf16.  Two runs give the same bits.  status (dev int32, may be NULL) becomes
+ * SAEM_ERR_TIMEOUT if a bounded device wait ran out.
+ * saem_mx_linear: the same with A quantised from x[m, k] (fp32 or bf16) on the way.  workspace (dev, 256-byte aligned, at
+ * least saem_mx_linear_workspace_bytes(m, k)): its first 4 bytes are the status word (zero them once), the rest is
+ * overwritten by every call; calls that share it must be ordered.
+ * Limits of both: m <= 2^23, n <= 2^22, k <= 2^24.  m == 0 is a no-op.
+ *
+ * saem_mx_pack_expert: one expert's gate[d_ff, d_model], up[d_ff, d_model], down[d_model, d_ff], quantised, to the slot
+ * layout of a SAEM_FFN_MX context (all dev, 16-byte aligned; packed_out: saem_slot_bytes(cfg)).  The result may be loaded
+ * with saem_cache_load, from device memory or through pinned host memory.
+ * Errors of all: INVALID_ARG (null, dtype), SHAPE, ALIGNMENT, WORKSPACE, UNSUPPORTED (pack for another ffn_path), CUDA.
+ */
+size_t saem_mx_codes_bytes(int64_t rows, int64_t cols);
+size_t saem_mx_scales_bytes(int64_t rows, int64_t cols);
+int saem_mx_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride, void* codes, void* scales,
+                     void* stream);
+int saem_mx_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* out, int dtype,
+                       int64_t row_stride, void* stream);
+int saem_mx_matmul(const void* a_codes, const void* a_scales, int64_t m, const void* w_codes, const void* w_scales,
+                   int64_t n, int64_t k, void* out, int out_dtype, int64_t out_stride, int32_t* status, void* stream);
+size_t saem_mx_linear_workspace_bytes(int64_t max_rows, int64_t k);
+int saem_mx_linear(const void* x, int x_dtype, int64_t m, int64_t x_stride, const void* w_codes, const void* w_scales,
+                   int64_t n, int64_t k, void* out, int out_dtype, int64_t out_stride, void* workspace,
+                   size_t workspace_bytes, void* stream);
+int saem_mx_pack_expert(const saem_config* cfg, const void* gate_codes, const void* gate_scales, const void* up_codes,
+                        const void* up_scales, const void* down_codes, const void* down_scales, void* packed_out,
+                        void* stream);
+
+/*
+ * The norms around a block, with its gate and residual scale, in one pass (no counterpart in the paper: what joins the
+ * expert step to the residual stream).  For every row, with x the residual stream and y the block's output:
+ *     z  = y / sqrt(mean(y^2) + eps) * w_post       (z = y if w_post is NULL)
+ *     x' = residual_scale * x + branch_scale * g * z
+ *     n  = x' / sqrt(mean(x'^2) + eps) * w_pre      (weight 1 if w_pre is NULL)
+ * y NULL: x' = x (before the first block); then gate, w_post and x_out must be NULL.  x_out and n_out may be NULL, not
+ * both; x_out has x's type and may be x itself (or y, if it has the same type and stride); the other buffers must not
+ * overlap.  gate: NULL with SAEM_GATE_NONE (g = 1), one value per row (SAEM_GATE_TOKEN, gate_stride apart), one per
+ * column (SAEM_GATE_CHANNEL), or [rows, cols] (SAEM_GATE_FULL); gate_sigmoid != 0: g = 1 / (1 + exp(-gate)).  Types are
+ * SAEM_OUT_*; arithmetic is fp32 and n comes from the unrounded x'.  cols <= 16384; strides in elements; every buffer
+ * aligned to its elements (16-byte aligned rows and cols % 8 == 0 are faster).  rows == 0 is a no-op.
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.
+ */
+typedef struct saem_norm_config {
+    int64_t rows;
+    int64_t x_stride, y_stride, gate_stride, x_out_stride, n_stride;
+    int32_t cols;
+    int32_t x_dtype, y_dtype, n_dtype, gate_dtype, w_dtype;
+    int32_t gate_mode;
+    int32_t gate_sigmoid;
+    float eps, residual_scale, branch_scale;
+} saem_norm_config;
+int saem_block_norm(const saem_norm_config* cfg, const void* x, const void* y, const void* gate, const void* w_post,
+                    const void* w_pre, void* x_out, void* n_out, void* stream);
 
 /* Reads and clears the sticky device status word (synchronises the device).  When the word is
  * SAEM_ERR_TIMEOUT the arrival counters of split reductions are cleared as well (a CTA that gave up

@@ -23,12 +23,21 @@ SAEM_TEMP = -2
 SAEM_HOST_MAPPED = -3
 SAEM_OUT_F32, SAEM_OUT_BF16 = 0, 1
 SAEM_FFN_AUTO, SAEM_FFN_SCALAR, SAEM_FFN_TENSOR, SAEM_FFN_TENSOR_PAIRS, SAEM_FFN_DECODE_FUSED = 0, 1, 2, 3, 4
+SAEM_FFN_MX = 5
+SAEM_GATE_NONE, SAEM_GATE_TOKEN, SAEM_GATE_CHANNEL, SAEM_GATE_FULL = 0, 1, 2, 3
 
 
 class saem_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "d_model", "d_ff", "n_experts", "top_k", "max_tokens", "n_layers", "slots_per_layer", "temp_slots",
         "renorm", "out_dtype", "ffn_path", "n_shared")]
+
+
+class saem_norm_config(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("rows", "x_stride", "y_stride", "gate_stride", "x_out_stride", "n_stride")] +
+                [(n, C.c_int32) for n in ("cols", "x_dtype", "y_dtype", "n_dtype", "gate_dtype", "w_dtype", "gate_mode",
+                                          "gate_sigmoid")] +
+                [(n, C.c_float) for n in ("eps", "residual_scale", "branch_scale")])
 
 
 class SaemError(RuntimeError):
@@ -42,7 +51,7 @@ def _load() -> C.CDLL:
     if not os.path.exists(path) or _build.stale():
         path = _build.build()           # raises if nvcc is missing or the build fails
     lib = C.CDLL(path)
-    vp, i32, sz = C.c_void_p, C.c_int, C.c_size_t
+    vp, i32, i64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
     cfgp = C.POINTER(saem_config)
     sig = {
         "saem_version": (C.c_int, []),
@@ -71,6 +80,15 @@ def _load() -> C.CDLL:
         "saem_launch_count": (C.c_longlong, [vp]),
         "saem_expert_ffn_static": (i32, [vp, vp, i32, i32, i32, i32, vp, vp, vp]),
         "saem_selftest_bounded_wait": (i32, [vp, i32, vp]),
+        "saem_mx_codes_bytes": (sz, [i64, i64]),
+        "saem_mx_scales_bytes": (sz, [i64, i64]),
+        "saem_mx_quantize": (i32, [vp, i32, i64, i64, i64, vp, vp, vp]),
+        "saem_mx_dequantize": (i32, [vp, vp, i64, i64, vp, i32, i64, vp]),
+        "saem_mx_matmul": (i32, [vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp, vp]),
+        "saem_mx_linear_workspace_bytes": (sz, [i64, i64]),
+        "saem_mx_linear": (i32, [vp, i32, i64, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]),
+        "saem_mx_pack_expert": (i32, [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "saem_block_norm": (i32, [C.POINTER(saem_norm_config), vp, vp, vp, vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -83,7 +101,9 @@ _lib = _load()
 EXPORTS = ("saem_version saem_status_string saem_slot_bytes saem_slot_region_bytes saem_workspace_bytes "
            "saem_create saem_destroy saem_pack_expert_host saem_route saem_route_fused saem_repack saem_expert_ffn saem_combine "
            "saem_moe_step saem_moe_step_host saem_moe_step_host_async saem_step_buffer saem_cache_load saem_cache_evict saem_cache_map_host saem_cache_query "
-           "saem_cache_wait saem_last_device_status saem_launch_count saem_expert_ffn_static saem_selftest_bounded_wait").split()
+           "saem_cache_wait saem_last_device_status saem_launch_count saem_expert_ffn_static saem_selftest_bounded_wait "
+           "saem_mx_codes_bytes saem_mx_scales_bytes saem_mx_quantize saem_mx_dequantize saem_mx_matmul "
+           "saem_mx_linear_workspace_bytes saem_mx_linear saem_mx_pack_expert saem_block_norm").split()
 
 
 def library_path() -> str:
@@ -297,6 +317,67 @@ def saem_expert_ffn_static(x_packed, offsets, n_experts, max_rows, d_model, d_ff
                                        _ptr(packed_experts), _ptr(y_packed), _stream(stream))
     if check:
         _check(code, "saem_expert_ffn_static")
+    return code
+
+
+def saem_mx_codes_bytes(rows: int, cols: int) -> int:
+    return _lib.saem_mx_codes_bytes(rows, cols)
+
+
+def saem_mx_scales_bytes(rows: int, cols: int) -> int:
+    return _lib.saem_mx_scales_bytes(rows, cols)
+
+
+def saem_mx_quantize(x, dtype, rows, cols, row_stride, codes, scales, stream=None, check=True) -> int:
+    code = _lib.saem_mx_quantize(_ptr(x), dtype, rows, cols, row_stride, _ptr(codes), _ptr(scales), _stream(stream))
+    if check:
+        _check(code, "saem_mx_quantize")
+    return code
+
+
+def saem_mx_dequantize(codes, scales, rows, cols, out, dtype, row_stride, stream=None, check=True) -> int:
+    code = _lib.saem_mx_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), dtype, row_stride, _stream(stream))
+    if check:
+        _check(code, "saem_mx_dequantize")
+    return code
+
+
+def saem_mx_matmul(a_codes, a_scales, m, w_codes, w_scales, n, k, out, out_dtype, out_stride, status=None, stream=None,
+                   check=True) -> int:
+    code = _lib.saem_mx_matmul(_ptr(a_codes), _ptr(a_scales), m, _ptr(w_codes), _ptr(w_scales), n, k, _ptr(out), out_dtype,
+                               out_stride, _ptr(status), _stream(stream))
+    if check:
+        _check(code, "saem_mx_matmul")
+    return code
+
+
+def saem_mx_linear_workspace_bytes(max_rows: int, k: int) -> int:
+    return _lib.saem_mx_linear_workspace_bytes(max_rows, k)
+
+
+def saem_mx_linear(x, x_dtype, m, x_stride, w_codes, w_scales, n, k, out, out_dtype, out_stride, workspace,
+                   workspace_bytes, stream=None, check=True) -> int:
+    code = _lib.saem_mx_linear(_ptr(x), x_dtype, m, x_stride, _ptr(w_codes), _ptr(w_scales), n, k, _ptr(out), out_dtype,
+                               out_stride, _ptr(workspace), workspace_bytes, _stream(stream))
+    if check:
+        _check(code, "saem_mx_linear")
+    return code
+
+
+def saem_mx_pack_expert(cfg: saem_config, gate_codes, gate_scales, up_codes, up_scales, down_codes, down_scales,
+                        packed_out, stream=None, check=True) -> int:
+    code = _lib.saem_mx_pack_expert(C.byref(cfg), _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes), _ptr(up_scales),
+                                    _ptr(down_codes), _ptr(down_scales), _ptr(packed_out), _stream(stream))
+    if check:
+        _check(code, "saem_mx_pack_expert")
+    return code
+
+
+def saem_block_norm(cfg: saem_norm_config, x, y, gate, w_post, w_pre, x_out, n_out, stream=None, check=True) -> int:
+    code = _lib.saem_block_norm(C.byref(cfg), _ptr(x), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(w_pre), _ptr(x_out),
+                                _ptr(n_out), _stream(stream))
+    if check:
+        _check(code, "saem_block_norm")
     return code
 
 

@@ -1,0 +1,86 @@
+// The microscaled 4-bit format (MXFP4) as the kernels see it.
+//
+// 32 consecutive elements of a row form a block with one power of two 2^(s - 127) (s: one byte, 255 = NaN); an
+// element is an E2M1 code of four bits: sign, then 0 .5 1 1.5 2 3 4 6.  Element 2i of a row is the low half of byte i.
+//
+//   codes  [rows][ceil(cols / 32) * 16 bytes]   row-major, the last block padded with zeros
+//   scales [ceil(rows / 128)][ceil(cols / 128)][512 bytes]   one 512-byte piece per 128 rows x 4 blocks: the four
+//          scales of row r (mod 128) are the 32-bit word at (r % 32) * 16 + (r / 32) * 4.  That is the order in which
+//          tcgen05.cp (32x128b) lays them into tensor memory for the block-scaled MMA, so that a piece is copied as is.
+#ifndef SAEM_MX_COMMON_CUH_
+#define SAEM_MX_COMMON_CUH_
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "saem_internal.h"
+
+namespace saem {
+
+constexpr int kMxBlock = 32;                // elements of a block
+constexpr int kMxSpan = 128;                // elements of four blocks: one 32-bit word of scales
+constexpr int kMxPiece = 512;               // bytes of the scales of 128 rows x kMxSpan elements
+
+// A packed expert (the slot layout of SAEM_FFN_MX contexts) is a sequence of units of 16 weight rows x 128 elements:
+// 1024 bytes of codes, then 64 bytes of scales.  Lane (g, t) = (lane / 4, lane % 4) of the warp that reads a unit takes
+// 16 bytes at lane * 16 for row g and 16 bytes at 512 + lane * 16 for row g + 8; their word b holds the elements
+// 32 b + 8 t .. + 7, i.e. the lane's part of two m16n8k16 MMAs over block b.  Row r's four scales are the word at
+// 1024 + 4 r.  Gate/up region: per 8 hidden units f0.., rows 0-7 are gate rows f0 + r and rows 8-15 up rows f0 + r - 8
+// (so that a thread's accumulators hold gate and up of the same hidden unit), units [d_ff / 8][d_model / 128].
+// Down region: units [d_model / 16][d_ff / 128].
+constexpr int kMxUnitBytes = 1088;
+constexpr int kMxUnitScales = 1024;
+
+__host__ __device__ inline size_t mx_scale_word(long long row, long long span, long long n_span) {
+    return ((size_t)(row >> 7) * n_span + span) * kMxPiece + (size_t)(row & 31) * 16 + ((row >> 5) & 3) * 4;
+}
+__host__ __device__ inline size_t mx_gate_up_units(int d, int f) { return (size_t)(f / 8) * (d / kMxSpan); }
+__host__ __device__ inline size_t mx_down_units(int d, int f) { return (size_t)(d / 16) * (f / kMxSpan); }
+
+#ifdef __CUDACC__
+// The four pairs of E2M1 values of a word of eight codes, low codes first.
+__device__ __forceinline__ void mx_decode8(uint32_t w, uint32_t (&h)[4]) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// Eight fp32 values (already divided by the block's scale) to codes: nearest, ties to even, saturated at 6.
+__device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8]) {
+    uint32_t w;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(w) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return w;
+}
+// The four scales of a word as floats: 2^(s - 127), NaN for 255.  bf16 holds every one of them, 2^-127 included.
+__device__ __forceinline__ void mx_scales4(uint32_t w, float (&s)[4]) {
+    uint32_t lo, hi;
+    asm("{\n\t.reg .b16 a, b;\n\t"
+        "mov.b32 {a, b}, %2;\n\t"
+        "cvt.rn.bf16x2.ue8m0x2 %0, a;\n\t"
+        "cvt.rn.bf16x2.ue8m0x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(w));
+    s[0] = __uint_as_float(lo << 16);
+    s[1] = __uint_as_float(lo & 0xFFFF0000u);
+    s[2] = __uint_as_float(hi << 16);
+    s[3] = __uint_as_float(hi & 0xFFFF0000u);
+}
+// Scale byte of a block whose largest magnitude has these fp32 bits: floor(log2) - 2, so that the largest element
+// lands in [4, 8) and saturates at 6 at worst; 255 if it is not finite.
+__device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits) {
+    const int e = (int)(amax_bits >> 23);
+    return e == 255 ? 255 : (e > 2 ? e - 2 : 0);
+}
+#endif
+
+}  // namespace saem
+
+#endif  // SAEM_MX_COMMON_CUH_

@@ -1,0 +1,330 @@
+// The microscaled 4-bit format: quantisation, the way back, and the packing of quantised expert matrices into slots.
+//
+// Quantisation of a block: s = max(floor(log2 max|x|) - 2, -127), code = E2M1(x * 2^-s) to the nearest (ties to the
+// even mantissa), saturated at 6.  Both the scaling and the way back are exact in fp32, so the only rounding is the one
+// to E2M1.  All three kernels read and write every byte once and are bound by DRAM (2.5 or 4.5 bytes per element);
+// four lanes share a block (8 elements and 16 or 32 bytes each), so that the loads and stores of a warp are whole
+// lines and the block's maximum is two shuffles.
+#include <cmath>
+#include <cstring>
+
+#include "mx_common.cuh"
+
+namespace saem {
+
+constexpr int kQuantThreads = 256;
+constexpr int kQuantChunk = 256;            // elements of a row that one warp takes at a time
+constexpr int kQuantUnroll = 4;             // chunks whose loads a warp has in flight
+
+// Eight elements of a row from `col` on as fp32; what lies beyond `cols` is zero.  VEC: the row is 16-byte aligned and
+// cols a multiple of 8.
+template <bool BF16, bool VEC>
+__device__ __forceinline__ void load8(const void* __restrict__ row, long long col, long long cols, float (&v)[8]) {
+    if (VEC) {
+        if (col >= cols) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        } else if (BF16) {
+            const uint4 q = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + col));
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        } else {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + col);
+            const float4 a = __ldcs(p), b = __ldcs(p + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.f;
+            if (col + i < cols)
+                v[i] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[col + i] << 16)
+                            : static_cast<const float*>(row)[col + i];
+        }
+    }
+}
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(kQuantThreads)
+mx_quantize_kernel(const void* __restrict__ x, long long rows, long long cols, long long row_stride, uint32_t n_chunk,
+                   uint32_t total, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const long long warp = (long long)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    const long long n_block = (cols + kMxBlock - 1) / kMxBlock, n_span = (cols + kMxSpan - 1) / kMxSpan;
+    const size_t esize = BF16 ? 2 : 4;
+    float v[kQuantUnroll][8];
+    uint32_t row[kQuantUnroll], ch[kQuantUnroll];
+#pragma unroll
+    for (int u = 0; u < kQuantUnroll; ++u) {
+        const long long c = warp * kQuantUnroll + u;
+        if (c < total) {
+            row[u] = (uint32_t)c / n_chunk;
+            ch[u] = (uint32_t)c - row[u] * n_chunk;
+            load8<BF16, VEC>(static_cast<const uint8_t*>(x) + (size_t)row[u] * row_stride * esize,
+                             (long long)ch[u] * kQuantChunk + lane * 8, cols, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kQuantUnroll; ++u) {
+        if (warp * kQuantUnroll + u >= total) break;
+        const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[u][i]) & 0x7FFFFFFFu);   // NaN above infinity
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const int s = mx_scale_byte(amax);
+        const float inv = __uint_as_float((uint32_t)(254 - min(s, 253)) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] *= inv;
+        const uint32_t w = s == 255 ? 0u : mx_encode8(v[u]);
+        if (col / kMxBlock < n_block)
+            *reinterpret_cast<uint32_t*>(codes + (size_t)row[u] * n_block * 16 + col / 2) = w;
+        // the four scales of a 128-element span meet in one word; blocks beyond the row's last one get scale 2^-127
+        uint32_t word = col / kMxBlock < n_block ? (uint32_t)s << (((lane >> 2) & 3) * 8) : 0u;
+        word |= __shfl_xor_sync(0xffffffffu, word, 4);
+        word |= __shfl_xor_sync(0xffffffffu, word, 8);
+        const long long span = col / kMxSpan;
+        if ((lane & 15) == 0 && span < n_span)
+            *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row[u], span, n_span)) = word;
+    }
+}
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(kQuantThreads)
+mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long rows, long long cols,
+                     long long row_stride, uint32_t n_chunk, uint32_t total, void* __restrict__ out) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const long long warp = (long long)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    const long long n_block = (cols + kMxBlock - 1) / kMxBlock, n_span = (cols + kMxSpan - 1) / kMxSpan;
+    uint32_t row[kQuantUnroll], ch[kQuantUnroll], w[kQuantUnroll], s[kQuantUnroll];
+#pragma unroll
+    for (int u = 0; u < kQuantUnroll; ++u) {
+        const long long c = warp * kQuantUnroll + u;
+        w[u] = s[u] = 0;
+        if (c < total) {
+            row[u] = (uint32_t)c / n_chunk;
+            ch[u] = (uint32_t)c - row[u] * n_chunk;
+            const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
+            if (col < cols) {
+                w[u] = *reinterpret_cast<const uint32_t*>(codes + (size_t)row[u] * n_block * 16 + col / 2);
+                s[u] = scales[mx_scale_word(row[u], col / kMxSpan, n_span) + ((col / kMxBlock) & 3)];
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kQuantUnroll; ++u) {
+        if (warp * kQuantUnroll + u >= total) break;
+        const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
+        if (col >= cols) continue;
+        const float scale = s[u] == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(s[u] ? s[u] << 23 : 1u << 22);
+        uint32_t h[4];
+        mx_decode8(w[u], h);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+            v[2 * i] = p.x * scale;
+            v[2 * i + 1] = p.y * scale;
+        }
+        const size_t at = (size_t)row[u] * row_stride + col;
+        if (BF16) {
+            uint16_t* o = static_cast<uint16_t*>(out) + at;
+            uint32_t b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 q = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact: one mantissa bit
+                b[i] = *reinterpret_cast<const uint32_t*>(&q);
+            }
+            if (VEC) {
+                *reinterpret_cast<uint4*>(o) = make_uint4(b[0], b[1], b[2], b[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (col + i < cols) o[i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
+            }
+        } else {
+            float* o = static_cast<float*>(out) + at;
+            if (VEC) {
+                reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (col + i < cols) o[i] = v[i];
+            }
+        }
+    }
+}
+
+struct MxMatrix {
+    const uint8_t* codes;
+    const uint8_t* scales;
+};
+
+// One warp per unit: re-orders 16 rows x 128 elements into the slot layout (mx_common.cuh).
+__global__ void __launch_bounds__(kQuantThreads)
+mx_pack_kernel(MxMatrix gate, MxMatrix up, MxMatrix down, int d, int f, uint8_t* __restrict__ out) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const size_t n_gu = mx_gate_up_units(d, f), n_all = n_gu + mx_down_units(d, f);
+    const size_t unit = (size_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    if (unit >= n_all) return;
+    const bool gu = unit < n_gu;
+    const size_t local = gu ? unit : unit - n_gu;
+    const int n_span = (gu ? d : f) / kMxSpan;
+    const int group = (int)(local / n_span), span = (int)(local % n_span);
+    uint8_t* dst = out + unit * kMxUnitBytes;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const MxMatrix& m = gu ? (half ? up : gate) : down;
+        const long long row = gu ? (long long)group * 8 + g : (long long)group * 16 + half * 8 + g;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(m.codes + ((size_t)row * n_span + span) * (kMxSpan / 2));
+        reinterpret_cast<uint4*>(dst + half * 512)[lane] = make_uint4(src[t], src[4 + t], src[8 + t], src[12 + t]);
+        if (t == 0)
+            *reinterpret_cast<uint32_t*>(dst + kMxUnitScales + (half * 8 + g) * 4) =
+                *reinterpret_cast<const uint32_t*>(m.scales + mx_scale_word(row, span, n_span));
+    }
+}
+
+// ---- the same on the host, for experts that stay in pinned memory --------------------------------------------------
+static uint8_t host_quantize_block(const uint16_t* x, uint8_t* codes16) {
+    uint32_t amax = 0;
+    float v[kMxBlock];
+    for (int i = 0; i < kMxBlock; ++i) {
+        const uint32_t b = (uint32_t)x[i] << 16;
+        memcpy(&v[i], &b, 4);
+        const uint32_t m = b & 0x7FFFFFFFu;
+        amax = m > amax ? m : amax;
+    }
+    const int e = (int)(amax >> 23);
+    memset(codes16, 0, 16);
+    if (e == 255) return 255;
+    const int s = e > 2 ? e - 2 : 0;
+    for (int i = 0; i < kMxBlock; ++i) {
+        const float a = std::ldexp(std::fabs(v[i]), 127 - s);
+        const int c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
+        codes16[i / 2] |= (uint8_t)((c | (std::signbit(v[i]) ? 8 : 0)) << (4 * (i & 1)));
+    }
+    return (uint8_t)s;
+}
+
+// The slot layout of one expert from bf16 matrices in host memory (see mx_pack_kernel).
+void mx_pack_expert_host(const uint16_t* gate, const uint16_t* up, const uint16_t* down, int d, int f, uint8_t* out) {
+    const size_t n_gu = mx_gate_up_units(d, f), n_all = n_gu + mx_down_units(d, f);
+    for (size_t unit = 0; unit < n_all; ++unit) {
+        const bool gu = unit < n_gu;
+        const size_t local = gu ? unit : unit - n_gu;
+        const int n_span = (gu ? d : f) / kMxSpan, K = gu ? d : f;
+        const size_t group = local / n_span, span = local % n_span;
+        uint8_t* dst = out + unit * kMxUnitBytes;
+        for (int r = 0; r < 16; ++r) {
+            const uint16_t* m = gu ? (r < 8 ? gate : up) : down;
+            const size_t row = gu ? group * 8 + (r & 7) : group * 16 + r;
+            for (int b = 0; b < 4; ++b) {
+                uint8_t codes[16];
+                dst[kMxUnitScales + r * 4 + b] = host_quantize_block(m + row * K + span * kMxSpan + b * kMxBlock, codes);
+                for (int t = 0; t < 4; ++t)
+                    memcpy(dst + (r >> 3) * 512 + ((r & 7) * 4 + t) * 16 + b * 4, codes + t * 4, 4);
+            }
+        }
+    }
+}
+
+cudaError_t launch_mx_quantize(const void* x, int bf16, long long rows, long long cols, long long row_stride,
+                               uint8_t* codes, uint8_t* scales, cudaStream_t st) {
+    const uint32_t n_chunk = (uint32_t)((cols + kQuantChunk - 1) / kQuantChunk);
+    const uint32_t total = (uint32_t)(rows * n_chunk);
+    const int per_cta = kQuantThreads / 32 * kQuantUnroll;
+    const dim3 grid((total + per_cta - 1) / per_cta);
+    const bool vec = cols % 8 == 0 && ((uintptr_t)x & 15) == 0 && row_stride * (bf16 ? 2 : 4) % 16 == 0;
+    auto k = bf16 ? (vec ? mx_quantize_kernel<true, true> : mx_quantize_kernel<true, false>)
+                  : (vec ? mx_quantize_kernel<false, true> : mx_quantize_kernel<false, false>);
+    return launch_pdl(k, grid, dim3(kQuantThreads), 0, st, x, rows, cols, row_stride, n_chunk, total, codes, scales);
+}
+
+}  // namespace saem
+
+using namespace saem;
+
+// rows, cols and the number of 256-element chunks a kernel counts in 32 bits
+static bool mx_shape_ok(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 1 || rows > 0x7FFFFFFFll || cols > 0x7FFFFFFFll) return false;
+    return rows * ((cols + kQuantChunk - 1) / kQuantChunk) <= 0x7FFFFFFFll;
+}
+
+extern "C" {
+
+size_t saem_mx_codes_bytes(int64_t rows, int64_t cols) {
+    if (!mx_shape_ok(rows, cols)) return 0;
+    return (size_t)rows * (size_t)((cols + kMxBlock - 1) / kMxBlock) * 16;
+}
+
+size_t saem_mx_scales_bytes(int64_t rows, int64_t cols) {
+    if (!mx_shape_ok(rows, cols)) return 0;
+    return (size_t)((rows + 127) / 128) * (size_t)((cols + kMxSpan - 1) / kMxSpan) * kMxPiece;
+}
+
+int saem_mx_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t row_stride, void* codes, void* scales,
+                     void* stream) {
+    if (dtype != SAEM_OUT_F32 && dtype != SAEM_OUT_BF16) return SAEM_ERR_INVALID_ARG;
+    if (!mx_shape_ok(rows, cols) || (rows > 1 && row_stride < cols)) return SAEM_ERR_SHAPE;
+    if (rows == 0) return SAEM_OK;
+    if (!x || !codes || !scales) return SAEM_ERR_INVALID_ARG;
+    if (((uintptr_t)codes | (uintptr_t)scales) & 15) return SAEM_ERR_ALIGNMENT;
+    if ((uintptr_t)x % (dtype == SAEM_OUT_BF16 ? 2 : 4)) return SAEM_ERR_ALIGNMENT;
+    return launch_mx_quantize(x, dtype == SAEM_OUT_BF16, rows, cols, row_stride, (uint8_t*)codes, (uint8_t*)scales,
+                              (cudaStream_t)stream) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+}
+
+int saem_mx_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* out, int dtype,
+                       int64_t row_stride, void* stream) {
+    if (dtype != SAEM_OUT_F32 && dtype != SAEM_OUT_BF16) return SAEM_ERR_INVALID_ARG;
+    if (!mx_shape_ok(rows, cols) || (rows > 1 && row_stride < cols)) return SAEM_ERR_SHAPE;
+    if (rows == 0) return SAEM_OK;
+    if (!out || !codes || !scales) return SAEM_ERR_INVALID_ARG;
+    if (((uintptr_t)codes | (uintptr_t)scales) & 15) return SAEM_ERR_ALIGNMENT;
+    const bool bf16 = dtype == SAEM_OUT_BF16;
+    if ((uintptr_t)out % (bf16 ? 2 : 4)) return SAEM_ERR_ALIGNMENT;
+    const uint32_t n_chunk = (uint32_t)((cols + kQuantChunk - 1) / kQuantChunk);
+    const uint32_t total = (uint32_t)(rows * n_chunk);
+    const int per_cta = kQuantThreads / 32 * kQuantUnroll;
+    const bool vec = cols % 8 == 0 && ((uintptr_t)out & 15) == 0 && row_stride * (bf16 ? 2 : 4) % 16 == 0;
+    auto k = bf16 ? (vec ? mx_dequantize_kernel<true, true> : mx_dequantize_kernel<true, false>)
+                  : (vec ? mx_dequantize_kernel<false, true> : mx_dequantize_kernel<false, false>);
+    return launch_pdl(k, dim3((total + per_cta - 1) / per_cta), dim3(kQuantThreads), 0, (cudaStream_t)stream,
+                      (const uint8_t*)codes, (const uint8_t*)scales, (long long)rows, (long long)cols,
+                      (long long)row_stride, n_chunk, total, out) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+}
+
+int saem_mx_pack_expert(const saem_config* cfg, const void* gate_codes, const void* gate_scales, const void* up_codes,
+                        const void* up_scales, const void* down_codes, const void* down_scales, void* packed_out,
+                        void* stream) {
+    const int v = validate_config(cfg);
+    if (v != SAEM_OK) return v;
+    if (cfg->ffn_path != SAEM_FFN_MX) return SAEM_ERR_UNSUPPORTED;
+    const void* p[7] = {gate_codes, gate_scales, up_codes, up_scales, down_codes, down_scales, packed_out};
+    for (const void* q : p)
+        if (!q) return SAEM_ERR_INVALID_ARG;
+    for (const void* q : p)
+        if ((uintptr_t)q & 15) return SAEM_ERR_ALIGNMENT;
+    const size_t units = mx_gate_up_units(cfg->d_model, cfg->d_ff) + mx_down_units(cfg->d_model, cfg->d_ff);
+    const int per_cta = kQuantThreads / 32;
+    const MxMatrix g = {(const uint8_t*)gate_codes, (const uint8_t*)gate_scales};
+    const MxMatrix u = {(const uint8_t*)up_codes, (const uint8_t*)up_scales};
+    const MxMatrix d = {(const uint8_t*)down_codes, (const uint8_t*)down_scales};
+    return launch_pdl(mx_pack_kernel, dim3((unsigned)((units + per_cta - 1) / per_cta)), dim3(kQuantThreads), 0,
+                      (cudaStream_t)stream, g, u, d, cfg->d_model, cfg->d_ff, (uint8_t*)packed_out) == cudaSuccess
+               ? SAEM_OK : SAEM_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -6,7 +6,7 @@
 #include <cstring>
 #include <new>
 
-#include "saem_internal.h"
+#include "mx_common.cuh"
 
 namespace saem {
 
@@ -24,7 +24,7 @@ int validate_config(const saem_config* c) {
     if (c->temp_slots < 0 || c->temp_slots > 4096) return SAEM_ERR_SHAPE;
     if ((long long)c->n_layers * c->slots_per_layer + c->temp_slots < 1) return SAEM_ERR_SHAPE;
     if (c->out_dtype != SAEM_OUT_F32 && c->out_dtype != SAEM_OUT_BF16) return SAEM_ERR_INVALID_ARG;
-    if (c->ffn_path < SAEM_FFN_AUTO || c->ffn_path > SAEM_FFN_DECODE_FUSED) return SAEM_ERR_INVALID_ARG;
+    if (c->ffn_path < SAEM_FFN_AUTO || c->ffn_path > SAEM_FFN_MX) return SAEM_ERR_INVALID_ARG;
     return SAEM_OK;
 }
 
@@ -44,7 +44,7 @@ WorkspaceLayout workspace_layout(const saem_config& c) {
     L.status = take(256);
     L.counters = take(sizeof(int) * (2 * kMaxCtas + 16));
     L.decode_sync = take(sizeof(int) * kDecodeSyncInts);
-    L.h = take(R * f * 2);
+    L.h = take(R * f * (c.ffn_path == SAEM_FFN_MX ? 4 : 2));
     {   // split-K partial tiles of the streaming kernels: token tiles of at most 64 rows, two slots per CTA
         size_t small_tile = (size_t)2 * (nt < 64 ? nt : 64) * kTileRows;
         L.partials = take((size_t)kMaxCtas * 2 * small_tile * sizeof(float));
@@ -112,6 +112,8 @@ const char* saem_status_string(int s) {
 
 size_t saem_slot_bytes(const saem_config* c) {
     if (validate_config(c) != SAEM_OK) return 0;
+    if (c->ffn_path == SAEM_FFN_MX)
+        return (mx_gate_up_units(c->d_model, c->d_ff) + mx_down_units(c->d_model, c->d_ff)) * kMxUnitBytes;
     return (size_t)3 * c->d_model * c->d_ff * 2;
 }
 
@@ -180,7 +182,7 @@ int saem_create(const saem_config* cfg, void* slot_region, size_t slot_region_by
     // the status word, the arrival counters and the decode step's barrier / tickets start at zero; nothing else needs clearing
     ok = ok && cudaMemsetAsync(c->ws + lay.status, 0, lay.h - lay.status, 0) == cudaSuccess;
     ok = ok && cudaStreamSynchronize(0) == cudaSuccess;
-    if (ok && cfg->ffn_path != SAEM_FFN_SCALAR) ok = ffn_tensor_init() == cudaSuccess;
+    if (ok && cfg->ffn_path != SAEM_FFN_SCALAR && cfg->ffn_path != SAEM_FFN_MX) ok = ffn_tensor_init() == cudaSuccess;
     if (!ok) {
         saem_destroy(c);
         return SAEM_ERR_CUDA;
@@ -227,6 +229,10 @@ int saem_pack_expert_host(const saem_config* cfg, const void* gate, const void* 
     if (!gate || !up || !down || !out) return SAEM_ERR_INVALID_ARG;
     int d = cfg->d_model, f = cfg->d_ff;
     uint8_t* o = (uint8_t*)out;
+    if (cfg->ffn_path == SAEM_FFN_MX) {
+        mx_pack_expert_host((const uint16_t*)gate, (const uint16_t*)up, (const uint16_t*)down, d, f, o);
+        return SAEM_OK;
+    }
     // gate/up region: per (f-block, k-chunk) a gate tile followed by the matching up tile
     pack_matrix((const uint16_t*)gate, f, d, o, 2 * kTileBytes, 0);
     pack_matrix((const uint16_t*)up, f, d, o, 2 * kTileBytes, kTileBytes);
@@ -407,7 +413,10 @@ int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t*
         a.stream_max_tile = (auto_path && (enough_items || g.d_ff < 4096)) ? 0 : 64;
     }
     int nl = 0;
-    if (g.ffn_path == SAEM_FFN_SCALAR) {
+    if (g.ffn_path == SAEM_FFN_MX) {
+        // tiles as high as the longest segment of a step of this many rows; longer ones take several tiles
+        CUDA_TRY(launch_mx_ffn(a, tab, (max_rows + g.top_k + g.n_shared - 1) / (g.top_k + g.n_shared), st, &nl));
+    } else if (g.ffn_path == SAEM_FFN_SCALAR) {
         CUDA_TRY(launch_ffn_scalar(a, tab, st, &nl));
     } else if (gemv_path) {
         CUDA_TRY(launch_ffn_gemv(a, tab, st, &nl));
@@ -576,7 +585,7 @@ int saem_cache_load(saem_ctx* c, int layer, int expert, int slot, const void* pi
     } else if (wait_layer >= 0 && c->read_recorded[wait_layer]) {
         if (cudaStreamWaitEvent(cs, c->read_ev[wait_layer], 0) != cudaSuccess) return SAEM_ERR_CUDA;
     }
-    if (cudaMemcpyAsync(c->slot_region + (size_t)gslot * c->slot_bytes, pinned, c->slot_bytes, cudaMemcpyHostToDevice,
+    if (cudaMemcpyAsync(c->slot_region + (size_t)gslot * c->slot_bytes, pinned, c->slot_bytes, cudaMemcpyDefault,
                         cs) != cudaSuccess)
         return SAEM_ERR_CUDA;
     if (cudaEventRecord(c->ready_ev[gslot], cs) != cudaSuccess) {
@@ -602,6 +611,7 @@ int saem_cache_map_host(saem_ctx* c, int layer, int expert, const void* pinned) 
     int s = check_le(c, layer, expert);
     if (s != SAEM_OK) return s;
     if (!pinned || ((uintptr_t)pinned & 15)) return pinned ? SAEM_ERR_ALIGNMENT : SAEM_ERR_INVALID_ARG;
+    if (c->cfg.ffn_path == SAEM_FFN_MX) return SAEM_ERR_UNSUPPORTED;
     size_t le = (size_t)layer * c->n_total + expert;
     if (c->slot_of[le] >= 0 || c->temp_of[le] >= 0) return SAEM_ERR_INVALID_ARG;     // it has a slot: evict first
     void* dev = nullptr;

@@ -33,7 +33,7 @@ struct WorkspaceLayout {
     size_t counters;      // int32[2 * kMaxCtas + 16] split-K arrival counters (gate/up, down) of the streaming kernels; the tiled
                           // kernels keep per-expert "h complete" / "seen" counts and the down launch's item counter there
     size_t decode_sync;   // int32[kDecodeSyncInts] grid barrier and (column group, token) tickets of the one-launch decode step
-    size_t h;             // bf16 [max_rows, d_ff]
+    size_t h;             // bf16 [max_rows, d_ff] (fp32 with SAEM_FFN_MX)
     size_t partials;      // fp32 [CTAs][2][2][n_tile][128]: 2 CTAs/SM for n_tile <= 64, else 1 CTA/SM
     size_t repack_hist;   // int32 [64][SAEM_MAX_EXPERTS] per-block histograms of the multi-CTA repack
     size_t repack_rank;   // uint16 [65536] rank of a pair inside its block and expert
@@ -134,6 +134,10 @@ struct FfnArgs {
 };
 cudaError_t launch_ffn_scalar(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
 cudaError_t launch_ffn_tensor(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
+// Microscaled 4-bit experts (SAEM_FFN_MX contexts), segments of at most max_segment rows; a.h is fp32 there (mx_moe.cu).
+cudaError_t launch_mx_ffn(const FfnArgs& a, const SlotTable& tab, int max_segment, cudaStream_t st, int* n_launch);
+// One expert's bf16 matrices in host memory to the packed layout of such a context (mx_quant.cu).
+void mx_pack_expert_host(const uint16_t* gate, const uint16_t* up, const uint16_t* down, int d, int f, uint8_t* out);
 // Segments of at most 8 rows (decode batches 1..8): row-split matrix-vector kernels.
 cudaError_t launch_ffn_gemv(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
 // The whole step for batches of at most 8 tokens (top_k at most 8) in one launch (two where a

@@ -59,6 +59,19 @@ class MoELayer:
         B.saem_cache_load(self.ctx.handle, layer, expert, slot, packed, self.copy_stream)
         return packed
 
+    def load_expert_mx(self, layer: int, expert: int, slot: int, gate, up, down) -> torch.Tensor:
+        """One expert of a SAEM_FFN_MX layer from quantised matrices on this device (mx.MxTensor: gate and up [d_ff, d_model],
+        down [d_model, d_ff]).  Returns the packed expert in device memory."""
+        for m, rows, cols in ((gate, self.f, self.d), (up, self.f, self.d), (down, self.d, self.f)):
+            if (m.rows, m.cols) != (rows, cols):
+                raise B.SaemError(B.SAEM_ERR_SHAPE, "load_expert_mx")
+        packed = torch.empty(self.ctx.slot_bytes, dtype=torch.uint8, device=self.device)
+        B.saem_mx_pack_expert(self.cfg, gate.codes, gate.scales, up.codes, up.scales, down.codes, down.scales, packed)
+        self.copy_stream.wait_stream(torch.cuda.current_stream(self.device))
+        packed.record_stream(self.copy_stream)
+        B.saem_cache_load(self.ctx.handle, layer, expert, slot, packed, self.copy_stream)
+        return packed
+
     def load_all(self, gate: Sequence[np.ndarray], up: Sequence[np.ndarray], down: Sequence[np.ndarray],
                  shared=None, layer: int = 0):
         """Every routed expert e into slot e of `layer` (needs slots_per_layer == n_experts)."""

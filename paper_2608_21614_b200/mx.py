@@ -1,0 +1,114 @@
+"""Matrices in the microscaled 4-bit format (MXFP4) and the products of them.
+
+Thin plumbing over the ``saem_mx_*`` calls: device memory and arguments here, arithmetic in
+libsaem's kernels.  Everything is enqueued on the current stream unless a stream is given.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+_DTYPE = {torch.float32: B.SAEM_OUT_F32, torch.bfloat16: B.SAEM_OUT_BF16}
+
+
+def _dtype(t: torch.Tensor) -> int:
+    try:
+        return _DTYPE[t.dtype]
+    except KeyError:
+        raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "float32 or bfloat16 wanted, not %s" % t.dtype) from None
+
+
+def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
+    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise B.SaemError(B.SAEM_ERR_INVALID_ARG, what + ": a matrix on the GPU with consecutive columns is wanted")
+    return t
+
+
+class MxTensor:
+    """A quantised matrix [rows, cols]: `codes` and `scales` as include/saem.h describes them (uint8)."""
+
+    __slots__ = ("rows", "cols", "codes", "scales")
+
+    def __init__(self, rows: int, cols: int, codes: torch.Tensor, scales: torch.Tensor):
+        for t, size in ((codes, B.saem_mx_codes_bytes(rows, cols)), (scales, B.saem_mx_scales_bytes(rows, cols))):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < size or (rows and not size):
+                raise B.SaemError(B.SAEM_ERR_SHAPE, "MxTensor")
+        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.scales.numel()
+
+
+def empty(rows: int, cols: int, device="cuda") -> MxTensor:
+    """An MxTensor whose contents are unspecified."""
+    return MxTensor(rows, cols, torch.empty(B.saem_mx_codes_bytes(rows, cols), dtype=torch.uint8, device=device),
+                    torch.empty(B.saem_mx_scales_bytes(rows, cols), dtype=torch.uint8, device=device))
+
+
+def quantize(x: torch.Tensor, out: Optional[MxTensor] = None, stream=None) -> MxTensor:
+    """x [rows, cols] float32 or bfloat16 to the microscaled format."""
+    _matrix(x, "quantize")
+    if out is None:
+        out = empty(x.shape[0], x.shape[1], x.device)
+    elif (out.rows, out.cols) != x.shape:
+        raise B.SaemError(B.SAEM_ERR_SHAPE, "quantize")
+    B.saem_mx_quantize(x, _dtype(x), out.rows, out.cols, x.stride(0), out.codes, out.scales, stream)
+    return out
+
+
+def dequantize(q: MxTensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """The values a quantised matrix stands for, as float32 or bfloat16 (exact in both)."""
+    if out is None:
+        out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.device)
+    elif _matrix(out, "dequantize").shape != (q.rows, q.cols):
+        raise B.SaemError(B.SAEM_ERR_SHAPE, "dequantize")
+    B.saem_mx_dequantize(q.codes, q.scales, q.rows, q.cols, out, _dtype(out), out.stride(0), stream)
+    return out
+
+
+def matmul(a: MxTensor, w: MxTensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+           status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[m, n] = sum_k a[m, k] * w[n, k], float32 sums, bfloat16 or float32 out."""
+    if out is None:
+        out = torch.empty(a.rows, w.rows, dtype=dtype, device=a.device)
+    if a.cols != w.cols or _matrix(out, "matmul").shape != (a.rows, w.rows):
+        raise B.SaemError(B.SAEM_ERR_SHAPE, "matmul")
+    B.saem_mx_matmul(a.codes, a.scales, a.rows, w.codes, w.scales, w.rows, w.cols, out, _dtype(out), out.stride(0), status, stream)
+    return out
+
+
+class Linear:
+    """A projection whose weights are quantised once and whose activations are quantised in every call.
+
+    `max_rows` sizes the workspace; calls of one Linear must be ordered on the GPU (they share it)."""
+
+    def __init__(self, weight: MxTensor, max_rows: int):
+        self.weight, self.max_rows = weight, max_rows
+        self.workspace = torch.empty(max(1, B.saem_mx_linear_workspace_bytes(max_rows, weight.cols)), dtype=torch.uint8,
+                                     device=weight.device)
+        self.workspace[:4].zero_()
+
+    def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                 stream=None) -> torch.Tensor:
+        """x [m, k] float32 or bfloat16 -> [m, n]."""
+        w = self.weight
+        _matrix(x, "Linear")
+        m = x.shape[0]
+        if out is None:
+            out = torch.empty(m, w.rows, dtype=dtype, device=x.device)
+        if x.shape[1] != w.cols or m > self.max_rows or _matrix(out, "Linear").shape != (m, w.rows):
+            raise B.SaemError(B.SAEM_ERR_SHAPE, "Linear")
+        B.saem_mx_linear(x, _dtype(x), m, x.stride(0), w.codes, w.scales, w.rows, w.cols, out, _dtype(out), out.stride(0),
+                         self.workspace, self.workspace.numel(), stream)
+        return out
+
+    def device_status(self) -> int:
+        """The status word of the calls so far (synchronises); 0 unless a device-side wait ran out."""
+        return int(self.workspace[:4].view(torch.int32).item())

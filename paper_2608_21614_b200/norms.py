@@ -1,0 +1,81 @@
+"""The norms around a block with its gate and residual scale: plumbing over ``saem_block_norm``."""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as B
+from .mx import _dtype, _matrix
+
+_GATES = {"none": B.SAEM_GATE_NONE, "token": B.SAEM_GATE_TOKEN, "channel": B.SAEM_GATE_CHANNEL, "full": B.SAEM_GATE_FULL}
+
+
+class BlockNorm:
+    """What stands between one block and the next on the residual stream x:
+
+        z  = y / sqrt(mean(y^2) + eps) * w_post              (z = y without w_post)
+        x' = residual_scale * x + branch_scale * g * z
+        n  = x' / sqrt(mean(x'^2) + eps) * w_pre
+
+    `gate`: "none" (g = 1), "token" [T] or [T, 1], "channel" [d] or [1, d], "full" [T, d]; with `gate_sigmoid`,
+    g = 1 / (1 + exp(-gate))."""
+
+    def __init__(self, d: int, w_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 residual_scale: float = 1.0, branch_scale: float = 1.0, gate: str = "none", gate_sigmoid: bool = False):
+        for w in (w_post, w_pre):
+            if w is not None and (w.shape != (d,) or not w.is_contiguous()):
+                raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm weight")
+        if w_post is not None and w_pre is not None and w_post.dtype != w_pre.dtype:
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm weights of one type are wanted")
+        self.d, self.w_post, self.w_pre = d, w_post, w_pre
+        w = w_post if w_post is not None else w_pre
+        self._cfg = B.saem_norm_config(cols=d, w_dtype=B.SAEM_OUT_F32 if w is None else _dtype(w), gate_mode=_GATES[gate],
+                                       gate_sigmoid=int(gate_sigmoid), eps=eps, residual_scale=residual_scale,
+                                       branch_scale=branch_scale)
+
+    def _rows(self, t: torch.Tensor, rows: int) -> int:
+        if _matrix(t, "BlockNorm").shape != (rows, self.d):
+            raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm")
+        return t.stride(0)
+
+    def enter(self, x: torch.Tensor, n_out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+              stream=None) -> torch.Tensor:
+        """The first block's input: n of x itself."""
+        T = x.shape[0]
+        if n_out is None:
+            n_out = torch.empty(T, self.d, dtype=dtype, device=x.device)
+        c = B.saem_norm_config.from_buffer_copy(self._cfg)
+        c.rows, c.x_dtype, c.n_dtype, c.gate_mode = T, _dtype(x), _dtype(n_out), B.SAEM_GATE_NONE
+        c.x_stride, c.n_stride = self._rows(x, T), self._rows(n_out, T)
+        B.saem_block_norm(c, x, None, None, None, self.w_pre, None, n_out, stream)
+        return n_out
+
+    def leave(self, x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None,
+              n_out: Optional[torch.Tensor] = None, next_norm: bool = True, dtype: torch.dtype = torch.bfloat16, stream=None):
+        """(x', n) after a block whose output is y; x_out may be x.  `next_norm` False: x' only (n is None)."""
+        T, c = x.shape[0], self._cfg
+        if x_out is None:
+            x_out = torch.empty(T, self.d, dtype=x.dtype, device=x.device)
+        if x_out.dtype != x.dtype:
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: x_out has x's type")
+        if n_out is None and next_norm:
+            n_out = torch.empty(T, self.d, dtype=dtype, device=x.device)
+        c.rows, c.x_dtype, c.y_dtype = T, _dtype(x), _dtype(y)
+        c.x_stride, c.y_stride, c.x_out_stride = self._rows(x, T), self._rows(y, T), self._rows(x_out, T)
+        if n_out is not None:
+            c.n_dtype, c.n_stride = _dtype(n_out), self._rows(n_out, T)
+        if (gate is None) != (c.gate_mode == B.SAEM_GATE_NONE):
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm gate")
+        if gate is not None:
+            c.gate_dtype = _dtype(gate)
+            if c.gate_mode == B.SAEM_GATE_FULL:
+                c.gate_stride = self._rows(gate, T)
+            elif c.gate_mode == B.SAEM_GATE_TOKEN:
+                if gate.shape not in ((T,), (T, 1)):
+                    raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm gate")
+                c.gate_stride = gate.stride(0)
+            elif gate.shape not in ((self.d,), (1, self.d)) or (self.d > 1 and gate.stride(-1) != 1):
+                raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm gate")
+        B.saem_block_norm(c, x, y, gate, self.w_post, self.w_pre if n_out is not None else None, x_out, n_out, stream)
+        return x_out, n_out

@@ -110,6 +110,10 @@ def library_path() -> str:
     return _build.LIB
 
 
+# the current stream's handle without building a Stream object (a few microseconds of every call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _ptr(t) -> Optional[int]:
     """Device/host address of a torch tensor, numpy array, int or None."""
     if t is None:
@@ -123,6 +127,8 @@ def _ptr(t) -> Optional[int]:
 
 def _stream(s) -> Optional[int]:
     if s is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(torch.cuda.current_device()) or None
         return torch.cuda.current_stream().cuda_stream or None
     if isinstance(s, torch.cuda.Stream):
         return s.cuda_stream or None

@@ -44,7 +44,7 @@ WorkspaceLayout workspace_layout(const saem_config& c) {
     L.status = take(256);
     L.counters = take(sizeof(int) * (2 * kMaxCtas + 16));
     L.decode_sync = take(sizeof(int) * kDecodeSyncInts);
-    L.h = take(R * f * (c.ffn_path == SAEM_FFN_MX ? 4 : 2));
+    L.h = take(c.ffn_path == SAEM_FFN_MX ? mx_workspace_bytes((long long)R, c.d_model, c.d_ff) : R * f * 2);
     {   // split-K partial tiles of the streaming kernels: token tiles of at most 64 rows, two slots per CTA
         size_t small_tile = (size_t)2 * (nt < 64 ? nt : 64) * kTileRows;
         L.partials = take((size_t)kMaxCtas * 2 * small_tile * sizeof(float));
@@ -385,6 +385,7 @@ int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t*
     a.slot_bytes = c->slot_bytes;
     a.slot_region_bytes = c->slot_bytes * (size_t)(c->n_fixed_slots + c->cfg.temp_slots);
     a.h = (uint16_t*)(c->ws + c->lay.h);
+    a.h_rows = g.max_tokens * (g.top_k + g.n_shared);
     a.y_packed = y_packed;
     a.status = (int*)(c->ws + c->lay.status);
     a.counters = (int*)(c->ws + c->lay.counters);
@@ -503,6 +504,25 @@ int saem_moe_step(saem_ctx* c, saem_ctx* sh, int layer, const float* logits, con
         a.status = (int*)(w + L.status);
         int nl = 0;
         CUDA_TRY(launch_decode_fused(a, tab, c->n_sm, st, &nl));
+        c->launches += nl;
+        return note_ffn_enqueued(c, layer, st, tab);
+    }
+    if (!sh && g.ffn_path == SAEM_FFN_MX && mx_few_supported(T, g.top_k, g.d_model)) {
+        if (layer < 0 || layer >= g.n_layers) return SAEM_ERR_INVALID_ARG;
+        if (misaligned(x) || misaligned(out)) return SAEM_ERR_ALIGNMENT;
+        cudaStream_t st = (cudaStream_t)stream;
+        SlotTable tab;
+        if ((s = resolve_slots(c, layer, nullptr, 0, st, tab)) != SAEM_OK) return s;
+        MxFewArgs a = {};
+        a.logits = logits; a.x = (const uint16_t*)x;
+        a.T = T; a.E = g.n_experts; a.S = g.n_shared; a.k = g.top_k; a.d = g.d_model; a.f = g.d_ff; a.renorm = g.renorm;
+        a.slot_region = c->slot_region; a.slot_bytes = c->slot_bytes;
+        a.h = (float*)(w + L.h);
+        a.out = out; a.out_bf16 = g.out_dtype == SAEM_OUT_BF16;
+        a.topk_idx = idx; a.topk_w = tw;
+        a.status = (int*)(w + L.status);
+        int nl = 0;
+        CUDA_TRY(launch_mx_few(a, tab, c->n_sm, st, &nl));
         c->launches += nl;
         return note_ffn_enqueued(c, layer, st, tab);
     }

@@ -33,7 +33,7 @@ struct WorkspaceLayout {
     size_t counters;      // int32[2 * kMaxCtas + 16] split-K arrival counters (gate/up, down) of the streaming kernels; the tiled
                           // kernels keep per-expert "h complete" / "seen" counts and the down launch's item counter there
     size_t decode_sync;   // int32[kDecodeSyncInts] grid barrier and (column group, token) tickets of the one-launch decode step
-    size_t h;             // bf16 [max_rows, d_ff] (fp32 with SAEM_FFN_MX)
+    size_t h;             // bf16 [max_rows, d_ff]; SAEM_FFN_MX: the regions of mx_moe.cu
     size_t partials;      // fp32 [CTAs][2][2][n_tile][128]: 2 CTAs/SM for n_tile <= 64, else 1 CTA/SM
     size_t repack_hist;   // int32 [64][SAEM_MAX_EXPERTS] per-block histograms of the multi-CTA repack
     size_t repack_rank;   // uint16 [65536] rank of a pair inside its block and expert
@@ -121,6 +121,7 @@ struct FfnArgs {
     size_t slot_bytes;
     size_t slot_region_bytes;   // whole region (every slot)
     uint16_t* h;                // [max_rows, f] bf16 workspace
+    int h_rows;                 // rows the workspace was made for
     float* y_packed;            // [max_rows, d]
     int* status;
     int* counters;              // [2 * kMaxCtas + 16]
@@ -134,8 +135,27 @@ struct FfnArgs {
 };
 cudaError_t launch_ffn_scalar(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
 cudaError_t launch_ffn_tensor(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
-// Microscaled 4-bit experts (SAEM_FFN_MX contexts), segments of at most max_segment rows; a.h is fp32 there (mx_moe.cu).
+// Microscaled 4-bit experts (SAEM_FFN_MX contexts, mx_moe.cu); a.h is a workspace of mx_workspace_bytes there, and row
+// tiles are made for segments of max_segment rows.
+size_t mx_workspace_bytes(long long rows, int d, int f);
 cudaError_t launch_mx_ffn(const FfnArgs& a, const SlotTable& tab, int max_segment, cudaStream_t st, int* n_launch);
+// The whole step over such experts for up to 8 tokens in two launches.
+struct MxFewArgs {
+    const float* logits;        // [T, E]
+    const uint16_t* x;          // [T, d]
+    int T, E, S, k, d, f, renorm;
+    const uint8_t* slot_region;
+    size_t slot_bytes;
+    float* h;                   // [T * (k + S), f] fp32 workspace, rows by pair id
+    void* out;                  // [T, d]
+    int out_bf16;
+    int32_t* topk_idx;
+    float* topk_w;
+    int* status;
+    int groups_a, chunk_b;      // set by the launcher
+};
+bool mx_few_supported(int T, int k, int d);
+cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStream_t st, int* n_launch);
 // One expert's bf16 matrices in host memory to the packed layout of such a context (mx_quant.cu).
 void mx_pack_expert_host(const uint16_t* gate, const uint16_t* up, const uint16_t* down, int d, int f, uint8_t* out);
 // Segments of at most 8 rows (decode batches 1..8): row-split matrix-vector kernels.

@@ -21,10 +21,14 @@ def _dtype(t: torch.Tensor) -> int:
         raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "float32 or bfloat16 wanted, not %s" % t.dtype) from None
 
 
-def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+def _matrix(t: torch.Tensor, what: str, rows: Optional[int] = None, cols: Optional[int] = None) -> int:
+    """The row stride of a matrix on the GPU whose columns are consecutive (and whose shape is [rows, cols], if given)."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or not t.is_cuda or (stride[1] != 1 and shape[1] > 1):
         raise B.SaemError(B.SAEM_ERR_INVALID_ARG, what + ": a matrix on the GPU with consecutive columns is wanted")
-    return t
+    if rows is not None and shape != (rows, cols):
+        raise B.SaemError(B.SAEM_ERR_SHAPE, what)
+    return stride[0]
 
 
 class MxTensor:
@@ -54,12 +58,10 @@ def empty(rows: int, cols: int, device="cuda") -> MxTensor:
 
 def quantize(x: torch.Tensor, out: Optional[MxTensor] = None, stream=None) -> MxTensor:
     """x [rows, cols] float32 or bfloat16 to the microscaled format."""
-    _matrix(x, "quantize")
     if out is None:
+        _matrix(x, "quantize")
         out = empty(x.shape[0], x.shape[1], x.device)
-    elif (out.rows, out.cols) != x.shape:
-        raise B.SaemError(B.SAEM_ERR_SHAPE, "quantize")
-    B.saem_mx_quantize(x, _dtype(x), out.rows, out.cols, x.stride(0), out.codes, out.scales, stream)
+    B.saem_mx_quantize(x, _dtype(x), out.rows, out.cols, _matrix(x, "quantize", out.rows, out.cols), out.codes, out.scales, stream)
     return out
 
 
@@ -67,20 +69,19 @@ def dequantize(q: MxTensor, out: Optional[torch.Tensor] = None, dtype: torch.dty
     """The values a quantised matrix stands for, as float32 or bfloat16 (exact in both)."""
     if out is None:
         out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.device)
-    elif _matrix(out, "dequantize").shape != (q.rows, q.cols):
-        raise B.SaemError(B.SAEM_ERR_SHAPE, "dequantize")
-    B.saem_mx_dequantize(q.codes, q.scales, q.rows, q.cols, out, _dtype(out), out.stride(0), stream)
+    B.saem_mx_dequantize(q.codes, q.scales, q.rows, q.cols, out, _dtype(out), _matrix(out, "dequantize", q.rows, q.cols), stream)
     return out
 
 
 def matmul(a: MxTensor, w: MxTensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
            status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[m, n] = sum_k a[m, k] * w[n, k], float32 sums, bfloat16 or float32 out."""
+    if a.cols != w.cols:
+        raise B.SaemError(B.SAEM_ERR_SHAPE, "matmul")
     if out is None:
         out = torch.empty(a.rows, w.rows, dtype=dtype, device=a.device)
-    if a.cols != w.cols or _matrix(out, "matmul").shape != (a.rows, w.rows):
-        raise B.SaemError(B.SAEM_ERR_SHAPE, "matmul")
-    B.saem_mx_matmul(a.codes, a.scales, a.rows, w.codes, w.scales, w.rows, w.cols, out, _dtype(out), out.stride(0), status, stream)
+    B.saem_mx_matmul(a.codes, a.scales, a.rows, w.codes, w.scales, w.rows, w.cols, out, _dtype(out),
+                     _matrix(out, "matmul", a.rows, w.rows), status, stream)
     return out
 
 
@@ -91,22 +92,21 @@ class Linear:
 
     def __init__(self, weight: MxTensor, max_rows: int):
         self.weight, self.max_rows = weight, max_rows
-        self.workspace = torch.empty(max(1, B.saem_mx_linear_workspace_bytes(max_rows, weight.cols)), dtype=torch.uint8,
+        self.workspace = torch.empty(max(256, B.saem_mx_linear_workspace_bytes(max_rows, weight.cols)), dtype=torch.uint8,
                                      device=weight.device)
         self.workspace[:4].zero_()
 
     def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
                  stream=None) -> torch.Tensor:
         """x [m, k] float32 or bfloat16 -> [m, n]."""
-        w = self.weight
-        _matrix(x, "Linear")
-        m = x.shape[0]
+        w, ws = self.weight, self.workspace
+        m = len(x)
+        if m > self.max_rows:
+            raise B.SaemError(B.SAEM_ERR_SHAPE, "Linear")
         if out is None:
             out = torch.empty(m, w.rows, dtype=dtype, device=x.device)
-        if x.shape[1] != w.cols or m > self.max_rows or _matrix(out, "Linear").shape != (m, w.rows):
-            raise B.SaemError(B.SAEM_ERR_SHAPE, "Linear")
-        B.saem_mx_linear(x, _dtype(x), m, x.stride(0), w.codes, w.scales, w.rows, w.cols, out, _dtype(out), out.stride(0),
-                         self.workspace, self.workspace.numel(), stream)
+        B.saem_mx_linear(x, _dtype(x), m, _matrix(x, "Linear", m, w.cols), w.codes, w.scales, w.rows, w.cols, out, _dtype(out),
+                         _matrix(out, "Linear", m, w.rows), ws, ws.numel(), stream)
         return out
 
     def device_status(self) -> int:

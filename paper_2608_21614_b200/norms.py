@@ -34,48 +34,42 @@ class BlockNorm:
                                        gate_sigmoid=int(gate_sigmoid), eps=eps, residual_scale=residual_scale,
                                        branch_scale=branch_scale)
 
-    def _rows(self, t: torch.Tensor, rows: int) -> int:
-        if _matrix(t, "BlockNorm").shape != (rows, self.d):
-            raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm")
-        return t.stride(0)
+    def _call(self, c, x, y, gate, w_post, w_pre, x_out, n_out, stream):
+        T, d = len(x), self.d
+        c.rows, c.x_dtype, c.x_stride = T, _dtype(x), _matrix(x, "BlockNorm", T, d)
+        if y is not None:
+            c.y_dtype, c.y_stride, c.x_out_stride = _dtype(y), _matrix(y, "BlockNorm", T, d), _matrix(x_out, "BlockNorm", T, d)
+        if n_out is not None:
+            c.n_dtype, c.n_stride = _dtype(n_out), _matrix(n_out, "BlockNorm", T, d)
+        B.saem_block_norm(c, x, y, gate, w_post, w_pre, x_out, n_out, stream)
 
     def enter(self, x: torch.Tensor, n_out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
               stream=None) -> torch.Tensor:
         """The first block's input: n of x itself."""
-        T = x.shape[0]
         if n_out is None:
-            n_out = torch.empty(T, self.d, dtype=dtype, device=x.device)
+            n_out = torch.empty(len(x), self.d, dtype=dtype, device=x.device)
         c = B.saem_norm_config.from_buffer_copy(self._cfg)
-        c.rows, c.x_dtype, c.n_dtype, c.gate_mode = T, _dtype(x), _dtype(n_out), B.SAEM_GATE_NONE
-        c.x_stride, c.n_stride = self._rows(x, T), self._rows(n_out, T)
-        B.saem_block_norm(c, x, None, None, None, self.w_pre, None, n_out, stream)
+        c.gate_mode = B.SAEM_GATE_NONE
+        self._call(c, x, None, None, None, self.w_pre, None, n_out, stream)
         return n_out
 
     def leave(self, x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None,
               n_out: Optional[torch.Tensor] = None, next_norm: bool = True, dtype: torch.dtype = torch.bfloat16, stream=None):
         """(x', n) after a block whose output is y; x_out may be x.  `next_norm` False: x' only (n is None)."""
-        T, c = x.shape[0], self._cfg
+        T, c = len(x), self._cfg
         if x_out is None:
             x_out = torch.empty(T, self.d, dtype=x.dtype, device=x.device)
-        if x_out.dtype != x.dtype:
+        elif x_out.dtype != x.dtype:
             raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: x_out has x's type")
         if n_out is None and next_norm:
             n_out = torch.empty(T, self.d, dtype=dtype, device=x.device)
-        c.rows, c.x_dtype, c.y_dtype = T, _dtype(x), _dtype(y)
-        c.x_stride, c.y_stride, c.x_out_stride = self._rows(x, T), self._rows(y, T), self._rows(x_out, T)
-        if n_out is not None:
-            c.n_dtype, c.n_stride = _dtype(n_out), self._rows(n_out, T)
-        if (gate is None) != (c.gate_mode == B.SAEM_GATE_NONE):
-            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm gate")
         if gate is not None:
-            c.gate_dtype = _dtype(gate)
-            if c.gate_mode == B.SAEM_GATE_FULL:
-                c.gate_stride = self._rows(gate, T)
-            elif c.gate_mode == B.SAEM_GATE_TOKEN:
-                if gate.shape not in ((T,), (T, 1)):
-                    raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm gate")
+            c.gate_dtype, mode, shape = _dtype(gate), c.gate_mode, gate.shape
+            if mode == B.SAEM_GATE_FULL:
+                c.gate_stride = _matrix(gate, "BlockNorm gate", T, self.d)
+            elif mode == B.SAEM_GATE_TOKEN and shape in ((T,), (T, 1)):
                 c.gate_stride = gate.stride(0)
-            elif gate.shape not in ((self.d,), (1, self.d)) or (self.d > 1 and gate.stride(-1) != 1):
+            elif not (mode == B.SAEM_GATE_CHANNEL and shape in ((self.d,), (1, self.d)) and (self.d == 1 or gate.stride(-1) == 1)):
                 raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm gate")
-        B.saem_block_norm(c, x, y, gate, self.w_post, self.w_pre if n_out is not None else None, x_out, n_out, stream)
+        self._call(c, x, y, gate, self.w_post, self.w_pre if n_out is not None else None, x_out, n_out, stream)
         return x_out, n_out

@@ -86,8 +86,11 @@ enum { SAEM_GATE_NONE = 0, SAEM_GATE_TOKEN = 1, SAEM_GATE_CHANNEL = 2, SAEM_GATE
  * up to 8); AUTO takes it up to 4 tokens, and up to 8 on layers whose experts are at most 20 MB
  * (3 * d_model * d_ff * 2 bytes) and numerous enough (see saem_moe_step).
  * SAEM_FFN_MX: the slots hold experts in the microscaled 4-bit format (see saem_mx_quantize): 3 * d_model * d_ff *
- * 17/32 bytes per slot instead of 3 * d_model * d_ff * 2, packed by saem_mx_pack_expert (device) or
- * saem_pack_expert_host (which then quantises); x stays bf16, the hidden activations are fp32 in the workspace.  All step
+ * 17/32 bytes per slot instead of 3 * d_model * d_ff * 2 (rows padded to multiples of 256 elements), packed by
+ * saem_mx_pack_expert (device) or saem_pack_expert_host (which then quantises).  Activations are not rounded to 4 bits: x is
+ * held to 2^-14 of the largest of 32 neighbours at worst (exactly in the form for up to 8 tokens) and so are the hidden
+ * activations (11 bits of each there).  saem_moe_step takes up to 8 tokens (top_k <= 8, T * d_model <= 32768, no
+ * shared_ctx) in two launches, which leave topk_idx and topk_w but none of the other intermediates in the workspace.  All step
  * and cache calls take such a context except saem_cache_map_host (UNSUPPORTED).
  * n_shared (0..16, n_experts + n_shared <= SAEM_MAX_EXPERTS): always-on shared experts of the same
  * width d_ff that run INSIDE the layer's grouped launch.  They are experts n_experts ..
@@ -117,7 +120,7 @@ typedef struct saem_config {
 int saem_version(void);
 const char* saem_status_string(int status);
 
-/* Bytes of one packed expert (= one slot): 3 * d_model * d_ff * 2 (SAEM_FFN_MX: * 17/32).  0 on an invalid config. */
+/* Bytes of one packed expert (= one slot): 3 * d_model * d_ff * 2 (SAEM_FFN_MX: about 17/32 instead of 2).  0 on an invalid config. */
 size_t saem_slot_bytes(const saem_config* cfg);
 /* Bytes the slot region must have: (n_layers * slots_per_layer + temp_slots) * saem_slot_bytes. */
 size_t saem_slot_region_bytes(const saem_config* cfg);

@@ -21,21 +21,21 @@ constexpr int kMxBlock = 32;                // elements of a block
 constexpr int kMxSpan = 128;                // elements of four blocks: one 32-bit word of scales
 constexpr int kMxPiece = 512;               // bytes of the scales of 128 rows x kMxSpan elements
 
-// A packed expert (the slot layout of SAEM_FFN_MX contexts) is a sequence of units of 16 weight rows x 128 elements:
-// 1024 bytes of codes, then 64 bytes of scales.  Lane (g, t) = (lane / 4, lane % 4) of the warp that reads a unit takes
-// 16 bytes at lane * 16 for row g and 16 bytes at 512 + lane * 16 for row g + 8; their word b holds the elements
-// 32 b + 8 t .. + 7, i.e. the lane's part of two m16n8k16 MMAs over block b.  Row r's four scales are the word at
-// 1024 + 4 r.  Gate/up region: per 8 hidden units f0.., rows 0-7 are gate rows f0 + r and rows 8-15 up rows f0 + r - 8
-// (so that a thread's accumulators hold gate and up of the same hidden unit), units [d_ff / 8][d_model / 128].
-// Down region: units [d_model / 16][d_ff / 128].
-constexpr int kMxUnitBytes = 1088;
-constexpr int kMxUnitScales = 1024;
+// A packed expert (the slot layout of SAEM_FFN_MX contexts) is a sequence of blocks of 128 weight rows x 256 elements,
+// 17 KB each and read with one bulk copy: 128 bytes of codes per row, 16-byte chunks XOR-swizzled by (row mod 8) as the
+// tensor cores want them, then the two 512-byte pieces of the scales.  Gate/up region: [d_ff / 128][ceil(d_model / 256)] of a
+// gate block and the up block of the same place; down region: [d_model / 128][ceil(d_ff / 256)].  Where the row's length is
+// an odd multiple of 128, the second half of its last block is zero.
+constexpr int kMxChunk = 256;               // elements of a block's rows
+constexpr int kMxBlockCodes = 128 * 128;
+constexpr int kMxBlockBytes = kMxBlockCodes + 2 * kMxPiece;
 
 __host__ __device__ inline size_t mx_scale_word(long long row, long long span, long long n_span) {
     return ((size_t)(row >> 7) * n_span + span) * kMxPiece + (size_t)(row & 31) * 16 + ((row >> 5) & 3) * 4;
 }
-__host__ __device__ inline size_t mx_gate_up_units(int d, int f) { return (size_t)(f / 8) * (d / kMxSpan); }
-__host__ __device__ inline size_t mx_down_units(int d, int f) { return (size_t)(d / 16) * (f / kMxSpan); }
+__host__ __device__ inline int mx_chunks(int k) { return (k + kMxChunk - 1) / kMxChunk; }
+__host__ __device__ inline size_t mx_gate_up_blocks(int d, int f) { return (size_t)(f / 128) * mx_chunks(d) * 2; }
+__host__ __device__ inline size_t mx_down_blocks(int d, int f) { return (size_t)(d / 128) * mx_chunks(f); }
 
 #ifdef __CUDACC__
 // The four pairs of E2M1 values of a word of eight codes, low codes first.

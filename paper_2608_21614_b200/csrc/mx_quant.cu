@@ -170,29 +170,41 @@ struct MxMatrix {
     const uint8_t* scales;
 };
 
-// One warp per unit: re-orders 16 rows x 128 elements into the slot layout (mx_common.cuh).
+// Which matrix, row tile and chunk a block of the slot layout holds.
+struct BlockPlace {
+    int matrix, tile, chunk;                // matrix: 0 gate, 1 up, 2 down
+};
+__host__ __device__ inline BlockPlace block_place(size_t block, int d, int f) {
+    const size_t n_gu = mx_gate_up_blocks(d, f);
+    if (block < n_gu) {
+        const int nc = mx_chunks(d);
+        return {(int)(block & 1), (int)(block / 2 / nc), (int)(block / 2 % nc)};
+    }
+    const int nc = mx_chunks(f);
+    return {2, (int)((block - n_gu) / nc), (int)((block - n_gu) % nc)};
+}
+
+// One CTA per block of the slot layout (mx_common.cuh).
 __global__ void __launch_bounds__(kQuantThreads)
 mx_pack_kernel(MxMatrix gate, MxMatrix up, MxMatrix down, int d, int f, uint8_t* __restrict__ out) {
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const size_t n_gu = mx_gate_up_units(d, f), n_all = n_gu + mx_down_units(d, f);
-    const size_t unit = (size_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
-    if (unit >= n_all) return;
-    const bool gu = unit < n_gu;
-    const size_t local = gu ? unit : unit - n_gu;
-    const int n_span = (gu ? d : f) / kMxSpan;
-    const int group = (int)(local / n_span), span = (int)(local % n_span);
-    uint8_t* dst = out + unit * kMxUnitBytes;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const MxMatrix& m = gu ? (half ? up : gate) : down;
-        const long long row = gu ? (long long)group * 8 + g : (long long)group * 16 + half * 8 + g;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(m.codes + ((size_t)row * n_span + span) * (kMxSpan / 2));
-        reinterpret_cast<uint4*>(dst + half * 512)[lane] = make_uint4(src[t], src[4 + t], src[8 + t], src[12 + t]);
-        if (t == 0)
-            *reinterpret_cast<uint32_t*>(dst + kMxUnitScales + (half * 8 + g) * 4) =
-                *reinterpret_cast<const uint32_t*>(m.scales + mx_scale_word(row, span, n_span));
+    const BlockPlace at = block_place(blockIdx.x, d, f);
+    const MxMatrix m = at.matrix == 0 ? gate : at.matrix == 1 ? up : down;
+    const int K = at.matrix == 2 ? f : d, n_span = K / kMxSpan;
+    uint8_t* dst = out + (size_t)blockIdx.x * kMxBlockBytes;
+    for (int i = threadIdx.x; i < 128 * 8; i += kQuantThreads) {
+        const int r = i >> 3, ch = i & 7, col = at.chunk * kMxChunk + ch * 32;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (col < K) v = *reinterpret_cast<const uint4*>(m.codes + (size_t)(at.tile * 128 + r) * (K / 2) + col / 2);
+        *reinterpret_cast<uint4*>(dst + r * 128 + ((ch ^ (r & 7)) << 4)) = v;
+    }
+    for (int i = threadIdx.x; i < 2 * kMxPiece / 16; i += kQuantThreads) {
+        const int span = at.chunk * 2 + i / (kMxPiece / 16);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (span < n_span)
+            v = reinterpret_cast<const uint4*>(m.scales + ((size_t)at.tile * n_span + span) * kMxPiece)[i % (kMxPiece / 16)];
+        reinterpret_cast<uint4*>(dst + kMxBlockCodes)[i] = v;
     }
 }
 
@@ -220,23 +232,20 @@ static uint8_t host_quantize_block(const uint16_t* x, uint8_t* codes16) {
 
 // The slot layout of one expert from bf16 matrices in host memory (see mx_pack_kernel).
 void mx_pack_expert_host(const uint16_t* gate, const uint16_t* up, const uint16_t* down, int d, int f, uint8_t* out) {
-    const size_t n_gu = mx_gate_up_units(d, f), n_all = n_gu + mx_down_units(d, f);
-    for (size_t unit = 0; unit < n_all; ++unit) {
-        const bool gu = unit < n_gu;
-        const size_t local = gu ? unit : unit - n_gu;
-        const int n_span = (gu ? d : f) / kMxSpan, K = gu ? d : f;
-        const size_t group = local / n_span, span = local % n_span;
-        uint8_t* dst = out + unit * kMxUnitBytes;
-        for (int r = 0; r < 16; ++r) {
-            const uint16_t* m = gu ? (r < 8 ? gate : up) : down;
-            const size_t row = gu ? group * 8 + (r & 7) : group * 16 + r;
-            for (int b = 0; b < 4; ++b) {
-                uint8_t codes[16];
-                dst[kMxUnitScales + r * 4 + b] = host_quantize_block(m + row * K + span * kMxSpan + b * kMxBlock, codes);
-                for (int t = 0; t < 4; ++t)
-                    memcpy(dst + (r >> 3) * 512 + ((r & 7) * 4 + t) * 16 + b * 4, codes + t * 4, 4);
+    const size_t n = mx_gate_up_blocks(d, f) + mx_down_blocks(d, f);
+    memset(out, 0, n * kMxBlockBytes);
+    for (size_t block = 0; block < n; ++block) {
+        const BlockPlace at = block_place(block, d, f);
+        const uint16_t* m = at.matrix == 0 ? gate : at.matrix == 1 ? up : down;
+        const int K = at.matrix == 2 ? f : d;
+        uint8_t* dst = out + block * kMxBlockBytes;
+        for (int r = 0; r < 128; ++r)
+            for (int ch = 0; ch < 8; ++ch) {
+                const int col = at.chunk * kMxChunk + ch * 32;
+                if (col >= K) break;
+                dst[kMxBlockCodes + (ch >> 2) * kMxPiece + (r & 31) * 16 + (r >> 5) * 4 + (ch & 3)] =
+                    host_quantize_block(m + (size_t)(at.tile * 128 + r) * K + col, dst + r * 128 + ((ch ^ (r & 7)) << 4));
             }
-        }
     }
 }
 
@@ -317,12 +326,11 @@ int saem_mx_pack_expert(const saem_config* cfg, const void* gate_codes, const vo
         if (!q) return SAEM_ERR_INVALID_ARG;
     for (const void* q : p)
         if ((uintptr_t)q & 15) return SAEM_ERR_ALIGNMENT;
-    const size_t units = mx_gate_up_units(cfg->d_model, cfg->d_ff) + mx_down_units(cfg->d_model, cfg->d_ff);
-    const int per_cta = kQuantThreads / 32;
+    const size_t blocks = mx_gate_up_blocks(cfg->d_model, cfg->d_ff) + mx_down_blocks(cfg->d_model, cfg->d_ff);
     const MxMatrix g = {(const uint8_t*)gate_codes, (const uint8_t*)gate_scales};
     const MxMatrix u = {(const uint8_t*)up_codes, (const uint8_t*)up_scales};
     const MxMatrix d = {(const uint8_t*)down_codes, (const uint8_t*)down_scales};
-    return launch_pdl(mx_pack_kernel, dim3((unsigned)((units + per_cta - 1) / per_cta)), dim3(kQuantThreads), 0,
+    return launch_pdl(mx_pack_kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0,
                       (cudaStream_t)stream, g, u, d, cfg->d_model, cfg->d_ff, (uint8_t*)packed_out) == cudaSuccess
                ? SAEM_OK : SAEM_ERR_CUDA;
 }

@@ -1,0 +1,35 @@
+// The block-scaled tensor-core instructions of the 4-bit kernels (tcgen05 kind::mxf4).
+#ifndef SAEM_MX_TC_CUH_
+#define SAEM_MX_TC_CUH_
+
+#include "mx_common.cuh"
+#include "tc_common.cuh"
+
+namespace saem {
+
+// Shared-memory matrix descriptor of a 512-byte scale piece for tcgen05.cp: no swizzle, 16-byte rows, 8-row groups 128
+// bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (8ull << 16) | (8ull << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void tc_cp_scales(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void tc_mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                            uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// Instruction descriptor of kind::mxf4: E2M1 x E2M1, K-major, UE8M0 scales, M = 128, N = n; `id` (0 or 2) selects the
+// upper or lower two scales of a 32-bit column for both operands.
+__device__ __forceinline__ uint32_t idesc_mxf4(int n, int id) {
+    return ((uint32_t)id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | (1u << 27) |
+           ((uint32_t)id << 29);
+}
+
+}  // namespace saem
+
+#endif  // SAEM_MX_TC_CUH_

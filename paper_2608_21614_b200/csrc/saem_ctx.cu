@@ -44,7 +44,7 @@ WorkspaceLayout workspace_layout(const saem_config& c) {
     L.status = take(256);
     L.counters = take(sizeof(int) * (2 * kMaxCtas + 16));
     L.decode_sync = take(sizeof(int) * kDecodeSyncInts);
-    L.h = take(c.ffn_path == SAEM_FFN_MX ? mx_workspace_bytes((long long)R, c.d_model, c.d_ff) : R * f * 2);
+    L.h = take(c.ffn_path == SAEM_FFN_MX ? mx_workspace_bytes(c.max_tokens, c.top_k, c.n_experts, c.n_shared, c.d_model, c.d_ff) : R * f * 2);
     {   // split-K partial tiles of the streaming kernels: token tiles of at most 64 rows, two slots per CTA
         size_t small_tile = (size_t)2 * (nt < 64 ? nt : 64) * kTileRows;
         L.partials = take((size_t)kMaxCtas * 2 * small_tile * sizeof(float));
@@ -113,7 +113,7 @@ const char* saem_status_string(int s) {
 size_t saem_slot_bytes(const saem_config* c) {
     if (validate_config(c) != SAEM_OK) return 0;
     if (c->ffn_path == SAEM_FFN_MX)
-        return (mx_gate_up_units(c->d_model, c->d_ff) + mx_down_units(c->d_model, c->d_ff)) * kMxUnitBytes;
+        return (mx_gate_up_blocks(c->d_model, c->d_ff) + mx_down_blocks(c->d_model, c->d_ff)) * kMxBlockBytes;
     return (size_t)3 * c->d_model * c->d_ff * 2;
 }
 
@@ -385,7 +385,7 @@ int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t*
     a.slot_bytes = c->slot_bytes;
     a.slot_region_bytes = c->slot_bytes * (size_t)(c->n_fixed_slots + c->cfg.temp_slots);
     a.h = (uint16_t*)(c->ws + c->lay.h);
-    a.h_rows = g.max_tokens * (g.top_k + g.n_shared);
+    a.tokens = (max_rows + g.top_k + g.n_shared - 1) / (g.top_k + g.n_shared);
     a.y_packed = y_packed;
     a.status = (int*)(c->ws + c->lay.status);
     a.counters = (int*)(c->ws + c->lay.counters);
@@ -415,8 +415,7 @@ int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t*
     }
     int nl = 0;
     if (g.ffn_path == SAEM_FFN_MX) {
-        // tiles as high as the longest segment of a step of this many rows; longer ones take several tiles
-        CUDA_TRY(launch_mx_ffn(a, tab, (max_rows + g.top_k + g.n_shared - 1) / (g.top_k + g.n_shared), st, &nl));
+        CUDA_TRY(launch_mx_ffn(a, tab, st, &nl));
     } else if (g.ffn_path == SAEM_FFN_SCALAR) {
         CUDA_TRY(launch_ffn_scalar(a, tab, st, &nl));
     } else if (gemv_path) {

@@ -121,7 +121,7 @@ struct FfnArgs {
     size_t slot_bytes;
     size_t slot_region_bytes;   // whole region (every slot)
     uint16_t* h;                // [max_rows, f] bf16 workspace
-    int h_rows;                 // rows the workspace was made for
+    int tokens;                 // tokens of a step with max_rows rows (SAEM_FFN_MX: sizes the row tiles)
     float* y_packed;            // [max_rows, d]
     int* status;
     int* counters;              // [2 * kMaxCtas + 16]
@@ -135,11 +135,10 @@ struct FfnArgs {
 };
 cudaError_t launch_ffn_scalar(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
 cudaError_t launch_ffn_tensor(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
-// Microscaled 4-bit experts (SAEM_FFN_MX contexts, mx_moe.cu); a.h is a workspace of mx_workspace_bytes there, and row
-// tiles are made for segments of max_segment rows.
-size_t mx_workspace_bytes(long long rows, int d, int f);
-cudaError_t launch_mx_ffn(const FfnArgs& a, const SlotTable& tab, int max_segment, cudaStream_t st, int* n_launch);
-// The whole step over such experts for up to 8 tokens in two launches.
+// Microscaled 4-bit experts (SAEM_FFN_MX contexts, mx_moe.cu); a.h is a workspace of mx_workspace_bytes there.
+size_t mx_workspace_bytes(int max_tokens, int k, int E, int S, int d, int f);
+cudaError_t launch_mx_ffn(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
+// The whole step over such experts for up to 8 tokens in two launches (mx_few.cu).
 struct MxFewArgs {
     const float* logits;        // [T, E]
     const uint16_t* x;          // [T, d]
@@ -152,7 +151,7 @@ struct MxFewArgs {
     int32_t* topk_idx;
     float* topk_w;
     int* status;
-    int groups_a, chunk_b;      // set by the launcher
+    int stages_a, stages_b, split_b;   // set by the launcher
 };
 bool mx_few_supported(int T, int k, int d);
 cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStream_t st, int* n_launch);

@@ -23,7 +23,8 @@ def test_sizes_and_host_side_refusals():
     assert B.saem_mx_scales_bytes(129, 129) == 4 * 512
     assert B.saem_mx_linear_workspace_bytes(3, 33) >= 256 + 96 + 512
     cfg = B.make_config(256, 384, 8, 2, 4, ffn_path=B.SAEM_FFN_MX)
-    assert B.saem_slot_bytes(cfg) == 3 * 256 * 384 * 17 // 32
+    assert B.saem_slot_bytes(cfg) == (3 * 1 * 2 + 2 * 2) * 17408                # blocks of 128 x 256: gate and up, then down
+    assert B.saem_slot_bytes(B.make_config(2048, 768, 128, 8, 8, ffn_path=B.SAEM_FFN_MX)) == 3 * 2048 * 768 * 17 // 32
     assert B.saem_slot_bytes(B.make_config(256, 384, 8, 2, 4, ffn_path=6)) == 0
     P = 4096                                                                    # an address that is never read
     code = lambda f, *a: f(*a, stream=0, check=False)                          # noqa: E731
@@ -82,19 +83,26 @@ def test_host_packer_holds_the_quantised_matrices(d, f):
     cfg = B.make_config(d, f, 1, 1, 4, ffn_path=B.SAEM_FFN_MX)
     packed = np.zeros(B.saem_slot_bytes(cfg), np.uint8)
     B.saem_pack_expert_host(cfg, *mats, packed)
-    units = packed.reshape(-1, 1088)
-    n_gu = (f // 8) * (d // 128)
-    for name, m, local in (("gate", mats[0], 0), ("up", mats[1], 1), ("down", mats[2], 2)):
+    blocks = packed.reshape(-1, 17408)
+    chunks = lambda n: (n + 255) // 256                                          # noqa: E731
+    n_gu = (f // 128) * chunks(d) * 2
+    assert len(blocks) == n_gu + (d // 128) * chunks(f)
+    for which, m in enumerate(mats):
         _, codes, scales = quantize(gen.bf16_bits_to_f32(m))
-        span_n = m.shape[1] // 128
+        K = m.shape[1]
         for row in range(m.shape[0]):
-            for span in range(span_n):
-                u, r = (((row // 8) * span_n + span, row % 8 + 8 * local) if local < 2 else (n_gu + (row // 16) * span_n + span, row % 16))
-                words = units[u][(r // 8) * 512:(r // 8) * 512 + 512].reshape(8, 4, 4, 4)[r % 8]   # [t][b][byte]
-                got = words.transpose(1, 0, 2).reshape(-1)                       # block b, elements 8 t ..
-                want = codes[row, span * 128:(span + 1) * 128]
-                assert np.array_equal(got & 15, want[0::2]) and np.array_equal(got >> 4, want[1::2]), (name, row, span)
-                assert np.array_equal(units[u][1024 + 4 * r:1028 + 4 * r], scales[row, 4 * span:4 * span + 4]), (name, row, span)
+            tile, r = divmod(row, 128)
+            for c in range(chunks(K)):
+                b = blocks[(tile * chunks(K) + c) * 2 + which] if which < 2 else blocks[n_gu + tile * chunks(K) + c]
+                want = np.zeros(256, np.int64)
+                part = codes[row, c * 256:(c + 1) * 256]
+                want[:len(part)] = part
+                got = b[r * 128:(r + 1) * 128].reshape(8, 16)[np.arange(8) ^ (r & 7)].reshape(-1)
+                assert np.array_equal(got & 15, want[0::2]) and np.array_equal(got >> 4, want[1::2]), (which, row, c)
+                s = np.zeros(8, np.int64)
+                s[:len(part) // 32] = scales[row, c * 8:(c + 1) * 8]
+                piece = b[16384:].reshape(2, 512)[:, (r % 32) * 16 + (r // 32) * 4:][:, :4]
+                assert np.array_equal(piece.reshape(-1), s), (which, row, c)
 
 
 def test_scale_offsets_cover_a_piece_once():

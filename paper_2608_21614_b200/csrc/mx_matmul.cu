@@ -123,8 +123,9 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 mbar_wait(smem_u32(&bar_full[(q - s0) % p.n_stage]), ((q - s0) / p.n_stage) & 1, abort_p, status);
                 abort_flag = 1;
             }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
+        const uint32_t on = elect_one();
         for (int s = s0; s < s1; ++s) {
             const int it = s - s0, i = it % p.n_stage;
             if (!mbar_wait(smem_u32(&bar_full[i]), (it / p.n_stage) & 1, abort_p, status)) break;
@@ -133,18 +134,19 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t tw = tmem_sf + i * sf_cols, ta = tw + 8;
             const int spans = min(2, n_span - 2 * s);
             for (int h = 0; h < spans; ++h) {
-                tc_cp_scales(tw + 4 * h, smem_desc_scales(sf + h * kMxPiece));
+                tc_cp_scales(on, tw + 4 * h, smem_desc_scales(sf + h * kMxPiece));
                 for (int q = 0; q < p.pieces; ++q)
-                    tc_cp_scales(ta + 4 * (h * p.pieces + q), smem_desc_scales(sf + ((1 + q) * 2 + h) * kMxPiece));
+                    tc_cp_scales(on, ta + 4 * (h * p.pieces + q), smem_desc_scales(sf + ((1 + q) * 2 + h) * kMxPiece));
             }
             const int steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
             const uint64_t dw = smem_desc_sw128(st), da = smem_desc_sw128(st + w_bytes);
-            for (int j = 0; j < steps; ++j)
-                tc_mma_mxf4(tmem, dw + 2 * j, da + 2 * j, idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < steps) tc_mma_mxf4(on, tmem, dw + 2 * j, da + 2 * j, idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
                             ta + 4 * (j >> 1) * p.pieces, s > s0 || j > 0);
-            tc_commit(smem_u32(&bar_empty[i]));
+            if (on) tc_commit(smem_u32(&bar_empty[i]));
         }
-        tc_commit(smem_u32(&bar_acc));
+        if (on) tc_commit(smem_u32(&bar_acc));
     }
     __syncwarp();
 

@@ -298,8 +298,9 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                 mbar_wait(smem_u32(&bar_full[q % F::kStages]), (q / F::kStages) & 1, abort_p, a.status);
                 abort_flag = 1;
             }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
+        const uint32_t on = elect_one();
         int it = 0, n = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
@@ -321,22 +322,23 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                     if (2 * h >= steps) break;
 #pragma unroll
                     for (int m = 0; m < (MODE == 0 ? 2 : 1); ++m)
-                        tc_cp_scales(sf + m * 8 + 4 * h, smem_desc_scales(wb + m * kMxBlockBytes + kMxBlockCodes + h * kMxPiece));
+                        tc_cp_scales(on, sf + m * 8 + 4 * h, smem_desc_scales(wb + m * kMxBlockBytes + kMxBlockCodes + h * kMxPiece));
 #pragma unroll
                     for (int q = 0; q < T::kPieces; ++q)
-                        tc_cp_scales(sfx + 4 * (h * T::kPieces + q), smem_desc_scales(xb + T::kN * 128 + (q * 2 + h) * kMxPiece));
+                        tc_cp_scales(on, sfx + 4 * (h * T::kPieces + q), smem_desc_scales(xb + T::kN * 128 + (q * 2 + h) * kMxPiece));
                 }
                 const uint64_t dx = smem_desc_sw128(xb);
 #pragma unroll
                 for (int m = 0; m < (MODE == 0 ? 2 : 1); ++m) {
                     const uint64_t dw = smem_desc_sw128(wb + m * kMxBlockBytes);
-                    for (int j = 0; j < steps; ++j)
-                        tc_mma_mxf4(acc + m * T::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(T::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1),
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < steps) tc_mma_mxf4(on, acc + m * T::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(T::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1),
                                     sfx + 4 * (j >> 1) * T::kPieces, c > 0 || j > 0);
                 }
-                tc_commit(smem_u32(&bar_empty[st]));
+                if (on) tc_commit(smem_u32(&bar_empty[st]));
             }
-            tc_commit(smem_u32(&bar_acc[set]));
+            if (on) tc_commit(smem_u32(&bar_acc[set]));
             ++n;
         }
     } else if (warp >= 2) {

@@ -22,7 +22,7 @@
 namespace saem {
 
 constexpr int kPlanes = 6;
-constexpr int kMoeThreads = 192;            // warp 0: copies, warp 1: MMA issue, warps 2-5: epilogue
+constexpr int kMoeThreads = 320;            // warp 0: copies, warp 1: MMA issue, warps 2-5 and 6-9: epilogue
 constexpr int kMoeMaxStages = 8;
 
 template <int R>
@@ -217,6 +217,43 @@ __device__ __forceinline__ void plane_sums(uint32_t taddr, float (&v)[8]) {
     }
 }
 
+// Eight rows' hidden units of one block (a lane holds one unit of each row) to the planes of tile columns r0 .. r0 + 7.
+template <int R>
+__device__ __forceinline__ void store_planes(float (&v)[8], int r0, int rows, uint8_t* dst, int blk, int lane) {
+    using T = TileShape<R>;
+    const int mine = r0 + (lane & 7);                                          // the row whose codes this lane stores
+    for (int p = 0; p < kPlanes; ++p) {
+        uint32_t w = 0, bytes = 0;
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) {                                       // two rows share a conversion
+            int sb[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                sb[z] = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q + z]) & 0x7FFFFFFFu));
+                if ((lane & 7) == q + z) bytes = (uint32_t)sb[z];
+            }
+            uint32_t code = encode2(v[q] * inverse_power(min(sb[0], 254)), v[q + 1] * inverse_power(min(sb[1], 254)));
+            const float2 back = decode2((uint16_t)code);
+            v[q] = sb[0] == 255 ? 0.f : v[q] - back.x * power_of_two(sb[0]);   // what is left: exact in fp32
+            v[q + 1] = sb[1] == 255 ? 0.f : v[q + 1] - back.y * power_of_two(sb[1]);
+            w |= code << (4 * q);                                              // codes under a NaN scale do not matter
+        }
+        // eight rows' codes of one unit to eight units' codes of one row: a transposition over eight lanes
+#pragma unroll
+        for (int s = 4; s > 0; s >>= 1) {
+            const uint32_t low = s == 4 ? 0x0000FFFFu : s == 2 ? 0x00FF00FFu : 0x0F0F0F0Fu;
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, w, s);
+            w = lane & s ? (w & ~low) | ((o >> (4 * s)) & low) : (w & low) | ((o << (4 * s)) & ~low);
+        }
+        const int col = p * R + mine;
+        if (mine < rows) {
+            *reinterpret_cast<uint32_t*>(dst + col * 128 + ((blk ^ (col & 7)) << 4) + (lane >> 3) * 4) = w;
+            if (lane < 8)
+                dst[T::kN * 128 + ((col >> 7) * 2 + (blk >> 2)) * kMxPiece + (col & 31) * 16 + ((col >> 5) & 3) * 4 + (blk & 3)] = (uint8_t)bytes;
+        }
+    }
+}
+
 template <int MODE, int R>
 __global__ void __launch_bounds__(kMoeThreads, 1)
 mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTable tab) {
@@ -238,7 +275,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bar_acc[i]), 1);
-            mbar_init(smem_u32(&bar_free[i]), 4);
+            mbar_init(smem_u32(&bar_free[i]), F::kSets == 2 ? 4 : 8);
         }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -343,20 +380,23 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
         }
     } else if (warp >= 2) {
         // ---------------------------------------------------------------- epilogue
-        const int quad = warp & 3;
+        // Two groups of four warps (one per quarter of the lanes): with two sets of accumulators each group has its own
+        // set, i.e. every other item; with one set they share the rows of every item.
+        const int quad = warp & 3, group = (warp - 2) >> 2;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         int n = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < total; i += gridDim.x) {
             const Item t = item_at(i);
             if (tab.slot[t.e] < 0) continue;
-            const int set = n % F::kSets;
-            ok = ok && mbar_wait(smem_u32(&bar_acc[set]), (n / F::kSets) & 1, abort_p, a.status);
+            const int set = n % F::kSets, turn = n / F::kSets;
+            ++n;
+            if (F::kSets == 2 && set != group) continue;
+            ok = ok && mbar_wait(smem_u32(&bar_acc[set]), turn & 1, abort_p, a.status);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             const uint32_t acc = tmem + set * F::kAccCols + lane_base;
-            ++n;
-            for (int r0 = 0; r0 < t.rows && ok; r0 += 8) {
+            for (int r0 = F::kSets == 2 ? 0 : 8 * group; r0 < t.rows && ok; r0 += F::kSets == 2 ? 8 : 16) {
                 float v[8];
                 plane_sums<R>(acc + r0, v);
                 if (MODE == 1) {
@@ -367,38 +407,10 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                     float u[8];
                     plane_sums<R>(acc + T::kN + r0, u);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = v[q] / (1.f + expf(-v[q])) * u[q];
+                    for (int q = 0; q < 8; ++q) v[q] = v[q] / (1.f + __expf(-v[q])) * u[q];
                     // the warp's 32 hidden units are one block of each row: chunk gb / 2 of the row, block (gb & 1) * 4 + quad
                     uint8_t* dst = a.h_tiles + ((size_t)t.tile * mx_chunks(a.f) + (t.gb >> 1)) * T::kBytes;
-                    const int blk = (t.gb & 1) * 4 + quad;
-                    for (int p = 0; p < kPlanes; ++p) {
-#pragma unroll
-                        for (int q = 0; q < 8; q += 2) {                       // two rows share a conversion
-                            int sb[2];
-#pragma unroll
-                            for (int z = 0; z < 2; ++z)
-                                sb[z] = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q + z]) & 0x7FFFFFFFu));
-                            uint16_t code = encode2(v[q] * inverse_power(min(sb[0], 254)), v[q + 1] * inverse_power(min(sb[1], 254)));
-                            const float2 back = decode2(code);
-#pragma unroll
-                            for (int z = 0; z < 2; ++z) {
-                                const bool finite = sb[z] != 255;
-                                v[q + z] = finite ? v[q + z] - (z ? back.y : back.x) * power_of_two(sb[z]) : 0.f;
-                                // eight lanes' codes meet in a word, four words are the block
-                                uint32_t w = finite ? (uint32_t)((code >> (4 * z)) & 15) << (4 * (lane & 7)) : 0u;
-                                w |= __shfl_xor_sync(0xffffffffu, w, 1);
-                                w |= __shfl_xor_sync(0xffffffffu, w, 2);
-                                w |= __shfl_xor_sync(0xffffffffu, w, 4);
-                                const int col = p * R + r0 + q + z;
-                                if (r0 + q + z >= t.rows) continue;
-                                if ((lane & 7) == 0)
-                                    *reinterpret_cast<uint32_t*>(dst + col * 128 + ((blk ^ (col & 7)) << 4) + (lane >> 3) * 4) = w;
-                                if (lane == 0)
-                                    dst[T::kN * 128 + ((col >> 7) * 2 + (t.gb & 1)) * kMxPiece + (col & 31) * 16 + ((col >> 5) & 3) * 4 + quad] =
-                                        (uint8_t)sb[z];
-                            }
-                        }
-                    }
+                    store_planes<R>(v, r0, t.rows, dst, (t.gb & 1) * 4 + quad, lane);
                 }
             }
             tc_fence_before();

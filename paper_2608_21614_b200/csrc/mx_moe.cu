@@ -60,7 +60,7 @@ __device__ __forceinline__ void read_segments(Segments& s, const int32_t* offset
     int v = 0;
     if (threadIdx.x < SAEM_MAX_EXPERTS) {
         const int e = threadIdx.x;
-        int lo = 0, hi = 0;
+        int lo = max_rows, hi = max_rows;                                      // what is beyond E starts behind the last row
         if (e < E) {
             lo = offsets ? offsets[e] : 0;
             hi = offsets ? offsets[e + 1] : max_rows;
@@ -115,31 +115,25 @@ __device__ __forceinline__ float2 decode2(uint16_t b) {
     return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// x's packed rows to tiles: one warp per row x 256 elements, eight elements per lane, four lanes per block.
+// x to tiles: one warp per token x 256 elements, eight elements per lane, four lanes per block.  The planes are made once
+// and stored in the token's k + S rows (inv_perm; the always-on experts' segments behind them).  inv_perm nullptr: x holds
+// packed rows already (k = 1, S = 0).
 template <int R>
 __global__ void __launch_bounds__(256)
-mx_tile_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ offsets, int max_rows, int E, int K, int most,
-               uint8_t* __restrict__ tiles, int* __restrict__ status) {
-    using T = TileShape<R>;
+mx_tile_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ inv_perm, const int32_t* __restrict__ offsets, int T, int k,
+               int S, int E, int K, int most, uint8_t* __restrict__ tiles, int* __restrict__ status) {
+    using Ts = TileShape<R>;
     __shared__ Segments s;
     pdl_wait();
     pdl_launch_dependents();
-    read_segments<R>(s, offsets, E, max_rows, most, status);
+    read_segments<R>(s, offsets, E, T * (k + S), most, status);
     const int lane = threadIdx.x & 31, nc = mx_chunks(K);
-    const long long total = (long long)max_rows * nc;
+    const long long total = (long long)T * nc;
     for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += (long long)gridDim.x * 8) {
-        const int row = (int)(i / nc), c = (int)(i - (long long)row * nc);
-        int e = -1;                                                          // the segment that holds the row
-        for (int q = lane; q < E; q += 32)
-            if (row >= s.start[q] && row < s.start[q] + s.rows[q]) e = q;
-        e = __reduce_max_sync(0xffffffffu, e);
-        if (e < 0) continue;                                                 // rows of dropped pairs
-        const int local = row - s.start[e], tile = s.tile0[e] + local / R, r = local % R;
-        uint8_t* dst = tiles + ((size_t)tile * nc + c) * T::kBytes;
-        const int col = c * kMxChunk + lane * 8;
+        const int t = (int)(i / nc), c = (int)(i - (long long)t * nc), col = c * kMxChunk + lane * 8;
         float v[8];
         if (col < K) {
-            const uint4 q = *reinterpret_cast<const uint4*>(x + (size_t)row * K + col);
+            const uint4 q = *reinterpret_cast<const uint4*>(x + (size_t)t * K + col);
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -150,6 +144,7 @@ mx_tile_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ offse
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = 0.f;
         }
+        uint32_t codes[kPlanes], scales[kPlanes];
 #pragma unroll
         for (int p = 0; p < kPlanes; ++p) {
             uint32_t m = 0;
@@ -162,23 +157,49 @@ mx_tile_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ offse
             float u[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[j] = v[j] * up;
-            const uint32_t w = sb == 255 ? 0u : mx_encode8(u);
+            codes[p] = sb == 255 ? 0u : mx_encode8(u);
             uint32_t h[4];
-            mx_decode8(w, h);
+            mx_decode8(codes[p], h);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {                                    // what is left: exact in fp32
                 const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[j]));
                 v[2 * j] = sb == 255 ? 0.f : v[2 * j] - f.x * down;
                 v[2 * j + 1] = sb == 255 ? 0.f : v[2 * j + 1] - f.y * down;
             }
-            const int col_n = p * R + r;
-            *reinterpret_cast<uint32_t*>(dst + col_n * 128 + (((lane >> 2) ^ (col_n & 7)) << 4) + (lane & 3) * 4) = w;
             uint32_t word = (uint32_t)sb << (((lane >> 2) & 3) * 8);
             word |= __shfl_xor_sync(0xffffffffu, word, 4);
             word |= __shfl_xor_sync(0xffffffffu, word, 8);
-            if ((lane & 15) == 0)
-                *reinterpret_cast<uint32_t*>(dst + T::kN * 128 + ((col_n >> 7) * 2 + (lane >> 4)) * kMxPiece + (col_n & 31) * 16 +
-                                             ((col_n >> 5) & 3) * 4) = word;
+            scales[p] = word;
+        }
+        for (int j0 = 0; j0 < k + S; j0 += 32) {
+            int place = -1;                                                  // tile * R + row of the tile, of this lane's copy
+            const int j = j0 + lane;
+            if (j < k + S) {
+                const int row = j >= k ? T * k + (j - k) * T + t : inv_perm ? inv_perm[t * k + j] : t;
+                if (row >= 0) {
+                    int e = 0;
+#pragma unroll
+                    for (int step = 64; step > 0; step >>= 1)                // the last segment that starts at or before the row
+                        if (s.start[e + step] <= row) e += step;
+                    const int local = row - s.start[e];
+                    if (local < s.rows[e]) place = (s.tile0[e] + local / R) * R + local % R;
+                }
+            }
+            const int now = min(32, k + S - j0);
+            for (int q = 0; q < now; ++q) {
+                const int at = __shfl_sync(0xffffffffu, place, q);
+                if (at < 0) continue;                                        // a dropped pair
+                const int r = at % R;
+                uint8_t* dst = tiles + ((size_t)(at / R) * nc + c) * Ts::kBytes;
+#pragma unroll
+                for (int p = 0; p < kPlanes; ++p) {
+                    const int n = p * R + r;
+                    *reinterpret_cast<uint32_t*>(dst + n * 128 + (((lane >> 2) ^ (n & 7)) << 4) + (lane & 3) * 4) = codes[p];
+                    if ((lane & 15) == 0)
+                        *reinterpret_cast<uint32_t*>(dst + Ts::kN * 128 + ((n >> 7) * 2 + (lane >> 4)) * kMxPiece + (n & 31) * 16 +
+                                                     ((n >> 5) & 3) * 4) = scales[p];
+                }
+            }
         }
     }
 }
@@ -447,7 +468,7 @@ size_t mx_workspace_bytes(int max_tokens, int k, int E, int S, int d, int f) {
 }
 
 template <int R>
-static cudaError_t launch_tiles(const FfnArgs& f, const SlotTable& tab, cudaStream_t st) {
+static cudaError_t launch_tiles(const FfnArgs& f, const MxTokens& x, const SlotTable& tab, cudaStream_t st) {
     static bool done[64];
     using A = FfnShape<0, R>;
     using B = FfnShape<1, R>;
@@ -462,9 +483,10 @@ static cudaError_t launch_tiles(const FfnArgs& f, const SlotTable& tab, cudaStre
     MoeArgs a = {};
     a.tiles = x_tiles; a.offsets = f.offsets; a.max_rows = f.max_rows; a.E = f.E; a.d = f.d; a.f = f.f; a.most = most;
     a.slot_region = f.slot_region; a.slot_bytes = f.slot_bytes; a.h_tiles = h_tiles; a.y = f.y_packed; a.status = f.status;
-    const long long tasks = (long long)f.max_rows * mx_chunks(f.d), ctas = (tasks + 7) / 8, wave = (long long)f.n_sm * 8;
-    e = launch_pdl(mx_tile_kernel<R>, dim3((unsigned)(ctas < wave ? ctas : wave)), dim3(256), 0, st, f.x_packed, f.offsets, f.max_rows, f.E, f.d,
-                   most, x_tiles, f.status);
+    const int T = x.inv_perm ? x.T : f.max_rows, k = x.inv_perm ? x.k : 1, S = x.inv_perm ? x.S : 0;
+    const long long tasks = (long long)T * mx_chunks(f.d), ctas = (tasks + 7) / 8, wave = (long long)f.n_sm * 8;
+    e = launch_pdl(mx_tile_kernel<R>, dim3((unsigned)(ctas < wave ? ctas : wave)), dim3(256), 0, st, f.x_packed, x.inv_perm, f.offsets, T, k, S,
+                   f.E, f.d, most, x_tiles, f.status);
     if (e != cudaSuccess) return e;
     e = launch_pdl(mx_ffn_kernel<0, R>, dim3((unsigned)f.n_sm), dim3(kMoeThreads), (size_t)A::kSmem, st, a, tab);
     if (e != cudaSuccess) return e;
@@ -472,9 +494,9 @@ static cudaError_t launch_tiles(const FfnArgs& f, const SlotTable& tab, cudaStre
     return launch_pdl(mx_ffn_kernel<1, R>, dim3((unsigned)f.n_sm), dim3(kMoeThreads), (size_t)B::kSmem, st, a, tab);
 }
 
-cudaError_t launch_mx_ffn(const FfnArgs& f, const SlotTable& tab, cudaStream_t st, int* n_launch) {
+cudaError_t launch_mx_ffn(const FfnArgs& f, const MxTokens& x, const SlotTable& tab, cudaStream_t st, int* n_launch) {
     const int R = tile_rows(f.tokens, f.max_rows / (f.tokens > 0 ? f.tokens : 1), f.E);
-    const cudaError_t e = R == 8 ? launch_tiles<8>(f, tab, st) : R == 16 ? launch_tiles<16>(f, tab, st) : launch_tiles<32>(f, tab, st);
+    const cudaError_t e = R == 8 ? launch_tiles<8>(f, x, tab, st) : R == 16 ? launch_tiles<16>(f, x, tab, st) : launch_tiles<32>(f, x, tab, st);
     if (e == cudaSuccess) *n_launch += 3;
     return e;
 }

@@ -12,7 +12,7 @@
 // shared memory (only CTA 0 writes the index outputs) and then copies its share of the rows, so
 // the whole repack is one launch.  Larger problems: the index phase runs on one CTA per 1024 pairs in
 // two passes (per-block histograms and ranks; offsets and scatter), then a grid-wide gather.
-#include "saem_internal.h"
+#include "route_row.cuh"
 
 namespace saem {
 
@@ -166,6 +166,43 @@ repack_fused_kernel(const int32_t* __restrict__ idx, const uint16_t* __restrict_
         copy_row(x + (size_t)(r % T) * d, x_packed + (size_t)(P + r) * d, d, threadIdx.x & 127, 128);
 }
 
+// Gate and index phase of a small batch in one CTA: a warp per token in turn, then the counting sort of their choices
+// (the same functions, so the same outputs, as route_kernel and the index phase of repack_fused_kernel).
+__global__ void __launch_bounds__(kRepackThreads)
+route_index_kernel(const float* __restrict__ logits, int T, int E, int S, int k, int renorm, int32_t* __restrict__ idx,
+                   float* __restrict__ w, int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm,
+                   int32_t* __restrict__ inv_perm, int* __restrict__ status) {
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int P = T * k, n_chunks = (P + 31) >> 5, lane = threadIdx.x & 31;
+    RepackSmem& sm = *reinterpret_cast<RepackSmem*>(smem_raw);
+    uint16_t* table = reinterpret_cast<uint16_t*>(smem_raw + sizeof(RepackSmem));
+    size_t off = sizeof(RepackSmem) + (((size_t)table_stride(n_chunks) * E * 2 + 15) & ~(size_t)15);
+    int32_t* perm_s = reinterpret_cast<int32_t*>(smem_raw + off);
+    int32_t* idx_s = perm_s + n_chunks * 32;
+    float* w_s = reinterpret_cast<float*>(idx_s + n_chunks * 32);
+    uint8_t* rank = reinterpret_cast<uint8_t*>(w_s + n_chunks * 32);
+    for (int i = threadIdx.x; i < n_chunks * 32; i += blockDim.x) perm_s[i] = -1;
+    for (int t = threadIdx.x >> 5; t < T; t += blockDim.x >> 5) route_row(logits + (size_t)t * E, E, k, renorm, lane, idx_s + t * k, w_s + t * k);
+    __syncthreads();
+    for (int i = threadIdx.x; i < P; i += blockDim.x) {
+        idx[i] = idx_s[i];
+        w[i] = w_s[i];
+    }
+    index_phase(idx_s, P, E, S, T, sm, table, rank, perm_s, true, counts, offsets, perm, inv_perm, status);
+}
+
+bool route_index_supported(int T, int k) { return T <= kRouteIndexTokens && T * k <= 1024; }
+
+cudaError_t launch_route_index(const float* logits, int T, int E, int S, int k, int renorm, int32_t* idx, float* w, int32_t* counts,
+                               int32_t* offsets, int32_t* perm, int32_t* inv_perm, int* status, cudaStream_t st) {
+    const int n_chunks = (T * k + 31) >> 5;
+    const size_t smem = sizeof(RepackSmem) + (((size_t)table_stride(n_chunks) * E * 2 + 15) & ~(size_t)15) + (size_t)n_chunks * 32 * 13;
+    return launch_pdl(route_index_kernel, dim3(1), dim3(kRepackThreads), smem, st, logits, T, E, S, k, renorm, idx, w, counts, offsets, perm,
+                      inv_perm, status);
+}
+
 // ---- larger problems: the index phase on many CTAs ----
 // Block b owns pairs [b * kBlockPairs, (b + 1) * kBlockPairs).  Pass 1: per block and expert the number of
 // pairs (hist[b][e]) and every pair's rank among the block's pairs of the same expert (rank16[p]), both by
@@ -295,6 +332,7 @@ cudaError_t launch_repack(const int32_t* idx, const uint16_t* x, int T, int E, i
                           int32_t* offsets, int32_t* perm, int32_t* inv_perm, uint16_t* x_packed, int* status,
                           int32_t* hist, uint16_t* rank16, int n_sm, cudaStream_t st, int* n_launch) {
     const int P = T * k, n_chunks = (P + 31) >> 5;
+    if (!x_packed) d = 0;                                // index outputs only: rows of no length
     static bool attr_done[64];
     if (first_call_on_device(attr_done)) {
         cudaError_t e = cudaFuncSetAttribute(repack_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024);
@@ -307,6 +345,7 @@ cudaError_t launch_repack(const int32_t* idx, const uint16_t* x, int T, int E, i
         int grid = (P + S * T + rows_per_cta - 1) / rows_per_cta;
         if (grid < 1) grid = 1;
         if (grid > n_sm) grid = n_sm;
+        if (!x_packed) grid = 1;
         *n_launch = 1;
         return launch_pdl(repack_fused_kernel, dim3(grid), dim3(kRepackThreads), smem, st, idx, x, T, E, S, k, d,
                           counts, offsets, perm, inv_perm, x_packed, status);
@@ -316,7 +355,7 @@ cudaError_t launch_repack(const int32_t* idx, const uint16_t* x, int T, int E, i
     if (e != cudaSuccess) return e;
     e = launch_pdl(repack_scatter_kernel, dim3(n_blocks), dim3(kBlockPairs), 0, st, idx, T, E, S, k, (const int32_t*)hist,
                    (const uint16_t*)rank16, counts, offsets, perm, inv_perm);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || !x_packed) { *n_launch = 2; return e; }
     *n_launch = 3;
     return launch_pdl(repack_gather_kernel, dim3(n_sm * 4), dim3(256), 0, st, x, perm, offsets, T, E, S, k, d, x_packed);
 }

@@ -354,8 +354,9 @@ static int note_ffn_enqueued(saem_ctx* c, int layer, cudaStream_t st, const Slot
     return SAEM_OK;
 }
 
-int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t* offsets, int max_rows,
-                    const int32_t* subset, int n_subset, float* y_packed, void* stream) {
+// saem_expert_ffn; `tokens` (SAEM_FFN_MX contexts only): x_packed is x itself, to be gathered by inv_perm.
+static int expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t* offsets, int max_rows,
+                      const int32_t* subset, int n_subset, float* y_packed, const MxTokens& tokens, void* stream) {
     if (!c) return SAEM_ERR_INVALID_ARG;
     const saem_config& g = c->cfg;
     if (layer < 0 || layer >= g.n_layers) return SAEM_ERR_INVALID_ARG;
@@ -415,7 +416,7 @@ int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t*
     }
     int nl = 0;
     if (g.ffn_path == SAEM_FFN_MX) {
-        CUDA_TRY(launch_mx_ffn(a, tab, st, &nl));
+        CUDA_TRY(launch_mx_ffn(a, tokens, tab, st, &nl));
     } else if (g.ffn_path == SAEM_FFN_SCALAR) {
         CUDA_TRY(launch_ffn_scalar(a, tab, st, &nl));
     } else if (gemv_path) {
@@ -425,6 +426,11 @@ int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t*
     }
     c->launches += nl;
     return note_ffn_enqueued(c, layer, st, tab);
+}
+
+int saem_expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_t* offsets, int max_rows,
+                    const int32_t* subset, int n_subset, float* y_packed, void* stream) {
+    return expert_ffn(c, layer, x_packed, offsets, max_rows, subset, n_subset, y_packed, MxTokens{}, stream);
 }
 
 int saem_combine(saem_ctx* c, const float* y, const int32_t* inv_perm, const float* w, int T, const float* shared_y,
@@ -524,6 +530,28 @@ int saem_moe_step(saem_ctx* c, saem_ctx* sh, int layer, const float* logits, con
         CUDA_TRY(launch_mx_few(a, tab, c->n_sm, st, &nl));
         c->launches += nl;
         return note_ffn_enqueued(c, layer, st, tab);
+    }
+    if (g.ffn_path == SAEM_FFN_MX) {
+        // x is gathered where it is split into planes, so x_packed is not produced; for small batches gate and index phase
+        // are one launch
+        if (layer < 0 || layer >= g.n_layers) return SAEM_ERR_INVALID_ARG;
+        if (misaligned(x) || misaligned(out)) return SAEM_ERR_ALIGNMENT;
+        cudaStream_t st = (cudaStream_t)stream;
+        int32_t *counts = (int32_t*)(w + L.counts), *perm = (int32_t*)(w + L.perm);
+        int* status = (int*)(w + L.status);
+        int nl = 1;
+        if (route_index_supported(T, g.top_k)) {
+            CUDA_TRY(launch_route_index(logits, T, g.n_experts, g.n_shared, g.top_k, g.renorm, idx, tw, counts, offsets, perm, inv, status, st));
+        } else {
+            if ((s = saem_route(c, logits, T, idx, tw, stream)) != SAEM_OK) return s;
+            CUDA_TRY(launch_repack(idx, nullptr, T, g.n_experts, g.n_shared, g.top_k, g.d_model, counts, offsets, perm, inv, nullptr, status,
+                                   (int32_t*)(w + L.repack_hist), (uint16_t*)(w + L.repack_rank), c->n_sm, st, &nl));
+        }
+        c->launches += nl;
+        if ((s = expert_ffn(c, layer, x, offsets, T * (g.top_k + g.n_shared), nullptr, 0, y, MxTokens{inv, T, g.top_k, g.n_shared}, stream)) != SAEM_OK)
+            return s;
+        if (sh && (s = saem_expert_ffn(sh, layer, x, nullptr, T, nullptr, 0, shy, stream)) != SAEM_OK) return s;
+        return saem_combine(c, y, inv, tw, T, sh ? shy : nullptr, out, stream);
     }
     if ((s = saem_route(c, logits, T, idx, tw, stream)) != SAEM_OK) return s;
     if ((s = saem_repack(c, idx, x, T, (int32_t*)(w + L.counts), offsets, (int32_t*)(w + L.perm), inv,

@@ -104,7 +104,7 @@ cudaError_t launch_route(const float* logits, int T, int E, int k, int renorm, i
                          cudaStream_t st);
 cudaError_t launch_route_fused(const uint16_t* x, const uint16_t* w_router, int T, int E, int d, int k, int renorm,
                                float* logits_out, int32_t* idx, float* w, cudaStream_t st);
-// Returns the number of kernels launched (1 or 3) in *n_launch.  hist [ceil(P / 1024)][E] and rank16 [P]: workspace
+// Returns the number of kernels launched (1 or 3) in *n_launch.  x_packed nullptr: the index outputs only (1 or 2).  hist [ceil(P / 1024)][E] and rank16 [P]: workspace
 // of the multi-CTA index phase (more than 2048 pairs).
 cudaError_t launch_repack(const int32_t* idx, const uint16_t* x, int T, int E, int S, int k, int d, int32_t* counts,
                           int32_t* offsets, int32_t* perm, int32_t* inv_perm, uint16_t* x_packed, int* status,
@@ -137,7 +137,16 @@ cudaError_t launch_ffn_scalar(const FfnArgs& a, const SlotTable& tab, cudaStream
 cudaError_t launch_ffn_tensor(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
 // Microscaled 4-bit experts (SAEM_FFN_MX contexts, mx_moe.cu); a.h is a workspace of mx_workspace_bytes there.
 size_t mx_workspace_bytes(int max_tokens, int k, int E, int S, int d, int f);
-cudaError_t launch_mx_ffn(const FfnArgs& a, const SlotTable& tab, cudaStream_t st, int* n_launch);
+struct MxTokens {               // how a.x_packed is read: with inv_perm it is x itself, row t of T tokens
+    const int32_t* inv_perm;    // nullptr: packed rows
+    int T, k, S;
+};
+cudaError_t launch_mx_ffn(const FfnArgs& a, const MxTokens& x, const SlotTable& tab, cudaStream_t st, int* n_launch);
+// saem_route and the index outputs of saem_repack in one launch (one CTA; at most kRouteIndexTokens tokens).
+constexpr int kRouteIndexTokens = 64;
+bool route_index_supported(int T, int k);
+cudaError_t launch_route_index(const float* logits, int T, int E, int S, int k, int renorm, int32_t* idx, float* w, int32_t* counts,
+                               int32_t* offsets, int32_t* perm, int32_t* inv_perm, int* status, cudaStream_t st);
 // The whole step over such experts for up to 8 tokens in two launches (mx_few.cu).
 struct MxFewArgs {
     const float* logits;        // [T, E]

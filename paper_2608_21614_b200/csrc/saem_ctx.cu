@@ -522,7 +522,7 @@ int saem_moe_step(saem_ctx* c, saem_ctx* sh, int layer, const float* logits, con
         a.logits = logits; a.x = (const uint16_t*)x;
         a.T = T; a.E = g.n_experts; a.S = g.n_shared; a.k = g.top_k; a.d = g.d_model; a.f = g.d_ff; a.renorm = g.renorm;
         a.slot_region = c->slot_region; a.slot_bytes = c->slot_bytes;
-        a.h = (float*)(w + L.h);
+        a.h_tiles = w + L.h;
         a.out = out; a.out_bf16 = g.out_dtype == SAEM_OUT_BF16;
         a.topk_idx = idx; a.topk_w = tw;
         a.status = (int*)(w + L.status);

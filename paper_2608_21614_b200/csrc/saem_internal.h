@@ -154,13 +154,13 @@ struct MxFewArgs {
     int T, E, S, k, d, f, renorm;
     const uint8_t* slot_region;
     size_t slot_bytes;
-    float* h;                   // [T * (k + S), f] fp32 workspace, rows by pair id
+    uint8_t* h_tiles;           // workspace: the active experts' hidden activations as tiles of 8 tokens
     void* out;                  // [T, d]
     int out_bf16;
     int32_t* topk_idx;
     float* topk_w;
     int* status;
-    int stages_a, stages_b, split_b;   // set by the launcher
+    int stages_a;               // set by the launcher
 };
 bool mx_few_supported(int T, int k, int d);
 cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStream_t st, int* n_launch);

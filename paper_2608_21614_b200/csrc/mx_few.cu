@@ -6,7 +6,7 @@
 //
 // The bytes of the active experts are the bound, and at one token the chain of latencies: launch, logits, top-k, first
 // weights, h, result.  Every CTA therefore routes the batch itself (a warp per token).  The products are those of
-// mx_moe.cu (4-bit weights straight from shared memory to tcgen05 kind::mxf4, activations as six 4-bit planes), but a
+// mx_moe.cu (4-bit weights straight from shared memory to tcgen05 kind::mxf4, activations as five 4-bit planes), but a
 // column is a token whatever the expert: x's tile stays in shared memory for all items, the second launch's k axis runs
 // over all active experts, and the merge over a token's experts costs nothing because h carries the gate weight.  (The
 // same two launches with mma.sync, the weights converted to f16, were bound by instruction issue: 50 us for 8 tokens of a
@@ -23,7 +23,7 @@ constexpr int kFewThreads = 320;                             // warp 0: copies, 
 constexpr int kFewMaxStages = 8;
 constexpr int kFewSplit = 8;                                 // CTAs of a cluster: parts of the down projection's k axis
 using FewTile = TileShape<kFewTokens>;
-constexpr int kFewStageA = 2 * kMxBlockBytes;
+constexpr int kFewHalf = kMxBlockCodes / 2 + 2 * kMxPiece;     // 64 rows of a block, and its scales
 constexpr int kFewStageB = kMxBlockBytes + FewTile::kBytes;
 constexpr int kFewStagesB = 4;
 constexpr int kFewSfA = 16 + FewTile::kScaleCols, kFewSfB = 8 + FewTile::kScaleCols;
@@ -39,6 +39,53 @@ struct FewShared {
     uint32_t tmem;
     int abort_flag;
 };
+
+// route_row (the same choices and weights) for k <= 8, on the critical path here: 32-bit keys, the winner of round j in
+// lane j.
+__device__ __forceinline__ void few_topk(const float* __restrict__ row, int E, int k, int renorm, int lane, int* idx_out, float* w_out) {
+    uint32_t key[kPerLane];
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) key[i] = lane + 32 * i < E ? order_key(row[lane + 32 * i]) : 0u;   // 0: below every real key
+    float all = 0.f, win = 0.f;
+    int mine = 0;
+    float vmax = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(key[0], key[1]), max(key[2], key[3])));
+        const int at = key[0] == top ? lane : key[1] == top ? lane + 32 : key[2] == top ? lane + 64 : key[3] == top ? lane + 96 : 128;
+        const int e = (int)__reduce_min_sync(0xffffffffu, (unsigned)at);
+        if (j == 0) {
+            vmax = key_value(top);
+            if (!renorm) {
+#pragma unroll
+                for (int i = 0; i < kPerLane; ++i)
+                    if (lane + 32 * i < E) all += expf(key_value(key[i]) - vmax);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i)
+            if (e == lane + 32 * i) key[i] = 0u;                               // taken
+        if (lane == j) {
+            win = key_value(top);
+            mine = e;
+        }
+    }
+    float z = 0.f;
+    if (lane < k)
+        z = vmax == CUDART_INF_F ? (win == CUDART_INF_F ? 1.f : 0.f) : vmax == -CUDART_INF_F ? 1.f : expf(win - vmax);
+    float sum = z;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);   // k <= 8: the other lanes hold nothing
+    if (!renorm && vmax != CUDART_INF_F && vmax != -CUDART_INF_F) {
+        sum = all;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    if (lane < k) {
+        idx_out[lane] = mine;
+        w_out[lane] = z / sum;
+    }
+}
 
 // Barriers; routes the batch (one warp per token) and lists the active experts in ascending order, the always-on ones
 // last; experts without a slot are left out (status word).  All threads call it; ends with a barrier.
@@ -59,7 +106,7 @@ __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, cons
     }
     if (threadIdx.x < 4) s.mask[threadIdx.x] = 0;
     for (int i = threadIdx.x; i < kFewActive * kFewTokens; i += kFewThreads) (&s.weight[0][0])[i] = 0.f;
-    if (warp < a.T) route_row(a.logits + (size_t)warp * a.E, a.E, a.k, a.renorm, lane, s.idx + warp * a.k, s.w + warp * a.k);
+    if (warp < a.T) few_topk(a.logits + (size_t)warp * a.E, a.E, a.k, a.renorm, lane, s.idx + warp * a.k, s.w + warp * a.k);
     __syncthreads();
     const int e = threadIdx.x < P ? s.idx[threadIdx.x] : -1;
     const bool have = e >= 0 && tab.slot[e] >= 0;
@@ -109,15 +156,20 @@ __device__ __forceinline__ void few_free(uint32_t tmem, uint32_t cols) {
     }
 }
 
-// Gate, and gate/up projection: items are (active expert, 128 hidden units).
+// Gate, and gate/up projection: items are (active expert, 128 hidden units), or halves of that (HALF) while those would not
+// occupy the SMs: a stage then holds 64 rows of the gate block and of the up block, and the MMA's other 64 rows read
+// whatever lies beside them (inside the CTA's shared memory), for lanes that nobody looks at.
+template <bool HALF>
 __global__ void __launch_bounds__(kFewThreads, 1)
 mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ SlotTable tab) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ FewShared s;
-    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nc = mx_chunks(a.d), n = a.stages_a;
-    uint8_t* xs = smem_raw + (base - raw) + n * kFewStageA;                    // x's tiles, one per chunk
-    const uint32_t xs_addr = base + n * kFewStageA;
+    constexpr int kStage = 2 * (HALF ? kFewHalf : kMxBlockBytes);
+    constexpr int kCodes = HALF ? kMxBlockCodes / 2 : kMxBlockCodes;
+    const uint32_t raw = smem_u32(smem_raw), xs_addr = (raw + 1023u) & ~1023u;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, nc = mx_chunks(a.d), n = a.stages_a;
+    uint8_t* xs = smem_raw + (xs_addr - raw);                                  // x's tiles, one per chunk (7 KB each)
+    const uint32_t base = xs_addr + max(nc * FewTile::kBytes, 8192);           // the ring: 8 KB before it and behind it are ours
     volatile int* abort_p = &s.abort_flag;
     few_alloc(s, 512);
     pdl_wait();
@@ -135,66 +187,77 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         a.topk_idx[threadIdx.x] = s.idx[threadIdx.x];
         a.topk_w[threadIdx.x] = s.w[threadIdx.x];
     }
-    const uint32_t tmem = s.tmem, tmem_sf = tmem + 4 * FewTile::kN;
-    const int per = a.f / 128, total = s.n_active * per;
+    const uint32_t tmem = warp_uniform(s.tmem), tmem_sf = tmem + 4 * FewTile::kN;
+    const int per = a.f / 128 * (HALF ? 2 : 1), total = (int)warp_uniform(s.n_active) * per;
     if (warp == 0) {
-        if (lane == 0) {
-            // ------------------------------------------------------------ copies
-            int it = 0;
-            bool ok = true;
-            for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
-                const int act = i / per;
-                const uint8_t* w = a.slot_region + (size_t)tab.slot[s.expert[act]] * a.slot_bytes + (size_t)(i - act * per) * nc * kFewStageA;
-                for (int c = 0; c < nc; ++c, ++it, w += kFewStageA) {
-                    const int st = it % n;
-                    if (it >= n) {
-                        ok = mbar_wait(smem_u32(&s.empty[st]), (it / n - 1) & 1, abort_p, a.status);
-                        if (!ok) break;
-                    }
-                    mbar_expect_tx(smem_u32(&s.full[st]), kFewStageA);
-                    bulk_g2s(base + st * kFewStageA, w, kFewStageA, smem_u32(&s.full[st]));
+        // ---------------------------------------------------------------- copies
+        const uint32_t on = elect_one();
+        int it = 0, st = 0, turn = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
+            const int act = i / per, part = i - act * per, tile = HALF ? part >> 1 : part;
+            const uint8_t* w = a.slot_region + (size_t)warp_uniform(tab.slot[s.expert[act]]) * a.slot_bytes + (size_t)tile * nc * 2 * kMxBlockBytes;
+            for (int c = 0; c < nc; ++c, ++it, w += 2 * kMxBlockBytes) {
+                if (turn) {
+                    ok = mbar_wait_warp(smem_u32(&s.empty[st]), (turn - 1) & 1, abort_p, a.status);
+                    if (!ok) break;
                 }
+                const uint32_t bar = smem_u32(&s.full[st]), dst = base + st * kStage;
+                expect_tx_on(on, bar, kStage);
+                if (HALF) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {                              // codes of gate and up, then the scales of both
+                        bulk_g2s_on(on, dst + m * kCodes, w + m * kMxBlockBytes + (part & 1) * kCodes, kCodes, bar);
+                        bulk_g2s_on(on, dst + 2 * kCodes + m * 2 * kMxPiece, w + m * kMxBlockBytes + kMxBlockCodes, 2 * kMxPiece, bar);
+                    }
+                } else {
+                    bulk_g2s_on(on, dst, w, kStage, bar);
+                }
+                if (++st == n) { st = 0; ++turn; }
             }
-            if (!ok) few_drain(s, n, it, a.status);
         }
+        if (!ok && lane == 0) few_drain(s, n, it, a.status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
-        int it = 0, k = 0;
-        bool ok = mbar_wait(smem_u32(&s.x), 0, abort_p, a.status);
+        int st = 0, turn = 0, k = 0;
+        bool ok = mbar_wait_warp(smem_u32(&s.x), 0, abort_p, a.status);
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x, ++k) {
             const int set = k & 1;
             const uint32_t acc = tmem + set * 2 * FewTile::kN;
-            if (k >= 2) ok = mbar_wait(smem_u32(&s.free[set]), ((k >> 1) - 1) & 1, abort_p, a.status);
+            if (k >= 2) ok = mbar_wait_warp(smem_u32(&s.free[set]), ((k >> 1) - 1) & 1, abort_p, a.status);
             tc_fence_after();
-            for (int c = 0; c < nc && ok; ++c, ++it) {
-                const int st = it % n;
-                ok = mbar_wait(smem_u32(&s.full[st]), (it / n) & 1, abort_p, a.status);
+            for (int c = 0; c < nc && ok; ++c) {
+                ok = mbar_wait_warp(smem_u32(&s.full[st]), turn & 1, abort_p, a.status);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t wb = base + st * kFewStageA, xb = xs_addr + c * FewTile::kBytes;
+                const uint32_t stage = base + st * kStage, xb = xs_addr + c * FewTile::kBytes;
                 const uint32_t sf = tmem_sf + st * kFewSfA;
                 const int steps = min(4, (a.d - c * kMxChunk) / 64);
+                // scales of gate (m = 0) and up behind the codes of both, or behind each one's own
+                auto scales_at = [&](int m, int h) { return stage + (HALF ? 2 * kCodes + m * 2 * kMxPiece : m * kMxBlockBytes + kCodes) + h * kMxPiece; };
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (2 * h >= steps) break;
-                    tc_cp_scales(on, sf + 4 * h, smem_desc_scales(wb + kMxBlockCodes + h * kMxPiece));
-                    tc_cp_scales(on, sf + 8 + 4 * h, smem_desc_scales(wb + kMxBlockBytes + kMxBlockCodes + h * kMxPiece));
+                    tc_cp_scales(on, sf + 4 * h, smem_desc_scales(scales_at(0, h)));
+                    tc_cp_scales(on, sf + 8 + 4 * h, smem_desc_scales(scales_at(1, h)));
                     tc_cp_scales(on, sf + 16 + 4 * h, smem_desc_scales(xb + FewTile::kN * 128 + h * kMxPiece));
                 }
                 const uint64_t dx = smem_desc_sw128(xb);
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    const uint64_t dw = smem_desc_sw128(wb + m * kMxBlockBytes);
+                    // a second half's row 64 stands first: its block would begin 8 KB before
+                    const uint64_t dw = smem_desc_sw128(stage + (HALF ? m * kCodes - (i & 1) * kCodes : m * kMxBlockBytes));
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (j < steps)
                             tc_mma_mxf4(on, acc + m * FewTile::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(FewTile::kN, (j & 1) * 2),
                                         sf + m * 8 + 4 * (j >> 1), sf + 16 + 4 * (j >> 1), c > 0 || j > 0);
                 }
-                if (on) tc_commit(smem_u32(&s.empty[st]));
+                tc_commit_on(on, smem_u32(&s.empty[st]));
+                if (++st == n) { st = 0; ++turn; }
             }
-            if (on) tc_commit(smem_u32(&s.acc[set]));
+            tc_commit_on(on, smem_u32(&s.acc[set]));
         }
     } else {
         // ---------------------------------------------------------------- x's planes
@@ -217,11 +280,11 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         bool ok = true;
         for (int i = blockIdx.x; i < total; i += gridDim.x, ++k) {
             if ((k & 1) != group) continue;
-            const int act = i / per, gb = i - act * per;
+            const int act = i / per, part = i - act * per, tile = HALF ? part >> 1 : part;
             ok = ok && mbar_wait(smem_u32(&s.acc[group]), (k >> 1) & 1, abort_p, a.status);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
-            if (ok) {
+            if (ok && (!HALF || (quad >> 1) == (part & 1))) {
                 float v[8], u[8];
                 plane_sums<kFewTokens>(acc, v);
                 plane_sums<kFewTokens>(acc + FewTile::kN, u);
@@ -231,8 +294,8 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
                     const float w = s.weight[act][t];
                     v[t] = w != 0.f ? w * (v[t] / (1.f + __expf(-v[t])) * u[t]) : 0.f;   // columns of other tokens hold anything
                 }
-                store_planes<kFewTokens>(v, 0, a.T, a.h_tiles + ((size_t)act * mx_chunks(a.f) + (gb >> 1)) * FewTile::kBytes,
-                                         (gb & 1) * 4 + quad, lane);
+                store_planes<kFewTokens>(v, 0, a.T, a.h_tiles + ((size_t)act * mx_chunks(a.f) + (tile >> 1)) * FewTile::kBytes,
+                                         (tile & 1) * 4 + quad, lane);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&s.free[group]));
@@ -250,7 +313,7 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
     __shared__ FewShared s;
     __shared__ alignas(16) float sums[128 * kFewTokens];                       // [output column][token]
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int nc = mx_chunks(a.f);
     constexpr int n = kFewStagesB;
     volatile int* abort_p = &s.abort_flag;
@@ -259,47 +322,46 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
     // and no weight is written by the first launch: only h has to be waited for.
     few_route(s, a, tab, n, false);
     tc_fence_after();
-    const uint32_t tmem = s.tmem, tmem_sf = tmem + 64;
-    const int all = s.n_active * nc, rank = (int)cluster_ctarank();
+    const uint32_t tmem = warp_uniform(s.tmem), tmem_sf = tmem + 64;
+    const int all = (int)warp_uniform(s.n_active) * nc, rank = (int)cluster_ctarank();
     const int q0 = all * rank / kFewSplit, q1 = all * (rank + 1) / kFewSplit;
     const size_t tile = blockIdx.x / kFewSplit;
     if (warp == 0) {
-        if (lane == 0) {
-            // ------------------------------------------------------------ copies
-            auto weights = [&](int q) {
-                const int st = (q - q0) % n, act = q / nc;
-                mbar_expect_tx(smem_u32(&s.full[st]), kFewStageB);
-                bulk_g2s(base + st * kFewStageB,
-                         a.slot_region + (size_t)tab.slot[s.expert[act]] * a.slot_bytes +
-                             (mx_gate_up_blocks(a.d, a.f) + tile * nc + (q - act * nc)) * kMxBlockBytes,
-                         kMxBlockBytes, smem_u32(&s.full[st]));
-            };
-            const int early = min(q1, q0 + n);
-            for (int q = q0; q < early; ++q) weights(q);
-            pdl_wait();
-            pdl_launch_dependents();
-            bool ok = true;
-            int q = q0;
-            for (; q < q1; ++q) {
-                const int it = q - q0, st = it % n;
-                if (it >= n) {
-                    ok = mbar_wait(smem_u32(&s.empty[st]), (it / n - 1) & 1, abort_p, a.status);
-                    if (!ok) break;
-                    weights(q);
-                }
-                bulk_g2s(base + st * kFewStageB + kMxBlockBytes, a.h_tiles + (size_t)q * FewTile::kBytes, FewTile::kBytes,
-                         smem_u32(&s.full[st]));
+        // ---------------------------------------------------------------- copies
+        const uint32_t on = elect_one();
+        auto weights = [&](int q, int st) {
+            const int act = q / nc;
+            expect_tx_on(on, smem_u32(&s.full[st]), kFewStageB);
+            bulk_g2s_on(on, base + st * kFewStageB,
+                        a.slot_region + (size_t)warp_uniform(tab.slot[s.expert[act]]) * a.slot_bytes +
+                            (mx_gate_up_blocks(a.d, a.f) + tile * nc + (q - act * nc)) * kMxBlockBytes,
+                        kMxBlockBytes, smem_u32(&s.full[st]));
+        };
+        const int early = min(q1, q0 + n);
+        for (int q = q0; q < early; ++q) weights(q, q - q0);
+        pdl_wait();
+        pdl_launch_dependents();
+        bool ok = true;
+        int q = q0, st = 0, turn = 0;
+        for (; q < q1; ++q) {
+            if (turn) {
+                ok = mbar_wait_warp(smem_u32(&s.empty[st]), (turn - 1) & 1, abort_p, a.status);
+                if (!ok) break;
+                weights(q, st);
             }
-            if (!ok) few_drain(s, n, q - q0, a.status);
+            bulk_g2s_on(on, base + st * kFewStageB + kMxBlockBytes, a.h_tiles + (size_t)q * FewTile::kBytes, FewTile::kBytes, smem_u32(&s.full[st]));
+            if (++st == n) { st = 0; ++turn; }
         }
+        if (!ok && lane == 0) few_drain(s, n, q - q0, a.status);
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
         bool ok = true;
+        int st = 0, turn = 0;
         for (int q = q0; q < q1; ++q) {
-            const int it = q - q0, st = it % n, c = q % nc;
-            ok = mbar_wait(smem_u32(&s.full[st]), (it / n) & 1, abort_p, a.status);
+            const int c = q % nc;
+            ok = mbar_wait_warp(smem_u32(&s.full[st]), turn & 1, abort_p, a.status);
             if (!ok) break;
             tc_fence_after();
             const uint32_t wb = base + st * kFewStageB, xb = wb + kMxBlockBytes, sf = tmem_sf + st * kFewSfB;
@@ -315,10 +377,11 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             for (int j = 0; j < 4; ++j)
                 if (j < steps)
                     tc_mma_mxf4(on, tmem, dw + 2 * j, dx + 2 * j, idesc_mxf4(FewTile::kN, (j & 1) * 2), sf + 4 * (j >> 1), sf + 8 + 4 * (j >> 1),
-                                it > 0 || j > 0);
-            if (on) tc_commit(smem_u32(&s.empty[st]));
+                                q > q0 || j > 0);
+            tc_commit_on(on, smem_u32(&s.empty[st]));
+            if (++st == n) { st = 0; ++turn; }
         }
-        if (on) tc_commit(smem_u32(&s.acc[0]));
+        tc_commit_on(on, smem_u32(&s.acc[0]));
     } else if (warp < 6) {
         const int quad = warp & 3;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -360,17 +423,22 @@ cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStrea
     static bool done[64];
     constexpr int kMost = 222 * 1024, kSmemB = kFewStagesB * kFewStageB + 1024;
     if (first_call_on_device(done)) {
-        cudaError_t e = cudaFuncSetAttribute(mx_few_gate_up_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        cudaError_t e = cudaFuncSetAttribute(mx_few_gate_up_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_few_gate_up_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_few_down_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemB);
         if (e != cudaSuccess) return e;
     }
-    const int x_bytes = mx_chunks(a.d) * FewTile::kBytes;
-    a.stages_a = (kMost - 1024 - x_bytes) / kFewStageA;
-    if (a.stages_a > 5) a.stages_a = 5;                                        // tensor memory: 192 accumulator columns + 24 per stage
     const int pairs = a.T * a.k, active = (pairs < a.E ? pairs : a.E) + a.S;
-    const long long items = (long long)active * (a.f / 128);
-    cudaError_t e = launch_pdl(mx_few_gate_up_kernel, dim3((unsigned)(items < n_sm ? items : n_sm)), dim3(kFewThreads),
-                               (size_t)(1024 + x_bytes + a.stages_a * kFewStageA), st, a, tab);
+    long long items = (long long)active * (a.f / 128);
+    const bool half = items <= n_sm;
+    if (half) items *= 2;
+    const int x_bytes = mx_chunks(a.d) * FewTile::kBytes, before = x_bytes > 8192 ? x_bytes : 8192, stage = 2 * (half ? kFewHalf : kMxBlockBytes);
+    const int around = 1024 + before + (half ? 8192 : 0);
+    a.stages_a = (kMost - around) / stage;
+    const int most = half ? kFewMaxStages : 5;
+    if (a.stages_a > most) a.stages_a = most;                                  // tensor memory: 192 accumulator columns + 24 per stage
+    cudaError_t e = launch_pdl(half ? mx_few_gate_up_kernel<true> : mx_few_gate_up_kernel<false>, dim3((unsigned)(items < n_sm ? items : n_sm)),
+                               dim3(kFewThreads), (size_t)(around + a.stages_a * stage), st, a, tab);
     if (e != cudaSuccess) return e;
     *n_launch += 1;
     cudaLaunchAttribute attr[2];

@@ -46,7 +46,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     __shared__ uint32_t tmem_s;
     __shared__ int abort_flag;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
     const int n0 = blockIdx.y * 128, t0 = blockIdx.z * p.n_tile;
     const int tokens = min(p.n_tile, p.m - t0);
@@ -74,31 +74,32 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_s;
+    const uint32_t tmem = warp_uniform(tmem_s);
     const int acc_cols = (p.n_tile + 31) & ~31;
     const uint32_t tmem_sf = tmem + acc_cols;                                // per stage: 8 columns for W, 8 per piece for A
     const int sf_cols = 8 + 8 * p.pieces;
     const int w_bytes = 128 * 128, a_bytes = p.n_tile * 128;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         // ---------------------------------------------------------------- copies
+        const uint32_t on = elect_one();
         const int pieces = min(p.pieces, (tokens + 127) / 128);
         const int piece_t = t0 / 128, piece_w = n0 / 128;
         auto w_part = [&](int s) {
             const int i = (s - s0) % p.n_stage;
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
-            mbar_expect_tx(bar, w_bytes + a_bytes + spans * kMxPiece * (1 + pieces));
-            tma_2d(st, &map_w, s * 128, n0, bar);
-            bulk_g2s(st + w_bytes + a_bytes, p.w_scales + ((size_t)piece_w * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
+            expect_tx_on(on, bar, w_bytes + a_bytes + spans * kMxPiece * (1 + pieces));
+            tma_2d_on(on, st, &map_w, s * 128, n0, bar);
+            bulk_g2s_on(on, st + w_bytes + a_bytes, p.w_scales + ((size_t)piece_w * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
         };
         auto a_part = [&](int s) {
             const int i = (s - s0) % p.n_stage;
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
-            tma_2d(st + w_bytes, &map_a, s * 128, t0, bar);
+            tma_2d_on(on, st + w_bytes, &map_a, s * 128, t0, bar);
             for (int q = 0; q < pieces; ++q)
-                bulk_g2s(st + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
+                bulk_g2s_on(on, st + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
                          p.a_scales + ((size_t)(piece_t + q) * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
         };
         int early = 0;
@@ -111,13 +112,13 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         for (; s < s1; ++s) {
             const int it = s - s0;
             if (it >= p.n_stage) {
-                ok = mbar_wait(smem_u32(&bar_empty[it % p.n_stage]), (it / p.n_stage - 1) & 1, abort_p, status);
+                ok = mbar_wait_warp(smem_u32(&bar_empty[it % p.n_stage]), (it / p.n_stage - 1) & 1, abort_p, status);
                 if (!ok) break;
             }
             if (it >= early) w_part(s);
             a_part(s);
         }
-        if (!ok)                                                             // copies still under way land before the CTA ends
+        if (!ok && lane == 0)                                                // copies still under way land before the CTA ends
             for (int q = max(s0, s - p.n_stage); q < s; ++q) {
                 abort_flag = 0;
                 mbar_wait(smem_u32(&bar_full[(q - s0) % p.n_stage]), ((q - s0) / p.n_stage) & 1, abort_p, status);
@@ -128,7 +129,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         const uint32_t on = elect_one();
         for (int s = s0; s < s1; ++s) {
             const int it = s - s0, i = it % p.n_stage;
-            if (!mbar_wait(smem_u32(&bar_full[i]), (it / p.n_stage) & 1, abort_p, status)) break;
+            if (!mbar_wait_warp(smem_u32(&bar_full[i]), (it / p.n_stage) & 1, abort_p, status)) break;
             tc_fence_after();
             const uint32_t st = base + i * p.stage_bytes, sf = st + w_bytes + a_bytes;
             const uint32_t tw = tmem_sf + i * sf_cols, ta = tw + 8;
@@ -144,9 +145,9 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             for (int j = 0; j < 4; ++j)
                 if (j < steps) tc_mma_mxf4(on, tmem, dw + 2 * j, da + 2 * j, idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
                             ta + 4 * (j >> 1) * p.pieces, s > s0 || j > 0);
-            if (on) tc_commit(smem_u32(&bar_empty[i]));
+            tc_commit_on(on, smem_u32(&bar_empty[i]));
         }
-        if (on) tc_commit(smem_u32(&bar_acc));
+        tc_commit_on(on, smem_u32(&bar_acc));
     }
     __syncwarp();
 

@@ -3,8 +3,8 @@
 // of shared memory as they are.  (Converting them to f16 for mma.sync costs some 150 instructions per 1088 bytes, and that,
 // not DRAM, was the bound: 232 us against 140 us for 16 tokens of a 4096 x 14336 layer of 8 experts.)
 //
-// The other operand has to be 4-bit too: the activations are split into six 4-bit planes (mx_planes.cuh), whose
-// accumulators are added in fp32 in the epilogue.  Prefill pays for it: six times the work at four times bf16's rate.
+// The other operand has to be 4-bit too: the activations are split into five 4-bit planes (mx_planes.cuh), whose
+// accumulators are added in fp32 in the epilogue.  Prefill pays for it: five times the work at four times bf16's rate.
 //
 // A tile is R (8, 16, 32) rows of one expert; an item is a tile x 128 hidden units (gate and up accumulators side by
 // side) or x 128 output columns.  Tiles of the activations are laid out as the MMA wants them (swizzled codes of
@@ -147,7 +147,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
     __shared__ uint32_t tmem_s;
     __shared__ int abort_flag;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int K = MODE == 0 ? a.d : a.f, nc = mx_chunks(K), n_gb = (MODE == 0 ? a.f : a.d) / 128;
     volatile int* abort_p = &abort_flag;
     if (threadIdx.x == 0) {
@@ -174,8 +174,8 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
     if (MODE == 0 && blockIdx.x == 0)
         for (int e = threadIdx.x; e < a.E; e += kMoeThreads)
             if (s.rows[e] > 0 && tab.slot[e] < 0 && tab.in_subset[e]) atomicExch(a.status, SAEM_ERR_NOT_RESIDENT);
-    const uint32_t tmem = tmem_s, tmem_sf = tmem + F::kSets * F::kAccCols;
-    const int total = s.tile0[SAEM_MAX_EXPERTS] * n_gb;
+    const uint32_t tmem = warp_uniform(tmem_s), tmem_sf = tmem + F::kSets * F::kAccCols;
+    const int total = (int)warp_uniform(s.tile0[SAEM_MAX_EXPERTS]) * n_gb;
 
     // Items of an expert: its tiles fastest, so that a weight block is read from DRAM once.
     struct Item { int e, gb, tile, row0, rows; };
@@ -184,34 +184,37 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
 #pragma unroll
         for (int step = 64; step > 0; step >>= 1)                              // the last e whose first item is not beyond i
             if (s.tile0[e + step] * n_gb <= i) e += step;
-        const int tiles = s.tile0[e + 1] - s.tile0[e], rem = i - s.tile0[e] * n_gb;
+        e = (int)warp_uniform(e);
+        const int tile0 = (int)warp_uniform(s.tile0[e]), tiles = (int)warp_uniform(s.tile0[e + 1]) - tile0, rem = i - tile0 * n_gb;
         const int gb = rem / tiles, t = rem - gb * tiles;
-        return Item{e, gb, s.tile0[e] + t, s.start[e] + t * R, min(R, s.rows[e] - t * R)};
+        return Item{e, gb, tile0 + t, s.start[e] + t * R, min(R, s.rows[e] - t * R)};
     };
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         // ---------------------------------------------------------------- copies
+        const uint32_t on = elect_one();
         const size_t region = MODE == 0 ? 0 : mx_gate_up_blocks(a.d, a.f);
-        int it = 0;
+        int it = 0, st = 0, turn = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
             const Item t = item_at(i);
-            if (tab.slot[t.e] < 0) continue;
-            const uint8_t* w = a.slot_region + (size_t)tab.slot[t.e] * a.slot_bytes + region * kMxBlockBytes + (size_t)t.gb * nc * F::kWBytes;
+            const int slot = (int)warp_uniform(tab.slot[t.e]);
+            if (slot < 0) continue;
+            const uint8_t* w = a.slot_region + (size_t)slot * a.slot_bytes + region * kMxBlockBytes + (size_t)t.gb * nc * F::kWBytes;
             const uint8_t* x = a.tiles + (size_t)t.tile * nc * T::kBytes;
             for (int c = 0; c < nc; ++c, ++it, w += F::kWBytes, x += T::kBytes) {
-                const int st = it % F::kStages;
-                if (it >= F::kStages) {
-                    ok = mbar_wait(smem_u32(&bar_empty[st]), (it / F::kStages - 1) & 1, abort_p, a.status);
+                if (turn) {
+                    ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, a.status);
                     if (!ok) break;
                 }
                 const uint32_t bar = smem_u32(&bar_full[st]), dst = base + st * F::kStageBytes;
-                mbar_expect_tx(bar, F::kStageBytes);
-                bulk_g2s(dst, w, F::kWBytes, bar);
-                bulk_g2s(dst + F::kWBytes, x, T::kBytes, bar);
+                expect_tx_on(on, bar, F::kStageBytes);
+                bulk_g2s_on(on, dst, w, F::kWBytes, bar);
+                bulk_g2s_on(on, dst + F::kWBytes, x, T::kBytes, bar);
+                if (++st == F::kStages) { st = 0; ++turn; }
             }
         }
-        if (!ok)                                                               // copies still under way land before the CTA ends
+        if (!ok && lane == 0)                                                  // copies still under way land before the CTA ends
             for (int q = max(0, it - F::kStages); q < it; ++q) {
                 abort_flag = 0;
                 mbar_wait(smem_u32(&bar_full[q % F::kStages]), (q / F::kStages) & 1, abort_p, a.status);
@@ -220,17 +223,16 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
-        int it = 0, n = 0;
+        int st = 0, turn = 0, n = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
-            if (tab.slot[item_at(i).e] < 0) continue;
+            if ((int)warp_uniform(tab.slot[item_at(i).e]) < 0) continue;
             const int set = n % F::kSets;
             const uint32_t acc = tmem + set * F::kAccCols;
-            if (n >= F::kSets) ok = mbar_wait(smem_u32(&bar_free[set]), (n / F::kSets - 1) & 1, abort_p, a.status);
+            if (n >= F::kSets) ok = mbar_wait_warp(smem_u32(&bar_free[set]), (n / F::kSets - 1) & 1, abort_p, a.status);
             tc_fence_after();
-            for (int c = 0; c < nc && ok; ++c, ++it) {
-                const int st = it % F::kStages;
-                ok = mbar_wait(smem_u32(&bar_full[st]), (it / F::kStages) & 1, abort_p, a.status);
+            for (int c = 0; c < nc && ok; ++c) {
+                ok = mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t wb = base + st * F::kStageBytes, xb = wb + F::kWBytes;
@@ -252,12 +254,14 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                     const uint64_t dw = smem_desc_sw128(wb + m * kMxBlockBytes);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (j < steps) tc_mma_mxf4(on, acc + m * T::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(T::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1),
-                                    sfx + 4 * (j >> 1) * T::kPieces, c > 0 || j > 0);
+                        if (j < steps)
+                            tc_mma_mxf4(on, acc + m * T::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(T::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1),
+                                        sfx + 4 * (j >> 1) * T::kPieces, c > 0 || j > 0);
                 }
-                if (on) tc_commit(smem_u32(&bar_empty[st]));
+                tc_commit_on(on, smem_u32(&bar_empty[st]));
+                if (++st == F::kStages) { st = 0; ++turn; }
             }
-            if (on) tc_commit(smem_u32(&bar_acc[set]));
+            tc_commit_on(on, smem_u32(&bar_acc[set]));
             ++n;
         }
     } else if (warp >= 2) {

@@ -1,13 +1,16 @@
-// Activations for the block-scaled tensor cores without rounding them to 4 bits: six microscaled 4-bit planes.
+// Activations for the block-scaled tensor cores without rounding them to 4 bits: five microscaled 4-bit planes.
 //
-// Plane 0 is a row's block of 32 elements rounded to E2M1 with a scale that reaches its largest element, plane p the same
-// of what planes 0 .. p - 1 left (exact in fp32).  Each plane leaves at most a fifth of the block's largest, so that six
-// hold a block to 2^-14 of its largest element (2^-17 typically), between bf16's 2^-9 of every element and fp32.  The
-// planes are six more columns of the MMA's N -- rows x 6 columns, of which a decode batch leaves most unused anyway --
-// and their fp32 accumulators are added in the epilogue.  A block with an infinity or NaN becomes NaN.
+// A block of 32 elements of a row is scaled by the power of two that brings its largest element into [2, 4).  Plane 0 is
+// that rounded to E2M1; what is left, at most half a unit, is multiplied by 8 and so is in [-4, 4] again: the next plane,
+// with an eighth of the scale.  Every step is exact in fp32 but for the roundings that the next plane takes up, so five
+// planes hold a block to 2^-14 of its largest element at worst -- between bf16's 2^-9 of every element and fp32 -- and
+// only the first needs a maximum over the block.  (With a maximum for each plane, six planes reached the same; the chain
+// of shuffles took 1.5 us per 256 elements of a row.)  The planes are five columns of the MMA's N instead of one, of
+// which a decode batch leaves most unused anyway, and their fp32 accumulators are added in the epilogue.  A block with an
+// infinity or NaN becomes NaN.
 //
-// A tile is R rows x 256 elements as the MMA wants them: swizzled codes of kPlanes * R columns (plane p of row r is column
-// p R + r), then the 512-byte pieces of their scales, [column / 128][128 elements].
+// A tile is R rows x 256 elements as the MMA wants them: swizzled codes of 5 R columns (plane p of row r is column p R + r;
+// rounded up to 16), then the 512-byte pieces of their scales, [column / 128][128 elements].
 #ifndef SAEM_MX_PLANES_CUH_
 #define SAEM_MX_PLANES_CUH_
 
@@ -15,25 +18,23 @@
 
 namespace saem {
 
-constexpr int kPlanes = 6;
+constexpr int kPlanes = 5;
 
 template <int R>
 struct TileShape {
-    static constexpr int kN = kPlanes * R;                                  // MMA columns: plane p of row r is column p R + r
+    static constexpr int kN = (kPlanes * R + 15) / 16 * 16;                 // MMA columns
     static constexpr int kPieces = (kN + 127) / 128;
     static constexpr int kBytes = kN * 128 + kPieces * 2 * kMxPiece;        // one tile x 256 elements
     static constexpr int kScaleCols = 8 * kPieces;                          // tensor-memory columns of its scales
 };
-// Scale byte of a plane: the power of two that brings the block's largest magnitude into (3, 6].
+// Scale byte of plane 0, from the block's largest magnitude; plane p has kPlaneStep p less (no codes below 0).
+constexpr int kPlaneStep = 3;
 __device__ __forceinline__ int plane_scale_byte(uint32_t amax_bits) {
     const int e = (int)(amax_bits >> 23);
-    if (e == 255) return 255;
-    const int s = (e > 2 ? e - 2 : 0) + ((amax_bits & 0x7FFFFFu) > 0x400000u ? 1 : 0);
-    return s < 254 ? s : 254;
+    return e == 255 ? 255 : e > 1 ? e - 1 : 0;
 }
-__device__ __forceinline__ float power_of_two(int byte) { return __uint_as_float(byte ? (uint32_t)byte << 23 : 1u << 22); }
-__device__ __forceinline__ float inverse_power(int byte) {                  // of 2^(byte - 127)
-    return byte == 254 ? __uint_as_float(1u << 22) : __uint_as_float((uint32_t)(254 - byte) << 23);
+__device__ __forceinline__ float inverse_power(int byte) {                  // of 2^(byte - 127); 0 for NaN's 255, whose codes are 0
+    return byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23);
 }
 
 // Two values to a byte of codes (the first one low), and back.
@@ -60,31 +61,31 @@ __device__ __forceinline__ void widen8(uint4 q, float (&v)[8]) {
 // 256 elements of a row, eight per lane, four lanes per block: the lane's codes in each plane, and the scales of the
 // lane's 128 elements as a word.
 __device__ __forceinline__ void split_planes(float (&v)[8], int lane, uint32_t (&codes)[kPlanes], uint32_t (&scales)[kPlanes]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    const int sb = plane_scale_byte(m);
+    const float up = inverse_power(sb);
+    uint32_t word = (uint32_t)sb << (((lane >> 2) & 3) * 8);
+    word |= __shfl_xor_sync(0xffffffffu, word, 4);
+    word |= __shfl_xor_sync(0xffffffffu, word, 8);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = sb == 255 ? 0.f : v[j] * up;
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
-        uint32_t m = 0;
+        uint32_t w = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const int sb = plane_scale_byte(m);
-        const float up = inverse_power(min(sb, 254)), down = power_of_two(sb);
-        float u[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = v[j] * up;
-        codes[p] = sb == 255 ? 0u : mx_encode8(u);
-        uint32_t h[4];
-        mx_decode8(codes[p], h);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {                                    // what is left: exact in fp32
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[j]));
-            v[2 * j] = sb == 255 ? 0.f : v[2 * j] - f.x * down;
-            v[2 * j + 1] = sb == 255 ? 0.f : v[2 * j + 1] - f.y * down;
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t code = encode2(v[2 * j], v[2 * j + 1]);
+            const float2 back = decode2((uint16_t)code);
+            v[2 * j] = (v[2 * j] - back.x) * 8.f;
+            v[2 * j + 1] = (v[2 * j + 1] - back.y) * 8.f;
+            w |= code << (8 * j);
         }
-        uint32_t word = (uint32_t)sb << (((lane >> 2) & 3) * 8);
-        word |= __shfl_xor_sync(0xffffffffu, word, 4);
-        word |= __shfl_xor_sync(0xffffffffu, word, 8);
-        scales[p] = word;
+        codes[p] = sb >= kPlaneStep * p ? w : 0u;
+        scales[p] = __vsubus4(word, 0x01010101u * (kPlaneStep * p));         // per byte, not below 0
     }
 }
 // What split_planes made, to row r of the tile at dst.
@@ -99,26 +100,29 @@ __device__ __forceinline__ void store_tile_row(uint8_t* dst, int r, int lane, co
                                          ((n >> 5) & 3) * 4) = scales[p];
     }
 }
-// Eight rows' hidden units of one block (a lane holds one unit of each row) to the planes of tile columns r0 .. r0 + 7.
+// Eight rows' hidden units of one block (a lane holds one unit of each row) to the planes of rows r0 .. r0 + 7 of a tile.
 template <int R>
 __device__ __forceinline__ void store_planes(float (&v)[8], int r0, int rows, uint8_t* dst, int blk, int lane) {
     using T = TileShape<R>;
     const int mine = r0 + (lane & 7);                                          // the row whose codes this lane stores
+    int sb[8], my_scale = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sb[q] = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q]) & 0x7FFFFFFFu));
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        v[q] = sb[q] == 255 ? 0.f : v[q] * inverse_power(sb[q]);
+        if ((lane & 7) == q) my_scale = sb[q];
+    }
+#pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
-        uint32_t w = 0, bytes = 0;
+        uint32_t w = 0;
 #pragma unroll
         for (int q = 0; q < 8; q += 2) {                                       // two rows share a conversion
-            int sb[2];
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                sb[z] = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q + z]) & 0x7FFFFFFFu));
-                if ((lane & 7) == q + z) bytes = (uint32_t)sb[z];
-            }
-            uint32_t code = encode2(v[q] * inverse_power(min(sb[0], 254)), v[q + 1] * inverse_power(min(sb[1], 254)));
+            const uint32_t code = encode2(v[q], v[q + 1]);
             const float2 back = decode2((uint16_t)code);
-            v[q] = sb[0] == 255 ? 0.f : v[q] - back.x * power_of_two(sb[0]);   // what is left: exact in fp32
-            v[q + 1] = sb[1] == 255 ? 0.f : v[q + 1] - back.y * power_of_two(sb[1]);
-            w |= code << (4 * q);                                              // codes under a NaN scale do not matter
+            v[q] = (v[q] - back.x) * 8.f;
+            v[q + 1] = (v[q + 1] - back.y) * 8.f;
+            w |= code << (4 * q);
         }
         // eight rows' codes of one unit to eight units' codes of one row: a transposition over eight lanes
 #pragma unroll
@@ -127,11 +131,12 @@ __device__ __forceinline__ void store_planes(float (&v)[8], int r0, int rows, ui
             const uint32_t o = __shfl_xor_sync(0xffffffffu, w, s);
             w = lane & s ? (w & ~low) | ((o >> (4 * s)) & low) : (w & low) | ((o << (4 * s)) & ~low);
         }
-        const int col = p * R + mine;
+        const int col = p * R + mine, scale = my_scale - kPlaneStep * p;
         if (mine < rows) {
-            *reinterpret_cast<uint32_t*>(dst + col * 128 + ((blk ^ (col & 7)) << 4) + (lane >> 3) * 4) = w;
+            *reinterpret_cast<uint32_t*>(dst + col * 128 + ((blk ^ (col & 7)) << 4) + (lane >> 3) * 4) = scale >= 0 ? w : 0u;
             if (lane < 8)
-                dst[T::kN * 128 + ((col >> 7) * 2 + (blk >> 2)) * kMxPiece + (col & 31) * 16 + ((col >> 5) & 3) * 4 + (blk & 3)] = (uint8_t)bytes;
+                dst[T::kN * 128 + ((col >> 7) * 2 + (blk >> 2)) * kMxPiece + (col & 31) * 16 + ((col >> 5) & 3) * 4 + (blk & 3)] =
+                    (uint8_t)max(scale, 0);
         }
     }
 }
@@ -151,7 +156,7 @@ __device__ __forceinline__ void plane_sums(uint32_t taddr, float (&v)[8]) {
     tc_wait_ld();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        asm volatile("" : "+r"(r[0][i]), "+r"(r[1][i]), "+r"(r[2][i]), "+r"(r[3][i]), "+r"(r[4][i]), "+r"(r[5][i]) :: "memory");
+        asm volatile("" : "+r"(r[0][i]), "+r"(r[1][i]), "+r"(r[2][i]), "+r"(r[3][i]), "+r"(r[4][i]) :: "memory");
         v[i] = 0.f;
 #pragma unroll
         for (int p = kPlanes - 1; p >= 0; --p) v[i] += __uint_as_float(r[p][i]);   // the small planes first

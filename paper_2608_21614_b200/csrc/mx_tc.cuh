@@ -12,9 +12,40 @@ namespace saem {
 __device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (8ull << 16) | (8ull << 32) | (1ull << 46);
 }
-// The issuing warp runs its loop as a whole, operands in uniform registers, and one elected lane (`on`) issues: inside an
-// `if (lane == 0)` every operand has to be moved to a uniform register first, and an instruction took some 80 cycles to
-// issue (an MMA of 128 x 48 x 64 takes 44, a scale copy 8).
+// The warps that issue copies and MMAs run their loops as a whole, and one elected lane (`on`) issues.  What the
+// instructions take then stays in uniform registers: inside an `if (lane == 0)`, or behind a wait whose result the
+// compiler must take for different in every lane, each operand has to be moved to a uniform register first, and an MMA or
+// a copy took 80 to 120 cycles to issue (an MMA of 128 x 48 x 64 takes 44, a scale copy 8).
+__device__ __forceinline__ uint32_t warp_uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+}
+__device__ __forceinline__ void expect_tx_on(uint32_t on, uint32_t bar, uint32_t bytes) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %2, 0;\n\t"
+        "@p mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(on) : "memory");
+}
+__device__ __forceinline__ void bulk_g2s_on(uint32_t on, uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
+        ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "r"(on) : "memory");
+}
+__device__ __forceinline__ void tma_2d_on(uint32_t on, uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "@p cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"(on) : "memory");
+}
+__device__ __forceinline__ void tc_commit_on(uint32_t on, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %1, 0;\n\t"
+        "@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(on) : "memory");
+}
 __device__ __forceinline__ uint32_t elect_one() {
     uint32_t r;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));

@@ -30,8 +30,7 @@ constexpr int kFewSfA = 16 + FewTile::kScaleCols, kFewSfB = 8 + FewTile::kScaleC
 
 struct FewShared {
     alignas(8) uint64_t full[kFewMaxStages], empty[kFewMaxStages], acc[2], free[2], x;
-    int idx[kFewPairs];
-    float w[kFewPairs];
+    int slot[SAEM_MAX_EXPERTS];
     uint32_t mask[4];
     int n_active;
     int16_t expert[kFewActive];
@@ -40,31 +39,43 @@ struct FewShared {
     int abort_flag;
 };
 
-// route_row (the same choices and weights) for k <= 8, on the critical path here: 32-bit keys, the winner of round j in
-// lane j.
-__device__ __forceinline__ void few_topk(const float* __restrict__ row, int E, int k, int renorm, int lane, int* idx_out, float* w_out) {
+// route_row (the same choices and weights) for k <= 8, on the critical path here: a lane's four keys are sorted first, so
+// that a round looks at one of them; the winner of round j ends in lane j.
+__device__ __forceinline__ void few_topk(const float* __restrict__ row, int E, int k, int renorm, int lane, int& mine, float& weight) {
     uint32_t key[kPerLane];
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) key[i] = lane + 32 * i < E ? order_key(row[lane + 32 * i]) : 0u;   // 0: below every real key
+    int id[kPerLane];
     float all = 0.f, win = 0.f;
-    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        id[i] = lane + 32 * i;
+        key[i] = id[i] < E ? order_key(row[id[i]]) : 0u;                       // 0: below every real key
+    }
+    auto sort2 = [&](int x, int y) {                                           // larger first, equal keys by id
+        const bool swap = key[y] > key[x] || (key[y] == key[x] && id[y] < id[x]);
+        const uint32_t kx = key[x];
+        const int ix = id[x];
+        key[x] = swap ? key[y] : kx;  id[x] = swap ? id[y] : ix;
+        key[y] = swap ? kx : key[y];  id[y] = swap ? ix : id[y];
+    };
+    sort2(0, 1); sort2(2, 3); sort2(0, 2); sort2(1, 3); sort2(1, 2);
     float vmax = 0.f;
+    mine = 0;
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
-        const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(key[0], key[1]), max(key[2], key[3])));
-        const int at = key[0] == top ? lane : key[1] == top ? lane + 32 : key[2] == top ? lane + 64 : key[3] == top ? lane + 96 : 128;
-        const int e = (int)__reduce_min_sync(0xffffffffu, (unsigned)at);
+        const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
+        const int e = (int)__reduce_min_sync(0xffffffffu, key[0] == top ? (unsigned)id[0] : 0xffffffffu);
         if (j == 0) {
             vmax = key_value(top);
             if (!renorm) {
 #pragma unroll
                 for (int i = 0; i < kPerLane; ++i)
-                    if (lane + 32 * i < E) all += expf(key_value(key[i]) - vmax);
+                    if (key[i]) all += expf(key_value(key[i]) - vmax);
             }
         }
-#pragma unroll
-        for (int i = 0; i < kPerLane; ++i)
-            if (e == lane + 32 * i) key[i] = 0u;                               // taken
+        if (e == id[0]) {                                                      // taken
+            key[0] = key[1]; key[1] = key[2]; key[2] = key[3]; key[3] = 0u;
+            id[0] = id[1]; id[1] = id[2]; id[2] = id[3]; id[3] = 0x7FFFFFFF;
+        }
         if (lane == j) {
             win = key_value(top);
             mine = e;
@@ -81,16 +92,11 @@ __device__ __forceinline__ void few_topk(const float* __restrict__ row, int E, i
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
-    if (lane < k) {
-        idx_out[lane] = mine;
-        w_out[lane] = z / sum;
-    }
+    weight = z / sum;
 }
 
-// Barriers; routes the batch (one warp per token) and lists the active experts in ascending order, the always-on ones
-// last; experts without a slot are left out (status word).  All threads call it; ends with a barrier.
-__device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, const SlotTable& tab, int n_stage, bool report) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, P = a.T * a.k;
+// What needs no input: barriers, tables.  Ends with a barrier.
+__device__ __forceinline__ void few_init(FewShared& s, const MxFewArgs& a, const SlotTable& tab, int n_stage) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < n_stage; ++i) {
             mbar_init(smem_u32(&s.full[i]), 1);
@@ -105,24 +111,46 @@ __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x < 4) s.mask[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < a.E + a.S; i += kFewThreads) s.slot[i] = tab.slot[i];
     for (int i = threadIdx.x; i < kFewActive * kFewTokens; i += kFewThreads) (&s.weight[0][0])[i] = 0.f;
-    if (warp < a.T) few_topk(a.logits + (size_t)warp * a.E, a.E, a.k, a.renorm, lane, s.idx + warp * a.k, s.w + warp * a.k);
     __syncthreads();
-    const int e = threadIdx.x < P ? s.idx[threadIdx.x] : -1;
-    const bool have = e >= 0 && tab.slot[e] >= 0;
-    if (have) atomicOr(&s.mask[e >> 5], 1u << (e & 31));
-    else if (e >= 0 && report) atomicExch(a.status, SAEM_ERR_NOT_RESIDENT);
-    __syncthreads();
-    if (have) {
-        int p = __popc(s.mask[e >> 5] & ((1u << (e & 31)) - 1u));
-        for (int q = 0; q < (e >> 5); ++q) p += __popc(s.mask[q]);
-        s.expert[p] = (int16_t)e;
-        s.weight[p][threadIdx.x / a.k] = s.w[threadIdx.x];
+}
+// Routes the batch (one warp per token) and lists the active experts in ascending order, the always-on ones last; experts
+// without a slot are left out (status word).  All threads call it; ends with a barrier.
+__device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, bool report) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int e = -1;
+    float w = 0.f;
+    if (warp < a.T) {
+        few_topk(a.logits + (size_t)warp * a.E, a.E, a.k, a.renorm, lane, e, w);
+        if (lane >= a.k) {
+            e = -1;
+        } else {
+            if (report) {
+                a.topk_idx[warp * a.k + lane] = e;
+                a.topk_w[warp * a.k + lane] = w;
+            }
+            if (s.slot[e] >= 0) {
+                atomicOr(&s.mask[e >> 5], 1u << (e & 31));
+            } else {
+                if (report) atomicExch(a.status, SAEM_ERR_NOT_RESIDENT);
+                e = -1;
+            }
+        }
     }
-    if (threadIdx.x == 0) {
-        int n = __popc(s.mask[0]) + __popc(s.mask[1]) + __popc(s.mask[2]) + __popc(s.mask[3]);
+    __syncthreads();
+    const uint32_t m0 = s.mask[0], m1 = s.mask[1], m2 = s.mask[2], m3 = s.mask[3];
+    if (e >= 0) {
+        const int word = e >> 5;
+        const int p = __popc(s.mask[word] & ((1u << (e & 31)) - 1u)) + (word > 0 ? __popc(m0) : 0) + (word > 1 ? __popc(m1) : 0) +
+                      (word > 2 ? __popc(m2) : 0);
+        s.expert[p] = (int16_t)e;
+        s.weight[p][warp] = w;
+    }
+    if (threadIdx.x == kFewThreads - 1) {
+        int n = __popc(m0) + __popc(m1) + __popc(m2) + __popc(m3);
         for (int q = 0; q < a.S; ++q) {
-            if (tab.slot[a.E + q] < 0) {
+            if (s.slot[a.E + q] < 0) {
                 if (report) atomicExch(a.status, SAEM_ERR_NOT_RESIDENT);
                 continue;
             }
@@ -172,6 +200,7 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
     const uint32_t base = xs_addr + max(nc * FewTile::kBytes, 8192);           // the ring: 8 KB before it and behind it are ours
     volatile int* abort_p = &s.abort_flag;
     few_alloc(s, 512);
+    few_init(s, a, tab, n);
     pdl_wait();
     pdl_launch_dependents();
     // the first run of x that a warp will split is on its way while the batch is routed
@@ -181,12 +210,8 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         return i < tasks && col < a.d ? *reinterpret_cast<const uint4*>(a.x + (size_t)t * a.d + col) : make_uint4(0u, 0u, 0u, 0u);
     };
     uint4 q = warp >= 2 ? load_x(warp - 2) : make_uint4(0u, 0u, 0u, 0u);
-    few_route(s, a, tab, n, blockIdx.x == 0);
+    few_route(s, a, blockIdx.x == 0);
     tc_fence_after();
-    if (blockIdx.x == 0 && threadIdx.x < a.T * a.k) {
-        a.topk_idx[threadIdx.x] = s.idx[threadIdx.x];
-        a.topk_w[threadIdx.x] = s.w[threadIdx.x];
-    }
     const uint32_t tmem = warp_uniform(s.tmem), tmem_sf = tmem + 4 * FewTile::kN;
     const int per = a.f / 128 * (HALF ? 2 : 1), total = (int)warp_uniform(s.n_active) * per;
     if (warp == 0) {
@@ -196,7 +221,7 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         bool ok = true;
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
             const int act = i / per, part = i - act * per, tile = HALF ? part >> 1 : part;
-            const uint8_t* w = a.slot_region + (size_t)warp_uniform(tab.slot[s.expert[act]]) * a.slot_bytes + (size_t)tile * nc * 2 * kMxBlockBytes;
+            const uint8_t* w = a.slot_region + (size_t)warp_uniform(s.slot[s.expert[act]]) * a.slot_bytes + (size_t)tile * nc * 2 * kMxBlockBytes;
             for (int c = 0; c < nc; ++c, ++it, w += 2 * kMxBlockBytes) {
                 if (turn) {
                     ok = mbar_wait_warp(smem_u32(&s.empty[st]), (turn - 1) & 1, abort_p, a.status);
@@ -318,9 +343,10 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
     constexpr int n = kFewStagesB;
     volatile int* abort_p = &s.abort_flag;
     few_alloc(s, 128);
+    few_init(s, a, tab, n);
     // The logits are complete when this launch starts (the CTAs of the first one wait for them before they let it begin)
     // and no weight is written by the first launch: only h has to be waited for.
-    few_route(s, a, tab, n, false);
+    few_route(s, a, false);
     tc_fence_after();
     const uint32_t tmem = warp_uniform(s.tmem), tmem_sf = tmem + 64;
     const int all = (int)warp_uniform(s.n_active) * nc, rank = (int)cluster_ctarank();
@@ -333,7 +359,7 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             const int act = q / nc;
             expect_tx_on(on, smem_u32(&s.full[st]), kFewStageB);
             bulk_g2s_on(on, base + st * kFewStageB,
-                        a.slot_region + (size_t)warp_uniform(tab.slot[s.expert[act]]) * a.slot_bytes +
+                        a.slot_region + (size_t)warp_uniform(s.slot[s.expert[act]]) * a.slot_bytes +
                             (mx_gate_up_blocks(a.d, a.f) + tile * nc + (q - act * nc)) * kMxBlockBytes,
                         kMxBlockBytes, smem_u32(&s.full[st]));
         };

@@ -1,13 +1,13 @@
 // Activations for the block-scaled tensor cores without rounding them to 4 bits: five microscaled 4-bit planes.
 //
-// A block of 32 elements of a row is scaled by the power of two that brings its largest element into [2, 4).  Plane 0 is
-// that rounded to E2M1; what is left, at most half a unit, is multiplied by 8 and so is in [-4, 4] again: the next plane,
-// with an eighth of the scale.  Every step is exact in fp32 but for the roundings that the next plane takes up, so five
-// planes hold a block to 2^-14 of its largest element at worst -- between bf16's 2^-9 of every element and fp32 -- and
-// only the first needs a maximum over the block.  (With a maximum for each plane, six planes reached the same; the chain
-// of shuffles took 1.5 us per 256 elements of a row.)  The planes are five columns of the MMA's N instead of one, of
-// which a decode batch leaves most unused anyway, and their fp32 accumulators are added in the epilogue.  A block with an
-// infinity or NaN becomes NaN.
+// A block of 32 elements of a row is scaled by the power of two that brings its largest element into [1.7, 3.41) and each
+// element v is rounded once, to a multiple of 2^-12 -- 2^-13.8 of the block's largest at worst, between bf16's 2^-9 of
+// every element and fp32.  The integer 4096 v is written in radix 8 with digits d_0 .. d_4 of -4 .. 3,
+//     v = d_0 + d_1 / 8 + d_2 / 64 + d_3 / 512 + d_4 / 4096,
+// (at most 3.42) all of which E2M1 holds: plane p is the codes of d_p with 1 / 8^p of the scale.  The planes are five columns of the
+// MMA's N instead of one, of which a decode batch leaves most unused anyway, and their fp32 accumulators are added in the
+// epilogue.  One FMA with a large constant rounds an element and biases it so that its digits + 4 are plain bit fields;
+// a byte permutation looks four of them up at a time.  A block with an infinity or NaN becomes NaN.
 //
 // A tile is R rows x 256 elements as the MMA wants them: swizzled codes of 5 R columns (plane p of row r is column p R + r;
 // rounded up to 16), then the 512-byte pieces of their scales, [column / 128][128 elements].
@@ -30,23 +30,35 @@ struct TileShape {
 // Scale byte of plane 0, from the block's largest magnitude; plane p has kPlaneStep p less (no codes below 0).
 constexpr int kPlaneStep = 3;
 __device__ __forceinline__ int plane_scale_byte(uint32_t amax_bits) {
-    const int e = (int)(amax_bits >> 23);
-    return e == 255 ? 255 : e > 1 ? e - 1 : 0;
+    const int e = (int)(amax_bits >> 23) + ((amax_bits & 0x7FFFFFu) >= 0x5A0000u ? 1 : 0);   // 1.703 * 2^e on
+    return amax_bits >= 0x7F800000u ? 255 : max(e - 1, 0);
 }
-__device__ __forceinline__ float inverse_power(int byte) {                  // of 2^(byte - 127); 0 for NaN's 255, whose codes are 0
-    return byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23);
+__device__ __forceinline__ float inverse_power(int byte) {                  // of 2^(byte - 127)
+    return byte == 254 ? __uint_as_float(1u << 22) : __uint_as_float((uint32_t)(254 - byte) << 23);
 }
-
-// Two values to a byte of codes (the first one low), and back.
-__device__ __forceinline__ uint16_t encode2(float lo, float hi) {
-    uint16_t b;
-    asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %2, %1;\n\tmov.b16 %0, {c, 0};\n\t}" : "=h"(b) : "f"(lo), "f"(hi));
-    return b;
-}
-__device__ __forceinline__ float2 decode2(uint16_t b) {
-    uint32_t h;
-    asm("{\n\t.reg .b8 c, z;\n\tmov.b16 {c, z}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(h) : "h"(b));
-    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+// An element (already divided by its scale) rounded to 2^-12: digit p plus 4 is bits 12 - 3 p and up.  The constant is
+// 1.5 * 2^23 and 4 in every digit.
+__device__ __forceinline__ uint32_t plane_digits(float v) { return __float_as_uint(fmaf(v, 4096.f, 12582912.f + 18724.f)); }
+// Eight elements' digits to a word of eight codes for each plane.
+__device__ __forceinline__ void plane_words(const uint32_t (&y)[8], uint32_t (&w)[kPlanes]) {
+    uint32_t pair[4];                                                        // elements j and j + 4
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pair[j] = __byte_perm(y[j], y[j + 4], 0x5410);
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) {
+        const int at = 12 - 3 * p;
+        uint32_t sel = 0;                                                    // digits + 4 as selectors, elements 0-3 low, 4-7 high
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int up = 4 * j - at;
+            sel |= (up >= 0 ? pair[j] << up : pair[j] >> -up) & (0x00070007u << (4 * j));
+        }
+        // E2M1 codes of -4 .. 3
+        uint32_t lo = __byte_perm(0x0A0C0D0Eu, 0x05040200u, sel), hi = __byte_perm(0x0A0C0D0Eu, 0x05040200u, sel >> 16);
+        lo |= lo >> 4;                                                       // bytes 0 and 2: two codes each
+        hi |= hi >> 4;
+        w[p] = __byte_perm(lo, hi, 0x6420);
+    }
 }
 
 // Eight bf16 values.
@@ -60,31 +72,24 @@ __device__ __forceinline__ void widen8(uint4 q, float (&v)[8]) {
 }
 // 256 elements of a row, eight per lane, four lanes per block: the lane's codes in each plane, and the scales of the
 // lane's 128 elements as a word.
-__device__ __forceinline__ void split_planes(float (&v)[8], int lane, uint32_t (&codes)[kPlanes], uint32_t (&scales)[kPlanes]) {
+__device__ __forceinline__ void split_planes(const float (&v)[8], int lane, uint32_t (&codes)[kPlanes], uint32_t (&scales)[kPlanes]) {
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     const int sb = plane_scale_byte(m);
-    const float up = inverse_power(sb);
+    const float up = inverse_power(min(sb, 254));
     uint32_t word = (uint32_t)sb << (((lane >> 2) & 3) * 8);
     word |= __shfl_xor_sync(0xffffffffu, word, 4);
     word |= __shfl_xor_sync(0xffffffffu, word, 8);
+    uint32_t y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = sb == 255 ? 0.f : v[j] * up;
+    for (int j = 0; j < 8; ++j) y[j] = plane_digits(sb == 255 ? 0.f : v[j] * up);
+    plane_words(y, codes);
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t code = encode2(v[2 * j], v[2 * j + 1]);
-            const float2 back = decode2((uint16_t)code);
-            v[2 * j] = (v[2 * j] - back.x) * 8.f;
-            v[2 * j + 1] = (v[2 * j + 1] - back.y) * 8.f;
-            w |= code << (8 * j);
-        }
-        codes[p] = sb >= kPlaneStep * p ? w : 0u;
+        if (sb < kPlaneStep * p) codes[p] = 0u;
         scales[p] = __vsubus4(word, 0x01010101u * (kPlaneStep * p));         // per byte, not below 0
     }
 }
@@ -102,28 +107,21 @@ __device__ __forceinline__ void store_tile_row(uint8_t* dst, int r, int lane, co
 }
 // Eight rows' hidden units of one block (a lane holds one unit of each row) to the planes of rows r0 .. r0 + 7 of a tile.
 template <int R>
-__device__ __forceinline__ void store_planes(float (&v)[8], int r0, int rows, uint8_t* dst, int blk, int lane) {
+__device__ __forceinline__ void store_planes(const float (&v)[8], int r0, int rows, uint8_t* dst, int blk, int lane) {
     using T = TileShape<R>;
     const int mine = r0 + (lane & 7);                                          // the row whose codes this lane stores
-    int sb[8], my_scale = 0;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) sb[q] = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q]) & 0x7FFFFFFFu));
+    int my_scale = 0;
+    uint32_t y[8], codes[kPlanes];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        v[q] = sb[q] == 255 ? 0.f : v[q] * inverse_power(sb[q]);
-        if ((lane & 7) == q) my_scale = sb[q];
+        const int sb = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q]) & 0x7FFFFFFFu));
+        y[q] = plane_digits(sb == 255 ? 0.f : v[q] * inverse_power(min(sb, 254)));
+        if ((lane & 7) == q) my_scale = sb;
     }
+    plane_words(y, codes);
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int q = 0; q < 8; q += 2) {                                       // two rows share a conversion
-            const uint32_t code = encode2(v[q], v[q + 1]);
-            const float2 back = decode2((uint16_t)code);
-            v[q] = (v[q] - back.x) * 8.f;
-            v[q + 1] = (v[q + 1] - back.y) * 8.f;
-            w |= code << (4 * q);
-        }
+        uint32_t w = codes[p];
         // eight rows' codes of one unit to eight units' codes of one row: a transposition over eight lanes
 #pragma unroll
         for (int s = 4; s > 0; s >>= 1) {

@@ -26,7 +26,8 @@ using FewTile = TileShape<kFewTokens>;
 constexpr int kFewHalf = kMxBlockCodes / 2 + 2 * kMxPiece;     // 64 rows of a block, and its scales
 constexpr int kFewStageB = kMxBlockBytes + FewTile::kBytes;
 constexpr int kFewStagesB = 4;
-constexpr int kFewSfA = 16 + FewTile::kScaleCols, kFewSfB = 8 + FewTile::kScaleCols;
+constexpr int kFewSfB = 8 + FewTile::kScaleCols;             // tensor-memory columns of a stage's scales (gate/up: 16, x's are loaded once)
+constexpr int kFewMaxChunks = 16;                            // of x: d_model <= 4096
 
 struct FewShared {
     alignas(8) uint64_t full[kFewMaxStages], empty[kFewMaxStages], acc[2], free[2], x;
@@ -203,13 +204,18 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
     few_init(s, a, tab, n);
     pdl_wait();
     pdl_launch_dependents();
-    // the first run of x that a warp will split is on its way while the batch is routed
+    // the runs of x that a warp will split are on their way while the batch is routed
     const int tasks = a.T * nc;
-    auto load_x = [&](int i) {
-        const int t = i / nc, col = (i - t * nc) * kMxChunk + lane * 8;
-        return i < tasks && col < a.d ? *reinterpret_cast<const uint4*>(a.x + (size_t)t * a.d + col) : make_uint4(0u, 0u, 0u, 0u);
+    constexpr int kAhead = 8;
+    uint4 q[kAhead];
+    auto load_x = [&](int first) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = first + 8 * u, t = i / nc, col = (i - t * nc) * kMxChunk + lane * 8;
+            q[u] = i < tasks && col < a.d ? *reinterpret_cast<const uint4*>(a.x + (size_t)t * a.d + col) : make_uint4(0u, 0u, 0u, 0u);
+        }
     };
-    uint4 q = warp >= 2 ? load_x(warp - 2) : make_uint4(0u, 0u, 0u, 0u);
+    if (warp >= 2) load_x(warp - 2);
     few_route(s, a, blockIdx.x == 0);
     tc_fence_after();
     const uint32_t tmem = warp_uniform(s.tmem), tmem_sf = tmem + 4 * FewTile::kN;
@@ -245,8 +251,15 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
+        const uint64_t codes0 = smem_desc_sw128(base), x0 = smem_desc_sw128(xs_addr), scales0 = smem_desc_scales(base);
+        const uint64_t xscales0 = smem_desc_scales(xs_addr + FewTile::kN * 128);
         int st = 0, turn = 0, k = 0;
         bool ok = mbar_wait_warp(smem_u32(&s.x), 0, abort_p, a.status);
+        tc_fence_after();
+        const uint32_t tmem_x = tmem_sf + n * 16;                              // x's scales stay in tensor memory for all items
+        for (int c = 0; c < nc && ok; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) tc_cp_scales(on, tmem_x + c * 8 + 4 * h, desc_at(xscales0, c * FewTile::kBytes + h * kMxPiece));
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x, ++k) {
             const int set = k & 1;
             const uint32_t acc = tmem + set * 2 * FewTile::kN;
@@ -256,29 +269,25 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
                 ok = mbar_wait_warp(smem_u32(&s.full[st]), turn & 1, abort_p, a.status);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t stage = base + st * kStage, xb = xs_addr + c * FewTile::kBytes;
-                const uint32_t sf = tmem_sf + st * kFewSfA;
+                const uint32_t at = st * kStage, sf = tmem_sf + st * 16, sfx = tmem_x + c * 8;
+                const uint64_t ds = desc_at(scales0, at), dx = desc_at(x0, c * FewTile::kBytes);
                 const int steps = min(4, (a.d - c * kMxChunk) / 64);
-                // scales of gate (m = 0) and up behind the codes of both, or behind each one's own
-                auto scales_at = [&](int m, int h) { return stage + (HALF ? 2 * kCodes + m * 2 * kMxPiece : m * kMxBlockBytes + kCodes) + h * kMxPiece; };
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (2 * h >= steps) break;
-                    tc_cp_scales(on, sf + 4 * h, smem_desc_scales(scales_at(0, h)));
-                    tc_cp_scales(on, sf + 8 + 4 * h, smem_desc_scales(scales_at(1, h)));
-                    tc_cp_scales(on, sf + 16 + 4 * h, smem_desc_scales(xb + FewTile::kN * 128 + h * kMxPiece));
-                }
-                const uint64_t dx = smem_desc_sw128(xb);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    // a second half's row 64 stands first: its block would begin 8 KB before
-                    const uint64_t dw = smem_desc_sw128(stage + (HALF ? m * kCodes - (i & 1) * kCodes : m * kMxBlockBytes));
+                    for (int m = 0; m < 2; ++m)                                // behind the codes of both, or behind each one's own
+                        tc_cp_scales(on, sf + m * 8 + 4 * h, desc_at(ds, (HALF ? 2 * kCodes + m * 2 * kMxPiece : m * kMxBlockBytes + kCodes) + h * kMxPiece));
+                }
+                // a second half's row 64 stands first: its block would begin 8 KB before
+                const uint64_t dw = desc_at(codes0, at) - (HALF && (i & 1) ? kCodes / 16 : 0);
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (j < steps)
-                            tc_mma_mxf4(on, acc + m * FewTile::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(FewTile::kN, (j & 1) * 2),
-                                        sf + m * 8 + 4 * (j >> 1), sf + 16 + 4 * (j >> 1), c > 0 || j > 0);
-                }
+                            tc_mma_mxf4(on, acc + m * FewTile::kN, desc_at(dw, m * (HALF ? kCodes : kMxBlockBytes) + 32 * j), desc_at(dx, 32 * j),
+                                        idesc_mxf4(FewTile::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1), sfx + 4 * (j >> 1), c > 0 || j > 0);
                 tc_commit_on(on, smem_u32(&s.empty[st]));
                 if (++st == n) { st = 0; ++turn; }
             }
@@ -286,14 +295,18 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         }
     } else {
         // ---------------------------------------------------------------- x's planes
-        for (int i = warp - 2; i < tasks; i += 8) {
-            const int t = i / nc, c = i - t * nc;
-            float v[8];
-            widen8(q, v);
-            q = load_x(i + 8);
-            uint32_t codes[kPlanes], scales[kPlanes];
-            split_planes(v, lane, codes, scales);
-            store_tile_row<kFewTokens>(xs + (size_t)c * FewTile::kBytes, t, lane, codes, scales);
+        for (int first = warp - 2; first < tasks; first += 8 * kAhead) {
+            if (first > 7) load_x(first);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = first + 8 * u, t = i / nc, c = i - t * nc;
+                if (i >= tasks) break;
+                float v[8];
+                widen8(q[u], v);
+                uint32_t codes[kPlanes], scales[kPlanes];
+                split_planes(v, lane, codes, scales);
+                store_tile_row<kFewTokens>(xs + (size_t)c * FewTile::kBytes, t, lane, codes, scales);
+            }
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -317,7 +330,7 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
                     const float w = s.weight[act][t];
-                    v[t] = w != 0.f ? w * (v[t] / (1.f + __expf(-v[t])) * u[t]) : 0.f;   // columns of other tokens hold anything
+                    v[t] = w != 0.f ? w * swiglu(v[t], u[t]) : 0.f;            // columns of other tokens hold anything
                 }
                 store_planes<kFewTokens>(v, 0, a.T, a.h_tiles + ((size_t)act * mx_chunks(a.f) + (tile >> 1)) * FewTile::kBytes,
                                          (tile & 1) * 4 + quad, lane);
@@ -384,26 +397,27 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
         bool ok = true;
+        const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base);
         int st = 0, turn = 0;
         for (int q = q0; q < q1; ++q) {
             const int c = q % nc;
             ok = mbar_wait_warp(smem_u32(&s.full[st]), turn & 1, abort_p, a.status);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t wb = base + st * kFewStageB, xb = wb + kMxBlockBytes, sf = tmem_sf + st * kFewSfB;
+            const uint32_t at = st * kFewStageB, sf = tmem_sf + st * kFewSfB;
+            const uint64_t dw = desc_at(codes0, at), dx = desc_at(codes0, at + kMxBlockBytes), ds = desc_at(scales0, at);
             const int steps = min(4, (a.f - c * kMxChunk) / 64);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (2 * h >= steps) break;
-                tc_cp_scales(on, sf + 4 * h, smem_desc_scales(wb + kMxBlockCodes + h * kMxPiece));
-                tc_cp_scales(on, sf + 8 + 4 * h, smem_desc_scales(xb + FewTile::kN * 128 + h * kMxPiece));
+                tc_cp_scales(on, sf + 4 * h, desc_at(ds, kMxBlockCodes + h * kMxPiece));
+                tc_cp_scales(on, sf + 8 + 4 * h, desc_at(ds, kMxBlockBytes + FewTile::kN * 128 + h * kMxPiece));
             }
-            const uint64_t dw = smem_desc_sw128(wb), dx = smem_desc_sw128(xb);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (j < steps)
-                    tc_mma_mxf4(on, tmem, dw + 2 * j, dx + 2 * j, idesc_mxf4(FewTile::kN, (j & 1) * 2), sf + 4 * (j >> 1), sf + 8 + 4 * (j >> 1),
-                                q > q0 || j > 0);
+                    tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(dx, 32 * j), idesc_mxf4(FewTile::kN, (j & 1) * 2), sf + 4 * (j >> 1),
+                                sf + 8 + 4 * (j >> 1), q > q0 || j > 0);
             tc_commit_on(on, smem_u32(&s.empty[st]));
             if (++st == n) { st = 0; ++turn; }
         }
@@ -443,7 +457,7 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
 }
 
 // x's tiles (7 KB per 256 elements) stand beside three stages of weights at least.
-bool mx_few_supported(int T, int k, int d) { return T <= kFewTokens && k <= kFewTokens && mx_chunks(d) <= 16; }
+bool mx_few_supported(int T, int k, int d) { return T <= kFewTokens && k <= kFewTokens && mx_chunks(d) <= kFewMaxChunks; }
 
 cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStream_t st, int* n_launch) {
     static bool done[64];
@@ -461,8 +475,8 @@ cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStrea
     const int x_bytes = mx_chunks(a.d) * FewTile::kBytes, before = x_bytes > 8192 ? x_bytes : 8192, stage = 2 * (half ? kFewHalf : kMxBlockBytes);
     const int around = 1024 + before + (half ? 8192 : 0);
     a.stages_a = (kMost - around) / stage;
-    const int most = half ? kFewMaxStages : 5;
-    if (a.stages_a > most) a.stages_a = most;                                  // tensor memory: 192 accumulator columns + 24 per stage
+    const int most = kFewMaxStages;                                            // tensor memory: 192 columns of sums, 16 per stage, 8 per chunk of x
+    if (a.stages_a > most) a.stages_a = most;
     cudaError_t e = launch_pdl(half ? mx_few_gate_up_kernel<true> : mx_few_gate_up_kernel<false>, dim3((unsigned)(items < n_sm ? items : n_sm)),
                                dim3(kFewThreads), (size_t)(around + a.stages_a * stage), st, a, tab);
     if (e != cudaSuccess) return e;

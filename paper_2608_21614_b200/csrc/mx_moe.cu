@@ -223,6 +223,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
+        const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base);
         int st = 0, turn = 0, n = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
@@ -235,7 +236,8 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                 ok = mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, a.status);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t wb = base + st * F::kStageBytes, xb = wb + F::kWBytes;
+                const uint32_t at = st * F::kStageBytes;
+                const uint64_t dw = desc_at(codes0, at), dx = desc_at(codes0, at + F::kWBytes), ds = desc_at(scales0, at);
                 const uint32_t sf = tmem_sf + st * F::kSfCols, sfx = sf + (MODE == 0 ? 16 : 8);
                 const int steps = min(4, (K - c * kMxChunk) / 64);             // K is a multiple of 128
 #pragma unroll
@@ -243,21 +245,18 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                     if (2 * h >= steps) break;
 #pragma unroll
                     for (int m = 0; m < (MODE == 0 ? 2 : 1); ++m)
-                        tc_cp_scales(on, sf + m * 8 + 4 * h, smem_desc_scales(wb + m * kMxBlockBytes + kMxBlockCodes + h * kMxPiece));
+                        tc_cp_scales(on, sf + m * 8 + 4 * h, desc_at(ds, m * kMxBlockBytes + kMxBlockCodes + h * kMxPiece));
 #pragma unroll
                     for (int q = 0; q < T::kPieces; ++q)
-                        tc_cp_scales(on, sfx + 4 * (h * T::kPieces + q), smem_desc_scales(xb + T::kN * 128 + (q * 2 + h) * kMxPiece));
+                        tc_cp_scales(on, sfx + 4 * (h * T::kPieces + q), desc_at(ds, F::kWBytes + T::kN * 128 + (q * 2 + h) * kMxPiece));
                 }
-                const uint64_t dx = smem_desc_sw128(xb);
 #pragma unroll
-                for (int m = 0; m < (MODE == 0 ? 2 : 1); ++m) {
-                    const uint64_t dw = smem_desc_sw128(wb + m * kMxBlockBytes);
+                for (int m = 0; m < (MODE == 0 ? 2 : 1); ++m)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (j < steps)
-                            tc_mma_mxf4(on, acc + m * T::kN, dw + 2 * j, dx + 2 * j, idesc_mxf4(T::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1),
-                                        sfx + 4 * (j >> 1) * T::kPieces, c > 0 || j > 0);
-                }
+                            tc_mma_mxf4(on, acc + m * T::kN, desc_at(dw, m * kMxBlockBytes + 32 * j), desc_at(dx, 32 * j),
+                                        idesc_mxf4(T::kN, (j & 1) * 2), sf + m * 8 + 4 * (j >> 1), sfx + 4 * (j >> 1) * T::kPieces, c > 0 || j > 0);
                 tc_commit_on(on, smem_u32(&bar_empty[st]));
                 if (++st == F::kStages) { st = 0; ++turn; }
             }
@@ -293,7 +292,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
                     float u[8];
                     plane_sums<R>(acc + T::kN + r0, u);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = v[q] / (1.f + __expf(-v[q])) * u[q];
+                    for (int q = 0; q < 8; ++q) v[q] = swiglu(v[q], u[q]);
                     // the warp's 32 hidden units are one block of each row: chunk gb / 2 of the row, block (gb & 1) * 4 + quad
                     uint8_t* dst = a.h_tiles + ((size_t)t.tile * mx_chunks(a.f) + (t.gb >> 1)) * T::kBytes;
                     store_planes<R>(v, r0, t.rows, dst, (t.gb & 1) * 4 + quad, lane);

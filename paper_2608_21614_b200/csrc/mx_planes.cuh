@@ -105,6 +105,7 @@ __device__ __forceinline__ void store_tile_row(uint8_t* dst, int r, int lane, co
                                          ((n >> 5) & 3) * 4) = scales[p];
     }
 }
+__device__ __forceinline__ float swiglu(float z, float up) { return __fdividef(z, 1.f + __expf(-z)) * up; }   // 2^-21 or so: far below the planes'
 // Eight rows' hidden units of one block (a lane holds one unit of each row) to the planes of rows r0 .. r0 + 7 of a tile.
 template <int R>
 __device__ __forceinline__ void store_planes(const float (&v)[8], int r0, int rows, uint8_t* dst, int blk, int lane) {
@@ -114,6 +115,8 @@ __device__ __forceinline__ void store_planes(const float (&v)[8], int r0, int ro
     uint32_t y[8], codes[kPlanes];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
+        y[q] = 0;
+        if (r0 + q >= rows) continue;
         const int sb = plane_scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[q]) & 0x7FFFFFFFu));
         y[q] = plane_digits(sb == 255 ? 0.f : v[q] * inverse_power(min(sb, 254)));
         if ((lane & 7) == q) my_scale = sb;

@@ -66,6 +66,8 @@ __device__ __forceinline__ void tc_mma_mxf4(uint32_t on, uint32_t d_tmem, uint64
         "@p tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(on) : "memory");
 }
+// Both kinds of descriptor count the address in units of 16 bytes in their low bits: `bytes` further on.
+__device__ __forceinline__ uint64_t desc_at(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
 // Instruction descriptor of kind::mxf4: E2M1 x E2M1, K-major, UE8M0 scales, M = 128, N = n; `id` (0 or 2) selects the
 // upper or lower two scales of a 32-bit column for both operands.
 __device__ __forceinline__ uint32_t idesc_mxf4(int n, int id) {

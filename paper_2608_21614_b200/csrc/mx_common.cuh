@@ -79,6 +79,52 @@ __device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits) {
     const int e = (int)(amax_bits >> 23);
     return e == 255 ? 255 : (e > 2 ? e - 2 : 0);
 }
+// Eight elements of a row from `col` on as fp32; what lies beyond `cols` is zero.  VEC: the row is 16-byte aligned and
+// cols a multiple of 8.
+template <bool BF16, bool VEC>
+__device__ __forceinline__ void load8(const void* __restrict__ row, long long col, long long cols, float (&v)[8]) {
+    if (VEC) {
+        if (col >= cols) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        } else if (BF16) {
+            const uint4 q = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + col));
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        } else {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + col);
+            const float4 a = __ldcs(p), b = __ldcs(p + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.f;
+            if (col + i < cols)
+                v[i] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[col + i] << 16)
+                            : static_cast<const float*>(row)[col + i];
+        }
+    }
+}
+
+// Eight elements of a block that four neighbouring lanes share to their codes, and the block's scale byte.
+__device__ __forceinline__ uint32_t mx_quantize8(const float (&v)[8], int& scale) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7FFFFFFFu);   // NaN above infinity
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+    scale = mx_scale_byte(amax);
+    const float inv = __uint_as_float((uint32_t)(254 - min(scale, 253)) << 23);
+    float u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = v[i] * inv;
+    return scale == 255 ? 0u : mx_encode8(u);
+}
 #endif
 
 }  // namespace saem

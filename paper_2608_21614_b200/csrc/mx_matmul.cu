@@ -7,17 +7,19 @@
 // consecutive n.  A stage is 256 elements of k: 128-byte rows of codes under the 128-byte swizzle (TMA) and the scales'
 // 512-byte pieces (plain bulk copies, moved to tensor memory by tcgen05.cp as they are).
 //
-// Few tokens: the weights' bytes are the bound, and n / 128 tiles are too few for the SMs.  The k range is then split
-// over a cluster of 2, 4 or 8 CTAs, whose partial sums meet in distributed shared memory in a fixed order (two runs give
-// the same bits; no workspace, no second launch).
+// Fewer tiles than SMs (few tokens: the weights' bytes are the bound): mx_matmul_kernel, a CTA per tile and part of the k
+// range; the parts of a tile are a cluster of 2, 4 or 8 CTAs, whose sums meet in distributed shared memory in a fixed
+// order (two runs give the same bits; no workspace, no second launch).  For up to 8 tokens the CTA quantises its part of
+// the activations itself.  More tiles: mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the
+// next tile's products.
 #include "mx_tc.cuh"
 
 namespace saem {
 
-constexpr int kMmThreads = 192;             // warp 0: copies, warp 1: MMA issue, warps 2-5: epilogue
+constexpr int kMmThreads = 192;             // warp 0: copies, warp 1: MMA issue, warps 2-5: quantisation, epilogue
 constexpr int kMmStageK = 256;              // elements of k per stage (128 bytes of codes)
 constexpr int kMmMaxStages = 12;
-constexpr int kMmSmem = 226 * 1024;         // dynamic shared memory: one CTA per SM
+constexpr int kMmSmem = 226 * 1024;         // dynamic shared memory at most
 
 __device__ int mx_status_sink;              // where a run-out wait is noted when the caller gave no status word
 
@@ -36,6 +38,9 @@ struct MmArgs {
     int split;                              // CTAs of the cluster
     int out_bf16;
     int w_early;                            // the launch before this one wrote only A: W may be read before it is complete
+    const void* x;                          // quantise A from here (every stage of the CTA has its place in the ring), or nullptr
+    long long x_stride;
+    int x_bf16, x_vec;
 };
 
 __global__ void __launch_bounds__(kMmThreads, 1)
@@ -60,7 +65,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.n_stage; ++i) {
-            mbar_init(smem_u32(&bar_full[i]), 1);
+            mbar_init(smem_u32(&bar_full[i]), p.x ? 5 : 1);
             mbar_init(smem_u32(&bar_empty[i]), 1);
         }
         mbar_init(smem_u32(&bar_acc), 1);
@@ -83,40 +88,38 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     if (warp == 0) {
         // ---------------------------------------------------------------- copies
         const uint32_t on = elect_one();
-        const int pieces = min(p.pieces, (tokens + 127) / 128);
+        const int pieces = p.x ? 0 : min(p.pieces, (tokens + 127) / 128);
         const int piece_t = t0 / 128, piece_w = n0 / 128;
-        auto w_part = [&](int s) {
-            const int i = (s - s0) % p.n_stage;
+        auto w_part = [&](int s, int i) {
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
-            expect_tx_on(on, bar, w_bytes + a_bytes + spans * kMxPiece * (1 + pieces));
+            expect_tx_on(on, bar, w_bytes + (p.x ? 0 : a_bytes) + spans * kMxPiece * (1 + pieces));
             tma_2d_on(on, st, &map_w, s * 128, n0, bar);
             bulk_g2s_on(on, st + w_bytes + a_bytes, p.w_scales + ((size_t)piece_w * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
         };
-        auto a_part = [&](int s) {
-            const int i = (s - s0) % p.n_stage;
+        auto a_part = [&](int s, int i) {
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
+            if (p.x) return;
             tma_2d_on(on, st + w_bytes, &map_a, s * 128, t0, bar);
             for (int q = 0; q < pieces; ++q)
                 bulk_g2s_on(on, st + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
-                         p.a_scales + ((size_t)(piece_t + q) * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
+                            p.a_scales + ((size_t)(piece_t + q) * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
         };
-        int early = 0;
-        if (p.w_early)
-            for (; early < p.n_stage && s0 + early < s1; ++early) w_part(s0 + early);
+        const int early = p.w_early ? min(p.n_stage, s1 - s0) : 0;
+        for (int i = 0; i < early; ++i) w_part(s0 + i, i);
         pdl_wait();
         pdl_launch_dependents();
-        int s = s0;
+        int s = s0, st = 0, turn = 0;
         bool ok = true;
         for (; s < s1; ++s) {
-            const int it = s - s0;
-            if (it >= p.n_stage) {
-                ok = mbar_wait_warp(smem_u32(&bar_empty[it % p.n_stage]), (it / p.n_stage - 1) & 1, abort_p, status);
+            if (turn) {
+                ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, status);
                 if (!ok) break;
             }
-            if (it >= early) w_part(s);
-            a_part(s);
+            if (s - s0 >= early) w_part(s, st);
+            a_part(s, st);
+            if (++st == p.n_stage) { st = 0; ++turn; }
         }
         if (!ok && lane == 0)                                                // copies still under way land before the CTA ends
             for (int q = max(s0, s - p.n_stage); q < s; ++q) {
@@ -127,27 +130,53 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
+        const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base);
+        int st = 0, turn = 0;
         for (int s = s0; s < s1; ++s) {
-            const int it = s - s0, i = it % p.n_stage;
-            if (!mbar_wait_warp(smem_u32(&bar_full[i]), (it / p.n_stage) & 1, abort_p, status)) break;
+            if (!mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, status)) break;
             tc_fence_after();
-            const uint32_t st = base + i * p.stage_bytes, sf = st + w_bytes + a_bytes;
-            const uint32_t tw = tmem_sf + i * sf_cols, ta = tw + 8;
-            const int spans = min(2, n_span - 2 * s);
+            const uint32_t at = st * p.stage_bytes, tw = tmem_sf + st * sf_cols, ta = tw + 8;
+            const uint64_t dw = desc_at(codes0, at), da = desc_at(codes0, at + w_bytes), ds = desc_at(scales0, at + w_bytes + a_bytes);
+            const int spans = min(2, n_span - 2 * s), steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
             for (int h = 0; h < spans; ++h) {
-                tc_cp_scales(on, tw + 4 * h, smem_desc_scales(sf + h * kMxPiece));
+                tc_cp_scales(on, tw + 4 * h, desc_at(ds, h * kMxPiece));
                 for (int q = 0; q < p.pieces; ++q)
-                    tc_cp_scales(on, ta + 4 * (h * p.pieces + q), smem_desc_scales(sf + ((1 + q) * 2 + h) * kMxPiece));
+                    tc_cp_scales(on, ta + 4 * (h * p.pieces + q), desc_at(ds, ((1 + q) * 2 + h) * kMxPiece));
             }
-            const int steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
-            const uint64_t dw = smem_desc_sw128(st), da = smem_desc_sw128(st + w_bytes);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (j < steps) tc_mma_mxf4(on, tmem, dw + 2 * j, da + 2 * j, idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
-                            ta + 4 * (j >> 1) * p.pieces, s > s0 || j > 0);
-            tc_commit_on(on, smem_u32(&bar_empty[i]));
+                if (j < steps)
+                    tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
+                                ta + 4 * (j >> 1) * p.pieces, s > s0 || j > 0);
+            tc_commit_on(on, smem_u32(&bar_empty[st]));
+            if (++st == p.n_stage) { st = 0; ++turn; }
         }
         tc_commit_on(on, smem_u32(&bar_acc));
+    } else if (p.x) {
+        // ---------------------------------------------------------------- quantisation of the CTA's part of A
+        pdl_wait();
+        uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
+        const size_t esize = p.x_bf16 ? 2 : 4;
+        for (int s = s0; s < s1; ++s) {
+            uint8_t* st = smem + (size_t)(s - s0) * p.stage_bytes + w_bytes;
+            for (int r = warp - 2; r < p.m; r += 4) {
+                const void* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.x_stride * esize;
+                const long long col = (long long)s * kMmStageK + lane * 8;
+                float v[8];
+                if (p.x_bf16) { if (p.x_vec) load8<true, true>(row, col, p.k, v); else load8<true, false>(row, col, p.k, v); }
+                else { if (p.x_vec) load8<false, true>(row, col, p.k, v); else load8<false, false>(row, col, p.k, v); }
+                int scale;
+                const uint32_t w = mx_quantize8(v, scale);
+                uint32_t word = (uint32_t)(col < kp ? scale : 0) << (((lane >> 2) & 3) * 8);
+                word |= __shfl_xor_sync(0xffffffffu, word, 4);
+                word |= __shfl_xor_sync(0xffffffffu, word, 8);
+                *reinterpret_cast<uint32_t*>(st + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = w;
+                if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(st + a_bytes + 2 * kMxPiece + (lane >> 4) * kMxPiece + r * 16) = word;   // r < 32
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_full[s - s0]));
+        }
     }
     __syncwarp();
 
@@ -159,9 +188,10 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
         else static_cast<float*>(p.out)[at] = v;
     };
+    const int pitch = n_mma + 4;                                             // floats between rows of partial sums: no bank twice
     bool done = false;
     if (warp >= 2) {
-        done = mbar_wait(smem_u32(&bar_acc), 0, abort_p, status) && !*abort_p;
+        done = mbar_wait_warp(smem_u32(&bar_acc), 0, abort_p, status) && !*abort_p;
         tc_fence_after();
         pdl_wait();                                                          // nothing is written before older kernels have ended
         if (done)
@@ -169,10 +199,11 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 float v[16];
                 tc_ld16(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
                 if (p.split > 1) {
-                    // partial sums [column][row] where the stages were: every MMA has read them
+                    // partial sums [row][column] where the stages were: every MMA has read them
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + ((c + i) * 128 + row) * 4), "f"(v[i]) : "memory");
+                    for (int i = 0; i < 16; i += 4)
+                        st_shared_v4(base + (row * pitch + c + i) * 4, __float_as_uint(v[i]), __float_as_uint(v[i + 1]),
+                                     __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3]));
                 } else if (store_row) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
@@ -185,16 +216,24 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         __syncthreads();
         cluster_sync_all();
         if (warp >= 2 && done)
-            for (int c = rank; c < tokens; c += p.split) {
-                float sum = 0.f;
-                for (int q = 0; q < p.split; ++q) {
-                    float v;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                                 : "=f"(v) : "r"(mapa_u32(base + (c * 128 + row) * 4, q)) : "memory");
-                    sum += v;
-                }
-                if (store_row) put(c, sum);
+            for (int c = rank * 4; c < tokens; c += 4 * p.split) {           // four columns at a time, the parts in order
+                float4 v[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q < p.split)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                     : "=f"(v[q].x), "=f"(v[q].y), "=f"(v[q].z), "=f"(v[q].w)
+                                     : "r"(mapa_u32(base + (row * pitch + c) * 4, q)));
+                float4 sum = v[0];
+#pragma unroll
+                for (int q = 1; q < 8; ++q)
+                    if (q < p.split) { sum.x += v[q].x; sum.y += v[q].y; sum.z += v[q].z; sum.w += v[q].w; }
+                const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (store_row && c + i < tokens) put(c + i, f[i]);
             }
+        __syncwarp();
         cluster_sync_all();                                                  // no CTA ends while another reads its shared memory
     } else {
         __syncthreads();
@@ -202,6 +241,158 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols));
+    }
+}
+
+// Many tiles: one persistent CTA per SM, 128 weight rows x 256 tokens at a time.  Tensor memory holds one set of
+// accumulators beside the scales; eight warps take it into registers (128 columns each), which frees it after a few
+// hundred cycles, and store while the next tile is under way.
+constexpr int kBigThreads = 320;            // warp 0: copies, warp 1: MMA issue, warps 2-9: epilogue
+constexpr int kBigTile = 256;
+constexpr int kBigStages = 4;
+constexpr int kBigStageBytes = 128 * 128 + kBigTile * 128 + 6 * kMxPiece;
+constexpr int kBigSmem = kBigStages * kBigStageBytes + 1024;
+constexpr int kBigSfCols = 24;
+
+__global__ void __launch_bounds__(kBigThreads, 1)
+mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ MmArgs p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ alignas(8) uint64_t bar_full[kBigStages], bar_empty[kBigStages], bar_acc, bar_free;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_flag;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int n_w = (p.n + 127) / 128, n_t = (p.m + kBigTile - 1) / kBigTile, total = n_w * n_t;
+    const long long kp = (p.k + kMxBlock - 1) / kMxBlock * kMxBlock;
+    const int n_span = (p.k + kMxSpan - 1) / kMxSpan, stages = (int)((kp + kMmStageK - 1) / kMmStageK);
+    int* const status = p.status ? p.status : &mx_status_sink;
+    volatile int* abort_p = &abort_flag;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kBigStages; ++i) {
+            mbar_init(smem_u32(&bar_full[i]), 1);
+            mbar_init(smem_u32(&bar_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&bar_acc), 1);
+        mbar_init(smem_u32(&bar_free), 8);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "n"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    pdl_wait();
+    pdl_launch_dependents();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = warp_uniform(tmem_s), tmem_sf = tmem + kBigTile;
+    constexpr int w_bytes = 128 * 128, a_bytes = kBigTile * 128;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- copies
+        const uint32_t on = elect_one();
+        int it = 0, st = 0, turn = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
+            const int tt = i / n_w, tw = i - tt * n_w;
+            const int pieces = min(2, (p.m - tt * kBigTile + 127) / 128);
+            for (int s = 0; s < stages; ++s, ++it) {
+                if (turn) {
+                    ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, status);
+                    if (!ok) break;
+                }
+                const uint32_t dst = base + st * kBigStageBytes, bar = smem_u32(&bar_full[st]);
+                const int bytes = min(2, n_span - 2 * s) * kMxPiece;
+                expect_tx_on(on, bar, w_bytes + a_bytes + bytes * (1 + pieces));
+                tma_2d_on(on, dst, &map_w, s * 128, tw * 128, bar);
+                tma_2d_on(on, dst + w_bytes, &map_a, s * 128, tt * kBigTile, bar);
+                bulk_g2s_on(on, dst + w_bytes + a_bytes, p.w_scales + ((size_t)tw * n_span + 2 * s) * kMxPiece, bytes, bar);
+                for (int q = 0; q < pieces; ++q)
+                    bulk_g2s_on(on, dst + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
+                                p.a_scales + ((size_t)(tt * 2 + q) * n_span + 2 * s) * kMxPiece, bytes, bar);
+                if (++st == kBigStages) { st = 0; ++turn; }
+            }
+        }
+        if (!ok && lane == 0)                                                  // copies still under way land before the CTA ends
+            for (int q = max(0, it - kBigStages); q < it; ++q) {
+                abort_flag = 0;
+                mbar_wait(smem_u32(&bar_full[q % kBigStages]), (q / kBigStages) & 1, abort_p, status);
+                abort_flag = 1;
+            }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMA issue
+        const uint32_t on = elect_one();
+        const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base);
+        int st = 0, turn = 0, k = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; i < total && ok; i += gridDim.x, ++k) {
+            const int n_mma = (min(kBigTile, p.m - i / n_w * kBigTile) + 15) & ~15;
+            if (k) ok = mbar_wait_warp(smem_u32(&bar_free), (k - 1) & 1, abort_p, status);
+            tc_fence_after();
+            for (int s = 0; s < stages && ok; ++s) {
+                ok = mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, status);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = st * kBigStageBytes, tw = tmem_sf + st * kBigSfCols, ta = tw + 8;
+                const uint64_t dw = desc_at(codes0, at), da = desc_at(codes0, at + w_bytes), ds = desc_at(scales0, at + w_bytes + a_bytes);
+                const int steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (2 * s + h >= n_span) break;
+                    tc_cp_scales(on, tw + 4 * h, desc_at(ds, h * kMxPiece));
+                    tc_cp_scales(on, ta + 8 * h, desc_at(ds, (2 + h) * kMxPiece));
+                    tc_cp_scales(on, ta + 8 * h + 4, desc_at(ds, (4 + h) * kMxPiece));
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < steps)
+                        tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
+                                    ta + 8 * (j >> 1), s > 0 || j > 0);
+                tc_commit_on(on, smem_u32(&bar_empty[st]));
+                if (++st == kBigStages) { st = 0; ++turn; }
+            }
+            tc_commit_on(on, smem_u32(&bar_acc));
+        }
+    } else {
+        // ---------------------------------------------------------------- epilogue
+        const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
+        bool ok = true;
+        int k = 0;
+        for (int i = blockIdx.x; i < total; i += gridDim.x, ++k) {
+            const int tt = i / n_w, tw = i - tt * n_w;
+            ok = ok && mbar_wait_warp(smem_u32(&bar_acc), k & 1, abort_p, status);
+            tc_fence_after();
+            uint32_t r[128];
+            if (ok) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tc_ld32_issue(tmem + ((uint32_t)(quad * 32) << 16) + half * 128 + q * 32, r + 32 * q);
+                tc_wait_ld();
+#pragma unroll
+                for (int q = 0; q < 8; ++q) tc_reg_fence16(r + 16 * q);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_free));
+            const int n = tw * 128 + row, t0 = tt * kBigTile + half * 128, tokens = min(128, p.m - t0);
+            if (!ok || n >= p.n) continue;
+            if (p.out_bf16) {
+                __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + (size_t)t0 * p.out_stride + n;
+#pragma unroll
+                for (int c = 0; c < 128; ++c)
+                    if (c < tokens) o[c * p.out_stride] = __float2bfloat16_rn(__uint_as_float(r[c]));
+            } else {
+                float* o = static_cast<float*>(p.out) + (size_t)t0 * p.out_stride + n;
+#pragma unroll
+                for (int c = 0; c < 128; ++c)
+                    if (c < tokens) o[c * p.out_stride] = __uint_as_float(r[c]);
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
     }
 }
 
@@ -222,7 +413,8 @@ static cudaError_t mx_matmul_init() {
         g_mx_encode = (EncodeTiledFn)fn;
     }
     if (!first_call_on_device(g_mx_done)) return cudaSuccess;
-    return cudaFuncSetAttribute(mx_matmul_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem);
+    const cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(mx_matmul_tiles_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
 }
 
 // Codes as a byte matrix: boxes of 128 bytes (256 elements) x `box_rows` rows; what lies outside reads as zero.
@@ -237,34 +429,61 @@ static bool make_code_map(CUtensorMap* m, const void* codes, long long rows, lon
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static cudaError_t launch_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int m, const uint8_t* w_codes,
-                                    const uint8_t* w_scales, int n, int k, void* out, int out_bf16, long long out_stride,
-                                    int* status, int w_early, cudaStream_t st) {
-    cudaError_t e = mx_matmul_init();
-    if (e != cudaSuccess) return e;
-    int dev, n_sm;
-    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if ((e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    MmArgs p = {};
-    p.a_scales = a_scales; p.w_scales = w_scales; p.out = out; p.status = status; p.out_stride = out_stride;
-    p.m = m; p.n = n; p.k = k; p.out_bf16 = out_bf16; p.w_early = w_early;
-    p.n_tile = m <= 256 ? round_up(m, 16) : 256;
-    p.pieces = (p.n_tile + 127) / 128;
-    p.stage_bytes = 128 * 128 + p.n_tile * 128 + 2 * kMxPiece * (1 + p.pieces);
-    p.stage_bytes = round_up(p.stage_bytes, 1024);
-    p.n_stage = (kMmSmem - 1024) / p.stage_bytes;
+// How a product is cut: decided from its sizes alone, so that saem_mx_linear knows whether A is to be quantised first.
+struct MmPlan {
+    bool big;                               // mx_matmul_tiles_kernel
+    bool fused;                             // A quantised by the product's CTAs (where it is not quantised already)
+    int n_tile, split, per_sm, n_stage, stage_bytes;
+};
+static MmPlan mm_plan(int m, int n, int k, int n_sm) {
+    MmPlan p = {};
+    const long long rows = (n + 127) / 128;
+    const int stages = (k + kMmStageK - 1) / kMmStageK;
+    if (rows * ((m + kBigTile - 1) / kBigTile) >= n_sm) {
+        p.big = true;
+        return p;
+    }
+    p.n_tile = m <= 128 ? round_up(m, 16) : 128;                               // tiles start at whole pieces of scales
+    const int pieces = 1;
+    p.stage_bytes = round_up(128 * 128 + p.n_tile * 128 + 2 * kMxPiece * (1 + pieces), 1024);
+    const long long tiles = rows * ((m + p.n_tile - 1) / p.n_tile);
+    p.per_sm = p.n_tile <= 64 ? 2 : 1;                                         // CTAs that share an SM
+    p.split = 1;
+    while (p.split < 8 && tiles * p.split * 2 <= (long long)n_sm * p.per_sm && p.split * 2 <= stages) p.split *= 2;
+    p.n_stage = (kMmSmem / p.per_sm - 2048) / p.stage_bytes;
     if (p.n_stage > kMmMaxStages) p.n_stage = kMmMaxStages;
-    const int need = round_up(p.n_tile, 32) + p.n_stage * (8 + 8 * p.pieces);
+    const int mine = (stages + p.split - 1) / p.split;
+    if (m <= 8) {                                                              // a place in the ring for every stage of the CTA
+        if (mine > p.n_stage && mine <= kMmMaxStages) {
+            p.n_stage = mine;
+            p.per_sm = 1;
+        }
+        p.fused = mine <= p.n_stage && mine * p.stage_bytes + 1024 <= kMmSmem;
+    }
+    if (p.n_stage > mine) p.n_stage = mine;
+    return p;
+}
+
+static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t* a_codes, const uint8_t* w_codes, int n_sm, cudaStream_t st) {
+    alignas(64) CUtensorMap map_w, map_a;
+    const int n_tile = plan.big ? kBigTile : plan.n_tile;
+    if (!make_code_map(&map_w, w_codes, p.n, p.k, 128)) return cudaErrorInvalidValue;
+    if (a_codes ? !make_code_map(&map_a, a_codes, p.m, p.k, n_tile) : (map_a = map_w, false)) return cudaErrorInvalidValue;
+    p.n_tile = n_tile;
+    if (plan.big) {
+        const long long tiles = (long long)((p.n + 127) / 128) * ((p.m + kBigTile - 1) / kBigTile);
+        return launch_pdl(mx_matmul_tiles_kernel, dim3((unsigned)(tiles < n_sm ? tiles : n_sm)), dim3(kBigThreads), (size_t)kBigSmem, st, map_w,
+                          map_a, p);
+    }
+    p.pieces = 1;
+    p.stage_bytes = plan.stage_bytes;
+    p.n_stage = plan.n_stage;
+    p.split = plan.split;
+    const int need = round_up(p.n_tile, 32) + p.n_stage * 16;
     p.tmem_cols = 32;
     while (p.tmem_cols < need) p.tmem_cols *= 2;
-    if (p.tmem_cols > 512) return cudaErrorInvalidValue;
-    const int stages = (k + kMmStageK - 1) / kMmStageK;
-    const long long tiles = (long long)((n + 127) / 128) * ((m + p.n_tile - 1) / p.n_tile);
-    p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= n_sm && p.split * 2 <= stages) p.split *= 2;
-    alignas(64) CUtensorMap map_w, map_a;
-    if (!make_code_map(&map_w, w_codes, n, k, 128) || !make_code_map(&map_a, a_codes, m, k, p.n_tile))
-        return cudaErrorInvalidValue;
+    // partial sums take the place of the stages
+    const int sums = 128 * (round_up(p.n_tile, 16) + 4) * 4, ring = p.n_stage * p.stage_bytes;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -272,13 +491,28 @@ static cudaError_t launch_mx_matmul(const uint8_t* a_codes, const uint8_t* a_sca
     attr[1].val.clusterDim.x = p.split;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.split, (n + 127) / 128, (m + p.n_tile - 1) / p.n_tile);
+    cfg.gridDim = dim3(p.split, (p.n + 127) / 128, (p.m + p.n_tile - 1) / p.n_tile);
     cfg.blockDim = dim3(kMmThreads);
-    cfg.dynamicSmemBytes = kMmSmem;
+    cfg.dynamicSmemBytes = 1024 + (p.split > 1 && sums > ring ? sums : ring);
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, mx_matmul_kernel, map_w, map_a, p);
+}
+
+// SMs of the current device.
+static cudaError_t sm_count(int* n) {
+    static int known[64];
+    int dev;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && known[dev]) {
+        *n = known[dev];
+        return cudaSuccess;
+    }
+    e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) known[dev] = *n;
+    return e;
 }
 
 }  // namespace saem
@@ -302,9 +536,13 @@ int saem_mx_matmul(const void* a_codes, const void* a_scales, int64_t m, const v
     if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return SAEM_ERR_INVALID_ARG;
     if (((uintptr_t)a_codes | (uintptr_t)a_scales | (uintptr_t)w_codes | (uintptr_t)w_scales) & 15) return SAEM_ERR_ALIGNMENT;
     if ((uintptr_t)out % (out_dtype == SAEM_OUT_BF16 ? 2 : 4) || ((uintptr_t)status & 3)) return SAEM_ERR_ALIGNMENT;
-    return launch_mx_matmul((const uint8_t*)a_codes, (const uint8_t*)a_scales, (int)m, (const uint8_t*)w_codes,
-                            (const uint8_t*)w_scales, (int)n, (int)k, out, out_dtype == SAEM_OUT_BF16, out_stride, status, 0,
-                            (cudaStream_t)stream) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+    int n_sm;
+    if (mx_matmul_init() != cudaSuccess || sm_count(&n_sm) != cudaSuccess) return SAEM_ERR_CUDA;
+    MmArgs p = {};
+    p.a_scales = (const uint8_t*)a_scales; p.w_scales = (const uint8_t*)w_scales; p.out = out; p.status = status; p.out_stride = out_stride;
+    p.m = (int)m; p.n = (int)n; p.k = (int)k; p.out_bf16 = out_dtype == SAEM_OUT_BF16;
+    return launch_mx_matmul(mm_plan(p.m, p.n, p.k, n_sm), p, (const uint8_t*)a_codes, (const uint8_t*)w_codes, n_sm, (cudaStream_t)stream) ==
+                   cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }
 
 size_t saem_mx_linear_workspace_bytes(int64_t max_rows, int64_t k) {
@@ -323,13 +561,30 @@ int saem_mx_linear(const void* x, int x_dtype, int64_t m, int64_t x_stride, cons
     if (((uintptr_t)w_codes | (uintptr_t)w_scales) & 15 || (uintptr_t)workspace & 255) return SAEM_ERR_ALIGNMENT;
     if ((uintptr_t)out % (out_dtype == SAEM_OUT_BF16 ? 2 : 4)) return SAEM_ERR_ALIGNMENT;
     if (workspace_bytes < saem_mx_linear_workspace_bytes(m, k)) return SAEM_ERR_WORKSPACE;
+    if (x_dtype != SAEM_OUT_F32 && x_dtype != SAEM_OUT_BF16) return SAEM_ERR_INVALID_ARG;
+    if (m > 1 && x_stride < k) return SAEM_ERR_SHAPE;
+    const size_t esize = x_dtype == SAEM_OUT_BF16 ? 2 : 4;
+    if ((uintptr_t)x % esize) return SAEM_ERR_ALIGNMENT;
+    int n_sm;
+    if (mx_matmul_init() != cudaSuccess || sm_count(&n_sm) != cudaSuccess) return SAEM_ERR_CUDA;
+    const MmPlan plan = mm_plan((int)m, (int)n, (int)k, n_sm);
     uint8_t* codes = (uint8_t*)workspace + 256;                              // the status word stands before them
     uint8_t* scales = codes + (saem_mx_codes_bytes(m, k) + 255) / 256 * 256;
-    const int q = saem_mx_quantize(x, x_dtype, m, k, x_stride, codes, scales, stream);
-    if (q != SAEM_OK) return q;
-    return launch_mx_matmul(codes, scales, (int)m, (const uint8_t*)w_codes, (const uint8_t*)w_scales, (int)n, (int)k, out,
-                            out_dtype == SAEM_OUT_BF16, out_stride, (int*)workspace, 1, (cudaStream_t)stream) == cudaSuccess
-               ? SAEM_OK : SAEM_ERR_CUDA;
+    MmArgs p = {};
+    p.a_scales = scales; p.w_scales = (const uint8_t*)w_scales; p.out = out; p.status = (int*)workspace; p.out_stride = out_stride;
+    p.m = (int)m; p.n = (int)n; p.k = (int)k; p.out_bf16 = out_dtype == SAEM_OUT_BF16;
+    if (plan.fused) {
+        p.x = x;
+        p.x_stride = x_stride;
+        p.x_bf16 = x_dtype == SAEM_OUT_BF16;
+        p.x_vec = k % 8 == 0 && ((uintptr_t)x & 15) == 0 && (m == 1 || x_stride * (long long)esize % 16 == 0);
+        codes = nullptr;
+    } else {
+        const int q = saem_mx_quantize(x, x_dtype, m, k, x_stride, codes, scales, stream);
+        if (q != SAEM_OK) return q;
+        p.w_early = 1;
+    }
+    return launch_mx_matmul(plan, p, codes, (const uint8_t*)w_codes, n_sm, (cudaStream_t)stream) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }
 
 }  // extern "C"

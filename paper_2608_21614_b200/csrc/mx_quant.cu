@@ -16,38 +16,6 @@ constexpr int kQuantThreads = 256;
 constexpr int kQuantChunk = 256;            // elements of a row that one warp takes at a time
 constexpr int kQuantUnroll = 4;             // chunks whose loads a warp has in flight
 
-// Eight elements of a row from `col` on as fp32; what lies beyond `cols` is zero.  VEC: the row is 16-byte aligned and
-// cols a multiple of 8.
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void load8(const void* __restrict__ row, long long col, long long cols, float (&v)[8]) {
-    if (VEC) {
-        if (col >= cols) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        } else if (BF16) {
-            const uint4 q = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + col));
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        } else {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + col);
-            const float4 a = __ldcs(p), b = __ldcs(p + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            if (col + i < cols)
-                v[i] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[col + i] << 16)
-                            : static_cast<const float*>(row)[col + i];
-        }
-    }
-}
-
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads)
 mx_quantize_kernel(const void* __restrict__ x, long long rows, long long cols, long long row_stride, uint32_t n_chunk,
@@ -74,16 +42,8 @@ mx_quantize_kernel(const void* __restrict__ x, long long rows, long long cols, l
     for (int u = 0; u < kQuantUnroll; ++u) {
         if (warp * kQuantUnroll + u >= total) break;
         const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[u][i]) & 0x7FFFFFFFu);   // NaN above infinity
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const int s = mx_scale_byte(amax);
-        const float inv = __uint_as_float((uint32_t)(254 - min(s, 253)) << 23);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] *= inv;
-        const uint32_t w = s == 255 ? 0u : mx_encode8(v[u]);
+        int s;
+        const uint32_t w = mx_quantize8(v[u], s);
         if (col / kMxBlock < n_block)
             *reinterpret_cast<uint32_t*>(codes + (size_t)row[u] * n_block * 16 + col / 2) = w;
         // the four scales of a 128-element span meet in one word; blocks beyond the row's last one get scale 2^-127

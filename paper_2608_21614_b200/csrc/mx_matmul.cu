@@ -7,11 +7,13 @@
 // consecutive n.  A stage is 256 elements of k: 128-byte rows of codes under the 128-byte swizzle (TMA) and the scales'
 // 512-byte pieces (plain bulk copies, moved to tensor memory by tcgen05.cp as they are).
 //
-// Fewer tiles than SMs (few tokens: the weights' bytes are the bound): mx_matmul_kernel, a CTA per tile and part of the k
-// range; the parts of a tile are a cluster of 2, 4 or 8 CTAs, whose sums meet in distributed shared memory in a fixed
-// order (two runs give the same bits; no workspace, no second launch).  For up to 8 tokens the CTA quantises its part of
-// the activations itself.  More tiles: mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the
-// next tile's products.
+// Two forms, by the number of tokens (measured side by side for n 2048 .. 14336 and k 1024, 4096).  More than 64:
+// mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the next tile's products (128 tokens of
+// 14336 x 4096: 12.2 us against 14.3 us).  Up to 64: mx_matmul_kernel, one CTA per tile, where the weights' bytes are the
+// bound and n / 128 tiles are too few for the SMs: the k range is then split over a cluster of 2 or 4 CTAs, whose sums meet
+// in distributed shared memory in a fixed order (16 tokens of 4096 x 4096: 5.3 us in four parts, 9 us in one; parts of
+// fewer than four stages, or eight parts, cost more than they give).  Up to 8 tokens the CTA quantises its part of the
+// activations itself.  Two runs give the same bits.
 #include "mx_tc.cuh"
 
 namespace saem {
@@ -20,6 +22,7 @@ constexpr int kMmThreads = 192;             // warp 0: copies, warp 1: MMA issue
 constexpr int kMmStageK = 256;              // elements of k per stage (128 bytes of codes)
 constexpr int kMmMaxStages = 12;
 constexpr int kMmSmem = 226 * 1024;         // dynamic shared memory at most
+constexpr int kMmSfCols = 16;               // tensor-memory columns of a stage's scales: 8 for W, 8 for A
 
 __device__ int mx_status_sink;              // where a run-out wait is noted when the caller gave no status word
 
@@ -30,8 +33,7 @@ struct MmArgs {
     int* status;
     long long out_stride;
     int m, n, k;
-    int n_tile;                             // tokens per tile
-    int pieces;                             // 128-row pieces of the token tile's scales
+    int n_tile;                             // tokens, rounded up to 16 (one tile)
     int n_stage;                            // stages of the ring
     int stage_bytes;
     int tmem_cols;
@@ -53,9 +55,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
-    const int n0 = blockIdx.y * 128, t0 = blockIdx.z * p.n_tile;
-    const int tokens = min(p.n_tile, p.m - t0);
-    const int n_mma = (tokens + 15) & ~15;
+    const int n0 = blockIdx.y * 128, tokens = p.m, n_mma = p.n_tile;
     const long long kp = (p.k + kMxBlock - 1) / kMxBlock * kMxBlock;        // padded with zeros to whole blocks
     const int n_span = (p.k + kMxSpan - 1) / kMxSpan;
     const int all = (int)((kp + kMmStageK - 1) / kMmStageK);
@@ -81,30 +81,25 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     tc_fence_after();
     const uint32_t tmem = warp_uniform(tmem_s);
     const int acc_cols = (p.n_tile + 31) & ~31;
-    const uint32_t tmem_sf = tmem + acc_cols;                                // per stage: 8 columns for W, 8 per piece for A
-    const int sf_cols = 8 + 8 * p.pieces;
+    const uint32_t tmem_sf = tmem + acc_cols;
     const int w_bytes = 128 * 128, a_bytes = p.n_tile * 128;
 
     if (warp == 0) {
         // ---------------------------------------------------------------- copies
         const uint32_t on = elect_one();
-        const int pieces = p.x ? 0 : min(p.pieces, (tokens + 127) / 128);
-        const int piece_t = t0 / 128, piece_w = n0 / 128;
         auto w_part = [&](int s, int i) {
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
-            expect_tx_on(on, bar, w_bytes + (p.x ? 0 : a_bytes) + spans * kMxPiece * (1 + pieces));
+            expect_tx_on(on, bar, w_bytes + spans * kMxPiece + (p.x ? 0 : a_bytes + spans * kMxPiece));
             tma_2d_on(on, st, &map_w, s * 128, n0, bar);
-            bulk_g2s_on(on, st + w_bytes + a_bytes, p.w_scales + ((size_t)piece_w * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
+            bulk_g2s_on(on, st + w_bytes + a_bytes, p.w_scales + ((size_t)blockIdx.y * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
         };
         auto a_part = [&](int s, int i) {
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
             if (p.x) return;
-            tma_2d_on(on, st + w_bytes, &map_a, s * 128, t0, bar);
-            for (int q = 0; q < pieces; ++q)
-                bulk_g2s_on(on, st + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
-                            p.a_scales + ((size_t)(piece_t + q) * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
+            tma_2d_on(on, st + w_bytes, &map_a, s * 128, 0, bar);
+            bulk_g2s_on(on, st + w_bytes + a_bytes + 2 * kMxPiece, p.a_scales + (size_t)2 * s * kMxPiece, spans * kMxPiece, bar);
         };
         const int early = p.w_early ? min(p.n_stage, s1 - s0) : 0;
         for (int i = 0; i < early; ++i) w_part(s0 + i, i);
@@ -135,19 +130,18 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         for (int s = s0; s < s1; ++s) {
             if (!mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, status)) break;
             tc_fence_after();
-            const uint32_t at = st * p.stage_bytes, tw = tmem_sf + st * sf_cols, ta = tw + 8;
+            const uint32_t at = st * p.stage_bytes, tw = tmem_sf + st * kMmSfCols, ta = tw + 8;
             const uint64_t dw = desc_at(codes0, at), da = desc_at(codes0, at + w_bytes), ds = desc_at(scales0, at + w_bytes + a_bytes);
             const int spans = min(2, n_span - 2 * s), steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
             for (int h = 0; h < spans; ++h) {
                 tc_cp_scales(on, tw + 4 * h, desc_at(ds, h * kMxPiece));
-                for (int q = 0; q < p.pieces; ++q)
-                    tc_cp_scales(on, ta + 4 * (h * p.pieces + q), desc_at(ds, ((1 + q) * 2 + h) * kMxPiece));
+                tc_cp_scales(on, ta + 4 * h, desc_at(ds, (2 + h) * kMxPiece));
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (j < steps)
                     tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
-                                ta + 4 * (j >> 1) * p.pieces, s > s0 || j > 0);
+                                ta + 4 * (j >> 1), s > s0 || j > 0);
             tc_commit_on(on, smem_u32(&bar_empty[st]));
             if (++st == p.n_stage) { st = 0; ++turn; }
         }
@@ -159,14 +153,22 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         const size_t esize = p.x_bf16 ? 2 : 4;
         for (int s = s0; s < s1; ++s) {
             uint8_t* st = smem + (size_t)(s - s0) * p.stage_bytes + w_bytes;
-            for (int r = warp - 2; r < p.m; r += 4) {
+            const long long col = (long long)s * kMmStageK + lane * 8;
+            float v[2][8];                                                   // p.m <= 8: two rows per warp at most
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int r = warp - 2 + 4 * u;
                 const void* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.x_stride * esize;
-                const long long col = (long long)s * kMmStageK + lane * 8;
-                float v[8];
-                if (p.x_bf16) { if (p.x_vec) load8<true, true>(row, col, p.k, v); else load8<true, false>(row, col, p.k, v); }
-                else { if (p.x_vec) load8<false, true>(row, col, p.k, v); else load8<false, false>(row, col, p.k, v); }
+                if (r >= p.m) break;
+                if (p.x_bf16) { if (p.x_vec) load8<true, true>(row, col, p.k, v[u]); else load8<true, false>(row, col, p.k, v[u]); }
+                else { if (p.x_vec) load8<false, true>(row, col, p.k, v[u]); else load8<false, false>(row, col, p.k, v[u]); }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int r = warp - 2 + 4 * u;
+                if (r >= p.m) break;
                 int scale;
-                const uint32_t w = mx_quantize8(v, scale);
+                const uint32_t w = mx_quantize8(v[u], scale);
                 uint32_t word = (uint32_t)(col < kp ? scale : 0) << (((lane >> 2) & 3) * 8);
                 word |= __shfl_xor_sync(0xffffffffu, word, 4);
                 word |= __shfl_xor_sync(0xffffffffu, word, 8);
@@ -184,7 +186,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const int quad = warp & 3, row = quad * 32 + lane;
     const bool store_row = n0 + row < p.n;
     auto put = [&](int c, float v) {
-        const size_t at = (size_t)(t0 + c) * p.out_stride + n0 + row;
+        const size_t at = (size_t)c * p.out_stride + n0 + row;
         if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
         else static_cast<float*>(p.out)[at] = v;
     };
@@ -217,16 +219,16 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         cluster_sync_all();
         if (warp >= 2 && done)
             for (int c = rank * 4; c < tokens; c += 4 * p.split) {           // four columns at a time, the parts in order
-                float4 v[8];
+                float4 v[4];
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
+                for (int q = 0; q < 4; ++q)
                     if (q < p.split)
                         asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
                                      : "=f"(v[q].x), "=f"(v[q].y), "=f"(v[q].z), "=f"(v[q].w)
                                      : "r"(mapa_u32(base + (row * pitch + c) * 4, q)));
                 float4 sum = v[0];
 #pragma unroll
-                for (int q = 1; q < 8; ++q)
+                for (int q = 1; q < 4; ++q)
                     if (q < p.split) { sum.x += v[q].x; sum.y += v[q].y; sum.z += v[q].z; sum.w += v[q].w; }
                 const float f[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
@@ -433,32 +435,22 @@ static bool make_code_map(CUtensorMap* m, const void* codes, long long rows, lon
 struct MmPlan {
     bool big;                               // mx_matmul_tiles_kernel
     bool fused;                             // A quantised by the product's CTAs (where it is not quantised already)
-    int n_tile, split, per_sm, n_stage, stage_bytes;
+    int n_tile, split, n_stage, stage_bytes;
 };
 static MmPlan mm_plan(int m, int n, int k, int n_sm) {
     MmPlan p = {};
-    const long long rows = (n + 127) / 128;
-    const int stages = (k + kMmStageK - 1) / kMmStageK;
-    if (rows * ((m + kBigTile - 1) / kBigTile) >= n_sm) {
-        p.big = true;
-        return p;
-    }
-    p.n_tile = m <= 128 ? round_up(m, 16) : 128;                               // tiles start at whole pieces of scales
-    const int pieces = 1;
-    p.stage_bytes = round_up(128 * 128 + p.n_tile * 128 + 2 * kMxPiece * (1 + pieces), 1024);
-    const long long tiles = rows * ((m + p.n_tile - 1) / p.n_tile);
-    p.per_sm = p.n_tile <= 64 ? 2 : 1;                                         // CTAs that share an SM
+    p.big = m > 64;
+    if (p.big) return p;
+    const int tiles = (n + 127) / 128, stages = (k + kMmStageK - 1) / kMmStageK;
+    p.n_tile = round_up(m, 16);
+    p.stage_bytes = 128 * 128 + p.n_tile * 128 + 4 * kMxPiece;
     p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= (long long)n_sm * p.per_sm && p.split * 2 <= stages) p.split *= 2;
-    p.n_stage = (kMmSmem / p.per_sm - 2048) / p.stage_bytes;
-    if (p.n_stage > kMmMaxStages) p.n_stage = kMmMaxStages;
+    while (p.split < 4 && tiles * p.split * 2 <= n_sm && stages >= 8 * p.split) p.split *= 2;
     const int mine = (stages + p.split - 1) / p.split;
-    if (m <= 8) {                                                              // a place in the ring for every stage of the CTA
-        if (mine > p.n_stage && mine <= kMmMaxStages) {
-            p.n_stage = mine;
-            p.per_sm = 1;
-        }
-        p.fused = mine <= p.n_stage && mine * p.stage_bytes + 1024 <= kMmSmem;
+    p.n_stage = (kMmSmem / 2 - 2048) / p.stage_bytes;                          // two CTAs per SM
+    if (m <= 8 && mine <= kMmMaxStages && mine * p.stage_bytes + 1024 <= kMmSmem) {
+        p.fused = true;                                                        // a place in the ring for every stage of the CTA
+        p.n_stage = mine;
     }
     if (p.n_stage > mine) p.n_stage = mine;
     return p;
@@ -475,15 +467,14 @@ static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t*
         return launch_pdl(mx_matmul_tiles_kernel, dim3((unsigned)(tiles < n_sm ? tiles : n_sm)), dim3(kBigThreads), (size_t)kBigSmem, st, map_w,
                           map_a, p);
     }
-    p.pieces = 1;
     p.stage_bytes = plan.stage_bytes;
     p.n_stage = plan.n_stage;
     p.split = plan.split;
-    const int need = round_up(p.n_tile, 32) + p.n_stage * 16;
+    const int need = round_up(p.n_tile, 32) + p.n_stage * kMmSfCols;
     p.tmem_cols = 32;
     while (p.tmem_cols < need) p.tmem_cols *= 2;
     // partial sums take the place of the stages
-    const int sums = 128 * (round_up(p.n_tile, 16) + 4) * 4, ring = p.n_stage * p.stage_bytes;
+    const int sums = 128 * (p.n_tile + 4) * 4, ring = p.n_stage * p.stage_bytes;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -491,7 +482,7 @@ static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t*
     attr[1].val.clusterDim.x = p.split;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.split, (p.n + 127) / 128, (p.m + p.n_tile - 1) / p.n_tile);
+    cfg.gridDim = dim3(p.split, (p.n + 127) / 128);
     cfg.blockDim = dim3(kMmThreads);
     cfg.dynamicSmemBytes = 1024 + (p.split > 1 && sums > ring ? sums : ring);
     cfg.stream = st;

@@ -334,11 +334,11 @@ int saem_expert_ffn_static(const void* x_packed, const int32_t* offsets, int n_e
  *   scales [ceil(rows / 128)][ceil(cols / 128)][512] bytes: the scales of blocks 4c .. 4c + 3 of row r are the four
  *          bytes at piece (r / 128, c), offset (r % 32) * 16 + (r / 32 % 4) * 4        (saem_mx_scales_bytes)
  * Both must be 16-byte aligned.  The scales of rows beyond the last in a piece are unspecified.  The size queries return
- * 0 for sizes that are not supported (rows < 0, cols < 1, more than 2^31 - 1 pieces of a row's 256 elements).
+ * 0 for sizes that are not supported (rows < 0, cols < 1, either or rows * ceil(cols / 1024) above 2^31 - 1).
  *
  * saem_mx_quantize: s = max(floor(log2 max|x|) - 2, -127) + 127 and the code nearest to x * 2^-(s - 127), ties to the even
  * mantissa, saturated at 6; a block with a NaN or an infinity gets s = 255.  x[rows, cols] fp32 or bf16 (dtype: SAEM_OUT_*),
- * row r at r * row_stride elements, aligned to its elements (16-byte aligned rows and cols % 8 == 0 are faster).
+ * row r at r * row_stride elements, aligned to its elements (16-byte aligned rows are faster).
  * saem_mx_dequantize: the values back, out[rows, cols] fp32 or bf16 (both exact).
  *
  * saem_mx_matmul: out[m, n] = sum_k A[m, k] * W[n, k] of two such matrices (row r of out at r * out_stride), block-scaled

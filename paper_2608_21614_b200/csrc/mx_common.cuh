@@ -79,15 +79,11 @@ __device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits) {
     const int e = (int)(amax_bits >> 23);
     return e == 255 ? 255 : (e > 2 ? e - 2 : 0);
 }
-// Eight elements of a row from `col` on as fp32; what lies beyond `cols` is zero.  VEC: the row is 16-byte aligned and
-// cols a multiple of 8.
+// Eight elements of a row from `col` on as fp32; what lies beyond `cols` is zero.  VEC: the row is 16-byte aligned.
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void load8(const void* __restrict__ row, long long col, long long cols, float (&v)[8]) {
-    if (VEC) {
-        if (col >= cols) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        } else if (BF16) {
+    if (VEC && col + 8 <= cols) {
+        if (BF16) {
             const uint4 q = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + col));
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -110,7 +106,6 @@ __device__ __forceinline__ void load8(const void* __restrict__ row, long long co
         }
     }
 }
-
 // Eight elements of a block that four neighbouring lanes share to their codes, and the block's scale byte.
 __device__ __forceinline__ uint32_t mx_quantize8(const float (&v)[8], int& scale) {
     uint32_t amax = 0;

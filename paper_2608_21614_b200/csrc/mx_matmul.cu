@@ -568,7 +568,7 @@ int saem_mx_linear(const void* x, int x_dtype, int64_t m, int64_t x_stride, cons
         p.x = x;
         p.x_stride = x_stride;
         p.x_bf16 = x_dtype == SAEM_OUT_BF16;
-        p.x_vec = k % 8 == 0 && ((uintptr_t)x & 15) == 0 && (m == 1 || x_stride * (long long)esize % 16 == 0);
+        p.x_vec = ((uintptr_t)x & 15) == 0 && (m == 1 || x_stride * (long long)esize % 16 == 0);
         codes = nullptr;
     } else {
         const int q = saem_mx_quantize(x, x_dtype, m, k, x_stride, codes, scales, stream);

@@ -1,10 +1,10 @@
 // The microscaled 4-bit format: quantisation, the way back, and the packing of quantised expert matrices into slots.
 //
 // Quantisation of a block: s = max(floor(log2 max|x|) - 2, -127), code = E2M1(x * 2^-s) to the nearest (ties to the
-// even mantissa), saturated at 6.  Both the scaling and the way back are exact in fp32, so the only rounding is the one
-// to E2M1.  All three kernels read and write every byte once and are bound by DRAM (2.5 or 4.5 bytes per element);
-// four lanes share a block (8 elements and 16 or 32 bytes each), so that the loads and stores of a warp are whole
-// lines and the block's maximum is two shuffles.
+// even mantissa), saturated at 6.  Both the scaling and the way back are exact, so the only rounding is the one to E2M1.
+// All kernels here read and write every byte once and are bound by DRAM (2.5 or 4.5 bytes per element) -- if the
+// instructions per element stay few: a lane takes 16 elements of bf16 (half a block; its maximum is found in packed
+// halves and scaled in packed halves) or 8 of fp32, and a warp four such pieces of one row, whose loads go out together.
 #include <cmath>
 #include <cstring>
 
@@ -13,113 +13,166 @@
 namespace saem {
 
 constexpr int kQuantThreads = 256;
-constexpr int kQuantChunk = 256;            // elements of a row that one warp takes at a time
-constexpr int kQuantUnroll = 4;             // chunks whose loads a warp has in flight
+constexpr int kQuantUnroll = 4;             // pieces of a row whose loads a warp has in flight
+constexpr int kQuantStrip = 1024;           // elements of a row that a warp takes at least (fp32: 4 x 256; bf16: 2048)
 
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads)
-mx_quantize_kernel(const void* __restrict__ x, long long rows, long long cols, long long row_stride, uint32_t n_chunk,
-                   uint32_t total, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+mx_quantize_kernel(const void* __restrict__ x, uint32_t rows, long long cols, long long row_stride, uint32_t n_strip,
+                   uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    constexpr int kPerLane = BF16 ? 16 : 8, kPiece = 32 * kPerLane, kLanes = kMxBlock / kPerLane;   // kLanes share a block
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const long long warp = (long long)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    const uint32_t unit = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5), row = unit / n_strip;
+    if (row >= rows) return;
     const long long n_block = (cols + kMxBlock - 1) / kMxBlock, n_span = (cols + kMxSpan - 1) / kMxSpan;
-    const size_t esize = BF16 ? 2 : 4;
-    float v[kQuantUnroll][8];
-    uint32_t row[kQuantUnroll], ch[kQuantUnroll];
+    const long long col0 = (long long)(unit - row * n_strip) * (kQuantUnroll * kPiece) + lane * kPerLane;
+    const uint8_t* src = static_cast<const uint8_t*>(x) + (size_t)row * row_stride * (BF16 ? 2 : 4);
+    uint8_t* dst = codes + (size_t)row * n_block * 16;
+    uint8_t* sdst = scales + mx_scale_word(row, 0, n_span);
+    // bf16: eight words of two elements; fp32: eight elements
+    uint32_t v[kQuantUnroll][8];
 #pragma unroll
     for (int u = 0; u < kQuantUnroll; ++u) {
-        const long long c = warp * kQuantUnroll + u;
-        if (c < total) {
-            row[u] = (uint32_t)c / n_chunk;
-            ch[u] = (uint32_t)c - row[u] * n_chunk;
-            load8<BF16, VEC>(static_cast<const uint8_t*>(x) + (size_t)row[u] * row_stride * esize,
-                             (long long)ch[u] * kQuantChunk + lane * 8, cols, v[u]);
+        const long long col = col0 + u * kPiece;
+        if (VEC && col + kPerLane <= cols) {
+            const uint4* p = reinterpret_cast<const uint4*>(src + col * (BF16 ? 2 : 4));
+            const uint4 a = __ldcs(p), b = __ldcs(p + 1);
+            v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w; v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
+        } else if (BF16) {
+            const uint16_t* p = reinterpret_cast<const uint16_t*>(src);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t lo = col + 2 * i < cols ? p[col + 2 * i] : 0u, hi = col + 2 * i + 1 < cols ? p[col + 2 * i + 1] : 0u;
+                v[u][i] = lo | hi << 16;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = col + i < cols ? reinterpret_cast<const uint32_t*>(src)[col + i] : 0u;
         }
     }
 #pragma unroll
     for (int u = 0; u < kQuantUnroll; ++u) {
-        if (warp * kQuantUnroll + u >= total) break;
-        const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
-        int s;
-        const uint32_t w = mx_quantize8(v[u], s);
-        if (col / kMxBlock < n_block)
-            *reinterpret_cast<uint32_t*>(codes + (size_t)row[u] * n_block * 16 + col / 2) = w;
+        const long long col = col0 + u * kPiece;
+        if (col0 - lane * kPerLane + u * kPiece >= n_span * kMxSpan) break;   // the same in every lane
+        uint32_t m = 0;                                                       // largest magnitude's bits, NaN above infinity
+        if (BF16) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = __vmaxu2(m, v[u][i] & 0x7FFF7FFFu);
+            m = max(m << 16, m & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, v[u][i] & 0x7FFFFFFFu);
+        }
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const int s = mx_scale_byte(m);
+        const uint32_t inv = (uint32_t)(254 - min(s, 253)) << 7;              // 2^(127 - s) in bf16
+        const bool in = col < n_block * kMxBlock;
+        if (BF16) {
+            const uint32_t inv2 = inv | inv << 16;
+            uint32_t w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // by a power of two: exact, but for elements so far below the block's largest that they round to 0
+                    const __nv_bfloat162 q = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[u][4 * h + i]),
+                                                     *reinterpret_cast<const __nv_bfloat162*>(&inv2));
+                    const uint32_t b = *reinterpret_cast<const uint32_t*>(&q);
+                    f[2 * i] = __uint_as_float(b << 16);
+                    f[2 * i + 1] = __uint_as_float(b & 0xFFFF0000u);
+                }
+                w[h] = s == 255 ? 0u : mx_encode8(f);
+            }
+            if (in) *reinterpret_cast<uint2*>(dst + col / 2) = make_uint2(w[0], w[1]);
+        } else {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[u][i]) * __uint_as_float(inv << 16);
+            if (in) *reinterpret_cast<uint32_t*>(dst + col / 2) = s == 255 ? 0u : mx_encode8(f);
+        }
         // the four scales of a 128-element span meet in one word; blocks beyond the row's last one get scale 2^-127
-        uint32_t word = col / kMxBlock < n_block ? (uint32_t)s << (((lane >> 2) & 3) * 8) : 0u;
-        word |= __shfl_xor_sync(0xffffffffu, word, 4);
-        word |= __shfl_xor_sync(0xffffffffu, word, 8);
+        uint32_t word = in ? (uint32_t)s << ((lane / kLanes & 3) * 8) : 0u;
+        word |= __shfl_xor_sync(0xffffffffu, word, kLanes);
+        word |= __shfl_xor_sync(0xffffffffu, word, 2 * kLanes);
         const long long span = col / kMxSpan;
-        if ((lane & 15) == 0 && span < n_span)
-            *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row[u], span, n_span)) = word;
+        if (lane % (4 * kLanes) == 0 && span < n_span) *reinterpret_cast<uint32_t*>(sdst + span * kMxPiece) = word;
     }
 }
 
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads)
-mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, long long rows, long long cols,
-                     long long row_stride, uint32_t n_chunk, uint32_t total, void* __restrict__ out) {
+mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, uint32_t rows, long long cols,
+                     long long row_stride, uint32_t n_strip, void* __restrict__ out) {
+    constexpr int kPerLane = BF16 ? 16 : 8, kPiece = 32 * kPerLane;
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const long long warp = (long long)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    const uint32_t unit = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5), row = unit / n_strip;
+    if (row >= rows) return;
     const long long n_block = (cols + kMxBlock - 1) / kMxBlock, n_span = (cols + kMxSpan - 1) / kMxSpan;
-    uint32_t row[kQuantUnroll], ch[kQuantUnroll], w[kQuantUnroll], s[kQuantUnroll];
+    const long long col0 = (long long)(unit - row * n_strip) * (kQuantUnroll * kPiece) + lane * kPerLane;
+    const uint8_t* src = codes + (size_t)row * n_block * 16;
+    const uint8_t* ssrc = scales + mx_scale_word(row, 0, n_span);
+    uint2 w[kQuantUnroll];
+    uint32_t s[kQuantUnroll];
 #pragma unroll
     for (int u = 0; u < kQuantUnroll; ++u) {
-        const long long c = warp * kQuantUnroll + u;
-        w[u] = s[u] = 0;
-        if (c < total) {
-            row[u] = (uint32_t)c / n_chunk;
-            ch[u] = (uint32_t)c - row[u] * n_chunk;
-            const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
-            if (col < cols) {
-                w[u] = *reinterpret_cast<const uint32_t*>(codes + (size_t)row[u] * n_block * 16 + col / 2);
-                s[u] = scales[mx_scale_word(row[u], col / kMxSpan, n_span) + ((col / kMxBlock) & 3)];
-            }
+        const long long col = col0 + u * kPiece;
+        w[u] = make_uint2(0u, 0u);
+        s[u] = 0;
+        if (col < cols) {
+            if (BF16) w[u] = __ldcs(reinterpret_cast<const uint2*>(src + col / 2));   // the row of codes is padded to whole blocks
+            else w[u].x = __ldcs(reinterpret_cast<const uint32_t*>(src + col / 2));
+            s[u] = ssrc[col / kMxSpan * kMxPiece + ((col / kMxBlock) & 3)];
         }
     }
 #pragma unroll
     for (int u = 0; u < kQuantUnroll; ++u) {
-        if (warp * kQuantUnroll + u >= total) break;
-        const long long col = (long long)ch[u] * kQuantChunk + lane * 8;
+        const long long col = col0 + u * kPiece;
         if (col >= cols) continue;
         const float scale = s[u] == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(s[u] ? s[u] << 23 : 1u << 22);
-        uint32_t h[4];
-        mx_decode8(w[u], h);
-        float v[8];
+        const size_t at = (size_t)row * row_stride + col;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-            v[2 * i] = p.x * scale;
-            v[2 * i + 1] = p.y * scale;
-        }
-        const size_t at = (size_t)row[u] * row_stride + col;
-        if (BF16) {
-            uint16_t* o = static_cast<uint16_t*>(out) + at;
-            uint32_t b[4];
+        for (int h = 0; h < kPerLane / 8; ++h) {
+            uint32_t p[4];
+            mx_decode8(h ? w[u].y : w[u].x, p);
+            float v[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 q = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact: one mantissa bit
-                b[i] = *reinterpret_cast<const uint32_t*>(&q);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p[i]));
+                v[2 * i] = f.x * scale;
+                v[2 * i + 1] = f.y * scale;
             }
-            if (VEC) {
-                *reinterpret_cast<uint4*>(o) = make_uint4(b[0], b[1], b[2], b[3]);
-            } else {
+            const long long c = col + 8 * h;
+            if (BF16) {
+                uint16_t* o = static_cast<uint16_t*>(out) + at + 8 * h;
+                uint32_t b[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (col + i < cols) o[i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
-            }
-        } else {
-            float* o = static_cast<float*>(out) + at;
-            if (VEC) {
-                reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
-            } else {
+                for (int i = 0; i < 4; ++i) {
+                    const __nv_bfloat162 q = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact: one mantissa bit
+                    b[i] = *reinterpret_cast<const uint32_t*>(&q);
+                }
+                if (VEC && c + 8 <= cols) {
+                    __stcs(reinterpret_cast<uint4*>(o), make_uint4(b[0], b[1], b[2], b[3]));
+                } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (col + i < cols) o[i] = v[i];
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < cols) o[i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
+                }
+            } else {
+                float* o = static_cast<float*>(out) + at;
+                if (VEC && c + 8 <= cols) {
+                    __stcs(reinterpret_cast<float4*>(o), make_float4(v[0], v[1], v[2], v[3]));
+                    __stcs(reinterpret_cast<float4*>(o) + 1, make_float4(v[4], v[5], v[6], v[7]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < cols) o[i] = v[i];
+                }
             }
         }
     }
@@ -209,26 +262,26 @@ void mx_pack_expert_host(const uint16_t* gate, const uint16_t* up, const uint16_
     }
 }
 
-cudaError_t launch_mx_quantize(const void* x, int bf16, long long rows, long long cols, long long row_stride,
-                               uint8_t* codes, uint8_t* scales, cudaStream_t st) {
-    const uint32_t n_chunk = (uint32_t)((cols + kQuantChunk - 1) / kQuantChunk);
-    const uint32_t total = (uint32_t)(rows * n_chunk);
-    const int per_cta = kQuantThreads / 32 * kQuantUnroll;
-    const dim3 grid((total + per_cta - 1) / per_cta);
-    const bool vec = cols % 8 == 0 && ((uintptr_t)x & 15) == 0 && row_stride * (bf16 ? 2 : 4) % 16 == 0;
-    auto k = bf16 ? (vec ? mx_quantize_kernel<true, true> : mx_quantize_kernel<true, false>)
-                  : (vec ? mx_quantize_kernel<false, true> : mx_quantize_kernel<false, false>);
-    return launch_pdl(k, grid, dim3(kQuantThreads), 0, st, x, rows, cols, row_stride, n_chunk, total, codes, scales);
+// Strips of a row, and CTAs for all of them.
+static uint32_t strips(long long cols, bool bf16) {
+    const long long n = bf16 ? 2 * kQuantStrip : kQuantStrip;
+    return (uint32_t)((cols + n - 1) / n);
+}
+static dim3 strip_grid(long long rows, uint32_t n_strip) {
+    return dim3((unsigned)(((unsigned long long)rows * n_strip + kQuantThreads / 32 - 1) / (kQuantThreads / 32)));
+}
+static bool vector_rows(const void* p, long long rows, long long row_stride, bool bf16) {
+    return ((uintptr_t)p & 15) == 0 && (rows == 1 || row_stride * (bf16 ? 2 : 4) % 16 == 0);
 }
 
 }  // namespace saem
 
 using namespace saem;
 
-// rows, cols and the number of 256-element chunks a kernel counts in 32 bits
+// rows, cols and the number of strips a kernel counts in 32 bits
 static bool mx_shape_ok(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || rows > 0x7FFFFFFFll || cols > 0x7FFFFFFFll) return false;
-    return rows * ((cols + kQuantChunk - 1) / kQuantChunk) <= 0x7FFFFFFFll;
+    return rows * ((cols + kQuantStrip - 1) / kQuantStrip) <= 0x7FFFFFFFll;
 }
 
 extern "C" {
@@ -251,8 +304,12 @@ int saem_mx_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64
     if (!x || !codes || !scales) return SAEM_ERR_INVALID_ARG;
     if (((uintptr_t)codes | (uintptr_t)scales) & 15) return SAEM_ERR_ALIGNMENT;
     if ((uintptr_t)x % (dtype == SAEM_OUT_BF16 ? 2 : 4)) return SAEM_ERR_ALIGNMENT;
-    return launch_mx_quantize(x, dtype == SAEM_OUT_BF16, rows, cols, row_stride, (uint8_t*)codes, (uint8_t*)scales,
-                              (cudaStream_t)stream) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+    const bool bf16 = dtype == SAEM_OUT_BF16, vec = vector_rows(x, rows, row_stride, bf16);
+    const uint32_t n_strip = strips(cols, bf16);
+    auto k = bf16 ? (vec ? mx_quantize_kernel<true, true> : mx_quantize_kernel<true, false>)
+                  : (vec ? mx_quantize_kernel<false, true> : mx_quantize_kernel<false, false>);
+    return launch_pdl(k, strip_grid(rows, n_strip), dim3(kQuantThreads), 0, (cudaStream_t)stream, x, (uint32_t)rows, (long long)cols,
+                      (long long)row_stride, n_strip, (uint8_t*)codes, (uint8_t*)scales) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }
 
 int saem_mx_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* out, int dtype,
@@ -264,15 +321,13 @@ int saem_mx_dequantize(const void* codes, const void* scales, int64_t rows, int6
     if (((uintptr_t)codes | (uintptr_t)scales) & 15) return SAEM_ERR_ALIGNMENT;
     const bool bf16 = dtype == SAEM_OUT_BF16;
     if ((uintptr_t)out % (bf16 ? 2 : 4)) return SAEM_ERR_ALIGNMENT;
-    const uint32_t n_chunk = (uint32_t)((cols + kQuantChunk - 1) / kQuantChunk);
-    const uint32_t total = (uint32_t)(rows * n_chunk);
-    const int per_cta = kQuantThreads / 32 * kQuantUnroll;
-    const bool vec = cols % 8 == 0 && ((uintptr_t)out & 15) == 0 && row_stride * (bf16 ? 2 : 4) % 16 == 0;
+    const bool vec = vector_rows(out, rows, row_stride, bf16);
+    const uint32_t n_strip = strips(cols, bf16);
     auto k = bf16 ? (vec ? mx_dequantize_kernel<true, true> : mx_dequantize_kernel<true, false>)
                   : (vec ? mx_dequantize_kernel<false, true> : mx_dequantize_kernel<false, false>);
-    return launch_pdl(k, dim3((total + per_cta - 1) / per_cta), dim3(kQuantThreads), 0, (cudaStream_t)stream,
-                      (const uint8_t*)codes, (const uint8_t*)scales, (long long)rows, (long long)cols,
-                      (long long)row_stride, n_chunk, total, out) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+    return launch_pdl(k, strip_grid(rows, n_strip), dim3(kQuantThreads), 0, (cudaStream_t)stream, (const uint8_t*)codes,
+                      (const uint8_t*)scales, (uint32_t)rows, (long long)cols, (long long)row_stride, n_strip, out) == cudaSuccess
+               ? SAEM_OK : SAEM_ERR_CUDA;
 }
 
 int saem_mx_pack_expert(const saem_config* cfg, const void* gate_codes, const void* gate_scales, const void* up_codes,

@@ -381,7 +381,8 @@ int saem_mx_pack_expert(const saem_config* cfg, const void* gate_codes, const vo
  * overlap.  gate: NULL with SAEM_GATE_NONE (g = 1), one value per row (SAEM_GATE_TOKEN, gate_stride apart), one per
  * column (SAEM_GATE_CHANNEL), or [rows, cols] (SAEM_GATE_FULL); gate_sigmoid != 0: g = 1 / (1 + exp(-gate)).  Types are
  * SAEM_OUT_*; arithmetic is fp32 and n comes from the unrounded x'.  cols <= 16384; strides in elements; every buffer
- * aligned to its elements (16-byte aligned rows and cols % 8 == 0 are faster).  rows == 0 is a no-op.
+ * aligned to its elements (cols and strides that are multiples of 8 elements, on 32-byte aligned buffers, are faster).
+ * rows == 0 is a no-op.
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, CUDA.
  */
 typedef struct saem_norm_config {

@@ -112,6 +112,7 @@ def library_path() -> str:
 
 # the current stream's handle without building a Stream object (a few microseconds of every call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _ptr(t) -> Optional[int]:
@@ -127,8 +128,8 @@ def _ptr(t) -> Optional[int]:
 
 def _stream(s) -> Optional[int]:
     if s is None:
-        if _raw_stream is not None and torch.cuda.is_initialized():
-            return _raw_stream(torch.cuda.current_device()) or None
+        if _raw_stream is not None and _device is not None:
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream or None
     if isinstance(s, torch.cuda.Stream):
         return s.cuda_stream or None

@@ -491,21 +491,6 @@ static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t*
     return cudaLaunchKernelEx(&cfg, mx_matmul_kernel, map_w, map_a, p);
 }
 
-// SMs of the current device.
-static cudaError_t sm_count(int* n) {
-    static int known[64];
-    int dev;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 64 && known[dev]) {
-        *n = known[dev];
-        return cudaSuccess;
-    }
-    e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess && dev < 64) known[dev] = *n;
-    return e;
-}
-
 }  // namespace saem
 
 using namespace saem;

@@ -94,6 +94,21 @@ inline bool first_call_on_device(bool (&done)[64]) {
     done[dev] = true;
     return true;
 }
+// SMs of the current device.
+inline cudaError_t sm_count(int* n) {
+    static int known[64];
+    int dev;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && known[dev]) {
+        *n = known[dev];
+        return cudaSuccess;
+    }
+    e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) known[dev] = *n;
+    return e;
+}
+
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -100,7 +100,7 @@ class Linear:
                  stream=None) -> torch.Tensor:
         """x [m, k] float32 or bfloat16 -> [m, n]."""
         w, ws = self.weight, self.workspace
-        m = len(x)
+        m = x.shape[0]
         if m > self.max_rows:
             raise B.SaemError(B.SAEM_ERR_SHAPE, "Linear")
         if out is None:

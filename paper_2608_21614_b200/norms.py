@@ -35,7 +35,7 @@ class BlockNorm:
                                        branch_scale=branch_scale)
 
     def _call(self, c, x, y, gate, w_post, w_pre, x_out, n_out, stream):
-        T, d = len(x), self.d
+        T, d = x.shape[0], self.d
         c.rows, c.x_dtype, c.x_stride = T, _dtype(x), _matrix(x, "BlockNorm", T, d)
         if y is not None:
             c.y_dtype, c.y_stride, c.x_out_stride = _dtype(y), _matrix(y, "BlockNorm", T, d), _matrix(x_out, "BlockNorm", T, d)
@@ -47,7 +47,7 @@ class BlockNorm:
               stream=None) -> torch.Tensor:
         """The first block's input: n of x itself."""
         if n_out is None:
-            n_out = torch.empty(len(x), self.d, dtype=dtype, device=x.device)
+            n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
         c = B.saem_norm_config.from_buffer_copy(self._cfg)
         c.gate_mode = B.SAEM_GATE_NONE
         self._call(c, x, None, None, None, self.w_pre, None, n_out, stream)
@@ -56,14 +56,15 @@ class BlockNorm:
     def leave(self, x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None,
               n_out: Optional[torch.Tensor] = None, next_norm: bool = True, dtype: torch.dtype = torch.bfloat16, stream=None):
         """(x', n) after a block whose output is y; x_out may be x.  `next_norm` False: x' only (n is None)."""
-        T, c = len(x), self._cfg
+        c = self._cfg
         if x_out is None:
-            x_out = torch.empty(T, self.d, dtype=x.dtype, device=x.device)
-        elif x_out.dtype != x.dtype:
+            x_out = torch.empty(x.shape[0], self.d, dtype=x.dtype, device=x.device)
+        elif x_out.dtype is not x.dtype:
             raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: x_out has x's type")
         if n_out is None and next_norm:
-            n_out = torch.empty(T, self.d, dtype=dtype, device=x.device)
+            n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
         if gate is not None:
+            T = x.shape[0]
             c.gate_dtype, mode, shape = _dtype(gate), c.gate_mode, gate.shape
             if mode == B.SAEM_GATE_FULL:
                 c.gate_stride = _matrix(gate, "BlockNorm gate", T, self.d)

@@ -167,8 +167,8 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
-    pdl_wait();
-    pdl_launch_dependents();
+    // The launch before this one only writes activations; what it waited for itself (the offsets) is complete.  The segments
+    // and the first weights are on their way while it ends.
     read_segments<R>(s, a.offsets, a.E, a.max_rows, a.most, a.status);
     tc_fence_after();
     if (MODE == 0 && blockIdx.x == 0)
@@ -196,23 +196,43 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
         const size_t region = MODE == 0 ? 0 : mx_gate_up_blocks(a.d, a.f);
         int it = 0, st = 0, turn = 0;
         bool ok = true;
-        for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
-            const Item t = item_at(i);
-            const int slot = (int)warp_uniform(tab.slot[t.e]);
-            if (slot < 0) continue;
-            const uint8_t* w = a.slot_region + (size_t)slot * a.slot_bytes + region * kMxBlockBytes + (size_t)t.gb * nc * F::kWBytes;
-            const uint8_t* x = a.tiles + (size_t)t.tile * nc * T::kBytes;
-            for (int c = 0; c < nc; ++c, ++it, w += F::kWBytes, x += T::kBytes) {
-                if (turn) {
-                    ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, a.status);
-                    if (!ok) break;
-                }
-                const uint32_t bar = smem_u32(&bar_full[st]), dst = base + st * F::kStageBytes;
-                expect_tx_on(on, bar, F::kStageBytes);
-                bulk_g2s_on(on, dst, w, F::kWBytes, bar);
-                bulk_g2s_on(on, dst + F::kWBytes, x, T::kBytes, bar);
-                if (++st == F::kStages) { st = 0; ++turn; }
+        // Every stage's weights are requested `early` stages before its activations: all of the ring's before the wait for
+        // the launch before, none ahead afterwards.
+        struct Walk { int i, c; const uint8_t *w, *x; } ahead = {(int)blockIdx.x - (int)gridDim.x, nc, nullptr, nullptr}, now = ahead;
+        auto step = [&](Walk& k) {                                             // to the next stage; false: there is none
+            if (++k.c < nc) {
+                k.w += F::kWBytes;
+                k.x += T::kBytes;
+                return true;
             }
+            for (k.i += gridDim.x; k.i < total; k.i += gridDim.x) {
+                const Item t = item_at(k.i);
+                const int slot = (int)warp_uniform(tab.slot[t.e]);
+                if (slot < 0) continue;
+                k.c = 0;
+                k.w = a.slot_region + (size_t)slot * a.slot_bytes + region * kMxBlockBytes + (size_t)t.gb * nc * F::kWBytes;
+                k.x = a.tiles + (size_t)t.tile * nc * T::kBytes;
+                return true;
+            }
+            return false;
+        };
+        auto weights = [&](const Walk& k, int place) {
+            expect_tx_on(on, smem_u32(&bar_full[place]), F::kStageBytes);
+            bulk_g2s_on(on, base + place * F::kStageBytes, k.w, F::kWBytes, smem_u32(&bar_full[place]));
+        };
+        int early = 0;
+        while (early < F::kStages && step(ahead)) weights(ahead, early++);
+        pdl_wait();
+        pdl_launch_dependents();
+        while (step(now)) {
+            if (turn) {
+                ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, a.status);
+                if (!ok) break;
+                weights(now, st);
+            }
+            bulk_g2s_on(on, base + st * F::kStageBytes + F::kWBytes, now.x, T::kBytes, smem_u32(&bar_full[st]));
+            ++it;
+            if (++st == F::kStages) { st = 0; ++turn; }
         }
         if (!ok && lane == 0)                                                  // copies still under way land before the CTA ends
             for (int q = max(0, it - F::kStages); q < it; ++q) {
@@ -271,6 +291,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         int n = 0;
         bool ok = true;
+        pdl_wait();                                                            // nothing is written before older launches have ended
         for (int i = blockIdx.x; i < total; i += gridDim.x) {
             const Item t = item_at(i);
             if (tab.slot[t.e] < 0) continue;

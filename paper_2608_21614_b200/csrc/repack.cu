@@ -168,7 +168,9 @@ repack_fused_kernel(const int32_t* __restrict__ idx, const uint16_t* __restrict_
 
 // Gate and index phase of a small batch in one CTA: a warp per token in turn, then the counting sort of their choices
 // (the same functions, so the same outputs, as route_kernel and the index phase of repack_fused_kernel).
-__global__ void __launch_bounds__(kRepackThreads)
+constexpr int kRouteIndexThreads = 1024;
+
+__global__ void __launch_bounds__(kRouteIndexThreads)
 route_index_kernel(const float* __restrict__ logits, int T, int E, int S, int k, int renorm, int32_t* __restrict__ idx,
                    float* __restrict__ w, int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm,
                    int32_t* __restrict__ inv_perm, int* __restrict__ status) {
@@ -184,7 +186,20 @@ route_index_kernel(const float* __restrict__ logits, int T, int E, int S, int k,
     float* w_s = reinterpret_cast<float*>(idx_s + n_chunks * 32);
     uint8_t* rank = reinterpret_cast<uint8_t*>(w_s + n_chunks * 32);
     for (int i = threadIdx.x; i < n_chunks * 32; i += blockDim.x) perm_s[i] = -1;
-    for (int t = threadIdx.x >> 5; t < T; t += blockDim.x >> 5) route_row(logits + (size_t)t * E, E, k, renorm, lane, idx_s + t * k, w_s + t * k);
+    for (int t = threadIdx.x >> 5; t < T; t += blockDim.x >> 5) {
+        const float* row = logits + (size_t)t * E;
+        if (k > 8) {
+            route_row(row, E, k, renorm, lane, idx_s + t * k, w_s + t * k);
+            continue;
+        }
+        int e;
+        float weight;
+        route_few(row, E, k, renorm, lane, e, weight);
+        if (lane < k) {
+            idx_s[t * k + lane] = e;
+            w_s[t * k + lane] = weight;
+        }
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < P; i += blockDim.x) {
         idx[i] = idx_s[i];
@@ -199,7 +214,7 @@ cudaError_t launch_route_index(const float* logits, int T, int E, int S, int k, 
                                int32_t* offsets, int32_t* perm, int32_t* inv_perm, int* status, cudaStream_t st) {
     const int n_chunks = (T * k + 31) >> 5;
     const size_t smem = sizeof(RepackSmem) + (((size_t)table_stride(n_chunks) * E * 2 + 15) & ~(size_t)15) + (size_t)n_chunks * 32 * 13;
-    return launch_pdl(route_index_kernel, dim3(1), dim3(kRepackThreads), smem, st, logits, T, E, S, k, renorm, idx, w, counts, offsets, perm,
+    return launch_pdl(route_index_kernel, dim3(1), dim3(kRouteIndexThreads), smem, st, logits, T, E, S, k, renorm, idx, w, counts, offsets, perm,
                       inv_perm, status);
 }
 

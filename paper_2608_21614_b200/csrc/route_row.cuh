@@ -104,6 +104,62 @@ __device__ __forceinline__ void route_row(const float* __restrict__ row, int E, 
     }
 }
 
+// route_row (the same choices and weights) for k <= 8, where the gate is on the critical path: a lane's four keys are sorted first, so
+// that a round looks at one of them; the winner of round j ends in lane j.
+__device__ __forceinline__ void route_few(const float* __restrict__ row, int E, int k, int renorm, int lane, int& mine, float& weight) {
+    uint32_t key[kPerLane];
+    int id[kPerLane];
+    float all = 0.f, win = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        id[i] = lane + 32 * i;
+        key[i] = id[i] < E ? order_key(row[id[i]]) : 0u;                       // 0: below every real key
+    }
+    auto sort2 = [&](int x, int y) {                                           // larger first, equal keys by id
+        const bool swap = key[y] > key[x] || (key[y] == key[x] && id[y] < id[x]);
+        const uint32_t kx = key[x];
+        const int ix = id[x];
+        key[x] = swap ? key[y] : kx;  id[x] = swap ? id[y] : ix;
+        key[y] = swap ? kx : key[y];  id[y] = swap ? ix : id[y];
+    };
+    sort2(0, 1); sort2(2, 3); sort2(0, 2); sort2(1, 3); sort2(1, 2);
+    float vmax = 0.f;
+    mine = 0;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
+        const int e = (int)__reduce_min_sync(0xffffffffu, key[0] == top ? (unsigned)id[0] : 0xffffffffu);
+        if (j == 0) {
+            vmax = key_value(top);
+            if (!renorm) {
+#pragma unroll
+                for (int i = 0; i < kPerLane; ++i)
+                    if (key[i]) all += expf(key_value(key[i]) - vmax);
+            }
+        }
+        if (e == id[0]) {                                                      // taken
+            key[0] = key[1]; key[1] = key[2]; key[2] = key[3]; key[3] = 0u;
+            id[0] = id[1]; id[1] = id[2]; id[2] = id[3]; id[3] = 0x7FFFFFFF;
+        }
+        if (lane == j) {
+            win = key_value(top);
+            mine = e;
+        }
+    }
+    float z = 0.f;
+    if (lane < k)
+        z = vmax == CUDART_INF_F ? (win == CUDART_INF_F ? 1.f : 0.f) : vmax == -CUDART_INF_F ? 1.f : expf(win - vmax);
+    float sum = z;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);   // k <= 8: the other lanes hold nothing
+    if (!renorm && vmax != CUDART_INF_F && vmax != -CUDART_INF_F) {
+        sum = all;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    weight = z / sum;
+}
+
 }  // namespace saem
 
 #endif  // SAEM_ROUTE_ROW_CUH_

@@ -19,7 +19,8 @@ namespace saem {
 constexpr int kFewTokens = 8;
 constexpr int kFewPairs = kFewTokens * kFewTokens;           // top_k <= 8
 constexpr int kFewActive = kFewPairs + 16;                   // plus the always-on experts
-constexpr int kFewThreads = 320;                             // warp 0: copies, warp 1: MMA issue, warps 2-9: x's planes, epilogue
+constexpr int kFewThreads = 320;                             // warp 0: copies, warp 1: MMA issue, warps 2-9: epilogue
+constexpr int kGateUpThreads = kFewThreads + 256;            // gate/up: warps 10-17 split x into planes while the others route
 constexpr int kFewMaxStages = 8;
 constexpr int kFewSplit = 8;                                 // CTAs of a cluster: parts of the down projection's k axis
 using FewTile = TileShape<kFewTokens>;
@@ -51,17 +52,18 @@ __device__ __forceinline__ void few_init(FewShared& s, const MxFewArgs& a, const
             mbar_init(smem_u32(&s.acc[i]), 1);
             mbar_init(smem_u32(&s.free[i]), 4);
         }
-        mbar_init(smem_u32(&s.x), 8);
+        mbar_init(smem_u32(&s.x), 16);
         s.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x < 4) s.mask[threadIdx.x] = 0;
-    for (int i = threadIdx.x; i < a.E + a.S; i += kFewThreads) s.slot[i] = tab.slot[i];
-    for (int i = threadIdx.x; i < kFewActive * kFewTokens; i += kFewThreads) (&s.weight[0][0])[i] = 0.f;
+    for (int i = threadIdx.x; i < a.E + a.S; i += blockDim.x) s.slot[i] = tab.slot[i];
+    for (int i = threadIdx.x; i < kFewActive * kFewTokens; i += blockDim.x) (&s.weight[0][0])[i] = 0.f;
     __syncthreads();
 }
 // Routes the batch (one warp per token) and lists the active experts in ascending order, the always-on ones last; experts
-// without a slot are left out (status word).  All threads call it; ends with a barrier.
+// without a slot are left out (status word).  The first kFewThreads threads call it; ends with a barrier of theirs.
+__device__ __forceinline__ void few_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kFewThreads) : "memory"); }
 __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, bool report) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int e = -1;
@@ -83,7 +85,7 @@ __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, bool
             }
         }
     }
-    __syncthreads();
+    few_sync();
     const uint32_t m0 = s.mask[0], m1 = s.mask[1], m2 = s.mask[2], m3 = s.mask[3];
     if (e >= 0) {
         const int word = e >> 5;
@@ -105,7 +107,7 @@ __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, bool
         }
         s.n_active = n;
     }
-    __syncthreads();
+    few_sync();
 }
 // At an abort: copies that are still under way land before the CTA ends.
 __device__ __noinline__ void few_drain(FewShared& s, int n_stage, int issued, int* status) {
@@ -133,7 +135,7 @@ __device__ __forceinline__ void few_free(uint32_t tmem, uint32_t cols) {
 // occupy the SMs: a stage then holds 64 rows of the gate block and of the up block, and the MMA's other 64 rows read
 // whatever lies beside them (inside the CTA's shared memory), for lanes that nobody looks at.
 template <bool HALF>
-__global__ void __launch_bounds__(kFewThreads, 1)
+__global__ void __launch_bounds__(kGateUpThreads, 1)
 mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ SlotTable tab) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ FewShared s;
@@ -148,19 +150,34 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
     few_init(s, a, tab, n);
     pdl_wait();
     pdl_launch_dependents();
-    // the runs of x that a warp will split are on their way while the batch is routed
-    const int tasks = a.T * nc;
-    constexpr int kAhead = 8;
-    uint4 q[kAhead];
-    auto load_x = [&](int first) {
+    // x's planes: five eighths of the runs (all, if they are few) by warps 10-17 at once, the rest by warps 2-9 after routing
+    const int tasks = a.T * nc, mine = tasks <= 16 ? tasks : (tasks * 5 + 7) / 8;
+    auto split_x = [&](int begin, int end) {
+        constexpr int kAhead = 4;                                              // runs whose loads are under way
+        for (int first = begin; first < end; first += 8 * kAhead) {
+            uint4 q[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int i = first + 8 * u, t = i / nc, col = (i - t * nc) * kMxChunk + lane * 8;
-            q[u] = i < tasks && col < a.d ? *reinterpret_cast<const uint4*>(a.x + (size_t)t * a.d + col) : make_uint4(0u, 0u, 0u, 0u);
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = first + 8 * u, t = i / nc, col = (i - t * nc) * kMxChunk + lane * 8;
+                q[u] = i < end && col < a.d ? *reinterpret_cast<const uint4*>(a.x + (size_t)t * a.d + col) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = first + 8 * u, t = i / nc, c = i - t * nc;
+                if (i >= end) break;
+                float v[8];
+                uint32_t codes[kPlanes], scales[kPlanes];
+                widen8(q[u], v);
+                split_planes(v, lane, codes, scales);
+                store_tile_row<kFewTokens>(xs + (size_t)c * FewTile::kBytes, t, lane, codes, scales);
+            }
         }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s.x));
     };
-    if (warp >= 2) load_x(warp - 2);
-    few_route(s, a, blockIdx.x == 0);
+    if (warp >= 10) split_x(warp - 10, mine);
+    else few_route(s, a, blockIdx.x == 0);
     tc_fence_after();
     const uint32_t tmem = warp_uniform(s.tmem), tmem_sf = tmem + 4 * FewTile::kN;
     const int per = a.f / 128 * (HALF ? 2 : 1), total = (int)warp_uniform(s.n_active) * per;
@@ -237,30 +254,8 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
             }
             tc_commit_on(on, smem_u32(&s.acc[set]));
         }
-    } else {
-        // ---------------------------------------------------------------- x's planes
-        for (int first = warp - 2; first < tasks; first += 8 * kAhead) {
-            if (first > 7) load_x(first);
-#pragma unroll
-            for (int u = 0; u < kAhead; u += 2) {                              // two at a time, for the latency's sake
-                if (first + 8 * u >= tasks) break;
-                float v[2][8];
-                uint32_t codes[2][kPlanes], scales[2][kPlanes];
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    widen8(q[u + z], v[z]);
-                    split_planes(v[z], lane, codes[z], scales[z]);
-                }
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    const int i = first + 8 * (u + z), t = i / nc, c = i - t * nc;
-                    if (i < tasks) store_tile_row<kFewTokens>(xs + (size_t)c * FewTile::kBytes, t, lane, codes[z], scales[z]);
-                }
-            }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s.x));
+    } else if (warp < 10) {
+        split_x(mine + warp - 2, tasks);
         // ---------------------------------------------------------------- epilogue
         const int quad = warp & 3, group = (warp - 2) >> 2;                    // each group of four warps has its own accumulators
         const uint32_t acc = tmem + group * 2 * FewTile::kN + ((uint32_t)(quad * 32) << 16);
@@ -428,7 +423,7 @@ cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStrea
     const int most = kFewMaxStages;                                            // tensor memory: 192 columns of sums, 16 per stage, 8 per chunk of x
     if (a.stages_a > most) a.stages_a = most;
     cudaError_t e = launch_pdl(half ? mx_few_gate_up_kernel<true> : mx_few_gate_up_kernel<false>, dim3((unsigned)(items < n_sm ? items : n_sm)),
-                               dim3(kFewThreads), (size_t)(around + a.stages_a * stage), st, a, tab);
+                               dim3(kGateUpThreads), (size_t)(around + a.stages_a * stage), st, a, tab);
     if (e != cudaSuccess) return e;
     *n_launch += 1;
     cudaLaunchAttribute attr[2];

@@ -43,6 +43,7 @@ struct MmArgs {
     const void* x;                          // quantise A from here (every stage of the CTA has its place in the ring), or nullptr
     long long x_stride;
     int x_bf16, x_vec;
+    int out_pairs;                          // bf16 output whose rows begin at 4-byte addresses, n even
 };
 
 __global__ void __launch_bounds__(kMmThreads, 1)
@@ -256,6 +257,35 @@ constexpr int kBigStageBytes = 128 * 128 + kBigTile * 128 + 6 * kMxPiece;
 constexpr int kBigSmem = kBigStages * kBigStageBytes + 1024;
 constexpr int kBigSfCols = 24;
 
+// 128 tokens' sums of the output column n that this lane owns.  bf16 in pairs of columns where the output's rows allow it:
+// even lanes take over the pair for even tokens, odd ones for odd tokens.
+__device__ __forceinline__ void store_columns(const MmArgs& p, const uint32_t (&r)[128], int n, int t0, int lane) {
+    const int tokens = min(128, p.m - t0);
+    if (!p.out_bf16) {
+        float* o = static_cast<float*>(p.out) + (size_t)t0 * p.out_stride + n;
+        if (n < p.n)
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+                if (c < tokens) o[c * p.out_stride] = __uint_as_float(r[c]);
+    } else if (p.out_pairs) {
+        const int odd = lane & 1;
+        uint16_t* o = static_cast<uint16_t*>(p.out) + (size_t)(t0 + odd) * p.out_stride + (n & ~1);
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? r[c] : r[c + 1], 1);
+            const __nv_bfloat162 v = odd ? __floats2bfloat162_rn(__uint_as_float(other), __uint_as_float(r[c + 1]))
+                                         : __floats2bfloat162_rn(__uint_as_float(r[c]), __uint_as_float(other));
+            if (n < p.n && c + odd < tokens) *reinterpret_cast<__nv_bfloat162*>(o + c * p.out_stride) = v;
+        }
+    } else {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + (size_t)t0 * p.out_stride + n;
+        if (n < p.n)
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+                if (c < tokens) o[c * p.out_stride] = __float2bfloat16_rn(__uint_as_float(r[c]));
+    }
+}
+
 __global__ void __launch_bounds__(kBigThreads, 1)
 mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ MmArgs p) {
     extern __shared__ uint8_t smem_raw[];
@@ -376,25 +406,154 @@ mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bar_free));
-            const int n = tw * 128 + row, t0 = tt * kBigTile + half * 128, tokens = min(128, p.m - t0);
-            if (!ok || n >= p.n) continue;
-            if (p.out_bf16) {
-                __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out) + (size_t)t0 * p.out_stride + n;
-#pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if (c < tokens) o[c * p.out_stride] = __float2bfloat16_rn(__uint_as_float(r[c]));
-            } else {
-                float* o = static_cast<float*>(p.out) + (size_t)t0 * p.out_stride + n;
-#pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    if (c < tokens) o[c * p.out_stride] = __uint_as_float(r[c]);
-            }
+            if (ok) store_columns(p, r, tw * 128 + row, tt * kBigTile + half * 128, lane);
         }
     }
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
+    }
+}
+
+// The same with pairs of CTAs: 256 weight rows x 256 tokens.  One CTA alone has to bring 48 KB of codes into shared memory
+// and feed the MMA 48 KB out of it for every 512 cycles of MMAs, more than its 128 bytes per cycle; in a pair each CTA
+// loads its own 128 weight rows but half of the tokens, whose other half the hardware reads from the partner.  The
+// leader's barriers count both CTAs' copies (all of them tiled, the scales too: an untiled bulk copy cannot signal another
+// CTA's barrier) and one commit frees a stage, or hands over the accumulators, in both.
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = 2 * 128 * 128 + 6 * kMxPiece;
+constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024;
+
+__global__ void __launch_bounds__(kBigThreads, 1)
+mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a,
+                      const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_as, const __grid_constant__ MmArgs p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ alignas(8) uint64_t bar_full[kPairStages], bar_empty[kPairStages], bar_acc, bar_free;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_flag;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int rank = (int)cluster_ctarank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int n_w = (p.n + 255) / 256, n_t = (p.m + kBigTile - 1) / kBigTile, total = n_w * n_t;
+    const long long kp = (p.k + kMxBlock - 1) / kMxBlock * kMxBlock;
+    const int n_span = (p.k + kMxSpan - 1) / kMxSpan, stages = (int)((kp + kMmStageK - 1) / kMmStageK);
+    int* const status = p.status ? p.status : &mx_status_sink;
+    volatile int* abort_p = &abort_flag;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairStages; ++i) {
+            mbar_init(smem_u32(&bar_full[i]), 1);
+            mbar_init(smem_u32(&bar_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&bar_acc), 1);
+        mbar_init(smem_u32(&bar_free), 16);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "n"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    cluster_sync_all();                                                        // both CTAs' barriers exist
+    tc_fence_after();
+    pdl_wait();
+    pdl_launch_dependents();
+    const uint32_t tmem = warp_uniform(tmem_s), tmem_sf = tmem + kBigTile;
+    constexpr int half_bytes = 128 * 128, scales_at = 2 * half_bytes;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- copies (both CTAs)
+        const uint32_t on = elect_one();
+        int st = 0, turn = 0;
+        bool ok = true;
+        for (int i = pair; i < total && ok; i += pairs) {
+            const int tt = i / n_w, tw = (i - tt * n_w) * 2 + rank;
+            for (int s = 0; s < stages; ++s) {
+                if (turn) {
+                    ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, status);
+                    if (!ok) break;
+                }
+                const uint32_t dst = base + st * kPairStageBytes, full = mapa_u32(smem_u32(&bar_full[st]), 0);
+                // the leader alone arms its barrier, for both; the partner's copies may complete on it first
+                if (rank == 0) expect_tx_on(on, smem_u32(&bar_full[st]), 2 * kPairStageBytes);
+                tma_2d_pair_on(on, dst, &map_w, s * 128, tw * 128, full);
+                tma_2d_pair_on(on, dst + half_bytes, &map_a, s * 128, tt * kBigTile + rank * 128, full);
+                tma_2d_pair_on(on, dst + scales_at, &map_ws, 0, tw * n_span + 2 * s, full);
+                tma_2d_pair_on(on, dst + scales_at + 2 * kMxPiece, &map_as, 0, 2 * tt * n_span + 2 * s, full);
+                tma_2d_pair_on(on, dst + scales_at + 4 * kMxPiece, &map_as, 0, (2 * tt + 1) * n_span + 2 * s, full);
+                if (++st == kPairStages) { st = 0; ++turn; }
+            }
+        }
+        if (!ok) {                                                             // copies still under way land before the CTA ends
+            const unsigned long long t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 200000ull) {}
+        }
+    } else if (warp == 1) {
+        if (rank == 0) {
+            // ------------------------------------------------------------ MMA issue (leader)
+            const uint32_t on = elect_one();
+            const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base + scales_at);
+            int st = 0, turn = 0, k = 0;
+            bool ok = true;
+            for (int i = pair; i < total && ok; i += pairs, ++k) {
+                if (k) ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&bar_free), (k - 1) & 1, abort_p, status));
+                tc_fence_after();
+                for (int s = 0; s < stages && ok; ++s) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&bar_full[st]), turn & 1, abort_p, status));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t at = st * kPairStageBytes, tw = tmem_sf + st * kBigSfCols, ta = tw + 8;
+                    const uint64_t dw = desc_at(codes0, at), da = desc_at(codes0, at + half_bytes), ds = desc_at(scales0, at);
+                    const int steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (2 * s + h >= n_span) break;
+                        tc_cp_scales_pair(on, tw + 4 * h, desc_at(ds, h * kMxPiece));
+                        tc_cp_scales_pair(on, ta + 8 * h, desc_at(ds, (2 + h) * kMxPiece));
+                        tc_cp_scales_pair(on, ta + 8 * h + 4, desc_at(ds, (4 + h) * kMxPiece));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < steps)
+                            tc_mma_mxf4_pair(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4_pair(kBigTile, (j & 1) * 2),
+                                             tw + 4 * (j >> 1), ta + 8 * (j >> 1), s > 0 || j > 0);
+                    tc_commit_pair_on(on, smem_u32(&bar_empty[st]));
+                    if (++st == kPairStages) { st = 0; ++turn; }
+                }
+                tc_commit_pair_on(on, smem_u32(&bar_acc));
+            }
+        }
+    } else {
+        // ---------------------------------------------------------------- epilogue (both CTAs)
+        const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
+        bool ok = true;
+        int k = 0;
+        for (int i = pair; i < total && ok; i += pairs, ++k) {
+            const int tt = i / n_w, tw = (i - tt * n_w) * 2 + rank;
+            ok = mbar_wait_warp(smem_u32(&bar_acc), k & 1, abort_p, status);
+            tc_fence_after();
+            uint32_t r[128];
+            if (ok) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tc_ld32_issue(tmem + ((uint32_t)(quad * 32) << 16) + half * 128 + q * 32, r + 32 * q);
+                tc_wait_ld();
+#pragma unroll
+                for (int q = 0; q < 8; ++q) tc_reg_fence16(r + 16 * q);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&bar_free), 0));
+            if (ok) store_columns(p, r, tw * 128 + row, tt * kBigTile + half * 128, lane);
+        }
+    }
+    // neither CTA leaves, or frees tensor memory, while the other may still touch it
+    __syncwarp();
+    tc_fence_before();
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
     }
 }
 
@@ -416,7 +575,9 @@ static cudaError_t mx_matmul_init() {
     }
     if (!first_call_on_device(g_mx_done)) return cudaSuccess;
     const cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(mx_matmul_tiles_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
+    if (e != cudaSuccess) return e;
+    const cudaError_t f = cudaFuncSetAttribute(mx_matmul_tiles_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
+    return f != cudaSuccess ? f : cudaFuncSetAttribute(mx_matmul_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
 }
 
 // Codes as a byte matrix: boxes of 128 bytes (256 elements) x `box_rows` rows; what lies outside reads as zero.
@@ -434,12 +595,15 @@ static bool make_code_map(CUtensorMap* m, const void* codes, long long rows, lon
 // How a product is cut: decided from its sizes alone, so that saem_mx_linear knows whether A is to be quantised first.
 struct MmPlan {
     bool big;                               // mx_matmul_tiles_kernel
+    bool pairs;                             // mx_matmul_pair_kernel
     bool fused;                             // A quantised by the product's CTAs (where it is not quantised already)
     int n_tile, split, n_stage, stage_bytes;
 };
 static MmPlan mm_plan(int m, int n, int k, int n_sm) {
     MmPlan p = {};
     p.big = m > 64;
+    // every pair of SMs has a tile of 256 x 256 at least
+    p.pairs = p.big && (long long)((n + 255) / 256) * ((m + 255) / 256) >= n_sm / 2;
     if (p.big) return p;
     const int tiles = (n + 127) / 128, stages = (k + kMmStageK - 1) / kMmStageK;
     p.n_tile = round_up(m, 16);
@@ -456,12 +620,32 @@ static MmPlan mm_plan(int m, int n, int k, int n_sm) {
     return p;
 }
 
+// Scales as rows of 512 bytes: two pieces of a row tile, which follow each other along k.
+static bool make_scale_map(CUtensorMap* m, const void* scales, long long rows, long long cols) {
+    const cuuint64_t dims[2] = {128, (cuuint64_t)((rows + 127) / 128 * ((cols + kMxSpan - 1) / kMxSpan))};
+    const cuuint64_t strides[1] = {kMxPiece};
+    const cuuint32_t box[2] = {128, 2};
+    const cuuint32_t estr[2] = {1, 1};
+    return g_mx_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(scales), dims, strides, box, estr,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t* a_codes, const uint8_t* w_codes, int n_sm, cudaStream_t st) {
     alignas(64) CUtensorMap map_w, map_a;
     const int n_tile = plan.big ? kBigTile : plan.n_tile;
     if (!make_code_map(&map_w, w_codes, p.n, p.k, 128)) return cudaErrorInvalidValue;
     if (a_codes ? !make_code_map(&map_a, a_codes, p.m, p.k, n_tile) : (map_a = map_w, false)) return cudaErrorInvalidValue;
     p.n_tile = n_tile;
+    p.out_pairs = p.out_bf16 && p.n % 2 == 0 && ((uintptr_t)p.out & 3) == 0 && (p.out_stride % 2 == 0 || p.m == 1);
+    if (plan.pairs) {
+        alignas(64) CUtensorMap map_ws, map_as;
+        if (!make_code_map(&map_a, a_codes, p.m, p.k, 128) || !make_scale_map(&map_ws, p.w_scales, p.n, p.k) ||
+            !make_scale_map(&map_as, p.a_scales, p.m, p.k))
+            return cudaErrorInvalidValue;
+        return launch_pdl_pairs(mx_matmul_pair_kernel, dim3((unsigned)(n_sm & ~1)), dim3(kBigThreads), (size_t)kPairSmem, st, map_w, map_a, map_ws,
+                                map_as, p);
+    }
     if (plan.big) {
         const long long tiles = (long long)((p.n + 127) / 128) * ((p.m + kBigTile - 1) / kBigTile);
         return launch_pdl(mx_matmul_tiles_kernel, dim3((unsigned)(tiles < n_sm ? tiles : n_sm)), dim3(kBigThreads), (size_t)kBigSmem, st, map_w,

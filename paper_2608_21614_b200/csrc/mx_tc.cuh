@@ -75,6 +75,40 @@ __device__ __forceinline__ uint32_t idesc_mxf4(int n, int id) {
            ((uint32_t)id << 29);
 }
 
+// The same on a pair of CTAs (cta_group::2): M = 256, 128 rows of A and half of B's rows in each CTA's shared memory; the
+// scales of A's own rows and of all of B's in each CTA's tensor memory.  One thread of the leader issues for both.
+__device__ __forceinline__ void tc_cp_scales_pair(uint32_t on, uint32_t taddr, uint64_t desc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %2, 0;\n\t"
+        "@p tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc), "r"(on) : "memory");
+}
+__device__ __forceinline__ void tc_mma_mxf4_pair(uint32_t on, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                 uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %7, 0;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@p tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], q;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(on) : "memory");
+}
+__device__ __forceinline__ void tma_2d_pair_on(uint32_t on, uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t cluster_bar) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "@p cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar), "r"(on) : "memory");
+}
+__device__ __forceinline__ void tc_commit_pair_on(uint32_t on, uint32_t bar) {
+    const uint16_t mask = 3;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %2, 0;\n\t"
+        "@p tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+        ::"r"(bar), "h"(mask), "r"(on) : "memory");
+}
+__device__ __forceinline__ uint32_t idesc_mxf4_pair(int n, int id) { return idesc_mxf4(n, id) + (1u << 27); }   // M = 256
+
 }  // namespace saem
 
 #endif  // SAEM_MX_TC_CUH_

@@ -104,7 +104,7 @@ def operands(m, n, k, seed):
 SHAPES = [(1, 1, 1), (1, 128, 32), (1, 300, 4096), (2, 127, 31), (3, 129, 64), (8, 256, 96), (15, 64, 128), (16, 384, 160),
           (17, 130, 256), (33, 16, 288), (64, 1, 512), (100, 257, 1000), (127, 128, 2112), (128, 200, 320), (129, 128, 256),
           (200, 40, 96), (256, 256, 768), (257, 129, 64), (300, 384, 1500), (513, 130, 257), (1000, 640, 544), (1024, 1024, 1024),
-          (2500, 1300, 416)]
+          (2500, 1300, 416), (2304, 2300, 600), (4000, 1501, 136), (1025, 4096, 1024)]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])

@@ -338,7 +338,7 @@ int saem_expert_ffn_static(const void* x_packed, const int32_t* offsets, int n_e
  *
  * saem_mx_quantize: s = max(floor(log2 max|x|) - 2, -127) + 127 and the code nearest to x * 2^-(s - 127), ties to the even
  * mantissa, saturated at 6; a block with a NaN or an infinity gets s = 255.  x[rows, cols] fp32 or bf16 (dtype: SAEM_OUT_*),
- * row r at r * row_stride elements, aligned to its elements (16-byte aligned rows are faster).
+ * row r at r * row_stride elements, aligned to its elements (32-byte aligned rows are faster).
  * saem_mx_dequantize: the values back, out[rows, cols] fp32 or bf16 (both exact).
  *
  * saem_mx_matmul: out[m, n] = sum_k A[m, k] * W[n, k] of two such matrices (row r of out at r * out_stride), block-scaled

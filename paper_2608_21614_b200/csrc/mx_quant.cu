@@ -4,7 +4,8 @@
 // even mantissa), saturated at 6.  Both the scaling and the way back are exact, so the only rounding is the one to E2M1.
 // All kernels here read and write every byte once and are bound by DRAM (2.5 or 4.5 bytes per element) -- if the
 // instructions per element stay few: a lane takes 16 elements of bf16 (half a block; its maximum is found in packed
-// halves and scaled in packed halves) or 8 of fp32, and a warp four such pieces of one row, whose loads go out together.
+// halves and scaled in packed halves) or 8 of fp32, 32 bytes in one access, and a warp four such pieces of one row, whose
+// loads go out together.
 #include <cmath>
 #include <cstring>
 
@@ -37,9 +38,9 @@ mx_quantize_kernel(const void* __restrict__ x, uint32_t rows, long long cols, lo
     for (int u = 0; u < kQuantUnroll; ++u) {
         const long long col = col0 + u * kPiece;
         if (VEC && col + kPerLane <= cols) {
-            const uint4* p = reinterpret_cast<const uint4*>(src + col * (BF16 ? 2 : 4));
-            const uint4 a = __ldcs(p), b = __ldcs(p + 1);
-            v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w; v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(v[u][0]), "=r"(v[u][1]), "=r"(v[u][2]), "=r"(v[u][3]), "=r"(v[u][4]), "=r"(v[u][5]), "=r"(v[u][6]), "=r"(v[u][7])
+                         : "l"(src + col * (BF16 ? 2 : 4)));
         } else if (BF16) {
             const uint16_t* p = reinterpret_cast<const uint16_t*>(src);
 #pragma unroll
@@ -136,44 +137,37 @@ mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restric
         if (col >= cols) continue;
         const float scale = s[u] == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(s[u] ? s[u] << 23 : 1u << 22);
         const size_t at = (size_t)row * row_stride + col;
+        uint32_t o[8];                                                        // the lane's 32 bytes: 16 bf16 or 8 fp32
 #pragma unroll
         for (int h = 0; h < kPerLane / 8; ++h) {
             uint32_t p[4];
             mx_decode8(h ? w[u].y : w[u].x, p);
-            float v[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p[i]));
-                v[2 * i] = f.x * scale;
-                v[2 * i + 1] = f.y * scale;
-            }
-            const long long c = col + 8 * h;
-            if (BF16) {
-                uint16_t* o = static_cast<uint16_t*>(out) + at + 8 * h;
-                uint32_t b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const __nv_bfloat162 q = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);   // exact: one mantissa bit
-                    b[i] = *reinterpret_cast<const uint32_t*>(&q);
-                }
-                if (VEC && c + 8 <= cols) {
-                    __stcs(reinterpret_cast<uint4*>(o), make_uint4(b[0], b[1], b[2], b[3]));
+                float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p[i]));
+                f.x *= scale;
+                f.y *= scale;
+                if (BF16) {
+                    const __nv_bfloat162 q = __float22bfloat162_rn(f);        // exact: one mantissa bit
+                    o[4 * h + i] = *reinterpret_cast<const uint32_t*>(&q);
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (c + i < cols) o[i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
-                }
-            } else {
-                float* o = static_cast<float*>(out) + at;
-                if (VEC && c + 8 <= cols) {
-                    __stcs(reinterpret_cast<float4*>(o), make_float4(v[0], v[1], v[2], v[3]));
-                    __stcs(reinterpret_cast<float4*>(o) + 1, make_float4(v[4], v[5], v[6], v[7]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (c + i < cols) o[i] = v[i];
+                    o[2 * i] = __float_as_uint(f.x);
+                    o[2 * i + 1] = __float_as_uint(f.y);
                 }
             }
+        }
+        if (VEC && col + kPerLane <= cols) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"(static_cast<uint8_t*>(out) + at * (BF16 ? 2 : 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]),
+                         "r"(o[6]), "r"(o[7]) : "memory");
+        } else if (BF16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (col + i < cols) static_cast<uint16_t*>(out)[at + i] = (uint16_t)(o[i / 2] >> (16 * (i & 1)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < cols) static_cast<uint32_t*>(out)[at + i] = o[i];
         }
     }
 }
@@ -271,7 +265,7 @@ static dim3 strip_grid(long long rows, uint32_t n_strip) {
     return dim3((unsigned)(((unsigned long long)rows * n_strip + kQuantThreads / 32 - 1) / (kQuantThreads / 32)));
 }
 static bool vector_rows(const void* p, long long rows, long long row_stride, bool bf16) {
-    return ((uintptr_t)p & 15) == 0 && (rows == 1 || row_stride * (bf16 ? 2 : 4) % 16 == 0);
+    return ((uintptr_t)p & 31) == 0 && (rows == 1 || row_stride * (bf16 ? 2 : 4) % 32 == 0);
 }
 
 }  // namespace saem

@@ -332,8 +332,9 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
-// Rows per tile: as many as a segment of a step of this many tokens has on average, times two (segments differ), in
-// tiles that the tensor memory holds.
+// Rows per tile, by the rows that a segment of a step of this many tokens has on average, times two (segments differ; per
+// token k routed and always-on rows over E experts): 8 up to 8 rows, 16 up to 24, else 32, which is what tensor memory
+// holds.  (64 tokens of a 2048 x 768 layer of 128 experts, 8 rows in twice the average: 8-row tiles.)
 static int tile_rows(int tokens, int k, int E) {
     const long long twice = 2LL * tokens * k / E;
     return tokens <= 8 || twice <= 8 ? 8 : tokens <= 16 || twice <= 24 ? 16 : 32;
@@ -341,14 +342,23 @@ static int tile_rows(int tokens, int k, int E) {
 static long long most_tiles(long long rows, int experts, int R) { return (rows < experts ? rows : experts) + rows / R; }
 static size_t tile_bytes(int R) { return R == 8 ? TileShape<8>::kBytes : R == 16 ? TileShape<16>::kBytes : TileShape<32>::kBytes; }
 
+// A step of fewer tokens than the context was made for may take smaller tiles: the largest of the three, each with the most
+// tokens that take it.  (The form for up to 8 tokens needs no more than 8-row tiles.)
 size_t mx_workspace_bytes(int max_tokens, int k, int E, int S, int d, int f) {
-    const long long rows = (long long)max_tokens * (k + S);
+    const int per = k + S, all = E + S;
     size_t most = 0;
-    for (int R = 8; R <= 32; R *= 2) {                                         // a step of fewer tokens may take smaller tiles
-        const size_t b = (size_t)most_tiles(rows, E + S, R) * tile_bytes(R) * (mx_chunks(d) + mx_chunks(f));
+    for (int R = 8; R <= 32; R *= 2) {
+        long long tokens = max_tokens;
+        if (R < 32) {
+            const long long twice = R == 8 ? 9 : 25, few = R == 8 ? 8 : 16;    // twice * all - 1 rows still round down to the limit
+            const long long fit = (twice * all - 1) / (2 * per);
+            tokens = fit > few ? fit : few;
+            if (tokens > max_tokens) tokens = max_tokens;
+        }
+        const size_t b = (size_t)most_tiles(tokens * per, all, R) * tile_bytes(R) * (mx_chunks(d) + mx_chunks(f));
         if (b > most) most = b;
     }
-    return most;                                                               // the form for up to 8 tokens needs no more than R = 8
+    return most;
 }
 
 template <int R>
@@ -379,7 +389,7 @@ static cudaError_t launch_tiles(const FfnArgs& f, const MxTokens& x, const SlotT
 }
 
 cudaError_t launch_mx_ffn(const FfnArgs& f, const MxTokens& x, const SlotTable& tab, cudaStream_t st, int* n_launch) {
-    const int R = tile_rows(f.tokens, f.max_rows / (f.tokens > 0 ? f.tokens : 1), f.E);
+    const int R = tile_rows(f.tokens, f.per_token, f.E);
     const cudaError_t e = R == 8 ? launch_tiles<8>(f, x, tab, st) : R == 16 ? launch_tiles<16>(f, x, tab, st) : launch_tiles<32>(f, x, tab, st);
     if (e == cudaSuccess) *n_launch += 3;
     return e;

@@ -115,6 +115,13 @@ __device__ __forceinline__ void route_few(const float* __restrict__ row, int E, 
         id[i] = lane + 32 * i;
         key[i] = id[i] < E ? order_key(row[id[i]]) : 0u;                       // 0: below every real key
     }
+    float vmax = 0.f;
+    if (!renorm) {                                                             // in the order of the ids, as route_row adds
+        vmax = key_value(__reduce_max_sync(0xffffffffu, max(max(key[0], key[1]), max(key[2], key[3]))));
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i)
+            if (id[i] < E) all += expf(key_value(key[i]) - vmax);
+    }
     auto sort2 = [&](int x, int y) {                                           // larger first, equal keys by id
         const bool swap = key[y] > key[x] || (key[y] == key[x] && id[y] < id[x]);
         const uint32_t kx = key[x];
@@ -123,20 +130,12 @@ __device__ __forceinline__ void route_few(const float* __restrict__ row, int E, 
         key[y] = swap ? kx : key[y];  id[y] = swap ? ix : id[y];
     };
     sort2(0, 1); sort2(2, 3); sort2(0, 2); sort2(1, 3); sort2(1, 2);
-    float vmax = 0.f;
     mine = 0;
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
         const uint32_t top = __reduce_max_sync(0xffffffffu, key[0]);
         const int e = (int)__reduce_min_sync(0xffffffffu, key[0] == top ? (unsigned)id[0] : 0xffffffffu);
-        if (j == 0) {
-            vmax = key_value(top);
-            if (!renorm) {
-#pragma unroll
-                for (int i = 0; i < kPerLane; ++i)
-                    if (key[i]) all += expf(key_value(key[i]) - vmax);
-            }
-        }
+        if (j == 0) vmax = key_value(top);
         if (e == id[0]) {                                                      // taken
             key[0] = key[1]; key[1] = key[2]; key[2] = key[3]; key[3] = 0u;
             id[0] = id[1]; id[1] = id[2]; id[2] = id[3]; id[3] = 0x7FFFFFFF;

@@ -386,7 +386,8 @@ static int expert_ffn(saem_ctx* c, int layer, const void* x_packed, const int32_
     a.slot_bytes = c->slot_bytes;
     a.slot_region_bytes = c->slot_bytes * (size_t)(c->n_fixed_slots + c->cfg.temp_slots);
     a.h = (uint16_t*)(c->ws + c->lay.h);
-    a.tokens = (max_rows + g.top_k + g.n_shared - 1) / (g.top_k + g.n_shared);
+    a.per_token = g.top_k + g.n_shared;
+    a.tokens = (max_rows + a.per_token - 1) / a.per_token;
     a.y_packed = y_packed;
     a.status = (int*)(c->ws + c->lay.status);
     a.counters = (int*)(c->ws + c->lay.counters);

@@ -136,7 +136,7 @@ struct FfnArgs {
     size_t slot_bytes;
     size_t slot_region_bytes;   // whole region (every slot)
     uint16_t* h;                // [max_rows, f] bf16 workspace
-    int tokens;                 // tokens of a step with max_rows rows (SAEM_FFN_MX: sizes the row tiles)
+    int tokens, per_token;      // tokens of a step with max_rows rows, rows per token (SAEM_FFN_MX: sizes the row tiles)
     float* y_packed;            // [max_rows, d]
     int* status;
     int* counters;              // [2 * kMaxCtas + 16]

@@ -333,6 +333,61 @@ def test_cache_calls_with_small_slots(T):
     layer.close()
 
 
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("E,k,T", [(128, 8, 8), (97, 5, 3), (20, 8, 8), (8, 2, 7), (1, 1, 2), (33, 1, 8), (64, 6, 40), (16, 12, 20)])
+def test_the_step_routes_as_saem_route_does(E, k, T, renorm):
+    """Ties, zeros of both signs, infinities and NaN among the logits: the same experts, and the same weights to the bit."""
+    from paper_2608_21614_b200 import binding as B, mx
+    from paper_2608_21614_b200.layer import MoELayer
+    rng = np.random.default_rng(E * k + T)
+    layer = MoELayer(128, 128, E, k, T, ffn_path=B.SAEM_FFN_MX, renorm=renorm)
+    q = [mx.quantize(torch.randn(128, 128, device="cuda")) for _ in range(3)]
+    for e in range(E):
+        layer.load_expert_mx(0, e, e, *q)
+    logits = np.round(rng.standard_normal((T, E)) * 2).astype(np.float32) / 2
+    odd = [0.0, -0.0, np.inf, -np.inf, np.nan, 1.0, 1.0]
+    for t in range(T):
+        logits[t, rng.integers(0, E, 3)] = rng.choice(odd, 3)
+    logits[0] = -np.inf
+    if T > 2:
+        logits[1], logits[2] = np.nan, 0.0
+    logits = torch.from_numpy(logits).cuda()
+    x = torch.randn(T, 128, device="cuda").to(torch.bfloat16)
+    out = torch.empty(T, 128, device="cuda")
+    layer.step_fused_call(logits, x, T, out)
+    idx = layer.ctx.step_tensor(0, (T, k), torch.int32).clone()
+    w = layer.ctx.step_tensor(1, (T, k), torch.float32).clone()
+    layer.route(logits, T)
+    assert torch.equal(idx, layer.topk_idx[:T]) and torch.equal(w, layer.topk_w[:T])
+    assert layer.device_status() == 0
+    layer.close()
+
+
+def test_expert_ffn_of_one_expert_without_offsets():
+    from paper_2608_21614_b200 import binding as B
+    layer, exact, rng = build(256, 384, 1, 1, 70)
+    x = torch.from_numpy(rng.standard_normal((70, 256)).astype(np.float32)).cuda().to(torch.bfloat16)
+    for rows in (1, 8, 33, 70):
+        y = torch.full((70, 256), 7.0, device="cuda")
+        B.saem_expert_ffn(layer.ctx.handle, 0, x, None, rows, None, y)
+        hid = ref.silu(f64(x)[:rows] @ exact[0][0].T) * (f64(x)[:rows] @ exact[1][0].T)
+        assert (np.abs(f64(y)[:rows] - hid @ exact[2][0].T) <= 2.0 ** -11 * (np.abs(hid) @ np.abs(exact[2][0]).T)).all()
+        assert (y[rows:] == 7).all()
+    layer.close()
+
+
+def test_all_rows_on_one_expert_of_many():
+    """Segments far longer than the average that the row tiles are made for, and a long batch."""
+    layer, exact, rng = build(128, 256, 32, 2, 300)
+    x = torch.from_numpy(rng.standard_normal((300, 128)).astype(np.float32)).cuda().to(torch.bfloat16)
+    logits = torch.from_numpy(rng.standard_normal((300, 32)).astype(np.float32)).cuda()
+    logits[:, 7] += 20
+    logits[:250, 30] += 10
+    for T in (300, 129, 64, 11):
+        check_step(layer, exact, logits[:T].contiguous(), x[:T].contiguous(), T)
+    layer.close()
+
+
 def test_subset_leaves_other_rows_alone():
     from paper_2608_21614_b200 import binding as B
     layer, exact, rng = build(256, 256, 4, 2, 10)

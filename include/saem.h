@@ -87,11 +87,11 @@ enum { SAEM_GATE_NONE = 0, SAEM_GATE_TOKEN = 1, SAEM_GATE_CHANNEL = 2, SAEM_GATE
  * (3 * d_model * d_ff * 2 bytes) and numerous enough (see saem_moe_step).
  * SAEM_FFN_MX: the slots hold experts in the microscaled 4-bit format (see saem_mx_quantize): 3 * d_model * d_ff *
  * 17/32 bytes per slot instead of 3 * d_model * d_ff * 2 (rows padded to multiples of 256 elements), packed by
- * saem_mx_pack_expert (device) or saem_pack_expert_host (which then quantises).  Activations are not rounded to 4 bits: x is
- * held to 2^-14 of the largest of 32 neighbours at worst (exactly in the form for up to 8 tokens) and so are the hidden
- * activations (11 bits of each there).  saem_moe_step takes up to 8 tokens (top_k <= 8, T * d_model <= 32768, no
- * shared_ctx) in two launches, which leave topk_idx and topk_w but none of the other intermediates in the workspace.  All step
- * and cache calls take such a context except saem_cache_map_host (UNSUPPORTED).
+ * saem_mx_pack_expert (device) or saem_pack_expert_host (which then quantises).  Activations are not rounded to 4 bits: x and
+ * the hidden activations are held to 2^-13.8 of the largest of 32 neighbours at worst.  saem_moe_step takes up to 8 tokens
+ * (top_k <= 8, d_model <= 4096, no shared_ctx) in two launches, which leave topk_idx and topk_w but none of the other
+ * intermediates in the workspace; beyond that it leaves all but x_packed, and h in a form of its own.  All step and cache calls
+ * take such a context except saem_cache_map_host (UNSUPPORTED).
  * n_shared (0..16, n_experts + n_shared <= SAEM_MAX_EXPERTS): always-on shared experts of the same
  * width d_ff that run INSIDE the layer's grouped launch.  They are experts n_experts ..
  * n_experts + n_shared - 1 of every layer for the cache calls (outside the routed cache-ratio
@@ -260,7 +260,7 @@ int saem_moe_step_host_async(saem_ctx* ctx, saem_ctx* shared_ctx, int layer, con
  * kernels' CTAs meet (arrivals at items whose reduction is split across CTAs; per expert, the hidden
  * activations completed by the gate/up launch and seen by the down launch, the down launch's item
  * counter): all zero between calls.  NULL for an unknown id.  The one-launch form of
- * the step (see saem_moe_step) does not produce x_packed. */
+ * the step (see saem_moe_step) does not produce x_packed, nor does a SAEM_FFN_MX context (see saem_config). */
 void* saem_step_buffer(saem_ctx* ctx, int which);
 
 /*

@@ -60,19 +60,6 @@ __device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8]) {
         : "=r"(w) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return w;
 }
-// The four scales of a word as floats: 2^(s - 127), NaN for 255.  bf16 holds every one of them, 2^-127 included.
-__device__ __forceinline__ void mx_scales4(uint32_t w, float (&s)[4]) {
-    uint32_t lo, hi;
-    asm("{\n\t.reg .b16 a, b;\n\t"
-        "mov.b32 {a, b}, %2;\n\t"
-        "cvt.rn.bf16x2.ue8m0x2 %0, a;\n\t"
-        "cvt.rn.bf16x2.ue8m0x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi) : "r"(w));
-    s[0] = __uint_as_float(lo << 16);
-    s[1] = __uint_as_float(lo & 0xFFFF0000u);
-    s[2] = __uint_as_float(hi << 16);
-    s[3] = __uint_as_float(hi & 0xFFFF0000u);
-}
 // Scale byte of a block whose largest magnitude has these fp32 bits: floor(log2) - 2, so that the largest element
 // lands in [4, 8) and saturates at 6 at worst; 255 if it is not finite.
 __device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits) {

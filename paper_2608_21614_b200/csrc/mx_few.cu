@@ -10,7 +10,9 @@
 // column is a token whatever the expert: x's tile stays in shared memory for all items, the second launch's k axis runs
 // over all active experts, and the merge over a token's experts costs nothing because h carries the gate weight.  (The
 // same two launches with mma.sync, the weights converted to f16, were bound by instruction issue: 50 us for 8 tokens of a
-// 2048 x 768 layer of 128 experts.)
+// 2048 x 768 layer of 128 experts against 26.5 us, 93 MB at 3.5 TB/s.)  One token takes 14 us: routing 1.7 us, the first
+// weights' way 1 us, the products 2.5 us, their sums and planes of h 2 us, the hand-over 1.2 us, the down projection with the
+// cluster's sum 3 us, and the two launches.
 #include "mx_planes.cuh"
 #include "route_row.cuh"
 

@@ -7,13 +7,19 @@
 // consecutive n.  A stage is 256 elements of k: 128-byte rows of codes under the 128-byte swizzle (TMA) and the scales'
 // 512-byte pieces (plain bulk copies, moved to tensor memory by tcgen05.cp as they are).
 //
-// Two forms, by the number of tokens (measured side by side for n 2048 .. 14336 and k 1024, 4096).  More than 64:
-// mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the next tile's products (128 tokens of
-// 14336 x 4096: 12.2 us against 14.3 us).  Up to 64: mx_matmul_kernel, one CTA per tile, where the weights' bytes are the
-// bound and n / 128 tiles are too few for the SMs: the k range is then split over a cluster of 2 or 4 CTAs, whose sums meet
-// in distributed shared memory in a fixed order (16 tokens of 4096 x 4096: 5.3 us in four parts, 9 us in one; parts of
-// fewer than four stages, or eight parts, cost more than they give).  Up to 8 tokens the CTA quantises its part of the
-// activations itself.  Two runs give the same bits.
+// Three forms, by the number of tokens and tiles (measured side by side for n 2048 .. 14336 and k 1024, 4096; the product
+// alone unless it says otherwise).
+//   up to 64 tokens   mx_matmul_kernel, one CTA per tile, where the weights' bytes are the bound and n / 128 tiles are too
+//                     few for the SMs: the k range is then split over a cluster of 2 or 4 CTAs, whose sums meet in
+//                     distributed shared memory in a fixed order (16 tokens of 4096 x 4096: 5.3 us in four parts, 9 us in
+//                     one; parts of fewer than four stages, or eight parts, cost more than they give).  Up to 8 tokens the
+//                     CTA quantises its part of the activations itself.
+//   more              mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the next tile's
+//                     products (128 tokens of 14336 x 4096: 12.2 us against 14.3 us).
+//   many tiles        mx_matmul_pair_kernel, CTA pairs (cta_group::2) with tiles of 256 x 256, when these are at least half as
+//                     many as the SMs: each operand crosses shared memory half as often, which is what bounds the products
+//                     (8192 tokens of 14336 x 4096, quantisation included: 199 us, 4.8 PFLOP/s, against 255 us).
+// Two runs give the same bits.
 #include "mx_tc.cuh"
 
 namespace saem {

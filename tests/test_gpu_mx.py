@@ -2,9 +2,9 @@
 
 Quantisation, the way back and packing are exact.  A product's terms are exact too; its fp32 sum rounds once per MMA (64
 terms), by at most one unit in the last place of what has been summed so far: |error| <= (k / 64 + 8) 2^-23 sum |a w|,
-with 2^-8 of the result more for a bf16 output (half a unit of 8 significant bits).  The expert layer rounds the hidden
-activations to 11 bits: 2^-12 of |Wd| |h|, doubled for the fp32 sums on the way; what is below fp32's smallest numbers
-(2^-149 each, a sum of a few hundred of them) may vanish."""
+with 2^-8 of the result more for a bf16 output (half a unit of 8 significant bits).  The expert layer holds the
+activations to 2^-13.8 of the largest of 32 neighbours; the tests allow 2^-12 of |Wd| |h|, doubled for the fp32 sums on the
+way; what is below fp32's smallest numbers (2^-149 each, a sum of a few hundred of them) may vanish."""
 import numpy as np
 import pytest
 import torch

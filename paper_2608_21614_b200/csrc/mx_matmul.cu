@@ -7,15 +7,17 @@
 // consecutive n.  A stage is 256 elements of k: 128-byte rows of codes under the 128-byte swizzle (TMA) and the scales'
 // 512-byte pieces (plain bulk copies, moved to tensor memory by tcgen05.cp as they are).
 //
-// Three forms, by the number of tokens and tiles (measured side by side for n 2048 .. 14336 and k 1024, 4096; the product
+// Three forms, by the number of tokens and tiles (measured side by side for n 1024 .. 14336 and k 1024 .. 4096; the product
 // alone unless it says otherwise).
-//   up to 64 tokens   mx_matmul_kernel, one CTA per tile, where the weights' bytes are the bound and n / 128 tiles are too
-//                     few for the SMs: the k range is then split over a cluster of 2 or 4 CTAs, whose sums meet in
-//                     distributed shared memory in a fixed order (16 tokens of 4096 x 4096: 5.3 us in four parts, 9 us in
-//                     one; parts of fewer than four stages, or eight parts, cost more than they give).  Up to 8 tokens the
-//                     CTA quantises its part of the activations itself.
+//   few tiles         mx_matmul_kernel, one CTA per tile of 128 x 64 (or fewer tokens), up to 64 tokens always and beyond while
+//                     all tiles are under way at once, two per SM (333 tokens of 2563 x 1500: 6.8 us against 10.8 us in tiles
+//                     of 256 tokens; 512 of 4096 x 4096 10.6 us against 10.8 us).  The weights' bytes and the latency of one tile
+//                     are the bound, so the k range is split over a cluster of 2 or 4 CTAs while there are SMs for them;
+//                     their sums meet in distributed shared memory in a fixed order (16 tokens of 4096 x 4096: 5.3 us
+//                     in four parts, 9 us in one; parts of fewer than four stages, or eight parts, cost more than they
+//                     give).  Up to 8 tokens the CTA quantises its part of the activations itself.
 //   more              mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the next tile's
-//                     products (128 tokens of 14336 x 4096: 12.2 us against 14.3 us).
+//                     products.
 //   many tiles        mx_matmul_pair_kernel, CTA pairs (cta_group::2) with tiles of 256 x 256, when these are at least half as
 //                     many as the SMs: each operand crosses shared memory half as often, which is what bounds the products
 //                     (8192 tokens of 14336 x 4096, quantisation included: 199 us, 4.8 PFLOP/s, against 255 us).
@@ -39,7 +41,7 @@ struct MmArgs {
     int* status;
     long long out_stride;
     int m, n, k;
-    int n_tile;                             // tokens, rounded up to 16 (one tile)
+    int n_tile;                             // tokens of a tile: all, rounded up to 16, or 64 or 128
     int n_stage;                            // stages of the ring
     int stage_bytes;
     int tmem_cols;
@@ -62,7 +64,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
-    const int n0 = blockIdx.y * 128, tokens = p.m, n_mma = p.n_tile;
+    const int n0 = blockIdx.y * 128, t0 = blockIdx.z * p.n_tile, tokens = min(p.n_tile, p.m - t0), n_mma = p.n_tile;
     const long long kp = (p.k + kMxBlock - 1) / kMxBlock * kMxBlock;        // padded with zeros to whole blocks
     const int n_span = (p.k + kMxSpan - 1) / kMxSpan;
     const int all = (int)((kp + kMmStageK - 1) / kMmStageK);
@@ -105,8 +107,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             const uint32_t st = base + i * p.stage_bytes, bar = smem_u32(&bar_full[i]);
             const int spans = min(2, n_span - 2 * s);
             if (p.x) return;
-            tma_2d_on(on, st + w_bytes, &map_a, s * 128, 0, bar);
-            bulk_g2s_on(on, st + w_bytes + a_bytes + 2 * kMxPiece, p.a_scales + (size_t)2 * s * kMxPiece, spans * kMxPiece, bar);
+            tma_2d_on(on, st + w_bytes, &map_a, s * 128, t0, bar);
+            bulk_g2s_on(on, st + w_bytes + a_bytes + 2 * kMxPiece, p.a_scales + ((size_t)(t0 / 128) * n_span + 2 * s) * kMxPiece, spans * kMxPiece, bar);
         };
         const int early = p.w_early ? min(p.n_stage, s1 - s0) : 0;
         for (int i = 0; i < early; ++i) w_part(s0 + i, i);
@@ -133,6 +135,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
         const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base);
+        const int half = t0 % 128 / 32;                                      // the second half of a piece: two columns on
         int st = 0, turn = 0;
         for (int s = s0; s < s1; ++s) {
             if (!mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, status)) break;
@@ -148,7 +151,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             for (int j = 0; j < 4; ++j)
                 if (j < steps)
                     tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
-                                ta + 4 * (j >> 1), s > s0 || j > 0);
+                                ta + 4 * (j >> 1) + half, s > s0 || j > 0);
             tc_commit_on(on, smem_u32(&bar_empty[st]));
             if (++st == p.n_stage) { st = 0; ++turn; }
         }
@@ -193,7 +196,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const int quad = warp & 3, row = quad * 32 + lane;
     const bool store_row = n0 + row < p.n;
     auto put = [&](int c, float v) {
-        const size_t at = (size_t)c * p.out_stride + n0 + row;
+        const size_t at = (size_t)(t0 + c) * p.out_stride + n0 + row;
         if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
         else static_cast<float*>(p.out)[at] = v;
     };
@@ -607,12 +610,15 @@ struct MmPlan {
 };
 static MmPlan mm_plan(int m, int n, int k, int n_sm) {
     MmPlan p = {};
-    p.big = m > 64;
+    const long long rows = (n + 127) / 128;
+    const int stages = (k + kMmStageK - 1) / kMmStageK;
     // every pair of SMs has a tile of 256 x 256 at least
-    p.pairs = p.big && (long long)((n + 255) / 256) * ((m + 255) / 256) >= n_sm / 2;
+    p.pairs = m > 64 && (long long)((n + 255) / 256) * ((m + 255) / 256) >= n_sm / 2;
+    // 64 tokens at a time while all tiles are under way at once
+    p.big = p.pairs || (m > 64 && rows * ((m + 63) / 64) > 2 * n_sm);
     if (p.big) return p;
-    const int tiles = (n + 127) / 128, stages = (k + kMmStageK - 1) / kMmStageK;
-    p.n_tile = round_up(m, 16);
+    p.n_tile = m <= 64 ? round_up(m, 16) : 64;
+    const int tiles = (int)rows * ((m + p.n_tile - 1) / p.n_tile);
     p.stage_bytes = 128 * 128 + p.n_tile * 128 + 4 * kMxPiece;
     p.split = 1;
     while (p.split < 4 && tiles * p.split * 2 <= n_sm && stages >= 8 * p.split) p.split *= 2;
@@ -672,7 +678,7 @@ static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t*
     attr[1].val.clusterDim.x = p.split;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.split, (p.n + 127) / 128);
+    cfg.gridDim = dim3(p.split, (p.n + 127) / 128, (p.m + p.n_tile - 1) / p.n_tile);
     cfg.blockDim = dim3(kMmThreads);
     cfg.dynamicSmemBytes = 1024 + (p.split > 1 && sums > ring ? sums : ring);
     cfg.stream = st;

@@ -48,7 +48,7 @@ class SaemError(RuntimeError):
 
 def _load() -> C.CDLL:
     path = _build.LIB
-    if not os.path.exists(path) or _build.stale():
+    if _build.stale():
         path = _build.build()           # raises if nvcc is missing or the build fails
     lib = C.CDLL(path)
     vp, i32, i64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t

@@ -1,14 +1,18 @@
-"""Builds libsaem.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libsaem.so (the C-ABI CUDA library, nvcc for sm_100a) and _host_calls.so (its inner-loop calls for Python) in-tree."""
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libsaem.so")
+HOST_LIB = os.path.join(_HERE, "_host_calls.so")
+HOST_SOURCE = os.path.join(CSRC, "host_calls.cpp")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
          "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -19,12 +23,33 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
-def stale() -> bool:
-    if not os.path.exists(LIB):
+def _older(lib, deps) -> bool:
+    if not os.path.exists(lib):
         return True
-    t = os.path.getmtime(LIB)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(_ROOT, "include", "*.h"))
+    t = os.path.getmtime(lib)
     return any(os.path.getmtime(p) > t for p in deps)
+
+
+def _headers():
+    return glob.glob(os.path.join(_ROOT, "include", "*.h"))
+
+
+def stale() -> bool:
+    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + _headers()
+    return _older(LIB, deps) or _older(HOST_LIB, [HOST_SOURCE] + _headers())
+
+
+def _build_host_calls() -> None:
+    """_host_calls.so, linked to the libsaem.so beside it and to torch."""
+    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    include = [os.path.join(_ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(torch_dir, "include"),
+               os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+    tmp = HOST_LIB + ".tmp%d" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *["-I" + p for p in include], HOST_SOURCE,
+                           "-o", tmp, "-L", os.path.join(torch_dir, "lib"), "-L", _HERE, "-l:" + os.path.basename(LIB), "-ltorch_python",
+                           "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, HOST_LIB)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -51,6 +76,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([NVCC, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", tmp, *objs])
     os.replace(tmp, LIB)
+    _build_host_calls()
     return LIB
 
 

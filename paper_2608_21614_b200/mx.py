@@ -10,6 +10,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
+from . import _host_calls as _calls     # behind binding, which builds it if need be
 
 _DTYPE = {torch.float32: B.SAEM_OUT_F32, torch.bfloat16: B.SAEM_OUT_BF16}
 
@@ -59,9 +60,11 @@ def empty(rows: int, cols: int, device="cuda") -> MxTensor:
 def quantize(x: torch.Tensor, out: Optional[MxTensor] = None, stream=None) -> MxTensor:
     """x [rows, cols] float32 or bfloat16 to the microscaled format."""
     if out is None:
-        _matrix(x, "quantize")
+        _dtype(x), _matrix(x, "quantize")
         out = empty(x.shape[0], x.shape[1], x.device)
-    B.saem_mx_quantize(x, _dtype(x), out.rows, out.cols, _matrix(x, "quantize", out.rows, out.cols), out.codes, out.scales, stream)
+    code = _calls.quantize(x, out.rows, out.cols, out.codes, out.scales, stream)
+    if code:
+        raise B.SaemError(code, "quantize")
     return out
 
 
@@ -69,7 +72,9 @@ def dequantize(q: MxTensor, out: Optional[torch.Tensor] = None, dtype: torch.dty
     """The values a quantised matrix stands for, as float32 or bfloat16 (exact in both)."""
     if out is None:
         out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.device)
-    B.saem_mx_dequantize(q.codes, q.scales, q.rows, q.cols, out, _dtype(out), _matrix(out, "dequantize", q.rows, q.cols), stream)
+    code = _calls.dequantize(q.codes, q.scales, q.rows, q.cols, out, stream)
+    if code:
+        raise B.SaemError(code, "dequantize")
     return out
 
 
@@ -80,8 +85,9 @@ def matmul(a: MxTensor, w: MxTensor, out: Optional[torch.Tensor] = None, dtype: 
         raise B.SaemError(B.SAEM_ERR_SHAPE, "matmul")
     if out is None:
         out = torch.empty(a.rows, w.rows, dtype=dtype, device=a.device)
-    B.saem_mx_matmul(a.codes, a.scales, a.rows, w.codes, w.scales, w.rows, w.cols, out, _dtype(out),
-                     _matrix(out, "matmul", a.rows, w.rows), status, stream)
+    code = _calls.matmul(a.codes, a.scales, a.rows, w.codes, w.scales, w.rows, w.cols, out, status, stream)
+    if code:
+        raise B.SaemError(code, "matmul")
     return out
 
 
@@ -99,14 +105,12 @@ class Linear:
     def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
                  stream=None) -> torch.Tensor:
         """x [m, k] float32 or bfloat16 -> [m, n]."""
-        w, ws = self.weight, self.workspace
-        m = x.shape[0]
-        if m > self.max_rows:
-            raise B.SaemError(B.SAEM_ERR_SHAPE, "Linear")
+        w = self.weight
         if out is None:
-            out = torch.empty(m, w.rows, dtype=dtype, device=x.device)
-        B.saem_mx_linear(x, _dtype(x), m, _matrix(x, "Linear", m, w.cols), w.codes, w.scales, w.rows, w.cols, out, _dtype(out),
-                         _matrix(out, "Linear", m, w.rows), ws, ws.numel(), stream)
+            out = torch.empty(x.shape[0], w.rows, dtype=dtype, device=x.device)
+        code = _calls.linear(x, w.codes, w.scales, w.rows, w.cols, out, self.workspace, self.max_rows, stream)
+        if code:
+            raise B.SaemError(code, "Linear")
         return out
 
     def device_status(self) -> int:

@@ -6,7 +6,8 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from .mx import _dtype, _matrix
+from . import _host_calls as _calls     # behind binding, which builds it if need be
+from .mx import _dtype
 
 _GATES = {"none": B.SAEM_GATE_NONE, "token": B.SAEM_GATE_TOKEN, "channel": B.SAEM_GATE_CHANNEL, "full": B.SAEM_GATE_FULL}
 
@@ -30,47 +31,30 @@ class BlockNorm:
             raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm weights of one type are wanted")
         self.d, self.w_post, self.w_pre = d, w_post, w_pre
         w = w_post if w_post is not None else w_pre
-        self._cfg = B.saem_norm_config(cols=d, w_dtype=B.SAEM_OUT_F32 if w is None else _dtype(w), gate_mode=_GATES[gate],
-                                       gate_sigmoid=int(gate_sigmoid), eps=eps, residual_scale=residual_scale,
-                                       branch_scale=branch_scale)
-
-    def _call(self, c, x, y, gate, w_post, w_pre, x_out, n_out, stream):
-        T, d = x.shape[0], self.d
-        c.rows, c.x_dtype, c.x_stride = T, _dtype(x), _matrix(x, "BlockNorm", T, d)
-        if y is not None:
-            c.y_dtype, c.y_stride, c.x_out_stride = _dtype(y), _matrix(y, "BlockNorm", T, d), _matrix(x_out, "BlockNorm", T, d)
-        if n_out is not None:
-            c.n_dtype, c.n_stride = _dtype(n_out), _matrix(n_out, "BlockNorm", T, d)
-        B.saem_block_norm(c, x, y, gate, w_post, w_pre, x_out, n_out, stream)
+        c = B.saem_norm_config(cols=d, w_dtype=B.SAEM_OUT_F32 if w is None else _dtype(w), gate_mode=_GATES[gate],
+                               gate_sigmoid=int(gate_sigmoid), eps=eps, residual_scale=residual_scale, branch_scale=branch_scale)
+        self._leave = bytes(c)              # rows, types and strides are the tensors'
+        c.gate_mode = B.SAEM_GATE_NONE
+        self._enter = bytes(c)
 
     def enter(self, x: torch.Tensor, n_out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
               stream=None) -> torch.Tensor:
         """The first block's input: n of x itself."""
         if n_out is None:
             n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
-        c = B.saem_norm_config.from_buffer_copy(self._cfg)
-        c.gate_mode = B.SAEM_GATE_NONE
-        self._call(c, x, None, None, None, self.w_pre, None, n_out, stream)
+        code = _calls.block_norm(self._enter, x, None, None, None, self.w_pre, None, n_out, stream)
+        if code:
+            raise B.SaemError(code, "BlockNorm")
         return n_out
 
     def leave(self, x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None,
               n_out: Optional[torch.Tensor] = None, next_norm: bool = True, dtype: torch.dtype = torch.bfloat16, stream=None):
-        """(x', n) after a block whose output is y; x_out may be x.  `next_norm` False: x' only (n is None)."""
-        c = self._cfg
+        """(x', n) after a block whose output is y; x_out (x's type) may be x.  `next_norm` False: x' only (n is None)."""
         if x_out is None:
             x_out = torch.empty(x.shape[0], self.d, dtype=x.dtype, device=x.device)
-        elif x_out.dtype is not x.dtype:
-            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: x_out has x's type")
         if n_out is None and next_norm:
             n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
-        if gate is not None:
-            T = x.shape[0]
-            c.gate_dtype, mode, shape = _dtype(gate), c.gate_mode, gate.shape
-            if mode == B.SAEM_GATE_FULL:
-                c.gate_stride = _matrix(gate, "BlockNorm gate", T, self.d)
-            elif mode == B.SAEM_GATE_TOKEN and shape in ((T,), (T, 1)):
-                c.gate_stride = gate.stride(0)
-            elif not (mode == B.SAEM_GATE_CHANNEL and shape in ((self.d,), (1, self.d)) and (self.d == 1 or gate.stride(-1) == 1)):
-                raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm gate")
-        self._call(c, x, y, gate, self.w_post, self.w_pre if n_out is not None else None, x_out, n_out, stream)
+        code = _calls.block_norm(self._leave, x, y, gate, self.w_post, self.w_pre if n_out is not None else None, x_out, n_out, stream)
+        if code:
+            raise B.SaemError(code, "BlockNorm")
         return x_out, n_out

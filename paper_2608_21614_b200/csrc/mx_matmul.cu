@@ -10,12 +10,13 @@
 // Three forms, by the number of tokens and tiles (measured side by side for n 1024 .. 14336 and k 1024 .. 4096; the product
 // alone unless it says otherwise).
 //   few tiles         mx_matmul_kernel, one CTA per tile of 128 x 64 (or fewer tokens), up to 64 tokens always and beyond while
-//                     all tiles are under way at once, two per SM (333 tokens of 2563 x 1500: 6.8 us against 10.8 us in tiles
-//                     of 256 tokens; 512 of 4096 x 4096 10.6 us against 10.8 us).  The weights' bytes and the latency of one tile
+//                     all tiles are under way at once, two per SM (333 tokens of 2563 x 1500: 5.5 us against 10.8 us in tiles
+//                     of 256 tokens; 512 of 4096 x 4096 9.8 us against 10.8 us).  The weights' bytes and the latency of one tile
 //                     are the bound, so the k range is split over a cluster of 2 or 4 CTAs while there are SMs for them;
 //                     their sums meet in distributed shared memory in a fixed order (16 tokens of 4096 x 4096: 5.3 us
 //                     in four parts, 9 us in one; parts of fewer than four stages, or eight parts, cost more than they
-//                     give).  Up to 8 tokens the CTA quantises its part of the activations itself.
+//                     give).  Up to 8 tokens the CTA quantises its part of the activations itself, if the parts fit into
+//                     the ring (16 tokens of 14336 x 4096 that way: 24 us against 9.7 us, quantisation launch included).
 //   more              mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the next tile's
 //                     products.
 //   many tiles        mx_matmul_pair_kernel, CTA pairs (cta_group::2) with tiles of 256 x 256, when these are at least half as
@@ -26,7 +27,7 @@
 
 namespace saem {
 
-constexpr int kMmThreads = 192;             // warp 0: copies, warp 1: MMA issue, warps 2-5: quantisation, epilogue
+constexpr int kMmThreads = 320;             // warp 0: copies, warp 1: MMA issue, warps 2-9: quantisation, epilogue
 constexpr int kMmStageK = 256;              // elements of k per stage (128 bytes of codes)
 constexpr int kMmMaxStages = 12;
 constexpr int kMmSmem = 226 * 1024;         // dynamic shared memory at most
@@ -74,7 +75,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.n_stage; ++i) {
-            mbar_init(smem_u32(&bar_full[i]), p.x ? 5 : 1);
+            mbar_init(smem_u32(&bar_full[i]), p.x ? 9 : 1);
             mbar_init(smem_u32(&bar_empty[i]), 1);
         }
         mbar_init(smem_u32(&bar_acc), 1);
@@ -128,8 +129,9 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         if (!ok && lane == 0)                                                // copies still under way land before the CTA ends
             for (int q = max(s0, s - p.n_stage); q < s; ++q) {
                 abort_flag = 0;
-                mbar_wait(smem_u32(&bar_full[(q - s0) % p.n_stage]), ((q - s0) / p.n_stage) & 1, abort_p, status);
+                const bool landed = mbar_wait(smem_u32(&bar_full[(q - s0) % p.n_stage]), ((q - s0) / p.n_stage) & 1, abort_p, status);
                 abort_flag = 1;
+                if (!landed) break;                                          // seconds later: nothing is under way any more
             }
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
@@ -158,42 +160,36 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         tc_commit_on(on, smem_u32(&bar_acc));
     } else if (p.x) {
         // ---------------------------------------------------------------- quantisation of the CTA's part of A
+        // (stage, row) pairs go to the eight warps in turn, so that a few tokens' loads are under way together as well
         pdl_wait();
         uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
         const size_t esize = p.x_bf16 ? 2 : 4;
-        for (int s = s0; s < s1; ++s) {
-            uint8_t* st = smem + (size_t)(s - s0) * p.stage_bytes + w_bytes;
-            const long long col = (long long)s * kMmStageK + lane * 8;
-            float v[2][8];                                                   // p.m <= 8: two rows per warp at most
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int r = warp - 2 + 4 * u;
+        for (int i = 0; i < s1 - s0; ++i) {
+            const int r = (warp - 2 - i * p.m) & 7;                          // p.m <= 8: a row at most
+            if (r < p.m) {
+                uint8_t* st = smem + (size_t)i * p.stage_bytes + w_bytes;
+                const long long col = (long long)(s0 + i) * kMmStageK + lane * 8;
                 const void* row = static_cast<const uint8_t*>(p.x) + (size_t)r * p.x_stride * esize;
-                if (r >= p.m) break;
-                if (p.x_bf16) { if (p.x_vec) load8<true, true>(row, col, p.k, v[u]); else load8<true, false>(row, col, p.k, v[u]); }
-                else { if (p.x_vec) load8<false, true>(row, col, p.k, v[u]); else load8<false, false>(row, col, p.k, v[u]); }
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int r = warp - 2 + 4 * u;
-                if (r >= p.m) break;
+                float v[8];
+                if (p.x_bf16) { if (p.x_vec) load8<true, true>(row, col, p.k, v); else load8<true, false>(row, col, p.k, v); }
+                else { if (p.x_vec) load8<false, true>(row, col, p.k, v); else load8<false, false>(row, col, p.k, v); }
                 int scale;
-                const uint32_t w = mx_quantize8(v[u], scale);
+                const uint32_t w = mx_quantize8(v, scale);
                 uint32_t word = (uint32_t)(col < kp ? scale : 0) << (((lane >> 2) & 3) * 8);
                 word |= __shfl_xor_sync(0xffffffffu, word, 4);
                 word |= __shfl_xor_sync(0xffffffffu, word, 8);
-                *reinterpret_cast<uint32_t*>(st + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = w;
-                if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(st + a_bytes + 2 * kMxPiece + (lane >> 4) * kMxPiece + r * 16) = word;   // r < 32
+                *reinterpret_cast<uint32_t*>(st + r * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4) = w;
+                if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(st + a_bytes + 2 * kMxPiece + (lane >> 4) * kMxPiece + r * 16) = word;
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_full[s - s0]));
+            if (lane == 0) mbar_arrive(smem_u32(&bar_full[i]));
         }
     }
     __syncwarp();
 
     // -------------------------------------------------------------------- epilogue
-    const int quad = warp & 3, row = quad * 32 + lane;
+    const int quad = warp & 3, group = (warp - 2) >> 2, row = quad * 32 + lane;   // two groups share the columns
     const bool store_row = n0 + row < p.n;
     auto put = [&](int c, float v) {
         const size_t at = (size_t)(t0 + c) * p.out_stride + n0 + row;
@@ -207,7 +203,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         tc_fence_after();
         pdl_wait();                                                          // nothing is written before older kernels have ended
         if (done)
-            for (int c = 0; c < n_mma; c += 16) {
+            for (int c = 16 * group; c < n_mma; c += 32) {
                 float v[16];
                 tc_ld16(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
                 if (p.split > 1) {
@@ -228,7 +224,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         __syncthreads();
         cluster_sync_all();
         if (warp >= 2 && done)
-            for (int c = rank * 4; c < tokens; c += 4 * p.split) {           // four columns at a time, the parts in order
+            for (int c = (rank * 2 + group) * 4; c < tokens; c += 8 * p.split) {   // four columns at a time, the parts in order
                 float4 v[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)

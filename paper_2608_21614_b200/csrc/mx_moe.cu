@@ -92,17 +92,24 @@ mx_tile_kernel(const uint16_t* __restrict__ x, const int32_t* __restrict__ inv_p
                int S, int E, int K, int most, uint8_t* __restrict__ tiles, int* __restrict__ status) {
     using Ts = TileShape<R>;
     __shared__ Segments s;
+    const int lane = threadIdx.x & 31, nc = mx_chunks(K);
+    const long long total = (long long)T * nc, first = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    uint32_t codes[kPlanes], scales[kPlanes];
+    auto split = [&](long long i) {
+        const int t = (int)(i / nc), col = (int)(i - (long long)t * nc) * kMxChunk + lane * 8;
+        float v[8];
+        widen8(col < K ? *reinterpret_cast<const uint4*>(x + (size_t)t * K + col) : make_uint4(0u, 0u, 0u, 0u), v);
+        split_planes(v, lane, codes, scales);
+    };
+    // Within a step x is older than the launch before this one (the routing): the first planes are made while that ends.
+    const bool early = inv_perm != nullptr;
+    if (early && first < total) split(first);
     pdl_wait();
     pdl_launch_dependents();
     read_segments<R>(s, offsets, E, T * (k + S), most, status);
-    const int lane = threadIdx.x & 31, nc = mx_chunks(K);
-    const long long total = (long long)T * nc;
-    for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < total; i += (long long)gridDim.x * 8) {
-        const int t = (int)(i / nc), c = (int)(i - (long long)t * nc), col = c * kMxChunk + lane * 8;
-        float v[8];
-        widen8(col < K ? *reinterpret_cast<const uint4*>(x + (size_t)t * K + col) : make_uint4(0u, 0u, 0u, 0u), v);
-        uint32_t codes[kPlanes], scales[kPlanes];
-        split_planes(v, lane, codes, scales);
+    for (long long i = first; i < total; i += (long long)gridDim.x * 8) {
+        const int t = (int)(i / nc), c = (int)(i - (long long)t * nc);
+        if (!early || i != first) split(i);
         for (int j0 = 0; j0 < k + S; j0 += 32) {
             int place = -1;                                                  // tile * R + row of the tile, of this lane's copy
             const int j = j0 + lane;

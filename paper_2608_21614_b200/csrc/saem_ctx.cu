@@ -542,7 +542,7 @@ int saem_moe_step(saem_ctx* c, saem_ctx* sh, int layer, const float* logits, con
         int* status = (int*)(w + L.status);
         int nl = 1;
         if (route_index_supported(T, g.top_k)) {
-            CUDA_TRY(launch_route_index(logits, T, g.n_experts, g.n_shared, g.top_k, g.renorm, idx, tw, counts, offsets, perm, inv, status, st));
+            CUDA_TRY(launch_route_index(logits, T, g.n_experts, g.n_shared, g.top_k, g.renorm, idx, tw, counts, offsets, perm, inv, st));
         } else {
             if ((s = saem_route(c, logits, T, idx, tw, stream)) != SAEM_OK) return s;
             CUDA_TRY(launch_repack(idx, nullptr, T, g.n_experts, g.n_shared, g.top_k, g.d_model, counts, offsets, perm, inv, nullptr, status,

@@ -161,7 +161,7 @@ cudaError_t launch_mx_ffn(const FfnArgs& a, const MxTokens& x, const SlotTable& 
 constexpr int kRouteIndexTokens = 64;
 bool route_index_supported(int T, int k);
 cudaError_t launch_route_index(const float* logits, int T, int E, int S, int k, int renorm, int32_t* idx, float* w, int32_t* counts,
-                               int32_t* offsets, int32_t* perm, int32_t* inv_perm, int* status, cudaStream_t st);
+                               int32_t* offsets, int32_t* perm, int32_t* inv_perm, cudaStream_t st);
 // The whole step over such experts for up to 8 tokens in two launches (mx_few.cu).
 struct MxFewArgs {
     const float* logits;        // [T, E]

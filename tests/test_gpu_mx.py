@@ -363,6 +363,26 @@ def test_the_step_routes_as_saem_route_does(E, k, T, renorm):
     layer.close()
 
 
+@pytest.mark.parametrize("E,k,T,S", [(16, 4, 9, 0), (64, 6, 33, 2), (128, 8, 64, 0), (20, 20, 51, 3), (1, 1, 64, 1), (128, 1, 32, 0)])
+def test_the_step_indexes_as_saem_repack_does(E, k, T, S):
+    from paper_2608_21614_b200 import binding as B, mx
+    from paper_2608_21614_b200.layer import MoELayer
+    layer = MoELayer(128, 128, E, k, T, d_ff_shared=128 * S, ffn_path=B.SAEM_FFN_MX)
+    q = [mx.quantize(torch.randn(128, 128, device="cuda")) for _ in range(3)]
+    for e in range(E + S):
+        layer.load_expert_mx(0, e, e, *q)
+    logits = torch.randn(T, E, device="cuda") + torch.linspace(0, 3, E, device="cuda")      # some experts stay empty
+    x = torch.randn(T, 128, device="cuda").to(torch.bfloat16)
+    layer.step_fused_call(logits, x, T, torch.empty(T, 128, device="cuda"))
+    got = [layer.ctx.step_tensor(which, (n,), torch.int32).clone() for which, n in ((2, E + S), (3, E + S + 1), (4, T * k), (5, T * k))]
+    layer.route(logits, T)
+    layer.repack(x, T)
+    for g, want in zip(got, (layer.counts, layer.offsets, layer.perm, layer.inv_perm)):
+        assert torch.equal(g, want[:len(g)])
+    assert layer.device_status() == 0
+    layer.close()
+
+
 def test_expert_ffn_of_one_expert_without_offsets():
     from paper_2608_21614_b200 import binding as B
     layer, exact, rng = build(256, 384, 1, 1, 70)

@@ -1,14 +1,14 @@
 // The expert FFN over microscaled 4-bit experts for rows packed by expert (SAEM_FFN_MX contexts, more than 8 tokens):
 // h = silu(Wg x) * (Wu x), y = Wd h on the block-scaled tensor cores (tcgen05 kind::mxf4), which take the 4-bit weights out
 // of shared memory as they are.  (Converting them to f16 for mma.sync costs some 150 instructions per 1088 bytes, and that,
-// not DRAM, was the bound: 232 us against 123 us now for 16 tokens of a 4096 x 14336 layer of 8 experts.)
+// not DRAM, was the bound: 232 us against 120 us now for 16 tokens of a 4096 x 14336 layer of 8 experts.)
 //
 // The other operand has to be 4-bit too: the activations are split into five 4-bit planes (mx_planes.cuh), whose
 // accumulators are added in fp32 in the epilogue.  Prefill pays for it: five times the work at four times bf16's rate.
 //
-// Few rows per expert: the bound is the weights' bytes.  The step just named moves 749 MB, 6.1 TB/s over all its
-// launches; 61 tokens of a 2560 x 1536 layer of 64 + 2 experts take 89 us for 372 MB, of which the launches around the
-// products (gate and indices, tiles of x, combine) are some 15 us.  Many rows: 2048 tokens of a 2048 x 1408 layer of 64 + 2
+// Few rows per expert: the bound is the weights' bytes.  The step just named moves 749 MB, 6.2 TB/s over all its
+// launches; 61 tokens of a 2560 x 1536 layer of 64 + 2 experts take 87 us for 372 MB, of which the launches around the
+// products (gate and indices, tiles of x, combine) are some 13 us.  Many rows: 2048 tokens of a 2048 x 1408 layer of 64 + 2
 // experts take 534 us (bf16 slots: 375 us), bound by the planes' products.
 //
 // A tile is R (8, 16, 32) rows of one expert; an item is a tile x 128 hidden units (gate and up accumulators side by

@@ -220,7 +220,9 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         bool ok = mbar_wait_warp(smem_u32(&s.x), 0, abort_p, a.status);
         tc_fence_after();
         const uint32_t tmem_x = tmem_sf + n * 16;                              // x's scales stay in tensor memory for all items
-        for (int c = 0; c < nc && ok; ++c)
+        // The copies are waited for with the first item's sums, so a CTA without an item (the grid is made for as many active
+        // experts as there can be) starts none: nothing would hold back the end of its memory until they have landed.
+        for (int c = 0; c < nc && ok && (int)blockIdx.x < total; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h) tc_cp_scales(on, tmem_x + c * 8 + 4 * h, desc_at(xscales0, c * FewTile::kBytes + h * kMxPiece));
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x, ++k) {

@@ -65,8 +65,11 @@ class MoELayer:
         for m, rows, cols in ((gate, self.f, self.d), (up, self.f, self.d), (down, self.d, self.f)):
             if (m.rows, m.cols) != (rows, cols):
                 raise B.SaemError(B.SAEM_ERR_SHAPE, "load_expert_mx")
+            if m.codes.device != self.out.device or m.scales.device != self.out.device:
+                raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "load_expert_mx: matrices on %s are wanted" % self.out.device)
         packed = torch.empty(self.ctx.slot_bytes, dtype=torch.uint8, device=self.device)
-        B.saem_mx_pack_expert(self.cfg, gate.codes, gate.scales, up.codes, up.scales, down.codes, down.scales, packed)
+        with torch.cuda.device(self.device):
+            B.saem_mx_pack_expert(self.cfg, gate.codes, gate.scales, up.codes, up.scales, down.codes, down.scales, packed)
         self.copy_stream.wait_stream(torch.cuda.current_stream(self.device))
         packed.record_stream(self.copy_stream)
         B.saem_cache_load(self.ctx.handle, layer, expert, slot, packed, self.copy_stream)

@@ -97,6 +97,8 @@ class Linear:
     `max_rows` sizes the workspace; calls of one Linear must be ordered on the GPU (they share it)."""
 
     def __init__(self, weight: MxTensor, max_rows: int):
+        if not (weight.codes.is_cuda and weight.codes.device == weight.scales.device):
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "Linear: weights on one GPU are wanted")
         self.weight, self.max_rows = weight, max_rows
         self.workspace = torch.empty(max(256, B.saem_mx_linear_workspace_bytes(max_rows, weight.cols)), dtype=torch.uint8,
                                      device=weight.device)

@@ -37,6 +37,9 @@ class MxMoEStack:
         self.n_layers, E = len(experts), len(experts[0])
         f, d = experts[0][0][0].shape
         self.d, self.top_k, self.max_tokens = d, top_k, max_tokens
+        for r in routers:                       # read by address
+            if r.shape != (E, d) or r.dtype != torch.bfloat16 or not r.is_contiguous() or r.device != head.device or not r.is_cuda:
+                raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "MxMoEStack: routers [E, d] in bfloat16 on the GPU are wanted")
         self.layer = MoELayer(d, f, E, top_k, max_tokens, n_layers=self.n_layers, ffn_path=B.SAEM_FFN_MX)
         for l, layer in enumerate(experts):
             for e, matrices in enumerate(layer):

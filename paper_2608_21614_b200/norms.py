@@ -27,8 +27,12 @@ class BlockNorm:
         for w in (w_post, w_pre):
             if w is not None and (w.shape != (d,) or not w.is_contiguous()):
                 raise B.SaemError(B.SAEM_ERR_SHAPE, "BlockNorm weight")
-        if w_post is not None and w_pre is not None and w_post.dtype != w_pre.dtype:
-            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm weights of one type are wanted")
+            if w is not None and not w.is_cuda:
+                raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: weights on the GPU are wanted")
+        if w_post is not None and w_pre is not None and (w_post.dtype, w_post.device) != (w_pre.dtype, w_pre.device):
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: weights of one type on one GPU are wanted")
+        if gate not in _GATES:
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "BlockNorm: gate %r" % (gate,))
         self.d, self.w_post, self.w_pre = d, w_post, w_pre
         w = w_post if w_post is not None else w_pre
         c = B.saem_norm_config(cols=d, w_dtype=B.SAEM_OUT_F32 if w is None else _dtype(w), gate_mode=_GATES[gate],

@@ -689,7 +689,7 @@ decode_step_kernel(DecodeArgs a, const __grid_constant__ SlotTable tab, int phas
 bool decode_fused_supported(int T, int k) { return T >= 1 && T <= kDfMaxTokens && k <= kDfMaxK; }
 
 // mode per device: 0 not decided, 1 cooperative + programmatic serialization, 2 cooperative, 3 two launches
-static int g_mode[64];
+static std::atomic<int> g_mode[64];
 
 static cudaError_t launch_step(const DecodeArgs& a, const SlotTable& tab, int grid, cudaStream_t st, int phase_mask,
                                bool cooperative, bool pdl) {
@@ -720,16 +720,18 @@ cudaError_t launch_decode_fused(const DecodeArgs& a, const SlotTable& tab, int n
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    static bool attr_done[64];
-    if (first_call_on_device(attr_done)) {
-        e = cudaFuncSetAttribute(decode_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDfRingBytes);
-        if (e != cudaSuccess) return e;
+    static DeviceOnce once;
+    e = once_on_device(once, [dev] {
+        const cudaError_t s = cudaFuncSetAttribute(decode_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDfRingBytes);
+        if (s != cudaSuccess) return s;
         int coop = 0, per_sm = 0;
         if (cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev) != cudaSuccess) coop = 0;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, decode_step_kernel, kDfThreads, kDfRingBytes) != cudaSuccess)
             per_sm = 0;
-        g_mode[dev] = (coop && per_sm >= 1) ? 0 : 3;
-    }
+        if (!coop || per_sm < 1) g_mode[dev] = 3;
+        return cudaSuccess;
+    });
+    if (e != cudaSuccess) return e;
     const int grid = n_sm;                     // one CTA per SM
     if (g_mode[dev] == 0) {                    // first step on this device: find out what the driver accepts
         e = launch_step(a, tab, grid, st, 3, true, true);

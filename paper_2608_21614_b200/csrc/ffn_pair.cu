@@ -366,19 +366,18 @@ ffn_pair_kernel(FfnArgs a, const __grid_constant__ SlotTable tab, const __grid_c
 }
 
 // ------------------------------------------------------------------------------------------- host
-static bool g_pr_init[64];
+static DeviceOnce g_pr_once;
 
 cudaError_t launch_ffn_pair(const FfnArgs& a, const SlotTable& tab, const CUtensorMap& map_x, const CUtensorMap& map_h,
                             const CUtensorMap& map_x128, const CUtensorMap& map_h128, const CUtensorMap& map_w, const CUtensorMap& map_h_store, const CUtensorMap& map_y_store,
                             cudaStream_t st, int* n_launch) {
-    if (first_call_on_device(g_pr_init)) {
-        cudaError_t e = cudaFuncSetAttribute(ffn_pair_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
-        if (e != cudaSuccess) return e;
-        e = cudaFuncSetAttribute(ffn_pair_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
-        if (e != cudaSuccess) return e;
-    }
+    cudaError_t e = once_on_device(g_pr_once, [] {
+        const cudaError_t s = cudaFuncSetAttribute(ffn_pair_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
+        return s != cudaSuccess ? s : cudaFuncSetAttribute(ffn_pair_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPrSmem);
+    });
+    if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)(a.n_sm & ~1)), block(kPrThreads);
-    cudaError_t e = launch_pdl_pairs(ffn_pair_kernel<0>, grid, block, (size_t)kPrSmem, st, a, tab, map_x, map_x128, map_w, map_h_store);
+    e = launch_pdl_pairs(ffn_pair_kernel<0>, grid, block, (size_t)kPrSmem, st, a, tab, map_x, map_x128, map_w, map_h_store);
     if (e != cudaSuccess) return e;
     e = launch_pdl_pairs(ffn_pair_kernel<1>, grid, block, (size_t)kPrSmem, st, a, tab, map_h, map_h128, map_w, map_y_store);
     *n_launch = 2;

@@ -544,15 +544,13 @@ ffn_prefill_kernel(FfnArgs a, const __grid_constant__ SlotTable tab, const __gri
 }
 
 // ------------------------------------------------------------------------------------------- host
-static bool g_pf_init[64];
+static DeviceOnce g_pf_once;
 
 cudaError_t ffn_prefill_init() {
-    if (!first_call_on_device(g_pf_init)) return cudaSuccess;
-    cudaError_t e = cudaFuncSetAttribute(ffn_prefill_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
-    if (e != cudaSuccess) return e;
-    e = cudaFuncSetAttribute(ffn_prefill_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
-    if (e != cudaSuccess) return e;
-    return cudaSuccess;
+    return once_on_device(g_pf_once, [] {
+        const cudaError_t e = cudaFuncSetAttribute(ffn_prefill_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(ffn_prefill_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPfSmem);
+    });
 }
 
 cudaError_t launch_ffn_prefill(const FfnArgs& a, const SlotTable& tab, const CUtensorMap& map_x, const CUtensorMap& map_h,

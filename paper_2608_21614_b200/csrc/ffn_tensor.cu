@@ -498,25 +498,24 @@ cudaError_t launch_bounded_wait_selftest(int* status, unsigned long long limit_n
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeTiledFn g_encode = nullptr;
-static bool g_init_done[64];
+static std::atomic<EncodeTiledFn> g_encode{nullptr};
+static DeviceOnce g_once;
 
 cudaError_t ffn_tensor_init() {
-    if (!first_call_on_device(g_init_done)) return cudaSuccess;
-    cudaError_t e;
-    if (!g_encode) {
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    return once_on_device(g_once, [] {
+        cudaError_t e;
+        if (!g_encode) {
+            void* fn = nullptr;
+            cudaDriverEntryPointQueryResult qres;
+            e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+            if (e != cudaSuccess) return e;
+            if (!fn || qres != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+            g_encode = (EncodeTiledFn)fn;
+        }
+        e = cudaFuncSetAttribute(ffn_tensor_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmemMax);
         if (e != cudaSuccess) return e;
-        if (!fn || qres != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
-        g_encode = (EncodeTiledFn)fn;
-    }
-    e = cudaFuncSetAttribute(ffn_tensor_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmemMax);
-    if (e != cudaSuccess) return e;
-    e = cudaFuncSetAttribute(ffn_tensor_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmemMax);
-    if (e != cudaSuccess) return e;
-    return cudaSuccess;
+        return cudaFuncSetAttribute(ffn_tensor_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmemMax);
+    });
 }
 
 static bool make_act_map(CUtensorMap* m, const void* base, int rows, int K, int box_rows) {
@@ -524,7 +523,7 @@ static bool make_act_map(CUtensorMap* m, const void* base, int rows, int K, int 
     cuuint64_t strides[1] = {(cuuint64_t)K * 2};
     cuuint32_t box[2] = {(cuuint32_t)kTileK, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+    CUresult r = g_encode.load(std::memory_order_relaxed)(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
@@ -536,7 +535,7 @@ static bool make_store_map(CUtensorMap* m, void* base, CUtensorMapDataType dt, i
     cuuint64_t strides[1] = {(cuuint64_t)cols * elem_bytes};
     cuuint32_t box[2] = {(cuuint32_t)(64 / elem_bytes), 32u};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = g_encode(m, dt, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    CUresult r = g_encode.load(std::memory_order_relaxed)(m, dt, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
 }
@@ -547,7 +546,7 @@ static bool make_weight_map(CUtensorMap* m, const void* base, size_t bytes) {
     cuuint64_t strides[1] = {128};
     cuuint32_t box[2] = {128, 128};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+    CUresult r = g_encode.load(std::memory_order_relaxed)(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;

@@ -409,14 +409,15 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
 bool mx_few_supported(int T, int k, int d) { return T <= kFewTokens && k <= kFewTokens && mx_chunks(d) <= kFewMaxChunks; }
 
 cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStream_t st, int* n_launch) {
-    static bool done[64];
+    static DeviceOnce once;
     constexpr int kMost = 222 * 1024, kSmemB = kFewStagesB * kFewStageB + 1024;
-    if (first_call_on_device(done)) {
-        cudaError_t e = cudaFuncSetAttribute(mx_few_gate_up_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_few_gate_up_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_few_down_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemB);
-        if (e != cudaSuccess) return e;
-    }
+    cudaError_t e = once_on_device(once, [] {
+        cudaError_t s = cudaFuncSetAttribute(mx_few_gate_up_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (s == cudaSuccess) s = cudaFuncSetAttribute(mx_few_gate_up_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (s == cudaSuccess) s = cudaFuncSetAttribute(mx_few_down_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemB);
+        return s;
+    });
+    if (e != cudaSuccess) return e;
     const int pairs = a.T * a.k, active = (pairs < a.E ? pairs : a.E) + a.S;
     long long items = (long long)active * (a.f / 128);
     const bool half = items <= n_sm;
@@ -426,7 +427,7 @@ cudaError_t launch_mx_few(MxFewArgs a, const SlotTable& tab, int n_sm, cudaStrea
     a.stages_a = (kMost - around) / stage;
     const int most = kFewMaxStages;                                            // tensor memory: 192 columns of sums, 16 per stage, 8 per chunk of x
     if (a.stages_a > most) a.stages_a = most;
-    cudaError_t e = launch_pdl(half ? mx_few_gate_up_kernel<true> : mx_few_gate_up_kernel<false>, dim3((unsigned)(items < n_sm ? items : n_sm)),
+    e = launch_pdl(half ? mx_few_gate_up_kernel<true> : mx_few_gate_up_kernel<false>, dim3((unsigned)(items < n_sm ? items : n_sm)),
                                dim3(kGateUpThreads), (size_t)(around + a.stages_a * stage), st, a, tab);
     if (e != cudaSuccess) return e;
     *n_launch += 1;

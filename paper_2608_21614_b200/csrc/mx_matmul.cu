@@ -566,23 +566,25 @@ mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeTiledFn g_mx_encode = nullptr;
-static bool g_mx_done[64];
+static std::atomic<EncodeTiledFn> g_mx_encode{nullptr};
+static DeviceOnce g_mx_once;
 
 static cudaError_t mx_matmul_init() {
-    if (!g_mx_encode) {
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+    return once_on_device(g_mx_once, [] {
+        cudaError_t e;
+        if (!g_mx_encode) {
+            void* fn = nullptr;
+            cudaDriverEntryPointQueryResult q;
+            e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+            if (e != cudaSuccess) return e;
+            if (!fn || q != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+            g_mx_encode = (EncodeTiledFn)fn;
+        }
+        e = cudaFuncSetAttribute(mx_matmul_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem);
         if (e != cudaSuccess) return e;
-        if (!fn || q != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
-        g_mx_encode = (EncodeTiledFn)fn;
-    }
-    if (!first_call_on_device(g_mx_done)) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(mx_matmul_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMmSmem);
-    if (e != cudaSuccess) return e;
-    const cudaError_t f = cudaFuncSetAttribute(mx_matmul_tiles_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
-    return f != cudaSuccess ? f : cudaFuncSetAttribute(mx_matmul_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+        e = cudaFuncSetAttribute(mx_matmul_tiles_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(mx_matmul_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+    });
 }
 
 // Codes as a byte matrix: boxes of 128 bytes (256 elements) x `box_rows` rows; what lies outside reads as zero.
@@ -592,7 +594,7 @@ static bool make_code_map(CUtensorMap* m, const void* codes, long long rows, lon
     const cuuint64_t strides[1] = {pitch};
     const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
-    return g_mx_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, estr,
+    return g_mx_encode.load(std::memory_order_relaxed)(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, estr,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -634,7 +636,7 @@ static bool make_scale_map(CUtensorMap* m, const void* scales, long long rows, l
     const cuuint64_t strides[1] = {kMxPiece};
     const cuuint32_t box[2] = {128, 2};
     const cuuint32_t estr[2] = {1, 1};
-    return g_mx_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(scales), dims, strides, box, estr,
+    return g_mx_encode.load(std::memory_order_relaxed)(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(scales), dims, strides, box, estr,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

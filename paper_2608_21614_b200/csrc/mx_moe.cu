@@ -375,14 +375,14 @@ size_t mx_workspace_bytes(int max_tokens, int k, int E, int S, int d, int f) {
 
 template <int R>
 static cudaError_t launch_tiles(const FfnArgs& f, const MxTokens& x, const SlotTable& tab, cudaStream_t st) {
-    static bool done[64];
+    static DeviceOnce once;
     using A = FfnShape<0, R>;
     using B = FfnShape<1, R>;
-    cudaError_t e;
-    if (first_call_on_device(done)) {
-        if ((e = cudaFuncSetAttribute(mx_ffn_kernel<0, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, A::kSmem)) != cudaSuccess) return e;
-        if ((e = cudaFuncSetAttribute(mx_ffn_kernel<1, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, B::kSmem)) != cudaSuccess) return e;
-    }
+    cudaError_t e = once_on_device(once, [] {
+        const cudaError_t s = cudaFuncSetAttribute(mx_ffn_kernel<0, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, A::kSmem);
+        return s != cudaSuccess ? s : cudaFuncSetAttribute(mx_ffn_kernel<1, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, B::kSmem);
+    });
+    if (e != cudaSuccess) return e;
     uint8_t* x_tiles = reinterpret_cast<uint8_t*>(f.h);
     const int most = (int)most_tiles(f.max_rows, f.E, R);
     uint8_t* h_tiles = x_tiles + (size_t)most * mx_chunks(f.d) * TileShape<R>::kBytes;

@@ -385,11 +385,11 @@ cudaError_t launch_repack(const int32_t* idx, const uint16_t* x, int T, int E, i
                           int32_t* hist, uint16_t* rank16, int n_sm, cudaStream_t st, int* n_launch) {
     const int P = T * k, n_chunks = (P + 31) >> 5;
     if (!x_packed) d = 0;                                // index outputs only: rows of no length
-    static bool attr_done[64];
-    if (first_call_on_device(attr_done)) {
-        cudaError_t e = cudaFuncSetAttribute(repack_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024);
-        if (e != cudaSuccess) return e;
-    }
+    static DeviceOnce once;
+    const cudaError_t ready = once_on_device(once, [] {
+        return cudaFuncSetAttribute(repack_fused_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024);
+    });
+    if (ready != cudaSuccess) return ready;
     if (P <= kFusedPairs) {
         size_t base = sizeof(RepackSmem) + (((size_t)table_stride(n_chunks) * E * 2 + 15) & ~(size_t)15);
         size_t smem = base + (size_t)n_chunks * 32 * 4 + (size_t)n_chunks * 32;

@@ -6,6 +6,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "device_once.h"
 #include "saem.h"
 
 namespace saem {
@@ -85,27 +86,15 @@ inline cudaError_t launch_pdl_pairs(void (*kernel)(KArgs...), dim3 grid, dim3 bl
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
-// Function attributes (large dynamic shared memory) are per device: returns true the first time it is
-// called for the current device with this flag array.
-inline bool first_call_on_device(bool (&done)[64]) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return true;
-    if (done[dev]) return false;
-    done[dev] = true;
-    return true;
-}
 // SMs of the current device.
 inline cudaError_t sm_count(int* n) {
-    static int known[64];
+    static std::atomic<int> known[64];
     int dev;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev < 64 && known[dev]) {
-        *n = known[dev];
-        return cudaSuccess;
-    }
+    if (dev < 64 && (*n = known[dev].load(std::memory_order_relaxed)) != 0) return cudaSuccess;
     e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess && dev < 64) known[dev] = *n;
+    if (e == cudaSuccess && dev < 64) known[dev].store(*n, std::memory_order_relaxed);
     return e;
 }
 

@@ -1,10 +1,12 @@
 """Matrices in the microscaled 4-bit format (MXFP4) and the products of them.
 
 Thin plumbing over the ``saem_mx_*`` calls: device memory and arguments here, arithmetic in
-libsaem's kernels.  Everything is enqueued on the current stream unless a stream is given.
+libsaem's kernels.  Everything is enqueued on the current stream unless a stream (or its handle) is given; a result that
+is allocated in such a call belongs to that stream, as if it were the current one.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import torch
@@ -30,6 +32,16 @@ def _matrix(t: torch.Tensor, what: str, rows: Optional[int] = None, cols: Option
     if rows is not None and shape != (rows, cols):
         raise B.SaemError(B.SAEM_ERR_SHAPE, what)
     return stride[0]
+
+
+def _allocated_on(stream):
+    """A context whose allocations belong to `stream` (None: the current stream).  Memory out of the current stream's pool may
+    still be in use by earlier work there, which the call's stream does not wait for."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 class MxTensor:
@@ -61,7 +73,8 @@ def quantize(x: torch.Tensor, out: Optional[MxTensor] = None, stream=None) -> Mx
     """x [rows, cols] float32 or bfloat16 to the microscaled format."""
     if out is None:
         _dtype(x), _matrix(x, "quantize")
-        out = empty(x.shape[0], x.shape[1], x.device)
+        with _allocated_on(stream):
+            out = empty(x.shape[0], x.shape[1], x.device)
     code = _calls.quantize(x, out.rows, out.cols, out.codes, out.scales, stream)
     if code:
         raise B.SaemError(code, "quantize")
@@ -71,7 +84,8 @@ def quantize(x: torch.Tensor, out: Optional[MxTensor] = None, stream=None) -> Mx
 def dequantize(q: MxTensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
     """The values a quantised matrix stands for, as float32 or bfloat16 (exact in both)."""
     if out is None:
-        out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.device)
+        with _allocated_on(stream):
+            out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.device)
     code = _calls.dequantize(q.codes, q.scales, q.rows, q.cols, out, stream)
     if code:
         raise B.SaemError(code, "dequantize")
@@ -84,7 +98,8 @@ def matmul(a: MxTensor, w: MxTensor, out: Optional[torch.Tensor] = None, dtype: 
     if a.cols != w.cols:
         raise B.SaemError(B.SAEM_ERR_SHAPE, "matmul")
     if out is None:
-        out = torch.empty(a.rows, w.rows, dtype=dtype, device=a.device)
+        with _allocated_on(stream):
+            out = torch.empty(a.rows, w.rows, dtype=dtype, device=a.device)
     code = _calls.matmul(a.codes, a.scales, a.rows, w.codes, w.scales, w.rows, w.cols, out, status, stream)
     if code:
         raise B.SaemError(code, "matmul")
@@ -109,7 +124,8 @@ class Linear:
         """x [m, k] float32 or bfloat16 -> [m, n]."""
         w = self.weight
         if out is None:
-            out = torch.empty(x.shape[0], w.rows, dtype=dtype, device=x.device)
+            with _allocated_on(stream):
+                out = torch.empty(x.shape[0], w.rows, dtype=dtype, device=x.device)
         code = _calls.linear(x, w.codes, w.scales, w.rows, w.cols, out, self.workspace, self.max_rows, stream)
         if code:
             raise B.SaemError(code, "Linear")

@@ -7,7 +7,7 @@ import torch
 
 from . import binding as B
 from . import _host_calls as _calls     # behind binding, which builds it if need be
-from .mx import _dtype
+from .mx import _allocated_on, _dtype
 
 _GATES = {"none": B.SAEM_GATE_NONE, "token": B.SAEM_GATE_TOKEN, "channel": B.SAEM_GATE_CHANNEL, "full": B.SAEM_GATE_FULL}
 
@@ -45,7 +45,8 @@ class BlockNorm:
               stream=None) -> torch.Tensor:
         """The first block's input: n of x itself."""
         if n_out is None:
-            n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
+            with _allocated_on(stream):
+                n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
         code = _calls.block_norm(self._enter, x, None, None, None, self.w_pre, None, n_out, stream)
         if code:
             raise B.SaemError(code, "BlockNorm")
@@ -55,9 +56,11 @@ class BlockNorm:
               n_out: Optional[torch.Tensor] = None, next_norm: bool = True, dtype: torch.dtype = torch.bfloat16, stream=None):
         """(x', n) after a block whose output is y; x_out (x's type) may be x.  `next_norm` False: x' only (n is None)."""
         if x_out is None:
-            x_out = torch.empty(x.shape[0], self.d, dtype=x.dtype, device=x.device)
+            with _allocated_on(stream):
+                x_out = torch.empty(x.shape[0], self.d, dtype=x.dtype, device=x.device)
         if n_out is None and next_norm:
-            n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
+            with _allocated_on(stream):
+                n_out = torch.empty(x.shape[0], self.d, dtype=dtype, device=x.device)
         code = _calls.block_norm(self._leave, x, y, gate, self.w_post, self.w_pre if n_out is not None else None, x_out, n_out, stream)
         if code:
             raise B.SaemError(code, "BlockNorm")

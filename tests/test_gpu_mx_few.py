@@ -4,6 +4,8 @@ import numpy as np
 import pytest
 import torch
 
+import mx_reference as ref
+from paper_2608_21614_b200 import inputs as gen
 from test_gpu_mx import build, check_step
 
 pytestmark = pytest.mark.gpu
@@ -26,4 +28,80 @@ def test_far_fewer_active_experts_than_the_grid_allows_for(T):
         again.fill_(float("nan"))
         layer.step_fused_call(logits, x, T, again)
         assert torch.equal(first, again)
+    layer.close()
+
+
+def build_of(d, f, E, k, T, distinct, seed=0, **kw):
+    """As build(), with `distinct` different experts that take turns (large layers in little time)."""
+    from paper_2608_21614_b200 import binding as B, mx
+    from paper_2608_21614_b200.layer import MoELayer
+    rng = np.random.default_rng(seed)
+    layer = MoELayer(d, f, E, k, T, ffn_path=B.SAEM_FFN_MX, **kw)
+    wide = [[torch.from_numpy(gen.bf16_bits_to_f32(m)) for m in gen.expert_weights(rng, d, f)] for _ in range(distinct)]
+    exact = [[ref.quantize(m[i].numpy())[0] for m in wide] for i in range(3)]
+    q = [[mx.quantize(m.cuda()) for m in ms] for ms in wide]
+    for e in range(E):
+        layer.load_expert_mx(0, e, e, *q[e % distinct])
+    torch.cuda.synchronize()
+    return layer, [[exact[i][e % distinct] for e in range(E)] for i in range(3)], rng
+
+
+# d_model, d_ff, experts, top_k, tokens, different experts
+FORMS = [
+    (512, 1280, 32, 8, 8, 5),       # whole blocks, two or three items per CTA; 20 units of each down part, four stages
+    (256, 768, 16, 8, 8, 5),        # halves, some CTAs with two items
+    (640, 1152, 20, 8, 7, 4),       # whole blocks, odd numbers of 128 in both axes
+    (4096, 128, 4, 2, 8, 4),        # sixteen runs of x, halves
+    (3968, 128, 5, 3, 3, 5),        # the last run is half full
+    (4096, 384, 64, 8, 8, 3),       # sixteen runs, whole blocks, a ring of three stages that goes round
+    (3968, 384, 64, 8, 6, 3),
+    (4096, 256, 8, 8, 1, 4),        # one token
+    (256, 4096, 8, 4, 8, 4),        # long down projection
+]
+
+
+@pytest.mark.parametrize("d,f,E,k,T,distinct", FORMS)
+def test_forms_of_the_two_launches(d, f, E, k, T, distinct):
+    layer, exact, rng = build_of(d, f, E, k, T, distinct, seed=d + f)
+    x = tokens(rng, T, d)
+    x[:, 5] *= 30
+    logits = torch.from_numpy(rng.standard_normal((T, E)).astype(np.float32)).cuda()
+    for t in range(T):                                                  # as many experts as the tokens can reach
+        logits[t, [(t * k + j) % E for j in range(k)]] += 6.0
+    first = check_step(layer, exact, logits, x, T)
+    again = torch.empty_like(first)
+    for _ in range(5):
+        again.fill_(float("nan"))
+        layer.step_fused_call(logits, x, T, again)
+        assert torch.equal(first, again)
+    layer.close()
+
+
+@pytest.mark.parametrize("d,f,E,k,T", [(4224, 128, 4, 2, 1), (4224, 256, 4, 2, 8), (8192, 128, 3, 2, 3), (256, 256, 16, 12, 5), (256, 128, 16, 9, 8),
+                                       (256, 128, 20, 20, 1)])
+def test_few_tokens_outside_the_two_launches(d, f, E, k, T):
+    layer, exact, rng = build_of(d, f, E, k, T, 3, seed=d + k)
+    logits = torch.from_numpy(rng.standard_normal((T, E)).astype(np.float32)).cuda()
+    check_step(layer, exact, logits, tokens(rng, T, d), T)
+    layer.close()
+
+
+@pytest.mark.parametrize("T", [1, 8, 9, 40])
+def test_a_shared_expert_of_another_width_in_a_second_context(T):
+    from paper_2608_21614_b200 import binding as B
+    from paper_2608_21614_b200.layer import MoELayer
+    d, f, fs, E, k = 256, 256, 384, 4, 2
+    rng = np.random.default_rng(T)
+    layer = MoELayer(d, f, E, k, T, d_ff_shared=fs, ffn_path=B.SAEM_FFN_MX)
+    assert layer.shared is not None
+    mats = [gen.expert_weights(rng, d, f) for _ in range(E)] + [gen.expert_weights(rng, d, fs)]
+    layer.load_all(*([m[i] for m in mats[:E]] for i in range(3)), shared=mats[E])
+    layer.copy_stream.synchronize()
+    exact = [[ref.quantize(gen.bf16_bits_to_f32(m[i]))[0] for m in mats] for i in range(3)]
+    logits = torch.from_numpy(rng.standard_normal((T, E)).astype(np.float32)).cuda()
+    x = tokens(rng, T, d)
+    check_step(layer, exact, logits, x, T, S=1)
+    whole = torch.empty(T, d, device="cuda")
+    layer.step_fused_call(logits, x, T, whole)
+    assert torch.equal(layer.step(logits, x, T), whole)                 # call by call: the same kernels
     layer.close()

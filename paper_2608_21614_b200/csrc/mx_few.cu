@@ -32,13 +32,15 @@ constexpr int kFewStagesB = 4;
 constexpr int kFewSfB = 8 + FewTile::kScaleCols;             // tensor-memory columns of a stage's scales (gate/up: 16, x's are loaded once)
 constexpr int kFewMaxChunks = 16;                            // of x: d_model <= 4096
 
+constexpr float kNotChosen = -1.f;                           // gate weights are 0 or more
+
 struct FewShared {
     alignas(8) uint64_t full[kFewMaxStages], empty[kFewMaxStages], acc[2], free[2], x;
     int slot[SAEM_MAX_EXPERTS];
     uint32_t mask[4];
     int n_active;
     int16_t expert[kFewActive];
-    float weight[kFewActive][kFewTokens];                    // gate weight of (active expert, token), 0: not chosen
+    float weight[kFewActive][kFewTokens];                    // gate weight of (active expert, token), or kNotChosen
     uint32_t tmem;
     int abort_flag;
 };
@@ -60,7 +62,7 @@ __device__ __forceinline__ void few_init(FewShared& s, const MxFewArgs& a, const
     }
     if (threadIdx.x < 4) s.mask[threadIdx.x] = 0;
     for (int i = threadIdx.x; i < a.E + a.S; i += blockDim.x) s.slot[i] = tab.slot[i];
-    for (int i = threadIdx.x; i < kFewActive * kFewTokens; i += blockDim.x) (&s.weight[0][0])[i] = 0.f;
+    for (int i = threadIdx.x; i < kFewActive * kFewTokens; i += blockDim.x) (&s.weight[0][0])[i] = kNotChosen;
     __syncthreads();
 }
 // Routes the batch (one warp per token) and lists the active experts in ascending order, the always-on ones last; experts
@@ -279,7 +281,7 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
                     const float w = s.weight[act][t];
-                    v[t] = w != 0.f ? w * swiglu(v[t], u[t]) : 0.f;            // columns of other tokens hold anything
+                    v[t] = w != kNotChosen ? w * swiglu(v[t], u[t]) : 0.f;     // columns of other tokens hold anything
                 }
                 store_planes<kFewTokens>(v, 0, a.T, a.h_tiles + ((size_t)act * mx_chunks(a.f) + (tile >> 1)) * FewTile::kBytes,
                                          (tile & 1) * 4 + quad, lane);
@@ -290,6 +292,52 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
     }
     __syncthreads();
     few_free(tmem, 512);
+}
+
+// One output of the down projection from its token's own experts alone, where the product over all active experts is NaN:
+// there an expert whose weights hold a NaN block reaches every token, since 0 * NaN is NaN.  Slow, and only for such outputs.
+// `row`: of the 128 rows of the column tile.
+__device__ __noinline__ float few_own_sum(const FewShared& s, const MxFewArgs& a, size_t tile, int tok, int row) {
+    const int nc = mx_chunks(a.f), blocks = a.f / kMxBlock, first = tok * 128;
+    float sum = 0.f;
+#pragma unroll 1
+    for (int act = 0; act < s.n_active; ++act) {
+        if (s.weight[act][tok] == kNotChosen) continue;
+        const uint8_t* w = a.slot_region + (size_t)s.slot[s.expert[act]] * a.slot_bytes + (mx_gate_up_blocks(a.d, a.f) + tile * nc) * kMxBlockBytes;
+        const uint8_t* h = a.h_tiles + (size_t)act * nc * FewTile::kBytes;
+#pragma unroll 1
+        for (int b = 0; b < blocks; ++b) {
+            const int at = b & 7, half = (at >> 2) * kMxPiece + (at & 3);       // of the 256 elements
+            const int ws = w[kMxBlockCodes + half + (row & 31) * 16 + (row >> 5) * 4];
+            if (ws == 255 || h[FewTile::kN * 128 + half + tok * 16] == 255) return __uint_as_float(0x7FC00000u);
+            const uint32_t* wc = reinterpret_cast<const uint32_t*>(w + row * 128 + ((at ^ (row & 7)) << 4));
+#pragma unroll 1
+            for (int p = kPlanes - 1; p >= 0; --p) {
+                const int col = p * kFewTokens + tok;                          // below 64: one piece of scales
+                const int hs = h[FewTile::kN * 128 + half + (col & 31) * 16 + (col >> 5) * 4];
+                const uint32_t* hc = reinterpret_cast<const uint32_t*>(h + first + p * kFewTokens * 128 + ((at ^ tok) << 4));
+                float part = 0.f;                                              // of 32 products of E2M1 values: exact
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t u[4], v[4];
+                    mx_decode8(wc[i], u);
+                    mx_decode8(hc[i], v);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u[q]));
+                        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v[q]));
+                        part += x.x * y.x + x.y * y.y;
+                    }
+                }
+                sum += ldexpf(part, ws + hs - 254);
+            }
+            if (at == 7) {
+                w += kMxBlockBytes;
+                h += FewTile::kBytes;
+            }
+        }
+    }
+    return sum;
 }
 
 // Down projection and merge.  A cluster owns 128 output columns, its CTAs equal parts of the k axis (active experts x
@@ -396,6 +444,7 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[r]) : "r"(mapa_u32(smem_u32(&sums[col * kFewTokens + tok]), r)));
 #pragma unroll
         for (int r = 0; r < kFewSplit; ++r) v += p[r];
+        if (v != v) v = few_own_sum(s, a, tile, tok, col);
         const size_t at = (size_t)tok * a.d + tile * 128 + col;
         if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
         else static_cast<float*>(a.out)[at] = v;

@@ -105,3 +105,37 @@ def test_a_shared_expert_of_another_width_in_a_second_context(T):
     layer.step_fused_call(logits, x, T, whole)
     assert torch.equal(layer.step(logits, x, T), whole)                 # call by call: the same kernels
     layer.close()
+
+
+@pytest.mark.parametrize("T", [4, 12])
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_an_expert_that_is_not_finite_reaches_its_own_tokens_only(which, T):
+    """NaN in one row of one expert's gate, up or down matrix: the tokens of the other experts stay as they are."""
+    from paper_2608_21614_b200 import binding as B, mx
+    d, f, E = 256, 384, 4
+    layer, exact, rng = build_of(d, f, E, 1, T, E, seed=3)
+    x = tokens(rng, T, d)
+    logits = torch.zeros(T, E, device="cuda")
+    logits[torch.arange(T), torch.arange(T) % E] = 5.0                  # token t on expert t % 4
+    clean = check_step(layer, exact, logits, x, T)
+    mats = [torch.from_numpy(exact[i][2].astype(np.float32)).cuda() for i in range(3)]
+    mats[which][7, 100] = float("nan")
+    B.saem_cache_evict(layer.ctx.handle, 0, 2)
+    layer.load_expert_mx(0, 2, 2, *(mx.quantize(m) for m in mats))
+    torch.cuda.synchronize()
+    out = torch.empty_like(clean)
+    layer.step_fused_call(logits, x, T, out)
+    own = torch.arange(T, device="cuda") % E == 2
+    limit = 2.0 ** -18 * clean[~own].abs().max()                        # the same terms, another order of fp32 sums at most
+    assert ((out[~own] - clean[~own]).abs() <= limit).all()
+    bad = torch.isnan(out[own])
+    want = torch.zeros_like(bad)
+    if which == 2:
+        want[:, 7] = True                                               # one output column
+    else:
+        want[:] = True                                                  # one hidden unit, hence every output
+    assert torch.equal(bad, want)
+    again = torch.empty_like(out)
+    layer.step_fused_call(logits, x, T, again)
+    assert torch.equal(out.view(torch.int32), again.view(torch.int32))
+    layer.close()

@@ -118,7 +118,8 @@ struct Call {
     template <class F>
     int launch(PyObject* stream, F f) {
         if (status != SAEM_OK) return status;
-        const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
+        c10::cuda::OptionalCUDAGuard guard;                                    // setting the device costs more than asking for it
+        if (c10::cuda::current_device() != device) guard.set_index((c10::DeviceIndex)device);
         void* st = stream_of(stream, device);
         return unlocked([&] { return f(st); });
     }

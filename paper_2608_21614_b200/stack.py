@@ -102,6 +102,8 @@ class StackRunner:
         # transfer); "host" -- it is bound to its pinned host buffer and the matrix-vector kernels read the
         # weights in place over the host link (batches of at most 8 tokens): no HBM write + read, no slot.
         assert miss_mode in ("temp", "host") and (miss_mode == "temp" or batch <= 8)
+        if miss_mode == "host" and ffn_path == B.SAEM_FFN_MX:      # its kernels take weights out of slots only
+            raise B.SaemError(B.SAEM_ERR_UNSUPPORTED, "StackRunner: host reads of 4-bit experts")
         self.miss_mode = miss_mode
         # With every expert resident nothing on the host depends on the routing; read_counts=False
         # then skips the per-layer read-back (and with it the activation log and the hit statistics).

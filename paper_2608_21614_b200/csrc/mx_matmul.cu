@@ -17,11 +17,11 @@
 //                     in four parts, 9 us in one; parts of fewer than four stages, or eight parts, cost more than they
 //                     give).  Up to 8 tokens the CTA quantises its part of the activations itself, if the parts fit into
 //                     the ring (16 tokens of 14336 x 4096 that way: 24 us against 9.7 us, quantisation launch included).
-//   more              mx_matmul_tiles_kernel, persistent, tiles of 128 x 256 with the epilogue beside the next tile's
-//                     products.
-//   many tiles        mx_matmul_pair_kernel, CTA pairs (cta_group::2) with tiles of 256 x 256, when these are at least half as
-//                     many as the SMs: each operand crosses shared memory half as often, which is what bounds the products
-//                     (8192 tokens of 14336 x 4096, quantisation included: 199 us, 4.8 PFLOP/s, against 255 us).
+//   more              mx_matmul_tiles_kernel, tiles of 128 x 256, a CTA each.
+//   many tiles        mx_matmul_pair_kernel, persistent CTA pairs (cta_group::2) with tiles of 256 x 256 and the epilogue beside
+//                     the next tile's products, when these are at least half as many as the SMs: each operand crosses shared
+//                     memory half as often (8192 tokens of 14336 x 4096, quantisation included: 199 to 240 us, 4.8 to
+//                     4.0 PFLOP/s, with the clock that a run gets; persistent tiles of 128 x 256 took 255 us).
 // Two runs give the same bits.
 #include "mx_tc.cuh"
 
@@ -42,7 +42,7 @@ struct MmArgs {
     int* status;
     long long out_stride;
     int m, n, k;
-    int n_tile;                             // tokens of a tile: all, rounded up to 16, or 64 or 128
+    int n_tile;                             // tokens of a tile: all, rounded up to 16, or 64 (256 in the other two kernels)
     int n_stage;                            // stages of the ring
     int stage_bytes;
     int tmem_cols;
@@ -252,9 +252,8 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
 }
 
-// Many tiles: one persistent CTA per SM, 128 weight rows x 256 tokens at a time.  Tensor memory holds one set of
-// accumulators beside the scales; eight warps take it into registers (128 columns each), which frees it after a few
-// hundred cycles, and store while the next tile is under way.
+// Tiles of 128 weight rows x 256 tokens, a CTA each: every SM has one at most, since the pair kernel takes over before there
+// are as many as SMs (mm_plan).  Eight warps take the accumulators into registers, 128 columns each, and store them.
 constexpr int kBigThreads = 320;            // warp 0: copies, warp 1: MMA issue, warps 2-9: epilogue
 constexpr int kBigTile = 256;
 constexpr int kBigStages = 4;
@@ -294,12 +293,12 @@ __device__ __forceinline__ void store_columns(const MmArgs& p, const uint32_t (&
 __global__ void __launch_bounds__(kBigThreads, 1)
 mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ MmArgs p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t bar_full[kBigStages], bar_empty[kBigStages], bar_acc, bar_free;
+    __shared__ alignas(8) uint64_t bar_full[kBigStages], bar_empty[kBigStages], bar_acc;
     __shared__ uint32_t tmem_s;
     __shared__ int abort_flag;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int n_w = (p.n + 127) / 128, n_t = (p.m + kBigTile - 1) / kBigTile, total = n_w * n_t;
+    const int n_w = (p.n + 127) / 128, tt = blockIdx.x / n_w, tw = blockIdx.x - tt * n_w;
     const long long kp = (p.k + kMxBlock - 1) / kMxBlock * kMxBlock;
     const int n_span = (p.k + kMxSpan - 1) / kMxSpan, stages = (int)((kp + kMmStageK - 1) / kMmStageK);
     int* const status = p.status ? p.status : &mx_status_sink;
@@ -310,7 +309,6 @@ mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             mbar_init(smem_u32(&bar_empty[i]), 1);
         }
         mbar_init(smem_u32(&bar_acc), 1);
-        mbar_init(smem_u32(&bar_free), 8);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -329,30 +327,27 @@ mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     if (warp == 0) {
         // ---------------------------------------------------------------- copies
         const uint32_t on = elect_one();
-        int it = 0, st = 0, turn = 0;
+        const int pieces = min(2, (p.m - tt * kBigTile + 127) / 128);
+        int s = 0, st = 0, turn = 0;
         bool ok = true;
-        for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
-            const int tt = i / n_w, tw = i - tt * n_w;
-            const int pieces = min(2, (p.m - tt * kBigTile + 127) / 128);
-            for (int s = 0; s < stages; ++s, ++it) {
-                if (turn) {
-                    ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, status);
-                    if (!ok) break;
-                }
-                const uint32_t dst = base + st * kBigStageBytes, bar = smem_u32(&bar_full[st]);
-                const int bytes = min(2, n_span - 2 * s) * kMxPiece;
-                expect_tx_on(on, bar, w_bytes + a_bytes + bytes * (1 + pieces));
-                tma_2d_on(on, dst, &map_w, s * 128, tw * 128, bar);
-                tma_2d_on(on, dst + w_bytes, &map_a, s * 128, tt * kBigTile, bar);
-                bulk_g2s_on(on, dst + w_bytes + a_bytes, p.w_scales + ((size_t)tw * n_span + 2 * s) * kMxPiece, bytes, bar);
-                for (int q = 0; q < pieces; ++q)
-                    bulk_g2s_on(on, dst + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
-                                p.a_scales + ((size_t)(tt * 2 + q) * n_span + 2 * s) * kMxPiece, bytes, bar);
-                if (++st == kBigStages) { st = 0; ++turn; }
+        for (; s < stages; ++s) {
+            if (turn) {
+                ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, status);
+                if (!ok) break;
             }
+            const uint32_t dst = base + st * kBigStageBytes, bar = smem_u32(&bar_full[st]);
+            const int bytes = min(2, n_span - 2 * s) * kMxPiece;
+            expect_tx_on(on, bar, w_bytes + a_bytes + bytes * (1 + pieces));
+            tma_2d_on(on, dst, &map_w, s * 128, tw * 128, bar);
+            tma_2d_on(on, dst + w_bytes, &map_a, s * 128, tt * kBigTile, bar);
+            bulk_g2s_on(on, dst + w_bytes + a_bytes, p.w_scales + ((size_t)tw * n_span + 2 * s) * kMxPiece, bytes, bar);
+            for (int q = 0; q < pieces; ++q)
+                bulk_g2s_on(on, dst + w_bytes + a_bytes + (1 + q) * 2 * kMxPiece,
+                            p.a_scales + ((size_t)(tt * 2 + q) * n_span + 2 * s) * kMxPiece, bytes, bar);
+            if (++st == kBigStages) { st = 0; ++turn; }
         }
         if (!ok && lane == 0)                                                  // copies still under way land before the CTA ends
-            for (int q = max(0, it - kBigStages); q < it; ++q) {
+            for (int q = max(0, s - kBigStages); q < s; ++q) {
                 abort_flag = 0;
                 mbar_wait(smem_u32(&bar_full[q % kBigStages]), (q / kBigStages) & 1, abort_p, status);
                 abort_flag = 1;
@@ -361,58 +356,45 @@ mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
         const uint64_t codes0 = smem_desc_sw128(base), scales0 = smem_desc_scales(base);
-        int st = 0, turn = 0, k = 0;
-        bool ok = true;
-        for (int i = blockIdx.x; i < total && ok; i += gridDim.x, ++k) {
-            const int n_mma = (min(kBigTile, p.m - i / n_w * kBigTile) + 15) & ~15;
-            if (k) ok = mbar_wait_warp(smem_u32(&bar_free), (k - 1) & 1, abort_p, status);
+        const int n_mma = (min(kBigTile, p.m - tt * kBigTile) + 15) & ~15;
+        int st = 0, turn = 0;
+        for (int s = 0; s < stages; ++s) {
+            if (!mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, status)) break;
             tc_fence_after();
-            for (int s = 0; s < stages && ok; ++s) {
-                ok = mbar_wait_warp(smem_u32(&bar_full[st]), turn & 1, abort_p, status);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t at = st * kBigStageBytes, tw = tmem_sf + st * kBigSfCols, ta = tw + 8;
-                const uint64_t dw = desc_at(codes0, at), da = desc_at(codes0, at + w_bytes), ds = desc_at(scales0, at + w_bytes + a_bytes);
-                const int steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
+            const uint32_t at = st * kBigStageBytes, sw = tmem_sf + st * kBigSfCols, sa = sw + 8;
+            const uint64_t dw = desc_at(codes0, at), da = desc_at(codes0, at + w_bytes), ds = desc_at(scales0, at + w_bytes + a_bytes);
+            const int steps = (int)min(4ll, (kp - (long long)s * kMmStageK + 63) / 64);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (2 * s + h >= n_span) break;
-                    tc_cp_scales(on, tw + 4 * h, desc_at(ds, h * kMxPiece));
-                    tc_cp_scales(on, ta + 8 * h, desc_at(ds, (2 + h) * kMxPiece));
-                    tc_cp_scales(on, ta + 8 * h + 4, desc_at(ds, (4 + h) * kMxPiece));
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < steps)
-                        tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4(n_mma, (j & 1) * 2), tw + 4 * (j >> 1),
-                                    ta + 8 * (j >> 1), s > 0 || j > 0);
-                tc_commit_on(on, smem_u32(&bar_empty[st]));
-                if (++st == kBigStages) { st = 0; ++turn; }
+            for (int h = 0; h < 2; ++h) {
+                if (2 * s + h >= n_span) break;
+                tc_cp_scales(on, sw + 4 * h, desc_at(ds, h * kMxPiece));
+                tc_cp_scales(on, sa + 8 * h, desc_at(ds, (2 + h) * kMxPiece));
+                tc_cp_scales(on, sa + 8 * h + 4, desc_at(ds, (4 + h) * kMxPiece));
             }
-            tc_commit_on(on, smem_u32(&bar_acc));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < steps)
+                    tc_mma_mxf4(on, tmem, desc_at(dw, 32 * j), desc_at(da, 32 * j), idesc_mxf4(n_mma, (j & 1) * 2), sw + 4 * (j >> 1),
+                                sa + 8 * (j >> 1), s > 0 || j > 0);
+            tc_commit_on(on, smem_u32(&bar_empty[st]));
+            if (++st == kBigStages) { st = 0; ++turn; }
         }
+        tc_commit_on(on, smem_u32(&bar_acc));
     } else {
         // ---------------------------------------------------------------- epilogue
         const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
-        bool ok = true;
-        int k = 0;
-        for (int i = blockIdx.x; i < total; i += gridDim.x, ++k) {
-            const int tt = i / n_w, tw = i - tt * n_w;
-            ok = ok && mbar_wait_warp(smem_u32(&bar_acc), k & 1, abort_p, status);
-            tc_fence_after();
+        const bool ok = mbar_wait_warp(smem_u32(&bar_acc), 0, abort_p, status) && !*abort_p;
+        tc_fence_after();
+        if (ok) {
             uint32_t r[128];
-            if (ok) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tc_ld32_issue(tmem + ((uint32_t)(quad * 32) << 16) + half * 128 + q * 32, r + 32 * q);
-                tc_wait_ld();
+            for (int q = 0; q < 4; ++q) tc_ld32_issue(tmem + ((uint32_t)(quad * 32) << 16) + half * 128 + q * 32, r + 32 * q);
+            tc_wait_ld();
 #pragma unroll
-                for (int q = 0; q < 8; ++q) tc_reg_fence16(r + 16 * q);
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_free));
-            if (ok) store_columns(p, r, tw * 128 + row, tt * kBigTile + half * 128, lane);
+            for (int q = 0; q < 8; ++q) tc_reg_fence16(r + 16 * q);
+            store_columns(p, r, tw * 128 + row, tt * kBigTile + half * 128, lane);
         }
+        tc_fence_before();
     }
     __syncthreads();
     if (warp == 1) {
@@ -601,7 +583,7 @@ static bool make_code_map(CUtensorMap* m, const void* codes, long long rows, lon
 
 // How a product is cut: decided from its sizes alone, so that saem_mx_linear knows whether A is to be quantised first.
 struct MmPlan {
-    bool big;                               // mx_matmul_tiles_kernel
+    bool big;                               // mx_matmul_tiles_kernel: fewer tiles of 128 x 256 than SMs
     bool pairs;                             // mx_matmul_pair_kernel
     bool fused;                             // A quantised by the product's CTAs (where it is not quantised already)
     int n_tile, split, n_stage, stage_bytes;
@@ -656,11 +638,9 @@ static cudaError_t launch_mx_matmul(const MmPlan& plan, MmArgs p, const uint8_t*
         return launch_pdl_pairs(mx_matmul_pair_kernel, dim3((unsigned)(n_sm & ~1)), dim3(kBigThreads), (size_t)kPairSmem, st, map_w, map_a, map_ws,
                                 map_as, p);
     }
-    if (plan.big) {
-        const long long tiles = (long long)((p.n + 127) / 128) * ((p.m + kBigTile - 1) / kBigTile);
-        return launch_pdl(mx_matmul_tiles_kernel, dim3((unsigned)(tiles < n_sm ? tiles : n_sm)), dim3(kBigThreads), (size_t)kBigSmem, st, map_w,
-                          map_a, p);
-    }
+    if (plan.big)
+        return launch_pdl(mx_matmul_tiles_kernel, dim3((unsigned)(((p.n + 127) / 128) * ((p.m + kBigTile - 1) / kBigTile))), dim3(kBigThreads),
+                          (size_t)kBigSmem, st, map_w, map_a, p);
     p.stage_bytes = plan.stage_bytes;
     p.n_stage = plan.n_stage;
     p.split = plan.split;

@@ -56,3 +56,13 @@ def test_where_the_ring_just_holds_a_part(m, n, k):
 @pytest.mark.parametrize("m", [9, 16, 17, 64, 65, 130])
 def test_split_with_a_quantisation_of_its_own(m):
     check(m, 384, 4096 + 160, "f32", ("dense", "odd"))
+
+
+@pytest.mark.parametrize("m,n,k", [(200, 16384, 2048), (512, 8191, 1500), (1000, 4096, 2336), (257, 9000, 1056), (2500, 1300, 1312)])
+def test_tiles_of_256_tokens_whose_ring_goes_round(m, n, k):
+    check(m, n, k, "bf16", ("dense",))
+
+
+@pytest.mark.parametrize("m,n,k", [(2304, 2300, 2080), (1025, 4096, 3000), (600, 7000, 1700)])
+def test_pairs_whose_ring_goes_round(m, n, k):
+    check(m, n, k, "f32", ("dense", "odd"))

@@ -10,3 +10,10 @@ raises if the library is missing -- there is no CPU fallback.
 """
 
 __all__ = ["inputs"]
+
+
+def __getattr__(name):
+    if name == "_host_calls":               # imported by name before mx or norms: built first if need be
+        from . import build
+        return build.host_calls()
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

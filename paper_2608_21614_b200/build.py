@@ -1,10 +1,16 @@
-"""Builds libsaem.so (the C-ABI CUDA library, nvcc for sm_100a) and _host_calls.so (its inner-loop calls for Python) in-tree."""
+"""Builds libsaem.so (the C-ABI CUDA library, nvcc for sm_100a) and _host_calls.so (its inner-loop calls for Python) in-tree.
+
+The library needs nvcc alone; the extension also Python's and torch's headers, and belongs to the Python and the torch that it
+was built with.  `binding` builds the one, `mx` and `norms` the other when they are imported."""
 from __future__ import annotations
 
 import glob
+import importlib
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
+import sys
 import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -35,21 +41,43 @@ def _headers():
 
 
 def stale() -> bool:
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + _headers()
-    return _older(LIB, deps) or _older(HOST_LIB, [HOST_SOURCE] + _headers())
+    return _older(LIB, sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + _headers())
 
 
-def _build_host_calls() -> None:
+def _built_for() -> str:
+    return "saem_host_calls for Python %s and torch %s" % (sysconfig.get_config_var("SOABI"), importlib.metadata.version("torch"))
+
+
+def host_stale() -> bool:
+    if _older(HOST_LIB, [HOST_SOURCE] + _headers()):
+        return True
+    with open(HOST_LIB, "rb") as f:
+        return (_built_for() + "\0").encode() not in f.read()
+
+
+def build_host_calls(force: bool = False) -> str:
     """_host_calls.so, linked to the libsaem.so beside it and to torch."""
+    if not force and not host_stale():
+        return HOST_LIB
+    build()
     torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
     cuda = os.path.dirname(os.path.dirname(NVCC))
     include = [os.path.join(_ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(torch_dir, "include"),
                os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
     tmp = HOST_LIB + ".tmp%d" % os.getpid()
-    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *["-I" + p for p in include], HOST_SOURCE,
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *["-I" + p for p in include],
+                           '-DSAEM_BUILT_FOR="%s"' % _built_for(), HOST_SOURCE,
                            "-o", tmp, "-L", os.path.join(torch_dir, "lib"), "-L", _HERE, "-l:" + os.path.basename(LIB), "-ltorch_python",
                            "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, HOST_LIB)
+    return HOST_LIB
+
+
+def host_calls():
+    """The module _host_calls, built first if need be (raises if that fails: there is no slower way behind it)."""
+    build_host_calls()
+    import torch                            # noqa: F401  (brings the libraries that the extension is linked to)
+    return importlib.import_module("._host_calls", __package__)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -76,10 +104,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([NVCC, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", tmp, *objs])
     os.replace(tmp, LIB)
-    _build_host_calls()
     return LIB
 
 
 if __name__ == "__main__":
-    import sys
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_host_calls(force="--force" in sys.argv))

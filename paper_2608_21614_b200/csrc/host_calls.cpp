@@ -252,6 +252,9 @@ PyMethodDef methods[] = {
     {"block_norm", (PyCFunction)(void (*)(void))block_norm, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
+// what this file was built for, looked for in the built file
+__attribute__((used)) const char built_for[] = SAEM_BUILT_FOR;
+
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -12,8 +12,9 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from . import _host_calls as _calls     # behind binding, which builds it if need be
+from .build import host_calls
 
+_calls = host_calls()
 _DTYPE = {torch.float32: B.SAEM_OUT_F32, torch.bfloat16: B.SAEM_OUT_BF16}
 
 

@@ -6,8 +6,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from . import _host_calls as _calls     # behind binding, which builds it if need be
-from .mx import _allocated_on, _dtype
+from .mx import _allocated_on, _calls, _dtype
 
 _GATES = {"none": B.SAEM_GATE_NONE, "token": B.SAEM_GATE_TOKEN, "channel": B.SAEM_GATE_CHANNEL, "full": B.SAEM_GATE_FULL}
 

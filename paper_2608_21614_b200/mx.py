@@ -133,5 +133,7 @@ class Linear:
         return out
 
     def device_status(self) -> int:
-        """The status word of the calls so far (synchronises); 0 unless a device-side wait ran out."""
+        """The status word of the calls so far, whatever their streams (synchronises the device); 0 unless a device-side wait ran
+        out."""
+        torch.cuda.synchronize(self.workspace.device)
         return int(self.workspace[:4].view(torch.int32).item())

@@ -47,3 +47,15 @@ def test_results_of_a_named_stream_keep_clear_of_the_current_one(name, named_by)
 def test_the_default_stream_by_its_handle():
     shape, dtype, call = cases()["dequantize"]
     assert torch.equal(call(0), call(None))
+
+
+def test_the_status_word_waits_for_calls_on_every_stream():
+    from paper_2608_21614_b200 import mx
+    linear = mx.Linear(mx.quantize(torch.randn(64, 64, device="cuda")), 4)
+    torch.zeros(1, dtype=torch.int32, device="cuda").fill_(3)           # loading the kernel would wait for the GPU
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                                       # as a call would that runs out of time late
+        torch.cuda._sleep(40_000_000)
+        linear.workspace[:4].view(torch.int32).fill_(7)
+    assert linear.device_status() == 7

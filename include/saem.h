@@ -90,8 +90,11 @@ enum { SAEM_GATE_NONE = 0, SAEM_GATE_TOKEN = 1, SAEM_GATE_CHANNEL = 2, SAEM_GATE
  * saem_mx_pack_expert (device) or saem_pack_expert_host (which then quantises).  Activations are not rounded to 4 bits: x and
  * the hidden activations are held to 2^-13.8 of the largest of 32 neighbours at worst.  saem_moe_step takes up to 8 tokens
  * (top_k <= 8, d_model <= 4096, no shared_ctx) in two launches, which leave topk_idx and topk_w but none of the other
- * intermediates in the workspace; beyond that it leaves all but x_packed, and h in a form of its own.  All step and cache calls
- * take such a context except saem_cache_map_host (UNSUPPORTED).
+ * intermediates in the workspace; beyond that it leaves all but x_packed, and h in a form of its own.  In the two launches an
+ * expert without a slot contributes nothing (status word NOT_RESIDENT), and an output that is NaN is summed again from its
+ * token's own experts, so that NaN weights of an expert reach only the tokens that chose it; beyond them its rows of y_packed
+ * are left untouched, as in saem_expert_ffn.  All step and cache calls take such a context except saem_cache_map_host
+ * (UNSUPPORTED).
  * n_shared (0..16, n_experts + n_shared <= SAEM_MAX_EXPERTS): always-on shared experts of the same
  * width d_ff that run INSIDE the layer's grouped launch.  They are experts n_experts ..
  * n_experts + n_shared - 1 of every layer for the cache calls (outside the routed cache-ratio
@@ -333,7 +336,8 @@ int saem_expert_ffn_static(const void* x_packed, const int32_t* offsets, int n_e
  *   codes  [rows][ceil(cols / 32) * 16] bytes, the last block padded with zeros        (saem_mx_codes_bytes)
  *   scales [ceil(rows / 128)][ceil(cols / 128)][512] bytes: the scales of blocks 4c .. 4c + 3 of row r are the four
  *          bytes at piece (r / 128, c), offset (r % 32) * 16 + (r / 32 % 4) * 4        (saem_mx_scales_bytes)
- * Both must be 16-byte aligned.  The scales of rows beyond the last in a piece are unspecified.  The size queries return
+ * Both must be 16-byte aligned.  The scales of rows beyond the last in a piece are unspecified; those of blocks beyond a
+ * row's last one in its word of four must not be 255 (saem_mx_quantize writes 0).  The size queries return
  * 0 for sizes that are not supported (rows < 0, cols < 1, either or rows * ceil(cols / 1024) above 2^31 - 1).
  *
  * saem_mx_quantize: s = max(floor(log2 max|x|) - 2, -127) + 127 and the code nearest to x * 2^-(s - 127), ties to the even

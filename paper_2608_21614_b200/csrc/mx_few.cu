@@ -12,7 +12,8 @@
 // same two launches with mma.sync, the weights converted to f16, were bound by instruction issue: 50 us for 8 tokens of a
 // 2048 x 768 layer of 128 experts against 26.5 us, 93 MB at 3.5 TB/s.)  One token takes 14 us: routing 1.7 us, the first
 // weights' way 1 us, the products 2.5 us, their sums and planes of h 2 us, the hand-over 1.2 us, the down projection with the
-// cluster's sum 3 us, and the two launches.
+// cluster's sum 3 us, and the two launches.  A CTA of the second launch (99 KB) finds no place beside one of the first (up to
+// 222 KB and all of tensor memory), so its routing and first weights begin when a CTA of the first launch ends on its SM.
 #include "mx_planes.cuh"
 #include "route_row.cuh"
 

@@ -20,8 +20,9 @@
 //   more              mx_matmul_tiles_kernel, tiles of 128 x 256, a CTA each.
 //   many tiles        mx_matmul_pair_kernel, persistent CTA pairs (cta_group::2) with tiles of 256 x 256 and the epilogue beside
 //                     the next tile's products, when these are at least half as many as the SMs: each operand crosses shared
-//                     memory half as often (8192 tokens of 14336 x 4096, quantisation included: 199 to 240 us, 4.8 to
-//                     4.0 PFLOP/s, with the clock that a run gets; persistent tiles of 128 x 256 took 255 us).
+//                     memory half as often (8192 tokens of 14336 x 4096, quantisation included: 205 us, 4.7 PFLOP/s, in a
+//                     burst at 1965 MHz, 239 us in seconds of it, at 1.44 to 1.5 GHz under the power cap; persistent tiles
+//                     of 128 x 256 took 255 us).
 // Two runs give the same bits.
 #include "mx_tc.cuh"
 

@@ -9,7 +9,9 @@
 // Few rows per expert: the bound is the weights' bytes.  The step just named moves 749 MB, 6.2 TB/s over all its
 // launches; 61 tokens of a 2560 x 1536 layer of 64 + 2 experts take 87 us for 372 MB, of which the launches around the
 // products (gate and indices, tiles of x, combine) are some 13 us.  Many rows: 2048 tokens of a 2048 x 1408 layer of 64 + 2
-// experts take 534 us (bf16 slots: 375 us), bound by the planes' products.
+// experts take 525 us (bf16 slots: 375 us).  The MMAs are not the bound there: the tensor pipe is busy for 33 % of the gate/up
+// launch and 46 % of the down launch.  With tiles of 32 rows tensor memory holds one set of the gate/up accumulators, so that
+// an epilogue and the next item's products take turns, and the ring has three stages.
 //
 // A tile is R (8, 16, 32) rows of one expert; an item is a tile x 128 hidden units (gate and up accumulators side by
 // side) or x 128 output columns.  Tiles of the activations are laid out as the MMA wants them (swizzled codes of

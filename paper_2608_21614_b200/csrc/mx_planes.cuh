@@ -105,7 +105,10 @@ __device__ __forceinline__ void store_tile_row(uint8_t* dst, int r, int lane, co
                                          ((n >> 5) & 3) * 4) = scales[p];
     }
 }
-__device__ __forceinline__ float swiglu(float z, float up) { return __fdividef(z, 1.f + __expf(-z)) * up; }   // 2^-21 or so: far below the planes'
+// The fast exponential's documented bound grows with its argument, 2 + 1.17 |z| units in the last place: 2^-21 of the result
+// for z near 0, 2^-18 at z = -20 and 2^-16 at z = -80, below what the planes keep of a block's largest element.  Below
+// z = -87.3, where the quotient is less than 2^-126 of z, it is 0.
+__device__ __forceinline__ float swiglu(float z, float up) { return __fdividef(z, 1.f + __expf(-z)) * up; }
 // Eight rows' hidden units of one block (a lane holds one unit of each row) to the planes of rows r0 .. r0 + 7 of a tile.
 template <int R>
 __device__ __forceinline__ void store_planes(const float (&v)[8], int r0, int rows, uint8_t* dst, int blk, int lane) {

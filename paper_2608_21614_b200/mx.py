@@ -110,7 +110,8 @@ def matmul(a: MxTensor, w: MxTensor, out: Optional[torch.Tensor] = None, dtype: 
 class Linear:
     """A projection whose weights are quantised once and whose activations are quantised in every call.
 
-    `max_rows` sizes the workspace; calls of one Linear must be ordered on the GPU (they share it)."""
+    `max_rows` sizes the workspace; calls of one Linear must be ordered on the GPU (they share it), and after the stream that
+    was current when it was made."""
 
     def __init__(self, weight: MxTensor, max_rows: int):
         if not (weight.codes.is_cuda and weight.codes.device == weight.scales.device):

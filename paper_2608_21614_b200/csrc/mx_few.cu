@@ -114,14 +114,6 @@ __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, bool
     }
     few_sync();
 }
-// At an abort: copies that are still under way land before the CTA ends.
-__device__ __noinline__ void few_drain(FewShared& s, int n_stage, int issued, int* status) {
-    for (int i = max(0, issued - n_stage); i < issued; ++i) {
-        s.abort_flag = 0;
-        mbar_wait(smem_u32(&s.full[i % n_stage]), (i / n_stage) & 1, &s.abort_flag, status);
-        s.abort_flag = 1;
-    }
-}
 __device__ __forceinline__ void few_alloc(FewShared& s, uint32_t cols) {
     if (threadIdx.x >> 5 == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(cols));
@@ -213,7 +205,7 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
                 if (++st == n) { st = 0; ++turn; }
             }
         }
-        if (!ok && lane == 0) few_drain(s, n, it, a.status);
+        ring_settle_warp(s.full, n, it, a.status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -261,6 +253,7 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
             }
             tc_commit_on(on, smem_u32(&s.acc[set]));
         }
+        if (k) mbar_settle_warp(smem_u32(&s.acc[(k - 1) & 1]), ((k - 1) >> 1) & 1, a.status);
     } else if (warp < 10) {
         split_x(mine + warp - 2, tasks);
         // ---------------------------------------------------------------- epilogue
@@ -389,8 +382,7 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             bulk_g2s_on(on, base + st * kFewStageB + kMxBlockBytes, a.h_tiles + (size_t)q * FewTile::kBytes, FewTile::kBytes, smem_u32(&s.full[st]));
             if (++st == n) { st = 0; ++turn; }
         }
-        if (!ok && lane == 0) few_drain(s, n, q - q0, a.status);
-        __syncwarp();
+        ring_settle_warp(s.full, n, q - q0, a.status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -420,6 +412,7 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             if (++st == n) { st = 0; ++turn; }
         }
         tc_commit_on(on, smem_u32(&s.acc[0]));
+        mbar_settle_warp(smem_u32(&s.acc[0]), 0, a.status);
     } else if (warp < 6) {
         const int quad = warp & 3;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};

@@ -127,13 +127,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             a_part(s, st);
             if (++st == p.n_stage) { st = 0; ++turn; }
         }
-        if (!ok && lane == 0)                                                // copies still under way land before the CTA ends
-            for (int q = max(s0, s - p.n_stage); q < s; ++q) {
-                abort_flag = 0;
-                const bool landed = mbar_wait(smem_u32(&bar_full[(q - s0) % p.n_stage]), ((q - s0) / p.n_stage) & 1, abort_p, status);
-                abort_flag = 1;
-                if (!landed) break;                                          // seconds later: nothing is under way any more
-            }
+        ring_settle_warp(bar_full, p.n_stage, s - s0, status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -159,6 +153,7 @@ mx_matmul_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             if (++st == p.n_stage) { st = 0; ++turn; }
         }
         tc_commit_on(on, smem_u32(&bar_acc));
+        mbar_settle_warp(smem_u32(&bar_acc), 0, status);
     } else if (p.x) {
         // ---------------------------------------------------------------- quantisation of the CTA's part of A
         // (stage, row) pairs go to the eight warps in turn, so that a few tokens' loads are under way together as well
@@ -347,12 +342,7 @@ mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
                             p.a_scales + ((size_t)(tt * 2 + q) * n_span + 2 * s) * kMxPiece, bytes, bar);
             if (++st == kBigStages) { st = 0; ++turn; }
         }
-        if (!ok && lane == 0)                                                  // copies still under way land before the CTA ends
-            for (int q = max(0, s - kBigStages); q < s; ++q) {
-                abort_flag = 0;
-                mbar_wait(smem_u32(&bar_full[q % kBigStages]), (q / kBigStages) & 1, abort_p, status);
-                abort_flag = 1;
-            }
+        ring_settle_warp(bar_full, kBigStages, s, status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -381,6 +371,7 @@ mx_matmul_tiles_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             if (++st == kBigStages) { st = 0; ++turn; }
         }
         tc_commit_on(on, smem_u32(&bar_acc));
+        mbar_settle_warp(smem_u32(&bar_acc), 0, status);
     } else {
         // ---------------------------------------------------------------- epilogue
         const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
@@ -453,11 +444,11 @@ mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     if (warp == 0) {
         // ---------------------------------------------------------------- copies (both CTAs)
         const uint32_t on = elect_one();
-        int st = 0, turn = 0;
+        int it = 0, st = 0, turn = 0;
         bool ok = true;
         for (int i = pair; i < total && ok; i += pairs) {
             const int tt = i / n_w, tw = (i - tt * n_w) * 2 + rank;
-            for (int s = 0; s < stages; ++s) {
+            for (int s = 0; s < stages; ++s, ++it) {
                 if (turn) {
                     ok = mbar_wait_warp(smem_u32(&bar_empty[st]), (turn - 1) & 1, abort_p, status);
                     if (!ok) break;
@@ -473,9 +464,17 @@ mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 if (++st == kPairStages) { st = 0; ++turn; }
             }
         }
-        if (!ok) {                                                             // copies still under way land before the CTA ends
+        // The leader's barriers count both CTAs' copies, and the partner waits for the leader below.  Where one CTA gave up and
+        // the other did not, their last stages differ, and a barrier may count too little to wait for: then by the clock, a
+        // hundred times what a copy takes.
+        if (!ok) {
             const unsigned long long t0 = globaltimer_ns();
             while (globaltimer_ns() - t0 < 200000ull) {}
+        } else if (rank == 0) {
+            for (int q = max(0, it - kPairStages); q < it; ++q) {
+                int never = 0;
+                if (!__all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&bar_full[q % kPairStages]), (q / kPairStages) & 1, &never, status))) break;
+            }
         }
     } else if (warp == 1) {
         if (rank == 0) {
@@ -511,6 +510,7 @@ mx_matmul_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 }
                 tc_commit_pair_on(on, smem_u32(&bar_acc));
             }
+            if (k) mbar_settle_warp(smem_u32(&bar_acc), (k - 1) & 1, status);
         }
     } else {
         // ---------------------------------------------------------------- epilogue (both CTAs)

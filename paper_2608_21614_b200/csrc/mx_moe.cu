@@ -248,12 +248,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
             ++it;
             if (++st == F::kStages) { st = 0; ++turn; }
         }
-        if (!ok && lane == 0)                                                  // copies still under way land before the CTA ends
-            for (int q = max(0, it - F::kStages); q < it; ++q) {
-                abort_flag = 0;
-                mbar_wait(smem_u32(&bar_full[q % F::kStages]), (q / F::kStages) & 1, abort_p, a.status);
-                abort_flag = 1;
-            }
+        ring_settle_warp(bar_full, F::kStages, it, a.status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -297,6 +292,7 @@ mx_ffn_kernel(const __grid_constant__ MoeArgs a, const __grid_constant__ SlotTab
             tc_commit_on(on, smem_u32(&bar_acc[set]));
             ++n;
         }
+        if (n) mbar_settle_warp(smem_u32(&bar_acc[(n - 1) % F::kSets]), ((n - 1) / F::kSets) & 1, a.status);
     } else if (warp >= 2) {
         // ---------------------------------------------------------------- epilogue
         // Two groups of four warps (one per quarter of the lanes): with two sets of accumulators each group has its own

@@ -20,6 +20,18 @@ __device__ __forceinline__ uint32_t warp_uniform(uint32_t v) { return __shfl_syn
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
 }
+// At the end of the warps that issue copies and MMAs: whatever is under way lands before the CTA gives its shared and tensor
+// memory back, also where another warp has given up meanwhile.  Bounded as every wait; without an abort the barriers have
+// completed, or will before the epilogue has.
+__device__ __forceinline__ bool mbar_settle_warp(uint32_t bar, uint32_t parity, int* status) {
+    int never = 0;
+    return mbar_wait_warp(bar, parity, &never, status);
+}
+// The last `n_stage` of `issued` copies; the first that does not come, seconds later, ends it.
+__device__ __forceinline__ void ring_settle_warp(const uint64_t* full, int n_stage, int issued, int* status) {
+    for (int q = max(0, issued - n_stage); q < issued; ++q)
+        if (!mbar_settle_warp(smem_u32(&full[q % n_stage]), (q / n_stage) & 1, status)) break;
+}
 __device__ __forceinline__ void expect_tx_on(uint32_t on, uint32_t bar, uint32_t bytes) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"

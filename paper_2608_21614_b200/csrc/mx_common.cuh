@@ -48,6 +48,14 @@ __device__ __forceinline__ void mx_decode8(uint32_t w, uint32_t (&h)[4]) {
         "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
+// Sum of the two products of two bytes of codes (low with low, high with high).
+__device__ __forceinline__ float mx_dot2(uint32_t u, uint32_t v) {
+    uint32_t a, b;
+    asm("{\n\t.reg .b8 c;\n\tcvt.u8.u32 c, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(a) : "r"(u));
+    asm("{\n\t.reg .b8 c;\n\tcvt.u8.u32 c, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(b) : "r"(v));
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&a)), y = __half22float2(*reinterpret_cast<const __half2*>(&b));
+    return x.x * y.x + x.y * y.y;
+}
 // Eight fp32 values (already divided by the block's scale) to codes: nearest, ties to even, saturated at 6.
 __device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8]) {
     uint32_t w;

@@ -114,6 +114,14 @@ __device__ __forceinline__ void few_route(FewShared& s, const MxFewArgs& a, bool
     }
     few_sync();
 }
+// Where a warp gave up a wait: the copies and MMAs that are still under way, which take microseconds, land before the CTA
+// ends.  By the clock: waiting on their barriers, as the other 4-bit kernels do, makes every call longer by its code alone
+// (one token 0.25 us of 14.6 us).  Behind a barrier of the CTA.
+__device__ __forceinline__ void few_settle(const FewShared& s) {
+    if (!s.abort_flag) return;
+    const unsigned long long t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) {}
+}
 __device__ __forceinline__ void few_alloc(FewShared& s, uint32_t cols) {
     if (threadIdx.x >> 5 == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(cols));
@@ -181,12 +189,12 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
     if (warp == 0) {
         // ---------------------------------------------------------------- copies
         const uint32_t on = elect_one();
-        int it = 0, st = 0, turn = 0;
+        int st = 0, turn = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
             const int act = i / per, part = i - act * per, tile = HALF ? part >> 1 : part;
             const uint8_t* w = a.slot_region + (size_t)warp_uniform(s.slot[s.expert[act]]) * a.slot_bytes + (size_t)tile * nc * 2 * kMxBlockBytes;
-            for (int c = 0; c < nc; ++c, ++it, w += 2 * kMxBlockBytes) {
+            for (int c = 0; c < nc; ++c, w += 2 * kMxBlockBytes) {
                 if (turn) {
                     ok = mbar_wait_warp(smem_u32(&s.empty[st]), (turn - 1) & 1, abort_p, a.status);
                     if (!ok) break;
@@ -205,7 +213,6 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
                 if (++st == n) { st = 0; ++turn; }
             }
         }
-        ring_settle_warp(s.full, n, it, a.status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -253,7 +260,6 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
             }
             tc_commit_on(on, smem_u32(&s.acc[set]));
         }
-        if (k) mbar_settle_warp(smem_u32(&s.acc[(k - 1) & 1]), ((k - 1) >> 1) & 1, a.status);
     } else if (warp < 10) {
         split_x(mine + warp - 2, tasks);
         // ---------------------------------------------------------------- epilogue
@@ -285,50 +291,35 @@ mx_few_gate_up_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant
         }
     }
     __syncthreads();
+    few_settle(s);
     few_free(tmem, 512);
 }
 
 // One output of the down projection from its token's own experts alone, where the product over all active experts is NaN:
 // there an expert whose weights hold a NaN block reaches every token, since 0 * NaN is NaN.  Slow, and only for such outputs.
 // `row`: of the 128 rows of the column tile.
-__device__ __noinline__ float few_own_sum(const FewShared& s, const MxFewArgs& a, size_t tile, int tok, int row) {
-    const int nc = mx_chunks(a.f), blocks = a.f / kMxBlock, first = tok * 128;
+__device__ __forceinline__ float few_own_sum(const FewShared& s, const MxFewArgs& a, size_t tile, int tok, int row) {
+    const int nc = mx_chunks(a.f), blocks = a.f / kMxBlock;
+    auto power = [](int byte) { return __uint_as_float(byte ? (uint32_t)byte << 23 : 1u << 22); };   // 2^(byte - 127)
     float sum = 0.f;
 #pragma unroll 1
-    for (int act = 0; act < s.n_active; ++act) {
+    for (int i = 0; i < s.n_active * blocks; ++i) {
+        const int act = i / blocks, b = i - act * blocks, at = b & 7, half = (at >> 2) * kMxPiece + (at & 3);
         if (s.weight[act][tok] == kNotChosen) continue;
-        const uint8_t* w = a.slot_region + (size_t)s.slot[s.expert[act]] * a.slot_bytes + (mx_gate_up_blocks(a.d, a.f) + tile * nc) * kMxBlockBytes;
-        const uint8_t* h = a.h_tiles + (size_t)act * nc * FewTile::kBytes;
+        const uint8_t* w = a.slot_region + (size_t)s.slot[s.expert[act]] * a.slot_bytes + (mx_gate_up_blocks(a.d, a.f) + tile * nc + (b >> 3)) * kMxBlockBytes;
+        const uint8_t* h = a.h_tiles + ((size_t)act * nc + (b >> 3)) * FewTile::kBytes;
+        const int ws = w[kMxBlockCodes + half + (row & 31) * 16 + (row >> 5) * 4];
+        if (ws == 255 || h[FewTile::kN * 128 + half + tok * 16] == 255) return __uint_as_float(0x7FC00000u);
+        w += row * 128 + ((at ^ (row & 7)) << 4);
 #pragma unroll 1
-        for (int b = 0; b < blocks; ++b) {
-            const int at = b & 7, half = (at >> 2) * kMxPiece + (at & 3);       // of the 256 elements
-            const int ws = w[kMxBlockCodes + half + (row & 31) * 16 + (row >> 5) * 4];
-            if (ws == 255 || h[FewTile::kN * 128 + half + tok * 16] == 255) return __uint_as_float(0x7FC00000u);
-            const uint32_t* wc = reinterpret_cast<const uint32_t*>(w + row * 128 + ((at ^ (row & 7)) << 4));
+        for (int p = kPlanes - 1; p >= 0; --p) {
+            const int col = p * kFewTokens + tok;                              // below 64: one piece of scales
+            const uint8_t* c = h + col * 128 + ((at ^ tok) << 4);
+            float part = 0.f;                                                  // of 32 products of E2M1 values: exact
 #pragma unroll 1
-            for (int p = kPlanes - 1; p >= 0; --p) {
-                const int col = p * kFewTokens + tok;                          // below 64: one piece of scales
-                const int hs = h[FewTile::kN * 128 + half + (col & 31) * 16 + (col >> 5) * 4];
-                const uint32_t* hc = reinterpret_cast<const uint32_t*>(h + first + p * kFewTokens * 128 + ((at ^ tok) << 4));
-                float part = 0.f;                                              // of 32 products of E2M1 values: exact
-#pragma unroll 1
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t u[4], v[4];
-                    mx_decode8(wc[i], u);
-                    mx_decode8(hc[i], v);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u[q]));
-                        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v[q]));
-                        part += x.x * y.x + x.y * y.y;
-                    }
-                }
-                sum += ldexpf(part, ws + hs - 254);
-            }
-            if (at == 7) {
-                w += kMxBlockBytes;
-                h += FewTile::kBytes;
-            }
+            for (int q = 0; q < 16; ++q) part += mx_dot2(w[q], c[q]);
+            const int e = ws + h[FewTile::kN * 128 + half + (col & 31) * 16 + (col >> 5) * 4] - 254, e0 = e / 2;
+            sum += part * power(127 + e0) * power(127 + e - e0);               // in two steps: neither power leaves fp32's range
         }
     }
     return sum;
@@ -371,18 +362,15 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
         for (int q = q0; q < early; ++q) weights(q, q - q0);
         pdl_wait();
         pdl_launch_dependents();
-        bool ok = true;
-        int q = q0, st = 0, turn = 0;
-        for (; q < q1; ++q) {
+        int st = 0, turn = 0;
+        for (int q = q0; q < q1; ++q) {
             if (turn) {
-                ok = mbar_wait_warp(smem_u32(&s.empty[st]), (turn - 1) & 1, abort_p, a.status);
-                if (!ok) break;
+                if (!mbar_wait_warp(smem_u32(&s.empty[st]), (turn - 1) & 1, abort_p, a.status)) break;
                 weights(q, st);
             }
             bulk_g2s_on(on, base + st * kFewStageB + kMxBlockBytes, a.h_tiles + (size_t)q * FewTile::kBytes, FewTile::kBytes, smem_u32(&s.full[st]));
             if (++st == n) { st = 0; ++turn; }
         }
-        ring_settle_warp(s.full, n, q - q0, a.status);
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMA issue
         const uint32_t on = elect_one();
@@ -412,7 +400,6 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             if (++st == n) { st = 0; ++turn; }
         }
         tc_commit_on(on, smem_u32(&s.acc[0]));
-        mbar_settle_warp(smem_u32(&s.acc[0]), 0, a.status);
     } else if (warp < 6) {
         const int quad = warp & 3;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -438,11 +425,12 @@ mx_few_down_kernel(const __grid_constant__ MxFewArgs a, const __grid_constant__ 
             asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p[r]) : "r"(mapa_u32(smem_u32(&sums[col * kFewTokens + tok]), r)));
 #pragma unroll
         for (int r = 0; r < kFewSplit; ++r) v += p[r];
-        if (v != v) v = few_own_sum(s, a, tile, tok, col);
+        if (__builtin_expect(v != v, 0)) v = few_own_sum(s, a, tile, tok, col);
         const size_t at = (size_t)tok * a.d + tile * 128 + col;
         if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
         else static_cast<float*>(a.out)[at] = v;
     }
+    few_settle(s);
     __syncwarp();
     cluster_sync_all();                                                        // no CTA ends while another reads its sums
     few_free(tmem, 128);

@@ -197,7 +197,9 @@ __device__ __forceinline__ float at1(const uint8_t* p, int i) {
 }
 __device__ __forceinline__ const uint8_t* row_of(const void* p, size_t at, bool f32) { return static_cast<const uint8_t*>(p) + at * (f32 ? 4 : 2); }
 
-// Any rows: PER elements per thread, blockDim.x apart.
+// Any rows: PER elements per thread, blockDim.x apart.  8192 rows of 4095 columns, x fp32, y bf16, a gate per row: 92 us
+// (4096 columns, the kernel above: 63 us).  Elements are loaded one by one, the weights behind
+// the first sum.
 template <bool XF, bool YF, bool WF, int PER, bool WARP>
 __global__ void __launch_bounds__(kNormMaxThreads)
 block_norm_any_kernel(const __grid_constant__ NormArgs a) {

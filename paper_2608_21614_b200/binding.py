@@ -21,7 +21,7 @@ SAEM_ERR_NOT_RESIDENT, SAEM_ERR_SLOT_BUSY, SAEM_ERR_TIMEOUT, SAEM_ERR_CUDA, SAEM
 SAEM_MAX_EXPERTS = 128
 SAEM_TEMP = -2
 SAEM_HOST_MAPPED = -3
-SAEM_OUT_F32, SAEM_OUT_BF16 = 0, 1
+SAEM_OUT_F32, SAEM_OUT_BF16, SAEM_OUT_F16 = 0, 1, 2
 SAEM_FFN_AUTO, SAEM_FFN_SCALAR, SAEM_FFN_TENSOR, SAEM_FFN_TENSOR_PAIRS, SAEM_FFN_DECODE_FUSED = 0, 1, 2, 3, 4
 SAEM_FFN_MX = 5
 SAEM_GATE_NONE, SAEM_GATE_TOKEN, SAEM_GATE_CHANNEL, SAEM_GATE_FULL = 0, 1, 2, 3
@@ -38,6 +38,39 @@ class saem_norm_config(C.Structure):
                 [(n, C.c_int32) for n in ("cols", "x_dtype", "y_dtype", "n_dtype", "gate_dtype", "w_dtype", "gate_mode",
                                           "gate_sigmoid")] +
                 [(n, C.c_float) for n in ("eps", "residual_scale", "branch_scale")])
+
+
+SAEM_ATTEND_HEAD_BYTES = 8192
+
+
+class saem_rotary_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "rotary_dim", "interleaved")] + [(n, C.c_float) for n in ("eps", "amplitude")]
+
+
+class saem_rotate_config(C.Structure):
+    _fields_ = ([("rotary", saem_rotary_config)] + [(n, C.c_int32) for n in ("x_dtype", "out_dtype", "w_dtype", "heads")] +
+                [(n, C.c_int64) for n in ("tokens", "x_token_stride", "x_head_stride", "out_token_stride", "out_head_stride")])
+
+
+class saem_kv_cache(C.Structure):
+    _fields_ = ([("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_int64)] +
+                [(n, C.c_int32) for n in ("page_size", "kv_heads", "head_dim", "dtype")])
+
+
+class saem_batch(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("offsets", "lengths", "table")] + [("table_stride", C.c_int64)] +
+                [(n, C.c_int32) for n in ("seqs", "tokens", "max_pages", "max_new")])
+
+
+class saem_append_config(C.Structure):
+    _fields_ = ([("rotary", saem_rotary_config)] + [(n, C.c_int32) for n in ("q_heads", "x_dtype", "w_dtype")] +
+                [(n, C.c_int64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
+                                          "v_head_stride", "out_token_stride", "out_head_stride")])
+
+
+class saem_attend_config(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("q_heads", "causal", "window")] + [("scale", C.c_float)] +
+                [(n, C.c_int64) for n in ("q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride")])
 
 
 class SaemError(RuntimeError):
@@ -89,6 +122,10 @@ def _load() -> C.CDLL:
         "saem_mx_linear": (i32, [vp, i32, i64, i64, vp, vp, i64, i64, vp, i32, i64, vp, sz, vp]),
         "saem_mx_pack_expert": (i32, [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "saem_block_norm": (i32, [C.POINTER(saem_norm_config), vp, vp, vp, vp, vp, vp, vp, vp]),
+        "saem_rotate": (i32, [C.POINTER(saem_rotate_config), vp, vp, vp, vp, vp, vp]),
+        "saem_kv_append": (i32, [C.POINTER(saem_append_config), C.POINTER(saem_kv_cache), C.POINTER(saem_batch)] + [vp] * 10),
+        "saem_attend_workspace_bytes": (sz, [C.POINTER(saem_kv_cache)]),
+        "saem_attend": (i32, [C.POINTER(saem_attend_config), C.POINTER(saem_kv_cache), C.POINTER(saem_batch), vp, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -103,7 +140,8 @@ EXPORTS = ("saem_version saem_status_string saem_slot_bytes saem_slot_region_byt
            "saem_moe_step saem_moe_step_host saem_moe_step_host_async saem_step_buffer saem_cache_load saem_cache_evict saem_cache_map_host saem_cache_query "
            "saem_cache_wait saem_last_device_status saem_launch_count saem_expert_ffn_static saem_selftest_bounded_wait "
            "saem_mx_codes_bytes saem_mx_scales_bytes saem_mx_quantize saem_mx_dequantize saem_mx_matmul "
-           "saem_mx_linear_workspace_bytes saem_mx_linear saem_mx_pack_expert saem_block_norm").split()
+           "saem_mx_linear_workspace_bytes saem_mx_linear saem_mx_pack_expert saem_block_norm "
+           "saem_rotate saem_kv_append saem_attend_workspace_bytes saem_attend").split()
 
 
 def library_path() -> str:
@@ -385,6 +423,39 @@ def saem_block_norm(cfg: saem_norm_config, x, y, gate, w_post, w_pre, x_out, n_o
                                 _ptr(n_out), _stream(stream))
     if check:
         _check(code, "saem_block_norm")
+    return code
+
+
+def _ref(struct):
+    return None if struct is None else C.byref(struct)
+
+
+def saem_rotate(cfg: saem_rotate_config, x, w, turns, positions, out, stream=None, check=True) -> int:
+    code = _lib.saem_rotate(_ref(cfg), _ptr(x), _ptr(w), _ptr(turns), _ptr(positions), _ptr(out), _stream(stream))
+    if check:
+        _check(code, "saem_rotate")
+    return code
+
+
+def saem_kv_append(cfg: saem_append_config, cache: saem_kv_cache, batch: saem_batch, q, k, v, w_q, w_k, turns, positions, q_out,
+                   status=None, stream=None, check=True) -> int:
+    code = _lib.saem_kv_append(_ref(cfg), _ref(cache), _ref(batch), _ptr(q), _ptr(k), _ptr(v), _ptr(w_q), _ptr(w_k), _ptr(turns),
+                               _ptr(positions), _ptr(q_out), _ptr(status), _stream(stream))
+    if check:
+        _check(code, "saem_kv_append")
+    return code
+
+
+def saem_attend_workspace_bytes(cache: saem_kv_cache) -> int:
+    return _lib.saem_attend_workspace_bytes(_ref(cache))
+
+
+def saem_attend(cfg: saem_attend_config, cache: saem_kv_cache, batch: saem_batch, q, out, lse, workspace, workspace_bytes, stream=None,
+                check=True) -> int:
+    code = _lib.saem_attend(_ref(cfg), _ref(cache), _ref(batch), _ptr(q), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes,
+                            _stream(stream))
+    if check:
+        _check(code, "saem_attend")
     return code
 
 

@@ -1,0 +1,350 @@
+// Attention of new tokens over a paged cache: o = sum_j softmax_j(scale q.k_j) v_j.  The form for few rows per key head, and the call.
+//
+// attend_rows_kernel: tiles of 16 rows (a decoding sequence's query heads that share a key head; further tokens are further rows) by
+// mma.sync m16n8k16.  With so few rows every key and value is used for little arithmetic and the bound is the cache's bytes, so that what
+// counts is how many of them are under way: each of a CTA's 8 warps takes every eighth chunk of 16 places through a ring of
+// its own in shared memory (cp.async, no barrier between warps), with its own running maximum, sum and output; they meet at
+// the end of an item.  tcgen05 takes 128 rows at least, of which a decoding sequence fills 4 or 8, and its results would have to
+// cross tensor memory twice for each tile.
+#include "attend_plan.cuh"
+#include "tc_common.cuh"
+
+namespace saem {
+
+constexpr int kRowsWarps = 8, kRowsThreads = kRowsWarps * 32;
+constexpr int kRowsR = 16, kRowsKeys = 16;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// DK: head_dim rounded up to 64 or 128.
+template <int DK>
+struct RowsShape {
+    static constexpr int kRow = DK * 2;                             // bytes of a place in shared memory
+    static constexpr int kStage = 2 * kRowsKeys * kRow;             // keys, then values
+    static constexpr int kStages = DK == 128 ? 3 : 6;
+    static constexpr int kRing = kRowsWarps * kStages * kStage;     // 192 KB
+    static constexpr int kSlot = kRowsR * (DK + 2);                 // floats of a partial result: maximum, sum, output
+    static_assert(kRowsWarps * kSlot * 4 <= kRing, "");
+};
+
+template <bool F16, int DK>
+__global__ void __launch_bounds__(kRowsThreads, 1)
+attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+    using Shape = RowsShape<DK>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ AttendPlan plan;
+    __shared__ int last_s;
+    __shared__ uint32_t nan_s;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    make_plan<kRowsR, kRowsKeys, kRowsWarps>(a, plan, kRowsWarps);
+    AttendWalk<kRowsR, kRowsKeys> walk;
+    walk.begin(a, plan);
+    const uint32_t ring = smem_u32(smem) + warp * Shape::kStages * Shape::kStage;
+    float* const meet = reinterpret_cast<float*>(smem);             // [warp][kSlot], once the rings are done with
+    const int quad = lane >> 2, two = (lane & 3) * 2;
+    const int n_k = (a.dim + 15) / 16;                              // steps of 16 of head_dim
+
+    AttendPart p;
+    while (walk.next(a, p)) {
+        // ---- this warp's chunks: key_begin + warp + 8 i
+        const int n_chunk = max(0, (p.key_end - p.key_begin - warp + kRowsWarps - 1) / kRowsWarps);
+        int pages = -1;                                             // lane l: page of chunk l of the 32 at hand
+        bool bad = false;
+        auto look_up = [&](int i0) {
+            const int i = i0 + lane;
+            pages = -1;
+            if (i < n_chunk) {
+                const long long place = (long long)(p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
+                pages = a.table[p.s * a.table_stride + place / a.page_size];
+                if (pages < 0 || pages >= a.pages) { pages = -1; bad = true; }
+            }
+        };
+        auto request = [&](int i) {
+            if (i < n_chunk) {
+                if (i % 32 == 0) look_up(i);
+                const int page = __shfl_sync(0xffffffffu, pages, i % 32);
+                const long long place = (long long)(p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
+                const long long from = page < 0 ? 0 : (((long long)page * a.kv_heads + p.h) * a.page_size + place % a.page_size) * a.dim * 2;
+                const int valid = page < 0 ? 0 : (int)min((long long)kRowsKeys, p.e.len - place);
+                const uint32_t to = ring + i % Shape::kStages * Shape::kStage;
+                constexpr int kPieces = DK / 8;                     // 16-byte pieces of a place
+#pragma unroll
+                for (int j = 0; j < kRowsKeys * kPieces / 32; ++j) {
+                    const int u = lane + 32 * j, row = u / kPieces, c = u % kPieces;
+                    const bool in = row < valid && c * 8 < a.dim;
+                    const long long off = in ? from + ((long long)row * a.dim + c * 8) * 2 : 0;
+                    const uint32_t at = to + row * Shape::kRow + ((c ^ (row & 7)) << 4);
+                    cp_async16(at, a.k + off, in ? 16 : 0);
+                    cp_async16(at + kRowsKeys * Shape::kRow, a.v + off, in ? 16 : 0);
+                }
+            }
+            cp_async_commit();
+        };
+#pragma unroll
+        for (int i = 0; i < Shape::kStages - 1; ++i) request(i);
+
+        // ---- queries, as the A operand; the bounds of the lane's two rows
+        const long long row0 = (long long)p.r * kRowsR;
+        uint32_t qf[DK / 16][4];
+        int lo[2], hi[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int row = quad + 8 * b;
+            const bool in = row < p.rows;
+            const long long token = p.e.first + (row0 + row) / a.group, head = (long long)p.h * a.group + (row0 + row) % a.group;
+            const uint8_t* q = a.q + (token * a.q_ts + head * a.q_hs) * 2;
+            row_bounds(a, p.e, row0 + row, in, lo[b], hi[b]);
+#pragma unroll
+            for (int k = 0; k < DK / 16; ++k)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int col = k * 16 + c * 8 + two;
+                    qf[k][b + 2 * c] = in && col < a.dim ? *reinterpret_cast<const uint32_t*>(q + col * 2) : 0u;
+                }
+        }
+        float o[DK / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DK / 8; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] = 0.f;
+
+        for (int i = 0; i < n_chunk; ++i) {
+            __syncwarp();                                           // the stage that the next request overwrites is read
+            request(i + Shape::kStages - 1);
+            cp_async_wait<Shape::kStages - 1>();
+            __syncwarp();
+            const uint32_t kt = ring + i % Shape::kStages * Shape::kStage, vt = kt + kRowsKeys * Shape::kRow;
+            float sc[2][4] = {};
+#pragma unroll
+            for (int k = 0; k < DK / 16; ++k) {
+                if (k < n_k) {
+                    // matrices: places 0-7 and elements 0-7, places 0-7 and 8-15, places 8-15 and 0-7, places 8-15 and 8-15
+                    const int row = (lane & 7) + (lane >> 4) * 8, c = 2 * k + ((lane >> 3) & 1);
+                    uint32_t f[4];
+                    ldmatrix4(f, kt + row * Shape::kRow + ((c ^ (row & 7)) << 4));
+                    mma16816<F16>(sc[0], qf[k], f[0], f[1]);
+                    mma16816<F16>(sc[1], qf[k], f[2], f[3]);
+                }
+            }
+            const int place = (p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
+            float mx[2] = {m[0], m[1]};
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = place + t * 8 + two + (e & 1), b = e >> 1;
+                    sc[t][e] = j >= lo[b] && j <= hi[b] ? sc[t][e] * a.scale_log2 : -INFINITY;
+                    mx[b] = fmaxf(mx[b], sc[t][e]);
+                }
+            float was[2], base[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
+                mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
+                base[b] = mx[b] == -INFINITY ? 0.f : mx[b];
+                was[b] = exp2f(m[b] - base[b]);
+                m[b] = mx[b];
+                l[b] *= was[b];
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[t][e] = exp2f(sc[t][e] - base[e >> 1]);
+                    l[e >> 1] += sc[t][e];
+                }
+            if (__any_sync(0xffffffffu, was[0] != 1.f || was[1] != 1.f)) {
+#pragma unroll
+                for (int d = 0; d < DK / 8; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[d][e] *= was[e >> 1];
+            }
+            const uint32_t w[4] = {pack2<F16>(sc[0][0], sc[0][1]), pack2<F16>(sc[0][2], sc[0][3]), pack2<F16>(sc[1][0], sc[1][1]), pack2<F16>(sc[1][2], sc[1][3])};
+#pragma unroll
+            for (int k = 0; k < DK / 16; ++k) {
+                if (k < n_k) {
+                    // transposed: places 0-7 and 8-15 of elements 16k .. 16k + 7, then of the eight behind them
+                    const int row = (lane & 7) + ((lane >> 3) & 1) * 8, c = 2 * k + (lane >> 4);
+                    uint32_t f[4];
+                    ldmatrix4_t(f, vt + row * Shape::kRow + ((c ^ (row & 7)) << 4));
+                    mma16816<F16>(o[2 * k], w, f[0], f[1]);
+                    mma16816<F16>(o[2 * k + 1], w, f[2], f[3]);
+                }
+            }
+        }
+        cp_async_wait<0>();
+        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            l[b] += __shfl_xor_sync(0xffffffffu, l[b], 1);
+            l[b] += __shfl_xor_sync(0xffffffffu, l[b], 2);
+        }
+
+        // ---- the warps meet: [0..15] maxima, [16..31] sums, then rows of outputs
+        __syncthreads();
+        float* const mine = meet + warp * Shape::kSlot;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int row = quad + 8 * b;
+            if (row < p.rows) {
+                if (two == 0) { mine[row] = m[b]; mine[kRowsR + row] = l[b]; }
+#pragma unroll
+                for (int d = 0; d < DK / 8; ++d)
+                    *reinterpret_cast<float2*>(mine + 2 * kRowsR + row * DK + d * 8 + two) = make_float2(o[d][2 * b], o[d][2 * b + 1]);
+            }
+        }
+        if (threadIdx.x == 0) nan_s = 0;
+        __syncthreads();
+        // n parts, `apart` floats from one to the next, read by `at`: four elements of a row, its maximum and its sum
+        auto join = [&](auto at, const float* from, const float* rest, int n, size_t apart, int row, int col, float (&v)[4], float& mx, float& sum) {
+            mx = -INFINITY;
+            for (int j = 0; j < n; ++j) mx = fmaxf(mx, at((j ? rest + j * apart : from) + row));
+            const float base = mx == -INFINITY ? 0.f : mx;
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = 0.f;
+            for (int j = 0; j < n; ++j) {
+                const float* f = j ? rest + j * apart : from;
+                const float w = exp2f(at(f + row) - base);
+                sum += w * at(f + kRowsR + row);
+                const float4 x = at(reinterpret_cast<const float4*>(f + 2 * kRowsR + row * DK + col));
+                v[0] = fmaf(w, x.x, v[0]); v[1] = fmaf(w, x.y, v[1]); v[2] = fmaf(w, x.z, v[2]); v[3] = fmaf(w, x.w, v[3]);
+            }
+        };
+        auto finish = [&](int row, int col, const float (&v)[4], float mx, float sum) {
+            const long long token = p.e.first + (row0 + row) / a.group, head = (long long)p.h * a.group + (row0 + row) % a.group;
+            const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+            const float x[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+            if (x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]) atomicOr(&nan_s, 1u << row);
+            if (col < a.dim)
+                *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + col) * 2) = make_uint2(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]));
+            if (a.lse && col == 0) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
+        };
+        constexpr int kCols = DK / 4, kPerRow = kRowsThreads / kCols;
+        const int col = threadIdx.x % kCols * 4;
+        bool done = p.whole;
+        float* const slot = a.partials + (size_t)p.slot * Shape::kSlot;
+        for (int row = threadIdx.x / kCols; row < p.rows; row += kPerRow) {
+            float v[4], mx, sum;
+            join([](auto* f) { return *f; }, meet, meet, kRowsWarps, Shape::kSlot, row, col, v, mx, sum);
+            if (p.whole) finish(row, col, v, mx, sum);
+            else {
+                if (col == 0) { __stcg(slot + row, mx); __stcg(slot + kRowsR + row, sum); }
+                __stcg(reinterpret_cast<float4*>(slot + 2 * kRowsR + row * DK + col), make_float4(v[0], v[1], v[2], v[3]));
+            }
+        }
+        if (!p.whole) {
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                last_s = atomicAdd(a.counters + p.first_cta, 1) == p.n_parts - 1;
+                if (last_s) a.counters[p.first_cta] = 0;
+            }
+            __syncthreads();
+            if (last_s) {
+                __threadfence();
+                done = true;
+                const float* first = a.partials + (size_t)p.first_slot * Shape::kSlot;
+                const float* rest = a.partials + (size_t)(2 * p.first_cta) * Shape::kSlot;
+                for (int row = threadIdx.x / kCols; row < p.rows; row += kPerRow) {
+                    float v[4], mx, sum;
+                    join([](auto* f) { return __ldcg(f); }, first, rest, p.n_parts, 2 * Shape::kSlot, row, col, v, mx, sum);
+                    finish(row, col, v, mx, sum);
+                }
+            }
+        }
+        __syncthreads();
+        if (done && nan_s)
+            for (int row = warp; row < p.rows; row += kRowsWarps)
+                if (nan_s >> row & 1) attend_row_again<F16>(a, p.e, p.s, p.h, row0 + row);
+        __syncthreads();
+    }
+}
+
+static size_t rows_partials(int n_sm) { return (size_t)2 * n_sm * RowsShape<kHeadDimMax>::kSlot * 4; }
+
+template <bool F16, int DK>
+static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t st) {
+    static DeviceOnce once;
+    const cudaError_t e = once_on_device(once, [] {
+        return cudaFuncSetAttribute(attend_rows_kernel<F16, DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DK>::kRing);
+    });
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attend_rows_kernel<F16, DK>, dim3(n_sm), dim3(kRowsThreads), RowsShape<DK>::kRing, st, a);
+}
+static cudaError_t launch_rows(const AttendArgs& a, bool f16, int n_sm, cudaStream_t st) {
+    if (a.dim <= 64) return f16 ? launch_rows_typed<true, 64>(a, n_sm, st) : launch_rows_typed<false, 64>(a, n_sm, st);
+    return f16 ? launch_rows_typed<true, 128>(a, n_sm, st) : launch_rows_typed<false, 128>(a, n_sm, st);
+}
+
+}  // namespace saem
+
+using namespace saem;
+
+extern "C" size_t saem_attend_workspace_bytes(const saem_kv_cache* c) {
+    int n_sm;
+    if (!c) return 0;
+    const int r = cache_status(*c);
+    if (r != SAEM_OK || sm_count(&n_sm) != cudaSuccess || n_sm > kAttendMaxCtas) return 0;
+    return SAEM_ATTEND_HEAD_BYTES + rows_partials(n_sm);
+}
+
+extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cache, const saem_batch* b, const void* q, void* out,
+                           float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!c || !cache || !b) return SAEM_ERR_INVALID_ARG;
+    int r = cache_status(*cache);
+    if (r == SAEM_OK) r = batch_shape(*b);
+    if (r != SAEM_OK) return r;
+    if (!(c->scale > 0.f) || !isfinite(c->scale)) return SAEM_ERR_INVALID_ARG;
+    if (c->q_heads < 1 || c->q_heads % cache->kv_heads || c->q_heads / cache->kv_heads > 128 || c->window < 0 || b->tokens > 0x7FFFFFFF / c->q_heads)
+        return SAEM_ERR_SHAPE;
+    if (b->tokens == 0 || b->seqs == 0) return SAEM_OK;
+    r = batch_status(*b);
+    if (r != SAEM_OK) return r;
+    if (!q || !out || !workspace) return SAEM_ERR_INVALID_ARG;
+    const int64_t strides[4] = {b->tokens > 1 ? c->q_token_stride : 0, c->q_heads > 1 ? c->q_head_stride : 0,
+                                b->tokens > 1 ? c->out_token_stride : 0, c->q_heads > 1 ? c->out_head_stride : 0};
+    if (strides[0] < 0 || strides[1] < 0 || !heads_apart(b->tokens, c->q_heads, cache->head_dim, c->out_token_stride, c->out_head_stride)) return SAEM_ERR_SHAPE;
+    if (((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)lse % 4 || (uintptr_t)workspace % 1024) return SAEM_ERR_ALIGNMENT;
+    for (int64_t s : strides)
+        if (s % 8) return SAEM_ERR_ALIGNMENT;
+    int n_sm;
+    if (sm_count(&n_sm) != cudaSuccess || n_sm > kAttendMaxCtas) return SAEM_ERR_CUDA;
+    if (workspace_bytes < SAEM_ATTEND_HEAD_BYTES + rows_partials(n_sm)) return SAEM_ERR_WORKSPACE;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    AttendArgs a = {};
+    a.q = static_cast<const uint8_t*>(q); a.out = static_cast<uint8_t*>(out); a.lse = lse;
+    a.q_ts = strides[0]; a.q_hs = strides[1]; a.out_ts = strides[2]; a.out_hs = strides[3];
+    a.k = static_cast<const uint8_t*>(cache->k); a.v = static_cast<const uint8_t*>(cache->v);
+    a.pages = cache->pages; a.page_size = cache->page_size; a.kv_heads = cache->kv_heads; a.dim = cache->head_dim;
+    a.group = c->q_heads / cache->kv_heads;
+    a.offsets = b->offsets; a.lengths = b->lengths; a.table = b->table; a.table_stride = b->table_stride;
+    a.seqs = b->seqs; a.tokens = b->tokens; a.max_pages = b->max_pages;
+    a.causal = c->causal != 0; a.window = c->window; a.scale = c->scale; a.scale_log2 = c->scale * 1.4426950408889634f;
+    a.status = reinterpret_cast<int*>(ws);
+    a.counters = reinterpret_cast<int*>(ws + kAttendCounters);
+    a.partials = reinterpret_cast<float*>(ws + SAEM_ATTEND_HEAD_BYTES);
+    return launch_rows(a, cache->dtype == SAEM_OUT_F16, n_sm, (cudaStream_t)stream) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+}

@@ -1,0 +1,281 @@
+// How the work of an attention call is dealt out, on the device alone: lengths, offsets and pages are never read on the host.
+//
+// An item is a tile of R rows of one sequence and one key head (row = token * group + query head within the group); its units are the
+// tiles of KEYS places that any of its rows may see, one at least, so that rows that see nothing are written too.  All units of
+// a call, in the order sequence, key head, row tile, are cut into as many equal ranges as there are CTAs: long and short
+// sequences, few and many rows load the SMs alike.  An item that is cut leaves sums of its parts in the workspace, and the CTA that
+// arrives last adds them up in the order of the parts, so that two runs give the same bits.
+#ifndef SAEM_ATTEND_PLAN_CUH_
+#define SAEM_ATTEND_PLAN_CUH_
+
+#include "attend_common.cuh"
+
+namespace saem {
+
+constexpr int kAttendMaxCtas = 640;         // SMs x CTAs per SM at most
+
+struct AttendArgs {
+    const uint8_t* q;
+    uint8_t* out;
+    float* lse;
+    long long q_ts, q_hs, out_ts, out_hs;   // strides in elements
+    const uint8_t* k;
+    const uint8_t* v;
+    long long pages;
+    int page_size, kv_heads, dim, group;
+    const int32_t* offsets;
+    const int32_t* lengths;
+    const int32_t* table;
+    long long table_stride;
+    int seqs, tokens, max_pages;
+    int causal, window;
+    float scale, scale_log2;                // scale * log2(e)
+    int* status;
+    int* counters;                          // [kAttendMaxCtas], zero between calls
+    float* partials;                        // two slots per CTA
+};
+constexpr size_t kAttendCounters = 256;     // byte offset of the counters in the workspace
+static_assert(kAttendCounters + 4 * kAttendMaxCtas <= SAEM_ATTEND_HEAD_BYTES, "");
+
+struct SeqExtent {
+    int first, n, len;                      // first row of the call's tokens, new tokens, places
+};
+__device__ __forceinline__ SeqExtent seq_extent(const AttendArgs& a, int s) {
+    const int lo = min(max(a.offsets[s], 0), a.tokens), hi = min(max(a.offsets[s + 1], lo), a.tokens);
+    const long long most = (long long)a.max_pages * a.page_size;
+    return {lo, hi - lo, (int)min((long long)max(a.lengths[s], 0), most)};
+}
+// The places that rows [row0, row1] may see, in tiles of KEYS.
+template <int KEYS>
+__device__ __forceinline__ void key_tiles(const AttendArgs& a, const SeqExtent& e, long long row0, long long row1, int& begin, int& end) {
+    const long long i0 = row0 / a.group, i1 = row1 / a.group;
+    const long long stop = a.causal ? min((long long)e.len, e.len - e.n + i1 + 1) : e.len;
+    const long long start = a.window ? max(0ll, e.len - e.n + i0 - a.window + 1) : 0;
+    begin = (int)(start / KEYS);
+    end = stop > start ? (int)((stop + KEYS - 1) / KEYS) : begin;
+}
+template <int R>
+__device__ __forceinline__ int row_tiles(const AttendArgs& a, const SeqExtent& e) { return (int)(((long long)e.n * a.group + R - 1) / R); }
+template <int R, int KEYS>
+__device__ __forceinline__ int item_units(const AttendArgs& a, const SeqExtent& e, int r) {
+    int b, t;
+    const long long rows = (long long)e.n * a.group;
+    key_tiles<KEYS>(a, e, (long long)r * R, min(rows, (long long)(r + 1) * R) - 1, b, t);
+    return max(1, t - b);
+}
+
+struct AttendPlan {                         // in shared memory
+    long long total, begin, end;            // units of the call, and this CTA's range
+    long long seq_begin;                    // unit at which sequence s begins
+    int s;
+    int ctas;                               // CTAs that have a range
+    long long scan[32];
+};
+
+// All threads of the CTA (WARPS whole warps); MIN_UNITS: a CTA takes no fewer units while there are others.
+template <int R, int KEYS, int WARPS>
+__device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p, int min_units) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kStep = WARPS * 32;
+    auto units_of = [&](int s) -> long long {
+        // a lane per sequence; the row tiles of a sequence with more than one are shared out over the warp
+        const bool in = s < a.seqs;
+        const SeqExtent e = in ? seq_extent(a, s) : SeqExtent{0, 0, 0};
+        const int tiles = row_tiles<R>(a, e);
+        long long u = tiles == 1 ? item_units<R, KEYS>(a, e, 0) : 0;
+        for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 1); many; many &= many - 1) {
+            const int src = __ffs(many) - 1;
+            const SeqExtent o = {0, __shfl_sync(0xffffffffu, e.n, src), __shfl_sync(0xffffffffu, e.len, src)};
+            const int t = __shfl_sync(0xffffffffu, tiles, src);
+            long long sum = 0;
+            for (int r = lane; r < t; r += 32) sum += item_units<R, KEYS>(a, o, r);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (lane == src) u = sum;
+        }
+        return u * a.kv_heads;
+    };
+    long long mine = units_of(warp * 32 + lane), sum = mine;
+    for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += units_of(s + lane);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane == 0) p.scan[warp] = sum;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) total += p.scan[w];
+    const long long most = (total + min_units - 1) / min_units;
+    const int ctas = (int)max(1ll, min((long long)gridDim.x, most));
+    const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : total, end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
+    if (threadIdx.x == 0) {
+        p.total = total; p.begin = begin; p.end = end; p.ctas = ctas;
+        p.s = a.seqs; p.seq_begin = total;
+    }
+    __syncthreads();
+    if (begin >= end) return;
+    long long before = 0;
+    for (int s0 = 0; s0 < a.seqs; s0 += kStep) {
+        const int s = s0 + warp * 32 + lane;
+        if (s0) mine = units_of(s);
+        long long incl = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 31) p.scan[warp] = incl;
+        __syncthreads();
+        long long base = before;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            if (w < warp) base += p.scan[w];
+            before += p.scan[w];
+        }
+        if (base + incl - mine <= begin && begin < base + incl) { p.s = s; p.seq_begin = base + incl - mine; }
+        __syncthreads();
+        if (before > begin) break;
+    }
+}
+
+// A part of an item: what one CTA does of it between two looks at the plan.
+struct AttendPart {
+    SeqExtent e;
+    int s, h, r;
+    int rows;                               // of the tile
+    int key_begin, key_end;                 // tiles of KEYS places; none where the rows see nothing
+    bool whole;                             // the item is not cut
+    int first_cta, n_parts, part, slot;     // where it is: which of the parts this is, and its place in the workspace
+    int first_slot;                         // the first part's place; part j has 2 * (first_cta + j)
+};
+// Walks through a CTA's range; every warp for itself, alike in all lanes.
+template <int R, int KEYS>
+struct AttendWalk {
+    long long at, end, item;                // next unit, end of the range, first unit of the item at hand
+    long long total;
+    int ctas;
+    int s, h, r, tiles;
+    SeqExtent e;
+    __device__ __forceinline__ void begin(const AttendArgs& a, const AttendPlan& p) {
+        at = p.begin; end = p.end; total = p.total; ctas = p.ctas; s = p.s;
+        if (at >= end) return;
+        e = seq_extent(a, s);
+        tiles = row_tiles<R>(a, e);
+        item = p.seq_begin;
+        // the item that holds the range's first unit: the head by division, the row tile by a warp's scan
+        const int lane = threadIdx.x & 31;
+        long long per_head = 0;
+        for (int t = lane; t < tiles; t += 32) per_head += item_units<R, KEYS>(a, e, t);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) per_head += __shfl_xor_sync(0xffffffffu, per_head, d);
+        h = (int)((at - item) / per_head);
+        item += h * per_head;
+        r = 0;
+        for (int t0 = 0; t0 < tiles; t0 += 32) {
+            const int u = t0 + lane < tiles ? item_units<R, KEYS>(a, e, t0 + lane) : 0;
+            int incl = u;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += o;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, item + incl > at);
+            if (past) {
+                const int l = __ffs(past) - 1;
+                r = t0 + l;
+                item += __shfl_sync(0xffffffffu, incl - u, l);
+                break;
+            }
+            item += __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    __device__ __forceinline__ bool next(const AttendArgs& a, AttendPart& p) {
+        if (at >= end) return false;
+        const long long rows = (long long)e.n * a.group, row0 = (long long)r * R, row1 = min(rows, row0 + R) - 1;
+        int b, t;
+        key_tiles<KEYS>(a, e, row0, row1, b, t);
+        const int units = max(1, t - b);
+        const long long stop = min(end, item + units);
+        p.e = e; p.s = s; p.h = h; p.r = r;
+        p.rows = (int)(row1 - row0 + 1);
+        p.key_begin = b + (int)(at - item);
+        p.key_end = min(t, b + (int)(stop - item));
+        p.whole = at == item && stop == item + units;
+        if (!p.whole) {
+            const int me = blockIdx.x;
+            p.first_cta = (int)(((item + 1) * ctas - 1) / total);
+            p.n_parts = (int)(((item + units) * ctas - 1) / total) - p.first_cta + 1;
+            p.part = me - p.first_cta;
+            p.first_slot = 2 * p.first_cta + (item > total * p.first_cta / ctas ? 1 : 0);
+            p.slot = p.part ? 2 * me : p.first_slot;
+        }
+        at = stop;
+        if (stop == item + units) {
+            item = stop;
+            if (++r == tiles) {
+                r = 0;
+                if (++h == a.kv_heads) {
+                    h = 0;
+                    e.n = 0;                        // some later sequence has the units that are left, if any are
+                    while (at < end && e.n == 0) {
+                        if (++s < a.seqs) e = seq_extent(a, s);
+                        else at = end;
+                    }
+                    tiles = row_tiles<R>(a, e);
+                }
+            }
+        }
+        return true;
+    }
+};
+
+// The rows' bounds: row (of the item) sees places lo .. hi.
+__device__ __forceinline__ void row_bounds(const AttendArgs& a, const SeqExtent& e, long long row, bool in, int& lo, int& hi) {
+    const long long place = e.len - e.n + row / a.group;
+    hi = !in ? -1 : (int)(a.causal ? min((long long)e.len - 1, place) : e.len - 1);
+    lo = a.window ? (int)max(0ll, place - a.window + 1) : 0;
+}
+
+// One row over again, by one warp, out of the cache and the places that it sees alone: for rows whose result is NaN.  In a product of
+// tiles a weight of 0 meets what other rows see, and 0 times an infinity or NaN there is NaN.
+template <bool F16>
+__device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExtent& e, int s, int h, long long row) {
+    const int lane = threadIdx.x & 31, at = lane * 4;
+    const bool here = at < a.dim;
+    int lo, hi;
+    row_bounds(a, e, row, true, lo, hi);
+    const long long token = e.first + row / a.group, head = (long long)h * a.group + row % a.group;
+    float q[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
+    auto four = [&](const uint8_t* p, long long i, float* v) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p + i * 2);
+        const float2 x = unpack2<F16>(w.x), y = unpack2<F16>(w.y);
+        v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
+    };
+    if (here) four(a.q, token * a.q_ts + head * a.q_hs + at, q);
+    for (int j = lo; j <= hi; ++j) {
+        const int page = a.table[s * a.table_stride + j / a.page_size];
+        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (here && page >= 0 && page < a.pages) {
+            const long long i = (((long long)page * a.kv_heads + h) * a.page_size + j % a.page_size) * a.dim + at;
+            four(a.k, i, k);
+            four(a.v, i, v);
+        }
+        float d = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
+        d *= a.scale_log2;
+        const float mn = fmaxf(m, d), base = mn == -INFINITY ? 0.f : mn, was = exp2f(m - base), p = exp2f(d - base);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(p, v[i], o[i] * was);
+        l = l * was + p;
+        m = mn;
+    }
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    if (here) {
+        const uint2 w = make_uint2(pack2<F16>(o[0] * inv, o[1] * inv), pack2<F16>(o[2] * inv, o[3] * inv));
+        *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + at) * 2) = w;
+    }
+}
+
+}  // namespace saem
+
+#endif  // SAEM_ATTEND_PLAN_CUH_

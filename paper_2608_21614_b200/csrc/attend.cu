@@ -11,8 +11,9 @@
 
 namespace saem {
 
-constexpr int kRowsWarps = 8, kRowsThreads = kRowsWarps * 32;
-constexpr int kRowsR = 16, kRowsKeys = 16;
+constexpr int kRowsWarps = 4, kRowsThreads = kRowsWarps * 32;
+constexpr int kRowsR = 16, kRowsKeys = 16, kRowsHead = 8;
+constexpr int kRowsPerSm = 2;               // CTAs
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -48,7 +49,7 @@ struct RowsShape {
 };
 
 template <bool F16, int DK>
-__global__ void __launch_bounds__(kRowsThreads, 1)
+__global__ void __launch_bounds__(kRowsThreads, kRowsPerSm)
 attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     using Shape = RowsShape<DK>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -58,8 +59,8 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    make_plan<kRowsR, kRowsKeys, kRowsWarps>(a, plan, kRowsWarps);
-    AttendWalk<kRowsR, kRowsKeys> walk;
+    make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsWarps>(a, plan, kRowsHead);
+    AttendWalk<kRowsR, kRowsKeys, kRowsHead> walk;
     walk.begin(a, plan);
     const uint32_t ring = smem_u32(smem) + warp * Shape::kStages * Shape::kStage;
     float* const meet = reinterpret_cast<float*>(smem);             // [warp][kSlot], once the rings are done with
@@ -68,62 +69,61 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 
     AttendPart p;
     while (walk.next(a, p)) {
-        // ---- this warp's chunks: key_begin + warp + 8 i
+        // ---- this warp's chunks: key_begin + warp + kRowsWarps * i
         const int n_chunk = max(0, (p.key_end - p.key_begin - warp + kRowsWarps - 1) / kRowsWarps);
+        const int32_t* const table = a.table + p.s * a.table_stride;
         int pages = -1;                                             // lane l: page of chunk l of the 32 at hand
         bool bad = false;
-        auto look_up = [&](int i0) {
-            const int i = i0 + lane;
+        auto look_up = [&](int i) {
             pages = -1;
-            if (i < n_chunk) {
-                const long long place = (long long)(p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
-                pages = a.table[p.s * a.table_stride + place / a.page_size];
-                if (pages < 0 || pages >= a.pages) { pages = -1; bad = true; }
-            }
+            if (i < n_chunk) pages = table[quotient((p.key_begin + warp + kRowsWarps * i) * kRowsKeys, a.by_page)];
         };
-        auto request = [&](int i) {
-            if (i < n_chunk) {
-                if (i % 32 == 0) look_up(i);
-                const int page = __shfl_sync(0xffffffffu, pages, i % 32);
-                const long long place = (long long)(p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
-                const long long from = page < 0 ? 0 : (((long long)page * a.kv_heads + p.h) * a.page_size + place % a.page_size) * a.dim * 2;
-                const int valid = page < 0 ? 0 : (int)min((long long)kRowsKeys, p.e.len - place);
-                const uint32_t to = ring + i % Shape::kStages * Shape::kStage;
-                constexpr int kPieces = DK / 8;                     // 16-byte pieces of a place
-#pragma unroll
-                for (int j = 0; j < kRowsKeys * kPieces / 32; ++j) {
-                    const int u = lane + 32 * j, row = u / kPieces, c = u % kPieces;
-                    const bool in = row < valid && c * 8 < a.dim;
-                    const long long off = in ? from + ((long long)row * a.dim + c * 8) * 2 : 0;
-                    const uint32_t at = to + row * Shape::kRow + ((c ^ (row & 7)) << 4);
-                    cp_async16(at, a.k + off, in ? 16 : 0);
-                    cp_async16(at + kRowsKeys * Shape::kRow, a.v + off, in ? 16 : 0);
-                }
-            }
-            cp_async_commit();
-        };
-#pragma unroll
-        for (int i = 0; i < Shape::kStages - 1; ++i) request(i);
-
+        look_up(lane);
         // ---- queries, as the A operand; the bounds of the lane's two rows
-        const long long row0 = (long long)p.r * kRowsR;
+        const int row0 = p.r * kRowsR;
         uint32_t qf[DK / 16][4];
         int lo[2], hi[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const int row = quad + 8 * b;
-            const bool in = row < p.rows;
-            const long long token = p.e.first + (row0 + row) / a.group, head = (long long)p.h * a.group + (row0 + row) % a.group;
-            const uint8_t* q = a.q + (token * a.q_ts + head * a.q_hs) * 2;
-            row_bounds(a, p.e, row0 + row, in, lo[b], hi[b]);
+            const int row = row0 + quad + 8 * b, i = quotient(row, a.by_group);
+            const bool in = quad + 8 * b < p.rows;
+            const uint8_t* q = a.q + ((p.e.first + i) * a.q_ts + (p.h * a.group + row - i * a.group) * a.q_hs + two) * 2;
+            row_bounds(a, p.e, row, in, lo[b], hi[b]);
 #pragma unroll
             for (int k = 0; k < DK / 16; ++k)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int col = k * 16 + c * 8 + two;
-                    qf[k][b + 2 * c] = in && col < a.dim ? *reinterpret_cast<const uint32_t*>(q + col * 2) : 0u;
-                }
+                for (int c = 0; c < 2; ++c)
+                    qf[k][b + 2 * c] = in && k * 16 + c * 8 < a.dim ? *reinterpret_cast<const uint32_t*>(q + (k * 16 + c * 8) * 2) : 0u;
         }
+        // A lane copies the same 16 bytes of every row that it takes.
+        constexpr int kPieces = DK / 8, kRowStep = 32 / kPieces;
+        const int piece = lane % kPieces, first_row = lane / kPieces;
+        const bool piece_in = piece * 8 < a.dim;
+        const int lane_off = piece_in ? (first_row * a.dim + piece * 8) * 2 : 0, row_off = kRowStep * a.dim * 2;
+        auto request = [&](int i) {
+            if (i < n_chunk) {
+                if (i % 32 == 0 && i) look_up(i + lane);
+                int page = __shfl_sync(0xffffffffu, pages, i % 32);
+                const int place = (p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
+                int valid = piece_in ? p.e.len - place : 0;
+                if (page < 0 || page >= a.pages) { page = 0; valid = 0; bad = true; }
+                const int in_page = place - quotient(place, a.by_page) * a.page_size;
+                const long long from = ((long long)page * a.kv_heads * a.page_size + p.h * a.page_size + in_page) * (a.dim * 2) + lane_off;
+                const uint8_t *k = a.k + from, *v = a.v + from;
+                const uint32_t to = ring + i % Shape::kStages * Shape::kStage;
+#pragma unroll
+                for (int j = 0; j < kRowsKeys / kRowStep; ++j) {
+                    const int row = first_row + j * kRowStep, bytes = row < valid ? 16 : 0;
+                    const uint32_t at = to + row * Shape::kRow + ((piece ^ (row & 7)) << 4);
+                    cp_async16(at, k + j * row_off, bytes);
+                    cp_async16(at + kRowsKeys * Shape::kRow, v + j * row_off, bytes);
+                }
+            }
+            cp_async_commit();
+        };
+#pragma unroll 1
+        for (int i = 0; i < Shape::kStages - 1; ++i) request(i);
+
         float o[DK / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < DK / 8; ++d)
@@ -164,7 +164,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                 mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
                 mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
                 base[b] = mx[b] == -INFINITY ? 0.f : mx[b];
-                was[b] = exp2f(m[b] - base[b]);
+                was[b] = fast_exp2(m[b] - base[b]);
                 m[b] = mx[b];
                 l[b] *= was[b];
             }
@@ -172,7 +172,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[t][e] = exp2f(sc[t][e] - base[e >> 1]);
+                    sc[t][e] = fast_exp2(sc[t][e] - base[e >> 1]);
                     l[e >> 1] += sc[t][e];
                 }
             if (__any_sync(0xffffffffu, was[0] != 1.f || was[1] != 1.f)) {
@@ -227,14 +227,15 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             for (int i = 0; i < 4; ++i) v[i] = 0.f;
             for (int j = 0; j < n; ++j) {
                 const float* f = j ? rest + j * apart : from;
-                const float w = exp2f(at(f + row) - base);
+                const float w = fast_exp2(at(f + row) - base);
                 sum += w * at(f + kRowsR + row);
                 const float4 x = at(reinterpret_cast<const float4*>(f + 2 * kRowsR + row * DK + col));
                 v[0] = fmaf(w, x.x, v[0]); v[1] = fmaf(w, x.y, v[1]); v[2] = fmaf(w, x.z, v[2]); v[3] = fmaf(w, x.w, v[3]);
             }
         };
         auto finish = [&](int row, int col, const float (&v)[4], float mx, float sum) {
-            const long long token = p.e.first + (row0 + row) / a.group, head = (long long)p.h * a.group + (row0 + row) % a.group;
+            const int i = quotient(row0 + row, a.by_group), head = p.h * a.group + row0 + row - i * a.group;
+            const long long token = p.e.first + i;
             const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
             const float x[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
             if (x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]) atomicOr(&nan_s, 1u << row);
@@ -283,7 +284,13 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     }
 }
 
-static size_t rows_partials(int n_sm) { return (size_t)2 * n_sm * RowsShape<kHeadDimMax>::kSlot * 4; }
+// Both forms have their partial results at the same place: calls that share a workspace are ordered.
+static size_t partials_bytes(int dim, int n_sm) {
+    const size_t rows = (size_t)2 * kRowsPerSm * n_sm * RowsShape<kHeadDimMax>::kSlot * 4, tiles = attend_tiles_partials(dim, n_sm);
+    return rows > tiles ? rows : tiles;
+}
+// The most rows of a sequence and key head that go to the form for few.
+constexpr long long kRowsMost = 16;
 
 template <bool F16, int DK>
 static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t st) {
@@ -292,7 +299,7 @@ static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t
         return cudaFuncSetAttribute(attend_rows_kernel<F16, DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DK>::kRing);
     });
     if (e != cudaSuccess) return e;
-    return launch_pdl(attend_rows_kernel<F16, DK>, dim3(n_sm), dim3(kRowsThreads), RowsShape<DK>::kRing, st, a);
+    return launch_pdl(attend_rows_kernel<F16, DK>, dim3(kRowsPerSm * n_sm), dim3(kRowsThreads), RowsShape<DK>::kRing, st, a);
 }
 static cudaError_t launch_rows(const AttendArgs& a, bool f16, int n_sm, cudaStream_t st) {
     if (a.dim <= 64) return f16 ? launch_rows_typed<true, 64>(a, n_sm, st) : launch_rows_typed<false, 64>(a, n_sm, st);
@@ -307,8 +314,8 @@ extern "C" size_t saem_attend_workspace_bytes(const saem_kv_cache* c) {
     int n_sm;
     if (!c) return 0;
     const int r = cache_status(*c);
-    if (r != SAEM_OK || sm_count(&n_sm) != cudaSuccess || n_sm > kAttendMaxCtas) return 0;
-    return SAEM_ATTEND_HEAD_BYTES + rows_partials(n_sm);
+    if (r != SAEM_OK || sm_count(&n_sm) != cudaSuccess || kRowsPerSm * n_sm > kAttendMaxCtas) return 0;
+    return SAEM_ATTEND_HEAD_BYTES + partials_bytes(c->head_dim, n_sm);
 }
 
 extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cache, const saem_batch* b, const void* q, void* out,
@@ -331,8 +338,8 @@ extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cac
     for (int64_t s : strides)
         if (s % 8) return SAEM_ERR_ALIGNMENT;
     int n_sm;
-    if (sm_count(&n_sm) != cudaSuccess || n_sm > kAttendMaxCtas) return SAEM_ERR_CUDA;
-    if (workspace_bytes < SAEM_ATTEND_HEAD_BYTES + rows_partials(n_sm)) return SAEM_ERR_WORKSPACE;
+    if (sm_count(&n_sm) != cudaSuccess || kRowsPerSm * n_sm > kAttendMaxCtas) return SAEM_ERR_CUDA;
+    if (workspace_bytes < SAEM_ATTEND_HEAD_BYTES + partials_bytes(cache->head_dim, n_sm)) return SAEM_ERR_WORKSPACE;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     AttendArgs a = {};
     a.q = static_cast<const uint8_t*>(q); a.out = static_cast<uint8_t*>(out); a.lse = lse;
@@ -340,11 +347,14 @@ extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cac
     a.k = static_cast<const uint8_t*>(cache->k); a.v = static_cast<const uint8_t*>(cache->v);
     a.pages = cache->pages; a.page_size = cache->page_size; a.kv_heads = cache->kv_heads; a.dim = cache->head_dim;
     a.group = c->q_heads / cache->kv_heads;
+    a.by_page = divisor_of(cache->page_size); a.by_group = divisor_of(a.group);
     a.offsets = b->offsets; a.lengths = b->lengths; a.table = b->table; a.table_stride = b->table_stride;
     a.seqs = b->seqs; a.tokens = b->tokens; a.max_pages = b->max_pages;
     a.causal = c->causal != 0; a.window = c->window; a.scale = c->scale; a.scale_log2 = c->scale * 1.4426950408889634f;
     a.status = reinterpret_cast<int*>(ws);
     a.counters = reinterpret_cast<int*>(ws + kAttendCounters);
     a.partials = reinterpret_cast<float*>(ws + SAEM_ATTEND_HEAD_BYTES);
-    return launch_rows(a, cache->dtype == SAEM_OUT_F16, n_sm, (cudaStream_t)stream) == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
+    const bool f16 = cache->dtype == SAEM_OUT_F16, few = (long long)b->max_new * a.group <= kRowsMost;
+    const cudaError_t e = few ? launch_rows(a, f16, n_sm, (cudaStream_t)stream) : launch_attend_tiles(a, f16, n_sm, (cudaStream_t)stream);
+    return e == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }

@@ -1,9 +1,11 @@
 // How the work of an attention call is dealt out, on the device alone: lengths, offsets and pages are never read on the host.
 //
 // An item is a tile of R rows of one sequence and one key head (row = token * group + query head within the group); its units are the
-// tiles of KEYS places that any of its rows may see, one at least, so that rows that see nothing are written too.  All units of
+// tiles of KEYS places that any of its rows may see, one at least, so that rows that see nothing are written too, behind HEAD units
+// for what an item costs by itself (queries, first bytes, the result).  All units of
 // a call, in the order sequence, key head, row tile, are cut into as many equal ranges as there are CTAs: long and short
-// sequences, few and many rows load the SMs alike.  An item that is cut leaves sums of its parts in the workspace, and the CTA that
+// sequences, few and many rows load the SMs alike.  A cut within an item's first HEAD units moves to its beginning.  An item that is cut leaves
+// sums of its parts in the workspace, and the CTA that
 // arrives last adds them up in the order of the parts, so that two runs give the same bits.
 #ifndef SAEM_ATTEND_PLAN_CUH_
 #define SAEM_ATTEND_PLAN_CUH_
@@ -14,6 +16,22 @@ namespace saem {
 
 constexpr int kAttendMaxCtas = 640;         // SMs x CTAs per SM at most
 
+// n / d for 0 <= n < 2^31 by a multiplication: with 2^s >= d, mul = ceil(2^(31 + s) / d) is off by less than 2^s / 2^31 of a quotient.
+struct Divisor {
+    uint32_t d, mul, shift;
+};
+inline Divisor divisor_of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), 31 + s};
+}
+__device__ __forceinline__ int quotient(int n, const Divisor& d) { return (int)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 struct AttendArgs {
     const uint8_t* q;
     uint8_t* out;
@@ -23,6 +41,7 @@ struct AttendArgs {
     const uint8_t* v;
     long long pages;
     int page_size, kv_heads, dim, group;
+    Divisor by_page, by_group;
     const int32_t* offsets;
     const int32_t* lengths;
     const int32_t* table;
@@ -34,6 +53,9 @@ struct AttendArgs {
     int* counters;                          // [kAttendMaxCtas], zero between calls
     float* partials;                        // two slots per CTA
 };
+// The form for many rows per key head (attend_tiles.cu), and the bytes that its partial results take.
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool f16, int n_sm, cudaStream_t st);
+size_t attend_tiles_partials(int dim, int n_sm);
 constexpr size_t kAttendCounters = 256;     // byte offset of the counters in the workspace
 static_assert(kAttendCounters + 4 * kAttendMaxCtas <= SAEM_ATTEND_HEAD_BYTES, "");
 
@@ -42,38 +64,37 @@ struct SeqExtent {
 };
 __device__ __forceinline__ SeqExtent seq_extent(const AttendArgs& a, int s) {
     const int lo = min(max(a.offsets[s], 0), a.tokens), hi = min(max(a.offsets[s + 1], lo), a.tokens);
-    const long long most = (long long)a.max_pages * a.page_size;
+    const long long most = min((long long)a.max_pages * a.page_size, 0x7FFF0000ll);      // sums of places stay within 32 bits
     return {lo, hi - lo, (int)min((long long)max(a.lengths[s], 0), most)};
 }
 // The places that rows [row0, row1] may see, in tiles of KEYS.
 template <int KEYS>
-__device__ __forceinline__ void key_tiles(const AttendArgs& a, const SeqExtent& e, long long row0, long long row1, int& begin, int& end) {
-    const long long i0 = row0 / a.group, i1 = row1 / a.group;
-    const long long stop = a.causal ? min((long long)e.len, e.len - e.n + i1 + 1) : e.len;
-    const long long start = a.window ? max(0ll, e.len - e.n + i0 - a.window + 1) : 0;
-    begin = (int)(start / KEYS);
-    end = stop > start ? (int)((stop + KEYS - 1) / KEYS) : begin;
+__device__ __forceinline__ void key_tiles(const AttendArgs& a, const SeqExtent& e, int row0, int row1, int& begin, int& end) {
+    const int before = e.len - e.n;         // may be negative
+    const int stop = a.causal ? before + quotient(row1, a.by_group) + 1 : e.len;
+    const int first = before + quotient(row0, a.by_group) + 1, start = a.window && first > a.window ? first - a.window : 0;
+    begin = start / KEYS;
+    end = stop > start ? (stop - 1) / KEYS + 1 : begin;
 }
 template <int R>
-__device__ __forceinline__ int row_tiles(const AttendArgs& a, const SeqExtent& e) { return (int)(((long long)e.n * a.group + R - 1) / R); }
-template <int R, int KEYS>
+__device__ __forceinline__ int row_tiles(const AttendArgs& a, const SeqExtent& e) { return (int)(((uint32_t)(e.n * a.group) + (R - 1)) / R); }
+template <int R, int KEYS, int HEAD>
 __device__ __forceinline__ int item_units(const AttendArgs& a, const SeqExtent& e, int r) {
     int b, t;
-    const long long rows = (long long)e.n * a.group;
-    key_tiles<KEYS>(a, e, (long long)r * R, min(rows, (long long)(r + 1) * R) - 1, b, t);
-    return max(1, t - b);
+    const int rows = e.n * a.group;
+    key_tiles<KEYS>(a, e, r * R, min(rows - r * R, R) + r * R - 1, b, t);
+    return HEAD + max(1, t - b);
 }
 
 struct AttendPlan {                         // in shared memory
-    long long total, begin, end;            // units of the call, and this CTA's range
+    long long per, begin, end;              // units of a range, and this CTA's
     long long seq_begin;                    // unit at which sequence s begins
     int s;
-    int ctas;                               // CTAs that have a range
     long long scan[32];
 };
 
 // All threads of the CTA (WARPS whole warps); MIN_UNITS: a CTA takes no fewer units while there are others.
-template <int R, int KEYS, int WARPS>
+template <int R, int KEYS, int HEAD, int WARPS>
 __device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p, int min_units) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kStep = WARPS * 32;
@@ -82,37 +103,56 @@ __device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p, in
         const bool in = s < a.seqs;
         const SeqExtent e = in ? seq_extent(a, s) : SeqExtent{0, 0, 0};
         const int tiles = row_tiles<R>(a, e);
-        long long u = tiles == 1 ? item_units<R, KEYS>(a, e, 0) : 0;
+        long long u = tiles == 1 ? item_units<R, KEYS, HEAD>(a, e, 0) : 0;
         for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 1); many; many &= many - 1) {
             const int src = __ffs(many) - 1;
             const SeqExtent o = {0, __shfl_sync(0xffffffffu, e.n, src), __shfl_sync(0xffffffffu, e.len, src)};
             const int t = __shfl_sync(0xffffffffu, tiles, src);
             long long sum = 0;
-            for (int r = lane; r < t; r += 32) sum += item_units<R, KEYS>(a, o, r);
+            for (int r = lane; r < t; r += 32) sum += item_units<R, KEYS, HEAD>(a, o, r);
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             if (lane == src) u = sum;
         }
         return u * a.kv_heads;
     };
+    auto range_of = [&](long long total) {
+        const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)min_units);
+        p.per = per; p.begin = min(total, per * blockIdx.x); p.end = min(total, p.begin + per);
+    };
+    if (a.seqs <= 32) {                     // one warp's work
+        if (warp == 0) {
+            const long long mine = units_of(lane);
+            long long incl = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += o;
+            }
+            const long long total = __shfl_sync(0xffffffffu, incl, 31);
+            if (lane == 0) range_of(total);
+            __syncwarp();
+            const long long begin = p.begin;
+            if (incl - mine <= begin && begin < incl) { p.s = lane; p.seq_begin = incl - mine; }
+        }
+        __syncthreads();
+        return;
+    }
     long long mine = units_of(warp * 32 + lane), sum = mine;
     for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += units_of(s + lane);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     if (lane == 0) p.scan[warp] = sum;
     __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) total += p.scan[w];
-    const long long most = (total + min_units - 1) / min_units;
-    const int ctas = (int)max(1ll, min((long long)gridDim.x, most));
-    const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : total, end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
     if (threadIdx.x == 0) {
-        p.total = total; p.begin = begin; p.end = end; p.ctas = ctas;
-        p.s = a.seqs; p.seq_begin = total;
+        long long total = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) total += p.scan[w];
+        range_of(total);
     }
     __syncthreads();
-    if (begin >= end) return;
+    const long long begin = p.begin;
+    if (begin >= p.end) return;
     long long before = 0;
     for (int s0 = 0; s0 < a.seqs; s0 += kStep) {
         const int s = s0 + warp * 32 + lane;
@@ -148,30 +188,35 @@ struct AttendPart {
     int first_slot;                         // the first part's place; part j has 2 * (first_cta + j)
 };
 // Walks through a CTA's range; every warp for itself, alike in all lanes.
-template <int R, int KEYS>
+template <int R, int KEYS, int HEAD>
 struct AttendWalk {
     long long at, end, item;                // next unit, end of the range, first unit of the item at hand
-    long long total;
-    int ctas;
+    long long per;                          // units of a range
     int s, h, r, tiles;
     SeqExtent e;
     __device__ __forceinline__ void begin(const AttendArgs& a, const AttendPlan& p) {
-        at = p.begin; end = p.end; total = p.total; ctas = p.ctas; s = p.s;
+        at = p.begin; end = p.end; per = p.per; s = p.s;
         if (at >= end) return;
         e = seq_extent(a, s);
         tiles = row_tiles<R>(a, e);
         item = p.seq_begin;
+        r = 0;
+        if (tiles == 1) {
+            const int units = item_units<R, KEYS, HEAD>(a, e, 0);
+            h = (int)((at - item) / units);
+            item += (long long)h * units;
+            return;
+        }
         // the item that holds the range's first unit: the head by division, the row tile by a warp's scan
         const int lane = threadIdx.x & 31;
         long long per_head = 0;
-        for (int t = lane; t < tiles; t += 32) per_head += item_units<R, KEYS>(a, e, t);
+        for (int t = lane; t < tiles; t += 32) per_head += item_units<R, KEYS, HEAD>(a, e, t);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) per_head += __shfl_xor_sync(0xffffffffu, per_head, d);
         h = (int)((at - item) / per_head);
         item += h * per_head;
-        r = 0;
         for (int t0 = 0; t0 < tiles; t0 += 32) {
-            const int u = t0 + lane < tiles ? item_units<R, KEYS>(a, e, t0 + lane) : 0;
+            const int u = t0 + lane < tiles ? item_units<R, KEYS, HEAD>(a, e, t0 + lane) : 0;
             int incl = u;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -190,22 +235,23 @@ struct AttendWalk {
     }
     __device__ __forceinline__ bool next(const AttendArgs& a, AttendPart& p) {
         if (at >= end) return false;
-        const long long rows = (long long)e.n * a.group, row0 = (long long)r * R, row1 = min(rows, row0 + R) - 1;
+        const int row0 = r * R, row1 = row0 + min(e.n * a.group - row0, R) - 1;
         int b, t;
         key_tiles<KEYS>(a, e, row0, row1, b, t);
-        const int units = max(1, t - b);
+        const int units = HEAD + max(1, t - b);
         const long long stop = min(end, item + units);
+        if (stop <= item + HEAD) return false;      // the range ends here; the next CTA begins this item
         p.e = e; p.s = s; p.h = h; p.r = r;
-        p.rows = (int)(row1 - row0 + 1);
-        p.key_begin = b + (int)(at - item);
-        p.key_end = min(t, b + (int)(stop - item));
-        p.whole = at == item && stop == item + units;
+        p.rows = row1 - row0 + 1;
+        p.key_begin = b + max(0, (int)(at - item) - HEAD);
+        p.key_end = min(t, b + (int)(stop - item) - HEAD);
+        p.whole = at <= item + HEAD && stop == item + units;
         if (!p.whole) {
             const int me = blockIdx.x;
-            p.first_cta = (int)(((item + 1) * ctas - 1) / total);
-            p.n_parts = (int)(((item + units) * ctas - 1) / total) - p.first_cta + 1;
+            p.first_cta = (int)((item + HEAD) / per);
+            p.n_parts = (int)((item + units - 1) / per) - p.first_cta + 1;
             p.part = me - p.first_cta;
-            p.first_slot = 2 * p.first_cta + (item > total * p.first_cta / ctas ? 1 : 0);
+            p.first_slot = 2 * p.first_cta + (item > per * p.first_cta ? 1 : 0);
             p.slot = p.part ? 2 * me : p.first_slot;
         }
         at = stop;
@@ -229,21 +275,22 @@ struct AttendWalk {
 };
 
 // The rows' bounds: row (of the item) sees places lo .. hi.
-__device__ __forceinline__ void row_bounds(const AttendArgs& a, const SeqExtent& e, long long row, bool in, int& lo, int& hi) {
-    const long long place = e.len - e.n + row / a.group;
-    hi = !in ? -1 : (int)(a.causal ? min((long long)e.len - 1, place) : e.len - 1);
-    lo = a.window ? (int)max(0ll, place - a.window + 1) : 0;
+__device__ __forceinline__ void row_bounds(const AttendArgs& a, const SeqExtent& e, int row, bool in, int& lo, int& hi) {
+    const int place = e.len - e.n + quotient(row, a.by_group);
+    hi = !in ? -1 : a.causal ? place : e.len - 1;
+    lo = a.window && place + 1 > a.window ? place + 1 - a.window : 0;
 }
 
 // One row over again, by one warp, out of the cache and the places that it sees alone: for rows whose result is NaN.  In a product of
 // tiles a weight of 0 meets what other rows see, and 0 times an infinity or NaN there is NaN.
 template <bool F16>
-__device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExtent& e, int s, int h, long long row) {
+__device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExtent& e, int s, int h, int row) {
     const int lane = threadIdx.x & 31, at = lane * 4;
     const bool here = at < a.dim;
     int lo, hi;
     row_bounds(a, e, row, true, lo, hi);
-    const long long token = e.first + row / a.group, head = (long long)h * a.group + row % a.group;
+    const long long token = e.first + row / a.group;
+    const int head = h * a.group + row % a.group;
     float q[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
     auto four = [&](const uint8_t* p, long long i, float* v) {
         const uint2 w = *reinterpret_cast<const uint2*>(p + i * 2);
@@ -263,7 +310,7 @@ __device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExte
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
         d *= a.scale_log2;
-        const float mn = fmaxf(m, d), base = mn == -INFINITY ? 0.f : mn, was = exp2f(m - base), p = exp2f(d - base);
+        const float mn = fmaxf(m, d), base = mn == -INFINITY ? 0.f : mn, was = fast_exp2(m - base), p = fast_exp2(d - base);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fmaf(p, v[i], o[i] * was);
         l = l * was + p;

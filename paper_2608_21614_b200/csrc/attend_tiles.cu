@@ -166,6 +166,30 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             ok = named_all(kAtBarAll, 256, ok);
             return ok && parts[turn % kAtParts].rows > 0;
         };
+        // An item's queries in the 128-byte swizzle: each warp its 32 rows, all of its loads under way at once.
+        auto load_queries = [&](const AttendPart& p) {
+            const int skip = p.rows <= 128 ? 0 : g * 128, row0 = p.r * kAtR + skip;
+            if (p.key_end - p.key_begin <= (skip ? 0 : p.rows <= 128 ? g : 0)) return;            // the group has no tiles
+            constexpr int kPieces = DK / 8, kRounds = 32 * kPieces / 32;
+            uint4 v[kRounds];
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) {
+                const int u = lane + 32 * i, r = quarter * 32 + u / kPieces, c = u % kPieces;
+                v[i] = make_uint4(0, 0, 0, 0);
+                if (skip + r < p.rows && c * 8 < a.dim) {
+                    const int t = quotient(row0 + r, a.by_group), head = p.h * a.group + row0 + r - t * a.group;
+                    v[i] = *reinterpret_cast<const uint4*>(a.q + ((p.e.first + t) * a.q_ts + head * a.q_hs + c * 8) * 2);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) {
+                const int u = lane + 32 * i, r = quarter * 32 + u / kPieces, c = u % kPieces;
+                st_shared_v4(base + g * kTile + c / 8 * kAtKeys * 128 + r * 128 + ((c % 8 ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(smem_u32(&bar_q[g]));
+        };
+        bool queries_there = false;
         for (; next_all(); finished()) {
             const AttendPart& p = parts[turn % kAtParts];
             const bool both = p.rows <= 128;                        // both groups on the same rows
@@ -173,22 +197,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             const int tile_row = (both ? 0 : g * 128) + own, row0 = p.r * kAtR + (both ? 0 : g * 128);
             const bool in = tile_row < p.rows;
             const bool warp_in = (both ? 0 : g * 128) + quarter * 32 < p.rows;
-            if (n > 0) {
-                // queries: the warp's 32 rows, in the 128-byte swizzle
-                constexpr int kPieces = DK / 8;
-#pragma unroll 4
-                for (int u = lane; u < 32 * kPieces; u += 32) {
-                    const int r = quarter * 32 + u / kPieces, c = u % kPieces;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (row0 - p.r * kAtR + r < p.rows && c * 8 < a.dim) {
-                        const int i = quotient(row0 + r, a.by_group), head = p.h * a.group + row0 + r - i * a.group;
-                        v = *reinterpret_cast<const uint4*>(a.q + ((p.e.first + i) * a.q_ts + head * a.q_hs + c * 8) * 2);
-                    }
-                    st_shared_v4(base + g * kTile + c / 8 * kAtKeys * 128 + r * 128 + ((c % 8 ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
-                }
-                fence_proxy_async_smem();
-                mbar_arrive(smem_u32(&bar_q[g]));
-            }
+            if (!queries_there) load_queries(p);
             int lo = 0, hi = INT_MAX;                               // rows that are none see everything: nobody reads them
             if (in) row_bounds(a, p.e, row0 + own, true, lo, hi);
             hi = min(hi, in ? p.e.len - 1 : INT_MAX);
@@ -253,6 +262,17 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_p[g]));
+            }
+            // the next item's queries, so that its first scores come while this one's results are written (the sum of two groups takes
+            // the queries' place)
+            queries_there = false;
+            if (ok && !both) {
+                const int then = turn + 1;
+                ok = mbar_wait_warp(smem_u32(&bar_part[then % kAtParts]), (then / kAtParts) & 1, abort_p, a.status);
+                if (ok && parts[then % kAtParts].rows > 0) {
+                    load_queries(parts[then % kAtParts]);
+                    queries_there = true;
+                }
             }
             if (ok && n > 0) {
                 ok = mbar_wait_warp(smem_u32(&bar_o[g]), n_o & 1, abort_p, a.status);

@@ -18,18 +18,19 @@
 
 namespace saem {
 
-constexpr int kAtThreads = 384;             // a warpgroup that copies and issues products (three of its warps), two with rows
+constexpr int kAtThreads = 384;             // a warpgroup that copies and issues products and looks ahead, two with rows
 constexpr int kAtRegsFew = 72, kAtRegsMany = 216;                   // of 168 per thread at launch: 72 + 2 * 216 = 3 * 168
 constexpr int kAtR = 256, kAtKeys = 128, kAtHead = 2;
 constexpr int kAtMaxStages = 10;
+constexpr int kAtStage = 32 * 128;          // a warp's place for 64 columns of its 32 rows' results
 constexpr int kAtParts = 3;                 // items read ahead
 enum { kAtBarAll = 1 };                     // named barrier of the eight warps with rows
 
 template <int DK>
 struct TilesShape {
     static constexpr int kTile = 128 * DK * 2;                      // bytes of 128 queries, keys or values
-    static constexpr int kStages = DK == 128 ? 5 : 10;
-    static constexpr int kSmem = 1024 + 2 * kTile + kStages * kTile;
+    static constexpr int kStages = DK == 128 ? 4 : 8;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kTile + 8 * kAtStage;
     static constexpr int kSlot = kAtR * (DK + 2);                   // floats of a partial result: maxima, sums, outputs [DK / 4][256][4]
     static_assert(kStages <= kAtMaxStages, "");
 };
@@ -124,7 +125,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
         for (int i = 0; i < kAtParts; ++i) {
             mbar_init(smem_u32(&bar_part[i]), 1);
-            mbar_init(smem_u32(&bar_done[i]), 10);
+            mbar_init(smem_u32(&bar_done[i]), 11);
         }
         abort_flag = 0;
         for (int i = 0; i < 8; ++i) nan_s[0][i] = 0;
@@ -306,32 +307,47 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     ms = top;
                 }
             }
-            const bool writes = in && (!both || g == 0);            // this thread has a row's sum
+            const bool warp_writes = warp_in && (!both || g == 0), writes = in && warp_writes;   // this thread has a row's sum
             const bool add = both && n_all > 1;
             const int token_i = quotient(row0 + own, a.by_group), head = p.h * a.group + row0 + own - token_i * a.group;
             const long long token = p.e.first + token_i;
-            uint8_t* const out = a.out + (token * a.out_ts + head * a.out_hs) * 2;
             float* const slot = a.partials + (size_t)p.slot * Shape::kSlot;
-            auto finish = [&](const float* v, int col, float inv) {                              // 32 columns
+            const uint32_t stage = base + (2 + kStages) * kTile + (warp - 4) * kAtStage;
+            // 32 of the row's columns; two calls are 64, which leave in whole rows of 128 bytes: a thread's own stores would touch a row each
+            auto finish = [&](const float* v, int c, float inv) {
                 bool bad = false;
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
+                for (int e = 0; e < 4; ++e) {
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float x = v[e + 2 * i] * inv, y = v[e + 2 * i + 1] * inv;
-                        bad |= (x != x || y != y) && col + e < a.dim;
+                        const float x = v[8 * e + 2 * i] * inv, y = v[8 * e + 2 * i + 1] * inv;
+                        bad |= (x != x || y != y) && c * 32 + e * 8 < a.dim;
                         w[i] = pack2<F16>(x, y);
                     }
-                    if (col + e < a.dim) *reinterpret_cast<uint4*>(out + (col + e) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                    st_shared_v4(stage + lane * 128 + ((((c & 1) * 4 + e) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
                 }
-                if (bad) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
+                if (bad && in) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
+                if (c & 1) {
+                    __syncwarp();
+                    const int col = (c >> 1) * 64 + (lane & 7) * 8;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = i * 4 + (lane >> 3), row = quarter * 32 + r, t = quotient(row0 + row, a.by_group);
+                        uint4 w;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                                     : "r"(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4)) : "memory");
+                        if ((both ? 0 : g * 128) + row < p.rows && col < a.dim)
+                            *reinterpret_cast<uint4*>(a.out + ((p.e.first + t) * a.out_ts + (p.h * a.group + row0 + row - t * a.group) * a.out_hs + col) * 2) = w;
+                    }
+                    __syncwarp();
+                }
             };
             auto finish_lse = [&](float mx, float sum) {
                 if (a.lse) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
             };
             bool done = p.whole;
-            if (warp_in && (!both || g == 0)) {
+            if (warp_writes) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll 1
                 for (int c = 0; c < DK / 32; ++c) {
@@ -348,9 +364,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                             v[4 * e + 2] = fmaf(x.z, w_other, v[4 * e + 2]); v[4 * e + 3] = fmaf(x.w, w_other, v[4 * e + 3]);
                         }
                     }
-                    if (!writes) continue;
-                    if (p.whole) finish(v, c * 32, inv);
-                    else {
+                    if (p.whole) finish(v, c, inv);
+                    else if (in) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             __stcg(reinterpret_cast<float4*>(slot + 2 * kAtR + ((c * 8 + e) * kAtR + tile_row) * 4), make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]));
@@ -377,7 +392,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (last_s) {
                     __threadfence();
                     done = true;
-                    if (writes) {
+                    if (warp_writes) {
                         auto part = [&](int j) { return a.partials + (size_t)(j ? 2 * (p.first_cta + j) : p.first_slot) * Shape::kSlot; };
                         float mx = -INFINITY, sum = 0.f;
 #pragma unroll 4
@@ -401,18 +416,22 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                                     v[4 * e + 2] = fmaf(x.z, w, v[4 * e + 2]); v[4 * e + 3] = fmaf(x.w, w, v[4 * e + 3]);
                                 }
                             }
-                            finish(v, c * 32, inv);
+                            finish(v, c, inv);
                         }
-                        finish_lse(mx, sum);
+                        if (in) finish_lse(mx, sum);
                     }
                 }
             }
             named_sync(kAtBarAll, 256);
             if (threadIdx.x == 128)
                 for (int i = 0; i < 8; ++i) nan_s[~turn & 1][i] = 0;
-            if (done && ok)
-                for (int r = warp - 4; r < p.rows; r += 8)
-                    if (nan_s[turn & 1][r >> 5] >> (r & 31) & 1) attend_row_again<F16>(a, p.e, p.s, p.h, p.r * kAtR + r);
+            const uint32_t again = done && ok && lane < 8 ? nan_s[turn & 1][lane] : 0u;
+            for (uint32_t words = __ballot_sync(0xffffffffu, again != 0); words; words &= words - 1) {
+                const int w = __ffs(words) - 1;
+                const uint32_t bits = __shfl_sync(0xffffffffu, again, w);
+                for (int r = warp - 4; r < 32; r += 8)
+                    if (bits >> r & 1) attend_row_again<F16>(a, p.e, p.s, p.h, p.r * kAtR + w * 32 + r);
+            }
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtRegsFew));
@@ -578,6 +597,16 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     mbar_arrive(smem_u32(&bar_part[at]));
                 }
                 __syncwarp();
+            }
+        } else {
+            // ---------------------------------------------------------------- queries of the items ahead, to L2
+            for (; next(); finished()) {
+                const AttendPart& p = parts[turn % kAtParts];
+                for (int u = lane; u < p.rows * (DK / 64); u += 32) {
+                    const int row = p.r * kAtR + u / (DK / 64), col = u % (DK / 64) * 64, t = quotient(row, a.by_group);
+                    if (col < a.dim)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.q + ((p.e.first + t) * a.q_ts + (p.h * a.group + row - t * a.group) * a.q_hs + col) * 2));
+                }
             }
         }
     }

@@ -75,6 +75,30 @@ __device__ __forceinline__ void tc_ld32_now(uint32_t taddr, uint32_t* r) {
     tc_reg_fence16(r + 16);
 }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Two fp32 values in a register pair: one instruction for both.
+__device__ __forceinline__ uint64_t pack_b32x2(uint32_t lo, uint32_t hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+    return d;
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) { return pack_b32x2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ float low_f32(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float high_f32(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // A barrier at which all learn whether all are well.
 __device__ __forceinline__ bool named_all(int id, int threads, bool v) {
     uint32_t r;
@@ -99,7 +123,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     using Shape = TilesShape<DK>;
     constexpr int kStages = Shape::kStages, kTile = Shape::kTile;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_tail, bar_end, bar_q[2], bar_s[2], bar_p[2], bar_o[2], bar_part[kAtParts], bar_done[kAtParts];
+    __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_tail, bar_end, bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_part[kAtParts], bar_done[kAtParts];
     __shared__ AttendPart parts[kAtParts];  // the items at hand; one without rows ends the range
     __shared__ AttendPlan plan;
     __shared__ uint32_t tmem_s, nan_s[2][8];     // rows with a NaN, of this item and the next
@@ -120,7 +144,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         for (int g = 0; g < 2; ++g) {
             mbar_init(smem_u32(&bar_q[g]), 128);
             mbar_init(smem_u32(&bar_s[g]), 1);
-            mbar_init(smem_u32(&bar_p[g]), 4);
+            mbar_init(smem_u32(&bar_p[g][0]), 4);
+            mbar_init(smem_u32(&bar_p[g][1]), 4);
             mbar_init(smem_u32(&bar_o[g]), 1);
         }
         for (int i = 0; i < kAtParts; ++i) {
@@ -224,8 +249,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    for (int c = 0; c < 128; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], __uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1]));
+                    const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
                     const bool move = (top - m) * a.scale_log2 > 8.f;           // false where both are -inf
                     if (__any_sync(0xffffffffu, move)) {
                         const float to = move ? top : m, was = move ? fast_exp2((m - to) * a.scale_log2) : 1.f;
@@ -243,26 +270,29 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : m * a.scale_log2;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint64_t by = pack_f32x2(a.scale_log2, a.scale_log2), less = pack_f32x2(-ref, -ref);
+                    uint64_t sum[2] = {0, 0};                                   // two sums each: zeros
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
+                    for (int c = 0; c < 2; ++c) {                               // half of the places at a time: its products need not wait for the rest
                         uint32_t w[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
-                            const float x = fast_exp2(fmaf(__uint_as_float(s[c * 64 + 2 * e]), a.scale_log2, -ref));
-                            const float y = fast_exp2(fmaf(__uint_as_float(s[c * 64 + 2 * e + 1]), a.scale_log2, -ref));
-                            sum[e & 1] += x;
-                            sum[2 + (e & 1)] += y;
-                            w[e] = pack2<F16>(x, y);
+                            const uint64_t x = fma_f32x2(pack_b32x2(s[c * 64 + 2 * e], s[c * 64 + 2 * e + 1]), by, less);
+                            const float p0 = fast_exp2(low_f32(x)), p1 = fast_exp2(high_f32(x));
+                            sum[e & 1] = add_f32x2(sum[e & 1], pack_f32x2(p0, p1));
+                            w[e] = pack2<F16>(p0, p1);
                         }
                         tc_st32(t_s + c * 32, w);
+                        tc_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bar_p[g][c]));
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tc_wait_st();
-                    tc_fence_before();
+                    const uint64_t both_sums = add_f32x2(sum[0], sum[1]);
+                    l += low_f32(both_sums) + high_f32(both_sums);
+                } else if (lane < 2) {
+                    mbar_arrive(smem_u32(&bar_p[g][lane]));
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bar_p[g]));
             }
             // the next item's queries, so that its first scores come while this one's results are written (the sum of two groups takes
             // the queries' place)
@@ -522,14 +552,17 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 tc_commit_on(on, smem_u32(&bar_s[g]));
             };
             auto outputs = [&](int g, int at, bool first, bool last) {
-                ok = ok && mbar_wait_warp(smem_u32(&bar_p[g]), n_p[g] & 1, abort_p, a.status);
-                ++n_p[g];
-                tc_fence_after();
-                if (!ok) return;
                 const uint64_t dv = desc_at(desc_v, 2 * kTile + at % kStages * kTile);
-    #pragma unroll
-                for (int k = 0; k < kAtKeys / 16; ++k)
-                    tc_mma_f16_ta_on(on, tmem + 256 + g * 128, tmem + g * 128 + k * 8, desc_at(dv, k * 16 * 128), idesc_o, !first || k > 0);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ok = ok && mbar_wait_warp(smem_u32(&bar_p[g][half]), n_p[g] & 1, abort_p, a.status);
+                    if (!ok) return;
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = half * 4; k < half * 4 + 4; ++k)
+                        tc_mma_f16_ta_on(on, tmem + 256 + g * 128, tmem + g * 128 + k * 8, desc_at(dv, k * 16 * 128), idesc_o, !first || k > 0);
+                }
+                ++n_p[g];
                 if (last) tc_commit_on(on, smem_u32(&bar_o[g]));
             };
             for (; next(); finished()) {

@@ -59,6 +59,12 @@ size_t attend_tiles_partials(int dim, int n_sm);
 constexpr size_t kAttendCounters = 256;     // byte offset of the counters in the workspace
 static_assert(kAttendCounters + 4 * kAttendMaxCtas <= SAEM_ATTEND_HEAD_BYTES, "");
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 struct SeqExtent {
     int first, n, len;                      // first row of the call's tokens, new tokens, places
 };

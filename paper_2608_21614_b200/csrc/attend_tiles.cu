@@ -123,14 +123,14 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     using Shape = TilesShape<DK>;
     constexpr int kStages = Shape::kStages, kTile = Shape::kTile;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_tail, bar_end, bar_q[2], bar_s[2], bar_p[2][2], bar_o[2], bar_part[kAtParts], bar_done[kAtParts];
+    __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_tail, bar_end, bar_q[2], bar_free[2], bar_s[2], bar_p[2][2], bar_o[2], bar_part[kAtParts], bar_done[kAtParts];
     __shared__ AttendPart parts[kAtParts];  // the items at hand; one without rows ends the range
     __shared__ AttendPlan plan;
     __shared__ uint32_t tmem_s, nan_s[2][8];     // rows with a NaN, of this item and the next
     __shared__ int abort_flag, last_s;
     __shared__ float other_s[2][128];       // the second group's maxima and sums, where both worked on the same rows
     const AttendArgs& a = args.a;
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * kTile;
+    const uint32_t base = warp_uniform((smem_u32(smem_raw) + 1023u) & ~1023u), ring = base + 2 * kTile;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     volatile int* abort_p = &abort_flag;
 
@@ -142,7 +142,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         mbar_init(smem_u32(&bar_tail), 1);
         mbar_init(smem_u32(&bar_end), 1);
         for (int g = 0; g < 2; ++g) {
-            mbar_init(smem_u32(&bar_q[g]), 128);
+            mbar_init(smem_u32(&bar_q[g]), 1);
+            mbar_init(smem_u32(&bar_free[g]), 9);
             mbar_init(smem_u32(&bar_s[g]), 1);
             mbar_init(smem_u32(&bar_p[g][0]), 4);
             mbar_init(smem_u32(&bar_p[g][1]), 4);
@@ -171,7 +172,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     int turn = 0;                                                   // items so far
     auto next = [&]() -> bool {                                     // false at the end, or when a wait has run out
         ok = ok && mbar_wait_warp(smem_u32(&bar_part[turn % kAtParts]), (turn / kAtParts) & 1, abort_p, a.status);
-        return ok && parts[turn % kAtParts].rows > 0;
+        return ok && (int)warp_uniform(parts[turn % kAtParts].rows) > 0;
     };
     auto finished = [&] {
         __syncwarp();
@@ -192,30 +193,6 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             ok = named_all(kAtBarAll, 256, ok);
             return ok && parts[turn % kAtParts].rows > 0;
         };
-        // An item's queries in the 128-byte swizzle: each warp its 32 rows, all of its loads under way at once.
-        auto load_queries = [&](const AttendPart& p) {
-            const int skip = p.rows <= 128 ? 0 : g * 128, row0 = p.r * kAtR + skip;
-            if (p.key_end - p.key_begin <= (skip ? 0 : p.rows <= 128 ? g : 0)) return;            // the group has no tiles
-            constexpr int kPieces = DK / 8, kRounds = 32 * kPieces / 32;
-            uint4 v[kRounds];
-#pragma unroll
-            for (int i = 0; i < kRounds; ++i) {
-                const int u = lane + 32 * i, r = quarter * 32 + u / kPieces, c = u % kPieces;
-                v[i] = make_uint4(0, 0, 0, 0);
-                if (skip + r < p.rows && c * 8 < a.dim) {
-                    const int t = quotient(row0 + r, a.by_group), head = p.h * a.group + row0 + r - t * a.group;
-                    v[i] = *reinterpret_cast<const uint4*>(a.q + ((p.e.first + t) * a.q_ts + head * a.q_hs + c * 8) * 2);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kRounds; ++i) {
-                const int u = lane + 32 * i, r = quarter * 32 + u / kPieces, c = u % kPieces;
-                st_shared_v4(base + g * kTile + c / 8 * kAtKeys * 128 + r * 128 + ((c % 8 ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
-            }
-            fence_proxy_async_smem();
-            mbar_arrive(smem_u32(&bar_q[g]));
-        };
-        bool queries_there = false;
         for (; next_all(); finished()) {
             const AttendPart& p = parts[turn % kAtParts];
             const bool both = p.rows <= 128;                        // both groups on the same rows
@@ -223,7 +200,11 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             const int tile_row = (both ? 0 : g * 128) + own, row0 = p.r * kAtR + (both ? 0 : g * 128);
             const bool in = tile_row < p.rows;
             const bool warp_in = (both ? 0 : g * 128) + quarter * 32 < p.rows;
-            if (!queries_there) load_queries(p);
+            // the tiles of queries may be filled again: here, or once the sum of the two groups, which takes their place, is read
+            auto free_queries = [&] {
+                if (lane < 2 && n_all > (both ? lane : 0)) mbar_arrive(smem_u32(&bar_free[lane]));
+            };
+            if (!both) free_queries();
             int lo = 0, hi = INT_MAX;                               // rows that are none see everything: nobody reads them
             if (in) row_bounds(a, p.e, row0 + own, true, lo, hi);
             hi = min(hi, in ? p.e.len - 1 : INT_MAX);
@@ -294,17 +275,6 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     mbar_arrive(smem_u32(&bar_p[g][lane]));
                 }
             }
-            // the next item's queries, so that its first scores come while this one's results are written (the sum of two groups takes
-            // the queries' place)
-            queries_there = false;
-            if (ok && !both) {
-                const int then = turn + 1;
-                ok = mbar_wait_warp(smem_u32(&bar_part[then % kAtParts]), (then / kAtParts) & 1, abort_p, a.status);
-                if (ok && parts[then % kAtParts].rows > 0) {
-                    load_queries(parts[then % kAtParts]);
-                    queries_there = true;
-                }
-            }
             if (ok && n > 0) {
                 ok = mbar_wait_warp(smem_u32(&bar_o[g]), n_o & 1, abort_p, a.status);
                 ++n_o;
@@ -337,38 +307,43 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     ms = top;
                 }
             }
+            const AttendPart e = parts[turn % kAtParts];
             const bool warp_writes = warp_in && (!both || g == 0), writes = in && warp_writes;   // this thread has a row's sum
             const bool add = both && n_all > 1;
-            const int token_i = quotient(row0 + own, a.by_group), head = p.h * a.group + row0 + own - token_i * a.group;
-            const long long token = p.e.first + token_i;
-            float* const slot = a.partials + (size_t)p.slot * Shape::kSlot;
+            const int token_i = quotient(row0 + own, a.by_group), head = e.h * a.group + row0 + own - token_i * a.group;
+            const long long token = e.e.first + token_i;
+            uint8_t* const out = in ? a.out + (token * a.out_ts + head * a.out_hs) * 2 : nullptr;
+            float* const slot = a.partials + (size_t)e.slot * Shape::kSlot;
             const uint32_t stage = base + (2 + kStages) * kTile + (warp - 4) * kAtStage;
             // 32 of the row's columns; two calls are 64, which leave in whole rows of 128 bytes: a thread's own stores would touch a row each
             auto finish = [&](const float* v, int c, float inv) {
-                bool bad = false;
+                float any = 0.f;                                    // NaN if one of them is, or an infinity (which comes out the same again)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float x = v[8 * e + 2 * i] * inv, y = v[8 * e + 2 * i + 1] * inv;
-                        bad |= (x != x || y != y) && c * 32 + e * 8 < a.dim;
+                        if (c * 32 + e * 8 < a.dim) any = fmaf(y, 0.f, fmaf(x, 0.f, any));
                         w[i] = pack2<F16>(x, y);
                     }
                     st_shared_v4(stage + lane * 128 + ((((c & 1) * 4 + e) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
                 }
-                if (bad && in) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
+                if (any != any && in) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
                 if (c & 1) {
                     __syncwarp();
                     const int col = (c >> 1) * 64 + (lane & 7) * 8;
+                    uint4 w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int r = i * 4 + (lane >> 3), row = quarter * 32 + r, t = quotient(row0 + row, a.by_group);
-                        uint4 w;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                                     : "r"(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4)) : "memory");
-                        if ((both ? 0 : g * 128) + row < p.rows && col < a.dim)
-                            *reinterpret_cast<uint4*>(a.out + ((p.e.first + t) * a.out_ts + (p.h * a.group + row0 + row - t * a.group) * a.out_hs + col) * 2) = w;
+                        const int r = i * 4 + (lane >> 3);
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w)
+                                     : "r"(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4)));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint8_t* const to = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, (unsigned long long)out, i * 4 + (lane >> 3)));
+                        if (to && col < a.dim) *reinterpret_cast<uint4*>(to + col * 2) = w[i];
                     }
                     __syncwarp();
                 }
@@ -376,7 +351,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             auto finish_lse = [&](float mx, float sum) {
                 if (a.lse) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
             };
-            bool done = p.whole;
+            bool done = e.whole;
             if (warp_writes) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll 1
@@ -385,65 +360,72 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     float v[32];
                     if (n > 0) tc_ld32_now(t_o + c * 32, o);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = n > 0 ? __uint_as_float(o[e]) * w_own : 0.f;
+                    for (int i = 0; i < 32; ++i) v[i] = n > 0 ? __uint_as_float(o[i]) * w_own : 0.f;
                     if (add) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float4 x = *reinterpret_cast<const float4*>(meet + ((c * 8 + e) * 128 + own) * 4);
-                            v[4 * e] = fmaf(x.x, w_other, v[4 * e]); v[4 * e + 1] = fmaf(x.y, w_other, v[4 * e + 1]);
-                            v[4 * e + 2] = fmaf(x.z, w_other, v[4 * e + 2]); v[4 * e + 3] = fmaf(x.w, w_other, v[4 * e + 3]);
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 x = *reinterpret_cast<const float4*>(meet + ((c * 8 + i) * 128 + own) * 4);
+                            v[4 * i] = fmaf(x.x, w_other, v[4 * i]); v[4 * i + 1] = fmaf(x.y, w_other, v[4 * i + 1]);
+                            v[4 * i + 2] = fmaf(x.z, w_other, v[4 * i + 2]); v[4 * i + 3] = fmaf(x.w, w_other, v[4 * i + 3]);
                         }
                     }
-                    if (p.whole) finish(v, c, inv);
+                    if (e.whole) finish(v, c, inv);
                     else if (in) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            __stcg(reinterpret_cast<float4*>(slot + 2 * kAtR + ((c * 8 + e) * kAtR + tile_row) * 4), make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]));
+                        for (int i = 0; i < 8; ++i)
+                            __stcg(reinterpret_cast<float4*>(slot + 2 * kAtR + ((c * 8 + i) * kAtR + tile_row) * 4), make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
                     }
                 }
                 if (writes) {
-                    if (p.whole) finish_lse(ms, l);
+                    if (e.whole) finish_lse(ms, l);
                     else {
                         __stcg(slot + tile_row, ms);
                         __stcg(slot + kAtR + tile_row, l);
                     }
                 }
             }
+            if (both) {
+                __syncwarp();
+                free_queries();
+            }
             tc_fence_before();                                      // O is read before the next item's products
-            if (!p.whole) {
+            if (!e.whole) {
                 __threadfence();
                 named_sync(kAtBarAll, 256);
                 if (threadIdx.x == 128) {
                     // a CTA that gave up leaves the item open
-                    last_s = !*abort_p && atomicAdd(a.counters + p.first_cta, 1) == p.n_parts - 1;
-                    if (last_s) a.counters[p.first_cta] = 0;
+                    last_s = !*abort_p && atomicAdd(a.counters + e.first_cta, 1) == e.n_parts - 1;
+                    if (last_s) a.counters[e.first_cta] = 0;
                 }
                 named_sync(kAtBarAll, 256);
                 if (last_s) {
                     __threadfence();
                     done = true;
                     if (warp_writes) {
-                        auto part = [&](int j) { return a.partials + (size_t)(j ? 2 * (p.first_cta + j) : p.first_slot) * Shape::kSlot; };
+                        auto part = [&](int j) { return a.partials + (size_t)(j ? 2 * (e.first_cta + j) : e.first_slot) * Shape::kSlot; };
                         float mx = -INFINITY, sum = 0.f;
 #pragma unroll 4
-                        for (int j = 0; j < p.n_parts; ++j) mx = fmaxf(mx, __ldcg(part(j) + tile_row));
+                        for (int j = 0; j < e.n_parts; ++j) mx = fmaxf(mx, __ldcg(part(j) + tile_row));
                         const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll 4
-                        for (int j = 0; j < p.n_parts; ++j) sum += fast_exp2(__ldcg(part(j) + tile_row) - ref) * __ldcg(part(j) + kAtR + tile_row);
+                        for (int j = 0; j < e.n_parts; ++j) sum += fast_exp2(__ldcg(part(j) + tile_row) - ref) * __ldcg(part(j) + kAtR + tile_row);
                         const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
 #pragma unroll 1
                         for (int c = 0; c < DK / 32; ++c) {
                             float v[32];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = 0.f;
-                            for (int j = 0; j < p.n_parts; ++j) {
+                            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 2
+                            for (int j = 0; j < e.n_parts; ++j) {
                                 const float* f = part(j);
+                                float4 x[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x[i] = __ldcg(reinterpret_cast<const float4*>(f + 2 * kAtR + ((c * 8 + i) * kAtR + tile_row) * 4));
                                 const float w = fast_exp2(__ldcg(f + tile_row) - ref);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const float4 x = __ldcg(reinterpret_cast<const float4*>(f + 2 * kAtR + ((c * 8 + e) * kAtR + tile_row) * 4));
-                                    v[4 * e] = fmaf(x.x, w, v[4 * e]); v[4 * e + 1] = fmaf(x.y, w, v[4 * e + 1]);
-                                    v[4 * e + 2] = fmaf(x.z, w, v[4 * e + 2]); v[4 * e + 3] = fmaf(x.w, w, v[4 * e + 3]);
+                                for (int i = 0; i < 8; ++i) {
+                                    v[4 * i] = fmaf(x[i].x, w, v[4 * i]); v[4 * i + 1] = fmaf(x[i].y, w, v[4 * i + 1]);
+                                    v[4 * i + 2] = fmaf(x[i].z, w, v[4 * i + 2]); v[4 * i + 3] = fmaf(x[i].w, w, v[4 * i + 3]);
                                 }
                             }
                             finish(v, c, inv);
@@ -460,7 +442,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 const int w = __ffs(words) - 1;
                 const uint32_t bits = __shfl_sync(0xffffffffu, again, w);
                 for (int r = warp - 4; r < 32; r += 8)
-                    if (bits >> r & 1) attend_row_again<F16>(a, p.e, p.s, p.h, p.r * kAtR + w * 32 + r);
+                    if (bits >> r & 1) attend_row_again<F16>(a, e.e, e.s, e.h, e.r * kAtR + w * 32 + r);
             }
         }
     } else {
@@ -535,7 +517,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 tc_fence_after();
             };
             auto give = [&](int at) { tc_commit_on(on, smem_u32(&bar_empty[at % kStages])); };
-            auto scores = [&](int g, int at, bool first) {
+            auto scores = [&](int g, int at, bool first, bool last) {
                 if (first) {
                     ok = ok && mbar_wait_warp(smem_u32(&bar_q[g]), n_q[g] & 1, abort_p, a.status);
                     ++n_q[g];
@@ -549,6 +531,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         const uint32_t off = k / 4 * kAtKeys * 128 + k % 4 * 32;
                         tc_mma_f16_on(on, tmem + g * 128, desc_at(dq, off), desc_at(dk, off), idesc_s, k > 0);
                     }
+                if (last) tc_commit_on(on, smem_u32(&bar_free[g]));
                 tc_commit_on(on, smem_u32(&bar_s[g]));
             };
             auto outputs = [&](int g, int at, bool first, bool last) {
@@ -567,13 +550,13 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             };
             for (; next(); finished()) {
                 const AttendPart& p = parts[turn % kAtParts];
-                const int n = p.key_end - p.key_begin;
+                const int n = (int)warp_uniform(p.key_end - p.key_begin);      // operands of the products stay in uniform registers
                 if (n <= 0) continue;
-                if (p.rows > 128) {
+                if (warp_uniform(p.rows) > 128) {
                     int k_at = pos++;
                     take(k_at);
-                    scores(0, k_at, true);
-                    scores(1, k_at, true);
+                    scores(0, k_at, true, n == 1);
+                    scores(1, k_at, true, n == 1);
                     give(k_at);
                     for (int j = 0; j < n && ok; ++j) {
                         const int v_at = pos++;
@@ -582,12 +565,12 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         if (j + 1 < n) {
                             k_at = pos++;
                             take(k_at);
-                            scores(0, k_at, false);
+                            scores(0, k_at, false, j + 2 == n);
                         }
                         outputs(1, v_at, j == 0, j == n - 1);
                         give(v_at);
                         if (j + 1 < n) {
-                            scores(1, k_at, false);
+                            scores(1, k_at, false, j + 2 == n);
                             give(k_at);
                         }
                     }
@@ -595,7 +578,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     for (int j = 0; j < min(n, 2) && ok; ++j) {
                         const int at = pos++;
                         take(at);
-                        scores(j, at, true);
+                        scores(j, at, true, j + 2 >= n);
                         give(at);
                     }
                     for (int j = 0; j < n && ok; ++j) {
@@ -606,7 +589,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         if (j + 2 < n) {
                             const int at = pos++;
                             take(at);
-                            scores(j & 1, at, false);
+                            scores(j & 1, at, false, j + 4 >= n);
                             give(at);
                         }
                     }
@@ -632,13 +615,30 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 __syncwarp();
             }
         } else {
-            // ---------------------------------------------------------------- queries of the items ahead, to L2
+            // ---------------------------------------------------------------- queries, in the 128-byte swizzle
+            int n_q[2] = {0, 0};
             for (; next(); finished()) {
-                const AttendPart& p = parts[turn % kAtParts];
-                for (int u = lane; u < p.rows * (DK / 64); u += 32) {
-                    const int row = p.r * kAtR + u / (DK / 64), col = u % (DK / 64) * 64, t = quotient(row, a.by_group);
-                    if (col < a.dim)
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.q + ((p.e.first + t) * a.q_ts + (p.h * a.group + row - t * a.group) * a.q_hs + col) * 2));
+                const AttendPart p = parts[turn % kAtParts];
+                const bool both = p.rows <= 128;
+                for (int g = 0; g < 2; ++g) {
+                    if (p.key_end - p.key_begin <= (both ? g : 0)) continue;                     // the group has no tiles
+                    if (n_q[g]) ok = ok && mbar_wait_warp(smem_u32(&bar_free[g]), (n_q[g] - 1) & 1, abort_p, a.status);
+                    if (!ok) break;
+                    ++n_q[g];
+                    constexpr int kPieces = DK / 8;
+                    const int skip = both ? 0 : g * 128, c = lane % kPieces;
+                    const uint32_t to = base + g * kTile + c / 8 * kAtKeys * 128;
+#pragma unroll 8
+                    for (int r = lane / kPieces; r < 128; r += 32 / kPieces) {
+                        const bool in = skip + r < p.rows && c * 8 < a.dim;
+                        const int row = p.r * kAtR + skip + (in ? r : 0), t = quotient(row, a.by_group), head = p.h * a.group + row - t * a.group;
+                        cp_async16(to + r * 128 + ((c % 8 ^ (r & 7)) << 4), a.q + ((p.e.first + t) * a.q_ts + head * a.q_hs + (in ? c * 8 : 0)) * 2, in ? 16 : 0);
+                    }
+                    cp_async_commit();
+                    cp_async_wait<0>();
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_q[g]));
                 }
             }
         }

@@ -37,16 +37,18 @@ struct RowsShape {
     static constexpr int kRow = DK * 2;                             // bytes of a place in shared memory
     static constexpr int kStage = 2 * kRowsKeys * kRow;             // keys, then values
     static constexpr int kStages = DK == 128 ? 3 : 6;
-    static constexpr int kRing = kRowsWarps * kStages * kStage;     // 192 KB
-    static constexpr int kSlot = kRowsR * (DK + 2);                 // floats of a partial result: maximum, sum, output
-    static_assert(kRowsWarps * kSlot * 4 <= kRing, "");
+    static constexpr int kRing = kRowsWarps * kStages * kStage;     // 96 KB
+    static constexpr int kMeet = 8 * (DK + 2);                      // floats of eight rows of a warp: maxima, sums, outputs
+    static constexpr int kSmem = kRing + kRowsWarps * kMeet * 4;
+    static constexpr int kSlot = kRowsR * (DK + 2);                 // floats of a partial result: maxima, sums, outputs
 };
 
 template <bool F16, int DK>
 __global__ void __launch_bounds__(kRowsThreads, kRowsPerSm)
 attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     using Shape = RowsShape<DK>;
-    extern __shared__ __align__(1024) uint8_t smem[];
+    constexpr int kStages = Shape::kStages;
+    extern __shared__ __align__(128) uint8_t smem[];
     __shared__ AttendPlan plan;
     __shared__ int last_s;
     __shared__ uint32_t nan_s;
@@ -56,80 +58,89 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsWarps>(a, plan, kRowsHead);
     AttendWalk<kRowsR, kRowsKeys, kRowsHead> walk;
     walk.begin(a, plan);
-    const uint32_t ring = smem_u32(smem) + warp * Shape::kStages * Shape::kStage;
-    float* const meet = reinterpret_cast<float*>(smem);             // [warp][kSlot], once the rings are done with
+    const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStage;
+    float* const meet = reinterpret_cast<float*>(smem + Shape::kRing);          // [warp][kMeet]
     const int quad = lane >> 2, two = (lane & 3) * 2;
     const int n_k = (a.dim + 15) / 16;                              // steps of 16 of head_dim
 
-    AttendPart p;
-    while (walk.next(a, p)) {
-        // ---- this warp's chunks: key_begin + warp + kRowsWarps * i
-        const int n_chunk = max(0, (p.key_end - p.key_begin - warp + kRowsWarps - 1) / kRowsWarps);
-        const int32_t* const table = a.table + p.s * a.table_stride;
-        int pages = -1;                                             // lane l: page of chunk l of the 32 at hand
-        bool bad = false;
-        auto look_up = [&](int i) {
-            pages = -1;
-            if (i < n_chunk) pages = table[quotient((p.key_begin + warp + kRowsWarps * i) * kRowsKeys, a.by_page)];
-        };
+    // ---- requests: the chunks key_begin + warp + kRowsWarps * i of the part `p`, the next one's begun before the last one's result is written
+    AttendPart p = {};
+    int n_chunk = 0, pages = -1;                                    // lane l: page of chunk l of the 32 at hand
+    const int32_t* table = a.table;
+    bool bad = false;
+    auto look_up = [&](int i) {
+        pages = -1;
+        if (i < n_chunk) pages = table[quotient((p.key_begin + warp + kRowsWarps * i) * kRowsKeys, a.by_page)];
+    };
+    // A lane copies the same 16 bytes of every row that it takes.
+    constexpr int kPieces = DK / 8, kRowStep = 32 / kPieces;
+    const int piece = lane % kPieces, first_row = lane / kPieces;
+    const bool piece_in = piece * 8 < a.dim;
+    const int lane_off = piece_in ? (first_row * a.dim + piece * 8) * 2 : 0, row_off = kRowStep * a.dim * 2;
+    auto request = [&](int i) {
+        if (i < n_chunk) {
+            if (i % 32 == 0 && i) look_up(i + lane);
+            int page = __shfl_sync(0xffffffffu, pages, i % 32);
+            const int place = (p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
+            int valid = piece_in ? p.e.len - place : 0;
+            if (page < 0 || page >= a.pages) { page = 0; valid = 0; bad = true; }
+            const int in_page = place - quotient(place, a.by_page) * a.page_size;
+            const long long from = ((long long)page * a.kv_heads * a.page_size + p.h * a.page_size + in_page) * (a.dim * 2) + lane_off;
+            const uint8_t *k = a.k + from, *v = a.v + from;
+            const uint32_t to = ring + i % kStages * Shape::kStage;
+#pragma unroll
+            for (int j = 0; j < kRowsKeys / kRowStep; ++j) {
+                const int row = first_row + j * kRowStep, bytes = row < valid ? 16 : 0;
+                const uint32_t at = to + row * Shape::kRow + ((piece ^ (row & 7)) << 4);
+                cp_async16(at, k + j * row_off, bytes);
+                cp_async16(at + kRowsKeys * Shape::kRow, v + j * row_off, bytes);
+            }
+        }
+        cp_async_commit();
+    };
+    auto begin_part = [&]() -> bool {
+        if (!walk.next(a, p)) return false;
+        n_chunk = max(0, (p.key_end - p.key_begin - warp + kRowsWarps - 1) / kRowsWarps);
+        table = a.table + p.s * a.table_stride;
         look_up(lane);
+#pragma unroll 1
+        for (int i = 0; i < kStages - 1; ++i) request(i);
+        return true;
+    };
+
+    bool more = begin_part();
+    if (threadIdx.x == 0) nan_s = 0;
+    while (more) {
         // ---- queries, as the A operand; the bounds of the lane's two rows
-        const int row0 = p.r * kRowsR;
+        const int row0 = p.r * kRowsR, rows = p.rows, head0 = p.h * a.group, s_now = p.s, h_now = p.h;
+        const SeqExtent ext = p.e;
         uint32_t qf[DK / 16][4];
         int lo[2], hi[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int row = row0 + quad + 8 * b, i = quotient(row, a.by_group);
-            const bool in = quad + 8 * b < p.rows;
-            const uint8_t* q = a.q + ((p.e.first + i) * a.q_ts + (p.h * a.group + row - i * a.group) * a.q_hs + two) * 2;
-            row_bounds(a, p.e, row, in, lo[b], hi[b]);
+            const bool in = quad + 8 * b < rows;
+            const uint8_t* q = a.q + ((ext.first + i) * a.q_ts + (head0 + row - i * a.group) * a.q_hs + two) * 2;
+            row_bounds(a, ext, row, in, lo[b], hi[b]);
 #pragma unroll
             for (int k = 0; k < DK / 16; ++k)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
                     qf[k][b + 2 * c] = in && k * 16 + c * 8 < a.dim ? *reinterpret_cast<const uint32_t*>(q + (k * 16 + c * 8) * 2) : 0u;
         }
-        // A lane copies the same 16 bytes of every row that it takes.
-        constexpr int kPieces = DK / 8, kRowStep = 32 / kPieces;
-        const int piece = lane % kPieces, first_row = lane / kPieces;
-        const bool piece_in = piece * 8 < a.dim;
-        const int lane_off = piece_in ? (first_row * a.dim + piece * 8) * 2 : 0, row_off = kRowStep * a.dim * 2;
-        auto request = [&](int i) {
-            if (i < n_chunk) {
-                if (i % 32 == 0 && i) look_up(i + lane);
-                int page = __shfl_sync(0xffffffffu, pages, i % 32);
-                const int place = (p.key_begin + warp + kRowsWarps * i) * kRowsKeys;
-                int valid = piece_in ? p.e.len - place : 0;
-                if (page < 0 || page >= a.pages) { page = 0; valid = 0; bad = true; }
-                const int in_page = place - quotient(place, a.by_page) * a.page_size;
-                const long long from = ((long long)page * a.kv_heads * a.page_size + p.h * a.page_size + in_page) * (a.dim * 2) + lane_off;
-                const uint8_t *k = a.k + from, *v = a.v + from;
-                const uint32_t to = ring + i % Shape::kStages * Shape::kStage;
-#pragma unroll
-                for (int j = 0; j < kRowsKeys / kRowStep; ++j) {
-                    const int row = first_row + j * kRowStep, bytes = row < valid ? 16 : 0;
-                    const uint32_t at = to + row * Shape::kRow + ((piece ^ (row & 7)) << 4);
-                    cp_async16(at, k + j * row_off, bytes);
-                    cp_async16(at + kRowsKeys * Shape::kRow, v + j * row_off, bytes);
-                }
-            }
-            cp_async_commit();
-        };
-#pragma unroll 1
-        for (int i = 0; i < Shape::kStages - 1; ++i) request(i);
-
         float o[DK / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < DK / 8; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[d][i] = 0.f;
 
+#pragma unroll 1
         for (int i = 0; i < n_chunk; ++i) {
             __syncwarp();                                           // the stage that the next request overwrites is read
-            request(i + Shape::kStages - 1);
-            cp_async_wait<Shape::kStages - 1>();
+            request(i + kStages - 1);
+            cp_async_wait<kStages - 1>();
             __syncwarp();
-            const uint32_t kt = ring + i % Shape::kStages * Shape::kStage, vt = kt + kRowsKeys * Shape::kRow;
+            const uint32_t kt = ring + i % kStages * Shape::kStage, vt = kt + kRowsKeys * Shape::kRow;
             float sc[2][4] = {};
 #pragma unroll
             for (int k = 0; k < DK / 16; ++k) {
@@ -189,93 +200,124 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             }
         }
         cp_async_wait<0>();
-        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
+        __syncwarp();
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             l[b] += __shfl_xor_sync(0xffffffffu, l[b], 1);
             l[b] += __shfl_xor_sync(0xffffffffu, l[b], 2);
         }
+        const bool whole = p.whole;
+        const int first_cta = p.first_cta, n_parts = p.n_parts, slot_i = p.slot, first_slot = p.first_slot;
+        more = begin_part();
 
-        // ---- the warps meet: [0..15] maxima, [16..31] sums, then rows of outputs
-        __syncthreads();
-        float* const mine = meet + warp * Shape::kSlot;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int row = quad + 8 * b;
-            if (row < p.rows) {
-                if (two == 0) { mine[row] = m[b]; mine[kRowsR + row] = l[b]; }
-#pragma unroll
-                for (int d = 0; d < DK / 8; ++d)
-                    *reinterpret_cast<float2*>(mine + 2 * kRowsR + row * DK + d * 8 + two) = make_float2(o[d][2 * b], o[d][2 * b + 1]);
-            }
-        }
-        if (threadIdx.x == 0) nan_s = 0;
-        __syncthreads();
-        // n parts, `apart` floats from one to the next, read by `at`: four elements of a row, its maximum and its sum
-        auto join = [&](auto at, const float* from, const float* rest, int n, size_t apart, int row, int col, float (&v)[4], float& mx, float& sum) {
-            mx = -INFINITY;
-            for (int j = 0; j < n; ++j) mx = fmaxf(mx, at((j ? rest + j * apart : from) + row));
-            const float base = mx == -INFINITY ? 0.f : mx;
-            sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = 0.f;
-            for (int j = 0; j < n; ++j) {
-                const float* f = j ? rest + j * apart : from;
-                const float w = fast_exp2(at(f + row) - base);
-                sum += w * at(f + kRowsR + row);
-                const float4 x = at(reinterpret_cast<const float4*>(f + 2 * kRowsR + row * DK + col));
-                v[0] = fmaf(w, x.x, v[0]); v[1] = fmaf(w, x.y, v[1]); v[2] = fmaf(w, x.z, v[2]); v[3] = fmaf(w, x.w, v[3]);
-            }
-        };
-        auto finish = [&](int row, int col, const float (&v)[4], float mx, float sum) {
-            const int i = quotient(row0 + row, a.by_group), head = p.h * a.group + row0 + row - i * a.group;
-            const long long token = p.e.first + i;
+        // ---- the warps meet, eight rows at a time, while the next part's first places are on their way
+        constexpr int kCols = DK / 4;
+        const int col = threadIdx.x % kCols * 4;
+        float* const slot = a.partials + (size_t)slot_i * Shape::kSlot;
+        auto finish = [&](int row, float4 v, float mx, float sum) {
+            const int i = quotient(row0 + row, a.by_group), head = head0 + row0 + row - i * a.group;
+            const long long token = ext.first + i;
             const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-            const float x[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-            if (x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]) atomicOr(&nan_s, 1u << row);
-            if (col < a.dim)
-                *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + col) * 2) = make_uint2(pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3]));
+            v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+            if (v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w) atomicOr(&nan_s, 1u << row);
+            if (col < a.dim) *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + col) * 2) = make_uint2(pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w));
             if (a.lse && col == 0) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
         };
-        constexpr int kCols = DK / 4, kPerRow = kRowsThreads / kCols;
-        const int col = threadIdx.x % kCols * 4;
-        bool done = p.whole;
-        float* const slot = a.partials + (size_t)p.slot * Shape::kSlot;
-        for (int row = threadIdx.x / kCols; row < p.rows; row += kPerRow) {
-            float v[4], mx, sum;
-            join([](auto* f) { return *f; }, meet, meet, kRowsWarps, Shape::kSlot, row, col, v, mx, sum);
-            if (p.whole) finish(row, col, v, mx, sum);
-            else {
-                if (col == 0) { __stcg(slot + row, mx); __stcg(slot + kRowsR + row, sum); }
-                __stcg(reinterpret_cast<float4*>(slot + 2 * kRowsR + row * DK + col), make_float4(v[0], v[1], v[2], v[3]));
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (b * 8 >= rows) break;
+            if (quad + b * 8 < rows) {
+                float* const mine = meet + warp * Shape::kMeet;
+                if (two == 0) { mine[quad] = m[b]; mine[8 + quad] = l[b]; }
+#pragma unroll
+                for (int d = 0; d < DK / 8; ++d)
+                    *reinterpret_cast<float2*>(mine + 16 + quad * DK + d * 8 + two) = make_float2(o[d][2 * b], o[d][2 * b + 1]);
             }
-        }
-        if (!p.whole) {
-            __threadfence();
             __syncthreads();
+#pragma unroll 1
+            for (int r = threadIdx.x / kCols; r < min(8, rows - b * 8); r += kRowsThreads / kCols) {
+                float w[kRowsWarps], top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < kRowsWarps; ++j) {
+                    w[j] = meet[j * Shape::kMeet + r];
+                    top = fmaxf(top, w[j]);
+                }
+                const float base = top == -INFINITY ? 0.f : top;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int j = 0; j < kRowsWarps; ++j) {
+                    w[j] = fast_exp2(w[j] - base);
+                    sum = fmaf(meet[j * Shape::kMeet + 8 + r], w[j], sum);
+                    const float4 x = *reinterpret_cast<const float4*>(meet + j * Shape::kMeet + 16 + r * DK + col);
+                    v.x = fmaf(x.x, w[j], v.x); v.y = fmaf(x.y, w[j], v.y); v.z = fmaf(x.z, w[j], v.z); v.w = fmaf(x.w, w[j], v.w);
+                }
+                const int row = b * 8 + r;
+                if (whole) {
+                    finish(row, v, top, sum);
+                } else {
+                    if (col == 0) { __stcg(slot + row, top); __stcg(slot + kRowsR + row, sum); }
+                    __stcg(reinterpret_cast<float4*>(slot + 2 * kRowsR + row * DK + col), v);
+                }
+            }
+            if (!whole) __threadfence();
+            __syncthreads();
+        }
+        if (!whole) {
             if (threadIdx.x == 0) {
-                last_s = atomicAdd(a.counters + p.first_cta, 1) == p.n_parts - 1;
-                if (last_s) a.counters[p.first_cta] = 0;
+                last_s = atomicAdd(a.counters + first_cta, 1) == n_parts - 1;
+                if (last_s) a.counters[first_cta] = 0;
             }
             __syncthreads();
             if (last_s) {
                 __threadfence();
-                done = true;
-                const float* first = a.partials + (size_t)p.first_slot * Shape::kSlot;
-                const float* rest = a.partials + (size_t)(2 * p.first_cta) * Shape::kSlot;
-                for (int row = threadIdx.x / kCols; row < p.rows; row += kPerRow) {
-                    float v[4], mx, sum;
-                    join([](auto* f) { return __ldcg(f); }, first, rest, p.n_parts, 2 * Shape::kSlot, row, col, v, mx, sum);
-                    finish(row, col, v, mx, sum);
+                const float* first = a.partials + (size_t)first_slot * Shape::kSlot;
+                const float* rest = a.partials + (size_t)(2 * first_cta) * Shape::kSlot;
+                constexpr int kAhead = 12;                          // parts whose loads are under way together
+#pragma unroll 1
+                for (int row = threadIdx.x / kCols; row < rows; row += kRowsThreads / kCols) {
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    float mx = -INFINITY, sum = 0.f;
+#pragma unroll 1
+                    for (int j0 = 0; j0 < n_parts; j0 += kAhead) {
+                        float pm[kAhead], pl[kAhead];
+                        float4 po[kAhead];
+#pragma unroll
+                        for (int j = 0; j < kAhead; ++j) {
+                            const float* f = j0 + j ? rest + (size_t)(j0 + j) * 2 * Shape::kSlot : first;
+                            const bool there = j0 + j < n_parts;
+                            pm[j] = there ? __ldcg(f + row) : -INFINITY;
+                            pl[j] = there ? __ldcg(f + kRowsR + row) : 0.f;
+                            po[j] = there ? __ldcg(reinterpret_cast<const float4*>(f + 2 * kRowsR + row * DK + col)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                        float top = mx;
+#pragma unroll
+                        for (int j = 0; j < kAhead; ++j) top = fmaxf(top, pm[j]);
+                        const float base = top == -INFINITY ? 0.f : top, was = fast_exp2(mx - base);
+                        mx = top;
+                        sum *= was;
+                        v = make_float4(v.x * was, v.y * was, v.z * was, v.w * was);
+#pragma unroll
+                        for (int j = 0; j < kAhead; ++j) {
+                            const float w = fast_exp2(pm[j] - base);
+                            sum = fmaf(pl[j], w, sum);
+                            v.x = fmaf(po[j].x, w, v.x); v.y = fmaf(po[j].y, w, v.y); v.z = fmaf(po[j].z, w, v.z); v.w = fmaf(po[j].w, w, v.w);
+                        }
+                    }
+                    finish(row, v, mx, sum);
                 }
+                __syncthreads();
             }
         }
-        __syncthreads();
-        if (done && nan_s)
-            for (int row = warp; row < p.rows; row += kRowsWarps)
-                if (nan_s >> row & 1) attend_row_again<F16>(a, p.e, p.s, p.h, row0 + row);
-        __syncthreads();
+        // rows with a NaN once more; the barriers above order this after their first results, and the next one before more are noted
+        if (nan_s) {
+            for (int row = warp; row < rows; row += kRowsWarps)
+                if (nan_s >> row & 1) attend_row_again<F16>(a, ext, s_now, h_now, row0 + row);
+            __syncthreads();
+            if (threadIdx.x == 0) nan_s = 0;
+            __syncthreads();
+        }
     }
+    if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
 }
 
 // Both forms have their partial results at the same place: calls that share a workspace are ordered.
@@ -290,10 +332,10 @@ template <bool F16, int DK>
 static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t st) {
     static DeviceOnce once;
     const cudaError_t e = once_on_device(once, [] {
-        return cudaFuncSetAttribute(attend_rows_kernel<F16, DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DK>::kRing);
+        return cudaFuncSetAttribute(attend_rows_kernel<F16, DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DK>::kSmem);
     });
     if (e != cudaSuccess) return e;
-    return launch_pdl(attend_rows_kernel<F16, DK>, dim3(kRowsPerSm * n_sm), dim3(kRowsThreads), RowsShape<DK>::kRing, st, a);
+    return launch_pdl(attend_rows_kernel<F16, DK>, dim3(kRowsPerSm * n_sm), dim3(kRowsThreads), RowsShape<DK>::kSmem, st, a);
 }
 static cudaError_t launch_rows(const AttendArgs& a, bool f16, int n_sm, cudaStream_t st) {
     if (a.dim <= 64) return f16 ? launch_rows_typed<true, 64>(a, n_sm, st) : launch_rows_typed<false, 64>(a, n_sm, st);

@@ -65,6 +65,7 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 struct SeqExtent {
     int first, n, len;                      // first row of the call's tokens, new tokens, places
 };
@@ -96,7 +97,7 @@ struct AttendPlan {                         // in shared memory
     long long per, begin, end;              // units of a range, and this CTA's
     long long seq_begin;                    // unit at which sequence s begins
     int s;
-    long long scan[32];
+    long long scan[12];                     // a warp each
 };
 
 // All threads of the CTA (WARPS whole warps); MIN_UNITS: a CTA takes no fewer units while there are others.

@@ -74,7 +74,6 @@ __device__ __forceinline__ void tc_ld32_now(uint32_t taddr, uint32_t* r) {
     tc_reg_fence16(r);
     tc_reg_fence16(r + 16);
 }
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

@@ -12,7 +12,8 @@
 namespace saem {
 
 constexpr int kRowsWarps = 4, kRowsThreads = kRowsWarps * 32;
-constexpr int kRowsR = 16, kRowsKeys = 16, kRowsHead = 8;
+constexpr int kRowsR = 16, kRowsKeys = 16, kRowsHead = 12;
+constexpr int kRowsLeast = 8;               // units of a CTA's range at least
 constexpr int kRowsPerSm = 2;               // CTAs
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
@@ -55,7 +56,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsWarps>(a, plan, kRowsHead);
+    make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsWarps>(a, plan, kRowsLeast);
     AttendWalk<kRowsR, kRowsKeys, kRowsHead> walk;
     walk.begin(a, plan);
     const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStage;

@@ -13,6 +13,7 @@ namespace saem {
 
 constexpr int kRowsWarps = 4, kRowsThreads = kRowsWarps * 32;
 constexpr int kRowsR = 16, kRowsKeys = 16, kRowsHead = 12;
+constexpr int kRowsSnap = 24;
 constexpr int kRowsLeast = 8;               // units of a CTA's range at least
 constexpr int kRowsPerSm = 2;               // CTAs
 
@@ -56,8 +57,8 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsWarps>(a, plan, kRowsLeast);
-    AttendWalk<kRowsR, kRowsKeys, kRowsHead> walk;
+    make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsLeast, kRowsWarps>(a, plan);
+    AttendWalk<kRowsR, kRowsKeys, kRowsHead, kRowsSnap> walk;
     walk.begin(a, plan);
     const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStage;
     float* const meet = reinterpret_cast<float*>(smem + Shape::kRing);          // [warp][kMeet]
@@ -208,7 +209,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             l[b] += __shfl_xor_sync(0xffffffffu, l[b], 2);
         }
         const bool whole = p.whole;
-        const int first_cta = p.first_cta, n_parts = p.n_parts, slot_i = p.slot, first_slot = p.first_slot;
+        const int first_cta = p.first_cta, n_parts = p.n_parts, slot_i = p.slot;
         more = begin_part();
 
         // ---- the warps meet, eight rows at a time, while the next part's first places are on their way
@@ -260,19 +261,17 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                     __stcg(reinterpret_cast<float4*>(slot + 2 * kRowsR + row * DK + col), v);
                 }
             }
-            if (!whole) __threadfence();
             __syncthreads();
         }
         if (!whole) {
             if (threadIdx.x == 0) {
+                __threadfence();                                    // what the barrier has ordered before it, too
                 last_s = atomicAdd(a.counters + first_cta, 1) == n_parts - 1;
                 if (last_s) a.counters[first_cta] = 0;
             }
             __syncthreads();
             if (last_s) {
                 __threadfence();
-                const float* first = a.partials + (size_t)first_slot * Shape::kSlot;
-                const float* rest = a.partials + (size_t)(2 * first_cta) * Shape::kSlot;
                 constexpr int kAhead = 12;                          // parts whose loads are under way together
 #pragma unroll 1
                 for (int row = threadIdx.x / kCols; row < rows; row += kRowsThreads / kCols) {
@@ -284,7 +283,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                         float4 po[kAhead];
 #pragma unroll
                         for (int j = 0; j < kAhead; ++j) {
-                            const float* f = j0 + j ? rest + (size_t)(j0 + j) * 2 * Shape::kSlot : first;
+                            const float* f = a.partials + (size_t)part_slot(first_cta, j0 + j) * Shape::kSlot;
                             const bool there = j0 + j < n_parts;
                             pm[j] = there ? __ldcg(f + row) : -INFINITY;
                             pl[j] = there ? __ldcg(f + kRowsR + row) : 0.f;

@@ -2,11 +2,11 @@
 //
 // An item is a tile of R rows of one sequence and one key head (row = token * group + query head within the group); its units are the
 // tiles of KEYS places that any of its rows may see, one at least, so that rows that see nothing are written too, behind HEAD units
-// for what an item costs by itself (queries, first bytes, the result).  All units of
-// a call, in the order sequence, key head, row tile, are cut into as many equal ranges as there are CTAs: long and short
-// sequences, few and many rows load the SMs alike.  A cut within an item's first HEAD units moves to its beginning.  An item that is cut leaves
-// sums of its parts in the workspace, and the CTA that
-// arrives last adds them up in the order of the parts, so that two runs give the same bits.
+// for what an item costs by itself (queries, first bytes, the result).  All units of a call, in the order sequence, key head, row
+// tile, are cut into as many equal ranges as there are CTAs: long and short sequences, few and many rows load the SMs alike.  A cut
+// within an item's first HEAD units moves to its beginning, and one within SNAP units (or a third of a range, if that is less) of either end of an
+// item moves there, because a cut costs about as much.  An item that is still cut leaves sums of its parts in the workspace, and the CTA
+// that arrives last adds them up in the order of the parts, so that two runs give the same bits.
 #ifndef SAEM_ATTEND_PLAN_CUH_
 #define SAEM_ATTEND_PLAN_CUH_
 
@@ -94,21 +94,21 @@ __device__ __forceinline__ int item_units(const AttendArgs& a, const SeqExtent& 
 }
 
 struct AttendPlan {                         // in shared memory
-    long long per, begin, end;              // units of a range, and this CTA's
-    long long seq_begin;                    // unit at which sequence s begins
-    int s;
+    long long per;                          // units of a range
+    long long begin, seq_begin;             // first unit of this CTA's range, and of the sequence s that it lies in
+    int s;                                  // seqs: the CTA has no range
     long long scan[12];                     // a warp each
 };
 
-// All threads of the CTA (WARPS whole warps); MIN_UNITS: a CTA takes no fewer units while there are others.
-template <int R, int KEYS, int HEAD, int WARPS>
-__device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p, int min_units) {
+// All threads of the CTA (WARPS whole warps); a range has LEAST units at least.
+template <int R, int KEYS, int HEAD, int LEAST, int WARPS>
+__device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p) {
+    static_assert(WARPS <= 12, "");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kStep = WARPS * 32;
     auto units_of = [&](int s) -> long long {
         // a lane per sequence; the row tiles of a sequence with more than one are shared out over the warp
-        const bool in = s < a.seqs;
-        const SeqExtent e = in ? seq_extent(a, s) : SeqExtent{0, 0, 0};
+        const SeqExtent e = s < a.seqs ? seq_extent(a, s) : SeqExtent{0, 0, 0};
         const int tiles = row_tiles<R>(a, e);
         long long u = tiles == 1 ? item_units<R, KEYS, HEAD>(a, e, 0) : 0;
         for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 1); many; many &= many - 1) {
@@ -123,65 +123,51 @@ __device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p, in
         }
         return u * a.kv_heads;
     };
-    auto range_of = [&](long long total) {
-        const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)min_units);
-        p.per = per; p.begin = min(total, per * blockIdx.x); p.end = min(total, p.begin + per);
+    auto inclusive = [&](long long v) {
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += o;
+        }
+        return v;
     };
+    auto range_of = [&](long long total) { return max((total + gridDim.x - 1) / gridDim.x, (long long)LEAST); };
+    if (threadIdx.x == 0) p.s = a.seqs;
     if (a.seqs <= 32) {                     // one warp's work
         if (warp == 0) {
-            const long long mine = units_of(lane);
-            long long incl = mine;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const long long o = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += o;
-            }
-            const long long total = __shfl_sync(0xffffffffu, incl, 31);
-            if (lane == 0) range_of(total);
+            const long long mine = units_of(lane), incl = inclusive(mine), per = range_of(__shfl_sync(0xffffffffu, incl, 31)), begin = per * blockIdx.x;
             __syncwarp();
-            const long long begin = p.begin;
-            if (incl - mine <= begin && begin < incl) { p.s = lane; p.seq_begin = incl - mine; }
+            if (incl - mine <= begin && begin < incl) { p.per = per; p.begin = begin; p.seq_begin = incl - mine; p.s = lane; }
         }
         __syncthreads();
         return;
     }
-    long long mine = units_of(warp * 32 + lane), sum = mine;
-    for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += units_of(s + lane);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    long long mine = units_of(warp * 32 + lane), incl = inclusive(mine), sum = __shfl_sync(0xffffffffu, incl, 31);
+    for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += __shfl_sync(0xffffffffu, inclusive(units_of(s + lane)), 31);
     if (lane == 0) p.scan[warp] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        long long total = 0;
+    long long total = 0;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) total += p.scan[w];
-        range_of(total);
-    }
-    __syncthreads();
-    const long long begin = p.begin;
-    if (begin >= p.end) return;
+    for (int w = 0; w < WARPS; ++w) total += p.scan[w];
+    const long long per = range_of(total), begin = per * blockIdx.x;
+    if (begin >= total) return;
     long long before = 0;
-    for (int s0 = 0; s0 < a.seqs; s0 += kStep) {
-        const int s = s0 + warp * 32 + lane;
-        if (s0) mine = units_of(s);
-        long long incl = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long o = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += o;
+    for (int s0 = 0; before <= begin; s0 += kStep) {
+        if (a.seqs > kStep) {               // the sums are not those of this step's sequences
+            if (s0) incl = inclusive(mine = units_of(s0 + warp * 32 + lane));
+            __syncthreads();
+            if (lane == 31) p.scan[warp] = incl;
+            __syncthreads();
         }
-        if (lane == 31) p.scan[warp] = incl;
-        __syncthreads();
         long long base = before;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
             if (w < warp) base += p.scan[w];
             before += p.scan[w];
         }
-        if (base + incl - mine <= begin && begin < base + incl) { p.s = s; p.seq_begin = base + incl - mine; }
-        __syncthreads();
-        if (before > begin) break;
+        if (base + incl - mine <= begin && begin < base + incl) { p.per = per; p.begin = begin; p.seq_begin = base + incl - mine; p.s = s0 + warp * 32 + lane; }
     }
+    __syncthreads();
 }
 
 // A part of an item: what one CTA does of it between two looks at the plan.
@@ -191,19 +177,25 @@ struct AttendPart {
     int rows;                               // of the tile
     int key_begin, key_end;                 // tiles of KEYS places; none where the rows see nothing
     bool whole;                             // the item is not cut
-    int first_cta, n_parts, part, slot;     // where it is: which of the parts this is, and its place in the workspace
-    int first_slot;                         // the first part's place; part j has 2 * (first_cta + j)
+    int first_cta, n_parts, slot;           // where it is: the CTA of its first part, the parts, and this one's place in the workspace
 };
+// The places in the workspace: a CTA has at most two parts of cut items, one that begins its item and one that does not.
+__device__ __forceinline__ int part_slot(int first_cta, int j) { return 2 * (first_cta + j) + (j == 0 ? 1 : 0); }
+
 // Walks through a CTA's range; every warp for itself, alike in all lanes.
-template <int R, int KEYS, int HEAD>
+template <int R, int KEYS, int HEAD, int SNAP>
 struct AttendWalk {
-    long long at, end, item;                // next unit, end of the range, first unit of the item at hand
-    long long per;                          // units of a range
+    long long item, per;                    // first unit of the item at hand; units of a range
+    int snap, low;
     int s, h, r, tiles;
     SeqExtent e;
     __device__ __forceinline__ void begin(const AttendArgs& a, const AttendPlan& p) {
-        at = p.begin; end = p.end; per = p.per; s = p.s;
-        if (at >= end) return;
+        s = p.s;
+        if (s >= a.seqs) return;
+        per = p.per;
+        snap = (int)min(per / 3, (long long)SNAP);
+        low = max(HEAD, snap);
+        const long long at = p.begin;
         e = seq_extent(a, s);
         tiles = row_tiles<R>(a, e);
         item = p.seq_begin;
@@ -241,43 +233,40 @@ struct AttendWalk {
         }
     }
     __device__ __forceinline__ bool next(const AttendArgs& a, AttendPart& p) {
-        if (at >= end) return false;
-        const int row0 = r * R, row1 = row0 + min(e.n * a.group - row0, R) - 1;
-        int b, t;
-        key_tiles<KEYS>(a, e, row0, row1, b, t);
-        const int units = HEAD + max(1, t - b);
-        const long long stop = min(end, item + units);
-        if (stop <= item + HEAD) return false;      // the range ends here; the next CTA begins this item
-        p.e = e; p.s = s; p.h = h; p.r = r;
-        p.rows = row1 - row0 + 1;
-        p.key_begin = b + max(0, (int)(at - item) - HEAD);
-        p.key_end = min(t, b + (int)(stop - item) - HEAD);
-        p.whole = at <= item + HEAD && stop == item + units;
-        if (!p.whole) {
-            const int me = blockIdx.x;
-            p.first_cta = (int)((item + HEAD) / per);
-            p.n_parts = (int)((item + units - 1) / per) - p.first_cta + 1;
-            p.part = me - p.first_cta;
-            p.first_slot = 2 * p.first_cta + (item > per * p.first_cta ? 1 : 0);
-            p.slot = p.part ? 2 * me : p.first_slot;
-        }
-        at = stop;
-        if (stop == item + units) {
-            item = stop;
+        const int me = blockIdx.x;
+        while (s < a.seqs) {
+            const int row0 = r * R, row1 = row0 + min(e.n * a.group - row0, R) - 1;
+            int b, t;
+            key_tiles<KEYS>(a, e, row0, row1, b, t);
+            const int units = HEAD + max(1, t - b);
+            // its parts begin with the item and at the cuts between item + low and item + units - snap
+            const int first = (int)((item + min(low, units - 1)) / per), last = max(first, (int)((item + units - snap - 1) / per));
+            if (first > me) return false;
+            const bool mine = me <= last;
+            if (mine) {
+                p.e = e; p.s = s; p.h = h; p.r = r;
+                p.rows = row1 - row0 + 1;
+                p.key_begin = me == first ? b : b + (int)(per * me - item) - HEAD;
+                p.key_end = me == last ? t : b + (int)(per * (me + 1) - item) - HEAD;
+                p.whole = first == last;
+                p.first_cta = first;
+                p.n_parts = last - first + 1;
+                p.slot = part_slot(first, me - first);
+                if (me < last) { s = a.seqs; return true; }
+            }
+            item += units;
             if (++r == tiles) {
                 r = 0;
                 if (++h == a.kv_heads) {
                     h = 0;
-                    e.n = 0;                        // some later sequence has the units that are left, if any are
-                    while (at < end && e.n == 0) {
-                        if (++s < a.seqs) e = seq_extent(a, s);
-                        else at = end;
-                    }
+                    do e.n = 0;
+                    while (++s < a.seqs && (e = seq_extent(a, s)).n == 0);
                     tiles = row_tiles<R>(a, e);
                 }
             }
+            if (mine) return true;
         }
-        return true;
+        return false;
     }
 };
 

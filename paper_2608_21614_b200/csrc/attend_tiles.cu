@@ -20,7 +20,7 @@ namespace saem {
 
 constexpr int kAtThreads = 384;             // a warpgroup that copies and issues products and looks ahead, two with rows
 constexpr int kAtRegsFew = 72, kAtRegsMany = 216;                   // of 168 per thread at launch: 72 + 2 * 216 = 3 * 168
-constexpr int kAtR = 256, kAtKeys = 128, kAtHead = 2;
+constexpr int kAtR = 256, kAtKeys = 128, kAtHead = 2, kAtSnap = 4;
 constexpr int kAtMaxStages = 10;
 constexpr int kAtStage = 32 * 128;          // a warp's place for 64 columns of its 32 rows' results
 constexpr int kAtParts = 3;                 // items read ahead
@@ -162,7 +162,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
     pdl_wait();
     pdl_launch_dependents();
-    make_plan<kAtR, kAtKeys, kAtHead, kAtThreads / 32>(a, plan, kAtHead + 1);
+    make_plan<kAtR, kAtKeys, kAtHead, kAtHead + 1, kAtThreads / 32>(a, plan);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -389,9 +389,9 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             }
             tc_fence_before();                                      // O is read before the next item's products
             if (!e.whole) {
-                __threadfence();
                 named_sync(kAtBarAll, 256);
                 if (threadIdx.x == 128) {
+                    __threadfence();                                // what the barrier has ordered before it, too
                     // a CTA that gave up leaves the item open
                     last_s = !*abort_p && atomicAdd(a.counters + e.first_cta, 1) == e.n_parts - 1;
                     if (last_s) a.counters[e.first_cta] = 0;
@@ -401,7 +401,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     __threadfence();
                     done = true;
                     if (warp_writes) {
-                        auto part = [&](int j) { return a.partials + (size_t)(j ? 2 * (e.first_cta + j) : e.first_slot) * Shape::kSlot; };
+                        auto part = [&](int j) { return a.partials + (size_t)part_slot(e.first_cta, j) * Shape::kSlot; };
                         float mx = -INFINITY, sum = 0.f;
 #pragma unroll 4
                         for (int j = 0; j < e.n_parts; ++j) mx = fmaxf(mx, __ldcg(part(j) + tile_row));
@@ -599,7 +599,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             mbar_settle_warp(smem_u32(&bar_end), 0, a.status);
         } else if (warp == 2) {
             // ---------------------------------------------------------------- items
-            AttendWalk<kAtR, kAtKeys, kAtHead> walk;
+            AttendWalk<kAtR, kAtKeys, kAtHead, kAtSnap> walk;
             walk.begin(a, plan);
             for (bool more = true; more; ++turn) {
                 const int at = turn % kAtParts;

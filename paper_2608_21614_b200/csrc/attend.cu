@@ -13,7 +13,7 @@ namespace saem {
 
 constexpr int kRowsWarps = 4, kRowsThreads = kRowsWarps * 32;
 constexpr int kRowsR = 16, kRowsKeys = 16, kRowsHead = 12;
-constexpr int kRowsSnap = 24;
+constexpr int kRowsSnap = 12;
 constexpr int kRowsLeast = 8;               // units of a CTA's range at least
 constexpr int kRowsPerSm = 2;               // CTAs
 
@@ -325,8 +325,10 @@ static size_t partials_bytes(int dim, int n_sm) {
     const size_t rows = (size_t)2 * kRowsPerSm * n_sm * RowsShape<kHeadDimMax>::kSlot * 4, tiles = attend_tiles_partials(dim, n_sm);
     return rows > tiles ? rows : tiles;
 }
-// The most rows of a sequence and key head that go to the form for few.
-constexpr long long kRowsMost = 16;
+// Which form, by the most rows of a sequence and key head (times in us, 8 key heads of 128 elements; few, many).  One tile of 16: few.  Two
+// tiles read the cache twice, from L2 where there is one sequence: 20 rows over 500 places 13.0, 17.0, over 4000 21.4, 27.6, over 16000
+// 33.5, 35.5; of 8 sequences 20.3, 20.1 and 47.9, 43.3 and 175, 98; 64 rows of one sequence over 16000 44.7, 37.3.
+static bool rows_are_few(long long rows, int seqs) { return rows <= 16 || (rows <= 32 && seqs == 1); }
 
 template <bool F16, int DK>
 static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t st) {
@@ -390,7 +392,7 @@ extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cac
     a.status = reinterpret_cast<int*>(ws);
     a.counters = reinterpret_cast<int*>(ws + kAttendCounters);
     a.partials = reinterpret_cast<float*>(ws + SAEM_ATTEND_HEAD_BYTES);
-    const bool f16 = cache->dtype == SAEM_OUT_F16, few = (long long)b->max_new * a.group <= kRowsMost;
+    const bool f16 = cache->dtype == SAEM_OUT_F16, few = rows_are_few((long long)b->max_new * a.group, b->seqs);
     const cudaError_t e = few ? launch_rows(a, f16, n_sm, (cudaStream_t)stream) : launch_attend_tiles(a, f16, n_sm, (cudaStream_t)stream);
     return e == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }

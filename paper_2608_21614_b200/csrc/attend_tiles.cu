@@ -20,7 +20,7 @@ namespace saem {
 
 constexpr int kAtThreads = 384;             // a warpgroup that copies and issues products and looks ahead, two with rows
 constexpr int kAtRegsFew = 72, kAtRegsMany = 216;                   // of 168 per thread at launch: 72 + 2 * 216 = 3 * 168
-constexpr int kAtR = 256, kAtKeys = 128, kAtHead = 2, kAtSnap = 4;
+constexpr int kAtR = 256, kAtKeys = 128, kAtHead = 4, kAtSnap = 4;
 constexpr int kAtMaxStages = 10;
 constexpr int kAtStage = 32 * 128;          // a warp's place for 64 columns of its 32 rows' results
 constexpr int kAtParts = 3;                 // items read ahead
@@ -400,8 +400,47 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (last_s) {
                     __threadfence();
                     done = true;
-                    if (warp_writes) {
-                        auto part = [&](int j) { return a.partials + (size_t)part_slot(e.first_cta, j) * Shape::kSlot; };
+                    auto part = [&](int j) { return a.partials + (size_t)part_slot(e.first_cta, j) * Shape::kSlot; };
+                    if (e.rows <= 64) {
+                        // few rows, and often many parts: the columns are shared out over the warps, and four parts are under way at once
+                        const int blocks = e.rows <= 32 ? 1 : 2, row = (warp & (blocks - 1)) * 32 + lane, wide = DK / 32 * blocks;   // fours of columns a warp
+                        const int at0 = (warp - 4) / blocks * wide, row_of_all = e.r * kAtR + row, t = quotient(row_of_all, a.by_group);
+                        if (row < e.rows) {
+                            const long long tok = e.e.first + t;
+                            const int hd = e.h * a.group + row_of_all - t * a.group;
+                            float mx = -INFINITY, sum = 0.f;
+#pragma unroll 8
+                            for (int j = 0; j < e.n_parts; ++j) mx = fmaxf(mx, __ldcg(part(j) + row));
+                            const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll 8
+                            for (int j = 0; j < e.n_parts; ++j) sum += fast_exp2(__ldcg(part(j) + row) - ref) * __ldcg(part(j) + kAtR + row);
+                            const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                            float any = 0.f;
+#pragma unroll 1
+                            for (int c = at0; c < at0 + wide; c += 2) {
+                                float4 v[2] = {};
+#pragma unroll 4
+                                for (int j = 0; j < e.n_parts; ++j) {
+                                    const float* f = part(j);
+                                    const float w = fast_exp2(__ldcg(f + row) - ref);
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        const float4 x = __ldcg(reinterpret_cast<const float4*>(f + 2 * kAtR + ((c + i) * kAtR + row) * 4));
+                                        v[i].x = fmaf(x.x, w, v[i].x); v[i].y = fmaf(x.y, w, v[i].y); v[i].z = fmaf(x.z, w, v[i].z); v[i].w = fmaf(x.w, w, v[i].w);
+                                    }
+                                }
+                                if (c * 4 < a.dim) {
+                                    const uint4 w = make_uint4(pack2<F16>(v[0].x * inv, v[0].y * inv), pack2<F16>(v[0].z * inv, v[0].w * inv),
+                                                               pack2<F16>(v[1].x * inv, v[1].y * inv), pack2<F16>(v[1].z * inv, v[1].w * inv));
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) any = fmaf(v[i].x * inv, 0.f, fmaf(v[i].y * inv, 0.f, fmaf(v[i].z * inv, 0.f, fmaf(v[i].w * inv, 0.f, any))));
+                                    *reinterpret_cast<uint4*>(a.out + (tok * a.out_ts + hd * a.out_hs + c * 4) * 2) = w;
+                                }
+                            }
+                            if (any != any) atomicOr(&nan_s[turn & 1][row >> 5], 1u << (row & 31));
+                            if (a.lse && at0 == 0) a.lse[tok * a.group * a.kv_heads + hd] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
+                        }
+                    } else if (warp_writes) {
                         float mx = -INFINITY, sum = 0.f;
 #pragma unroll 4
                         for (int j = 0; j < e.n_parts; ++j) mx = fmaxf(mx, __ldcg(part(j) + tile_row));

@@ -3,8 +3,9 @@
 //
 // A head is eight elements for each of 8 or 16 neighbouring lanes: two runs of four, which are the two halves of four pairs (half
 // layout) or four pairs next to each other (interleaved), so that a rotation stays within a lane and only the norm's sum crosses
-// them.  A group of lanes keeps the sines and cosines of one token for all the heads that it takes: they cost more
-// instructions than the rest of a head.  The bound is DRAM for many tokens; for one it is the launch and a chain of loads.
+// them.  A group of lanes takes some neighbouring heads of one token, all queries, all keys or all values, and keeps the token's sines and
+// cosines for them: they cost more instructions than the rest of a head.  Four heads are under way ahead of the one at hand.  The
+// bound is DRAM for many tokens; for one it is the launch and a chain of loads.
 //
 // The angle in turns is position * turns[i] mod 2^64 in integers, exact but for the frequency's own rounding (2^-65 turns
 // a position); its upper 32 bits, signed, times 2^-31 are the argument of sincospi in [-1, 1).
@@ -13,84 +14,99 @@
 namespace saem {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotBatch = 4;                // heads whose loads are under way together
+constexpr int kRotMost = 8;                 // heads of a group at most
+constexpr int kRotAhead = 4;                // heads whose loads are under way
 
 struct HeadsIn {
     const uint8_t* p;
-    long long ts, hs;                       // strides in elements
+    long long ts, hs;                       // strides in bytes
+    int heads, slices;                      // groups of lanes that share a token's heads
 };
 struct RotArgs {
     int dim, rot, interleaved;
-    float eps, amplitude;
+    float eps, amplitude, inv_dim;
     int w_bf16;
     const uint64_t* turns;
     const int32_t* positions;
     long long tokens;
-    int slices;                             // groups of lanes that share a token's heads
+    int per_group;                          // heads of a group
     HeadsIn x[3];                           // q, k, v; rotate: the first alone
     const void* w[2];
-    int heads[3];
     uint8_t* out;                           // q's
-    long long out_ts, out_hs;
+    long long out_ts, out_hs;               // in bytes
     int out_dtype;
     saem_kv_cache cache;
     saem_batch batch;
     int32_t* status;
 };
 
-// Four elements as they lie in memory.
-template <int DT, bool VEC>
-struct Run {
-    uint32_t w[DT == SAEM_OUT_F32 ? 4 : 2];
-    __device__ __forceinline__ void load(const uint8_t* p, long long at) {
-        if constexpr (DT == SAEM_OUT_F32) {
-            const float* f = reinterpret_cast<const float*>(p) + at;
-            if constexpr (VEC) {
-                const uint4 q = *reinterpret_cast<const uint4*>(f);
-                w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-            } else {
+// How a lane's eight elements lie: two runs of four anywhere (RUNS), one of eight (WHOLE), or at addresses that are aligned to their
+// elements only (SINGLE).
+enum { kRuns = 0, kWhole = 1, kSingle = 2 };
+constexpr int elem_of(int dtype) { return dtype == SAEM_OUT_F32 ? 4 : 2; }
+template <int DT, int FORM>
+struct Eight {
+    static constexpr int E = elem_of(DT);
+    uint32_t w[2 * E];
+    // p0, p1: the runs' first elements (WHOLE: p1 follows p0)
+    __device__ __forceinline__ void load(const uint8_t* p0, const uint8_t* p1) {
+        if constexpr (FORM == kSingle) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(f[i]);
+            for (int i = 0; i < 8; ++i) {
+                const uint8_t* p = i < 4 ? p0 + i * E : p1 + (i - 4) * E;
+                if constexpr (E == 4) w[i] = *reinterpret_cast<const uint32_t*>(p);
+                else if (i & 1) w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16;
+                else w[i / 2] = *reinterpret_cast<const uint16_t*>(p);
+            }
+        } else if constexpr (E == 4 || FORM == kWhole) {
+            const uint4 a = *reinterpret_cast<const uint4*>(p0);
+            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+            if constexpr (E == 4) {
+                const uint4 b = *reinterpret_cast<const uint4*>(p1);
+                w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
             }
         } else {
-            const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + at;
-            if constexpr (VEC) {
-                const uint2 q = *reinterpret_cast<const uint2*>(h);
-                w[0] = q.x; w[1] = q.y;
-            } else {
-                w[0] = h[0] | (uint32_t)h[1] << 16;
-                w[1] = h[2] | (uint32_t)h[3] << 16;
-            }
+            const uint2 a = *reinterpret_cast<const uint2*>(p0), b = *reinterpret_cast<const uint2*>(p1);
+            w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
         }
     }
-    __device__ __forceinline__ void widen(float* v) const {
-        if constexpr (DT == SAEM_OUT_F32) {
+    __device__ __forceinline__ void widen(float (&v)[8]) const {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
-        } else {
-            const float2 a = unpack2<DT == SAEM_OUT_F16>(w[0]), b = unpack2<DT == SAEM_OUT_F16>(w[1]);
-            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 4) {
+                v[2 * i] = __uint_as_float(w[2 * i]);
+                v[2 * i + 1] = __uint_as_float(w[2 * i + 1]);
+            } else {
+                const float2 x = unpack2<DT == SAEM_OUT_F16>(w[i]);
+                v[2 * i] = x.x;
+                v[2 * i + 1] = x.y;
+            }
         }
     }
 };
-template <bool VEC>
-__device__ __forceinline__ void store4(uint8_t* p, long long at, int dtype, const float* v) {
+template <int FORM>
+__device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int dtype, const float (&v)[8]) {
     if (dtype == SAEM_OUT_F32) {
-        float* f = reinterpret_cast<float*>(p) + at;
-        if constexpr (VEC) *reinterpret_cast<float4*>(f) = make_float4(v[0], v[1], v[2], v[3]);
-        else {
+        if constexpr (FORM == kSingle) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = v[i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<float*>(i < 4 ? p0 + i * 4 : p1 + (i - 4) * 4) = v[i];
+        } else {
+            *reinterpret_cast<float4*>(p0) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(p1) = make_float4(v[4], v[5], v[6], v[7]);
         }
         return;
     }
-    uint32_t a, b;
-    if (dtype == SAEM_OUT_F16) a = pack2<true>(v[0], v[1]), b = pack2<true>(v[2], v[3]);
-    else a = pack2<false>(v[0], v[1]), b = pack2<false>(v[2], v[3]);
-    uint16_t* h = reinterpret_cast<uint16_t*>(p) + at;
-    if constexpr (VEC) *reinterpret_cast<uint2*>(h) = make_uint2(a, b);
-    else {
-        h[0] = (uint16_t)a; h[1] = (uint16_t)(a >> 16); h[2] = (uint16_t)b; h[3] = (uint16_t)(b >> 16);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = dtype == SAEM_OUT_F16 ? pack2<true>(v[2 * i], v[2 * i + 1]) : pack2<false>(v[2 * i], v[2 * i + 1]);
+    if constexpr (FORM == kSingle) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint16_t*>(i < 4 ? p0 + i * 2 : p1 + (i - 4) * 2) = (uint16_t)(w[i / 2] >> (i & 1) * 16);
+    } else if constexpr (FORM == kWhole) {
+        *reinterpret_cast<uint4*>(p0) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        *reinterpret_cast<uint2*>(p0) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(p1) = make_uint2(w[2], w[3]);
     }
 }
 
@@ -109,7 +125,7 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int seqs, int
     return lo;
 }
 
-template <int DT, int LANES, bool VEC, bool APPEND>
+template <int DT, int LANES, int FORM, bool APPEND>
 __global__ void __launch_bounds__(kRotThreads)
 rotary_kernel(const __grid_constant__ RotArgs a) {
     pdl_wait();
@@ -117,109 +133,100 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
     const int lane = threadIdx.x % LANES;
     const int group_shift = (threadIdx.x & 31) / LANES * LANES;
     const uint32_t group_mask = (uint32_t)((1ull << LANES) - 1) << group_shift;
+    const int slices = APPEND ? a.x[0].slices + a.x[1].slices + a.x[2].slices : a.x[0].slices;
     const long long group = (long long)blockIdx.x * (kRotThreads / LANES) + threadIdx.x / LANES;
-    const long long t = group / a.slices;
-    const int slice = (int)(group % a.slices);
+    const long long t = group / slices;
+    int slice = (int)(group - t * slices), kind = 0;
     if (t >= a.tokens) return;
+    if (APPEND)
+        while (slice >= a.x[kind].slices) slice -= a.x[kind++].slices;
+    const HeadsIn& x = a.x[kind];
+    const int first = slice * a.per_group, count = min(a.per_group, x.heads - first);
     // where the lane's two runs of four lie in a head, and whether they turn
-    const int unit = lane, half = a.rot / 2;
-    const bool here = unit * 8 < a.dim, turn = unit * 8 < a.rot;
-    const bool across = turn && !a.interleaved;
-    const int at0 = across ? 4 * unit : 8 * unit, at1 = across ? half + 4 * unit : 8 * unit + 4;
-    const int n_heads = a.heads[0] + a.heads[1] + a.heads[2];
-
-    auto source = [&](int h) {
-        int kind = 0;
-        if (APPEND && h >= a.heads[0]) {
-            h -= a.heads[0];
-            kind = 1;
-            if (h >= a.heads[1]) { h -= a.heads[1]; kind = 2; }
-        }
-        const HeadsIn& x = a.x[APPEND ? kind : 0];
-        return x.p + (t * x.ts + h * x.hs) * (DT == SAEM_OUT_F32 ? 4 : 2);
-    };
-    Run<DT, VEC> raw[kRotBatch][2];
-    auto fetch = [&](int h) {
+    const int half = a.rot / 2;
+    const bool here = lane * 8 < a.dim, turn = lane * 8 < a.rot && kind < 2;
+    const bool across = lane * 8 < a.rot && !a.interleaved;
+    const int at0 = across ? 4 * lane : 8 * lane, at1 = across ? half + 4 * lane : 8 * lane + 4;
+    constexpr int E = elem_of(DT);
+    const uint8_t* src = x.p + t * x.ts + first * x.hs;
+    Eight<DT, FORM> raw[kRotAhead];
 #pragma unroll
-        for (int i = 0; i < kRotBatch; ++i) {
-            const int hi = h + i * a.slices;
-            if (here && hi < n_heads) {
-                const uint8_t* p = source(hi);
-                raw[i][0].load(p, at0);
-                raw[i][1].load(p, at1);
-            }
-        }
-    };
-    fetch(slice);                           // on its way while the token's place is looked up
+    for (int i = 0; i < kRotAhead; ++i)     // on their way while the token's place is looked up
+        if (here && i < count) raw[i].load(src + i * x.hs + at0 * E, src + i * x.hs + at1 * E);
+    src += kRotAhead * x.hs;
 
-    int place = 0, position;
-    long long row = -1;                     // the token's row in the cache at head 0, in units of head_dim
+    int position;
+    uint8_t* to;
+    long long step;
+    int out_elem = 2;
     if (APPEND) {
         const int seqs = a.batch.seqs;
         if (t >= a.batch.offsets[seqs]) return;
         const int s = sequence_of<LANES>(a.batch.offsets, seqs, (int)t, lane, group_mask, group_shift);
-        place = a.batch.lengths[s] - (a.batch.offsets[s + 1] - (int)t);
-        if (place >= 0) {
+        const int place = a.batch.lengths[s] - (a.batch.offsets[s + 1] - (int)t);
+        position = a.positions ? a.positions[t] : place;
+        if (kind == 0) {
+            to = a.out + t * a.out_ts + first * a.out_hs;
+            step = a.out_hs;
+        } else {
+            if (place < 0) return;
             const int entry = place / a.cache.page_size;
             const int page = entry < a.batch.max_pages ? a.batch.table[s * a.batch.table_stride + entry] : -1;
-            if (page >= 0 && page < a.cache.pages) row = (long long)page * a.cache.kv_heads * a.cache.page_size + place % a.cache.page_size;
-            else if (a.status && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
+            if (page < 0 || page >= a.cache.pages) {
+                if (a.status && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
+                return;
+            }
+            step = (long long)a.cache.page_size * a.dim * 2;
+            to = static_cast<uint8_t*>(kind == 1 ? a.cache.k : a.cache.v) +
+                 (((long long)page * a.cache.kv_heads + first) * a.cache.page_size + place % a.cache.page_size) * a.dim * 2;
         }
-        position = a.positions ? a.positions[t] : place;
     } else {
         position = a.positions[t];
+        to = a.out + t * a.out_ts + first * a.out_hs;
+        step = a.out_hs;
+        out_elem = a.out_dtype == SAEM_OUT_F32 ? 4 : 2;
     }
     float sn[4], cs[4];
     if (turn) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint64_t u = a.turns[4 * unit + i] * (uint64_t)(long long)position;
+            const uint64_t u = a.turns[4 * lane + i] * (uint64_t)(long long)position;
             sincospif((float)(int32_t)(u >> 32) * 0x1p-31f, &sn[i], &cs[i]);
             sn[i] *= a.amplitude;
             cs[i] *= a.amplitude;
         }
     }
-    float w[2][8];
+    const void* const weight = kind == 0 ? a.w[0] : kind == 1 ? a.w[1] : nullptr;
+    float w[8];
+    if (weight && here) {
 #pragma unroll
-    for (int k = 0; k < (APPEND ? 2 : 1); ++k)
-        if (a.w[k] && here) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = i < 4 ? at0 + i : at1 + i - 4;
-                w[k][i] = a.w_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.w[k])[at] << 16) : static_cast<const float*>(a.w[k])[at];
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int at = i < 4 ? at0 + i : at1 + i - 4;
+            w[i] = a.w_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(weight)[at] << 16) : static_cast<const float*>(weight)[at];
         }
-
-    for (int h0 = slice; h0 < n_heads; h0 += kRotBatch * a.slices) {
-        if (h0 != slice) fetch(h0);
+    }
+    uint8_t *to0 = to + at0 * out_elem, *to1 = to + at1 * out_elem;
+    for (int h0 = 0; h0 < count; h0 += kRotAhead) {
 #pragma unroll
-        for (int i = 0; i < kRotBatch; ++i) {
-            int h = h0 + i * a.slices;
-            if (h >= n_heads) break;
-            int kind = 0;
-            if (APPEND && h >= a.heads[0]) {
-                h -= a.heads[0];
-                kind = 1;
-                if (h >= a.heads[1]) { h -= a.heads[1]; kind = 2; }
-            }
-            float v[8];
+        for (int i = 0; i < kRotAhead; ++i) {
+            if (h0 + i >= count) break;
+            float v[8] = {};
             if (here) {
-                raw[i][0].widen(v);
-                raw[i][1].widen(v + 4);
+                raw[i].widen(v);
+                if (h0 + i + kRotAhead < count) raw[i].load(src + at0 * E, src + at1 * E);
             }
-            if (kind < 2 && a.w[kind]) {
+            src += x.hs;
+            if (weight) {
                 float s = 0.f;
-                if (here) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
-                }
+                for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
 #pragma unroll
                 for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(group_mask, s, o);
-                const float r = 1.f / sqrtf(s / (float)a.dim + a.eps);
+                const float r = rsqrtf(fmaf(s, a.inv_dim, a.eps));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= r * (APPEND && kind ? w[1][e] : w[0][e]);
+                for (int e = 0; e < 8; ++e) v[e] *= r * w[e];
             }
-            if (kind < 2 && turn) {
+            if (turn) {
                 if (a.interleaved) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -236,47 +243,50 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
                     }
                 }
             }
-            uint8_t* to;
-            if (!APPEND || kind == 0) {
-                to = a.out + (t * a.out_ts + h * a.out_hs) * (a.out_dtype == SAEM_OUT_F32 ? 4 : 2);
-            } else {
-                if (row < 0) continue;
-                to = static_cast<uint8_t*>(kind == 1 ? a.cache.k : a.cache.v) + (row + (long long)h * a.cache.page_size) * a.dim * 2;
-            }
-            if (here) {
-                store4<VEC>(to, at0, a.out_dtype, v);
-                store4<VEC>(to, at1, a.out_dtype, v + 4);
-            }
+            if (here) store8<FORM>(to0, to1, a.out_dtype, v);
+            to0 += step;
+            to1 += step;
         }
     }
 }
 
-template <int DT, bool VEC, bool APPEND>
+template <int DT, int FORM, bool APPEND>
 static cudaError_t launch_rotary_typed(RotArgs a, int n_sm, cudaStream_t st) {
-    const int lanes = a.dim <= 64 ? 8 : 16, n_heads = a.heads[0] + a.heads[1] + a.heads[2];
-    // as many groups as fill the SMs' threads, while a token has heads to share out
+    const int lanes = a.dim <= 64 ? 8 : 16, kinds = APPEND ? 3 : 1;
+    // as many heads to a group as leave groups for the SMs' threads
     const long long want = (long long)n_sm * 2048 / lanes;
-    a.slices = (int)((want + a.tokens - 1) / a.tokens);
-    if (a.slices > n_heads) a.slices = n_heads;
-    const long long per = kRotThreads / lanes, grid = (a.tokens * a.slices + per - 1) / per;
-    if (lanes == 8) return launch_pdl(rotary_kernel<DT, 8, VEC, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
-    return launch_pdl(rotary_kernel<DT, 16, VEC, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
+    long long slices = 0;
+    for (a.per_group = kRotMost; ; a.per_group /= 2) {
+        slices = 0;
+        for (int i = 0; i < kinds; ++i) slices += a.x[i].slices = (a.x[i].heads + a.per_group - 1) / a.per_group;
+        if (a.per_group == 1 || a.tokens * slices >= want) break;
+    }
+    const long long per = kRotThreads / lanes, grid = (a.tokens * slices + per - 1) / per;
+    if (lanes == 8) return launch_pdl(rotary_kernel<DT, 8, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
+    return launch_pdl(rotary_kernel<DT, 16, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
 }
+template <int DT, bool APPEND>
+static cudaError_t launch_rotary_form(const RotArgs& a, int aligned, int n_sm, cudaStream_t st) {
+    if (aligned >= 8 && (a.interleaved || a.rot == 0)) return launch_rotary_typed<DT, kWhole, APPEND>(a, n_sm, st);
+    return aligned >= 4 ? launch_rotary_typed<DT, kRuns, APPEND>(a, n_sm, st) : launch_rotary_typed<DT, kSingle, APPEND>(a, n_sm, st);
+}
+// aligned: the elements to which every head's address is a multiple (1, 4 or 8)
 template <bool APPEND>
-static int launch_rotary(const RotArgs& a, int x_dtype, bool vec, cudaStream_t st) {
+static int launch_rotary(const RotArgs& a, int x_dtype, int aligned, cudaStream_t st) {
     int n_sm;
     if (sm_count(&n_sm) != cudaSuccess) return SAEM_ERR_CUDA;
-    cudaError_t e;
-    if (x_dtype == SAEM_OUT_F32) e = vec ? launch_rotary_typed<SAEM_OUT_F32, true, APPEND>(a, n_sm, st) : launch_rotary_typed<SAEM_OUT_F32, false, APPEND>(a, n_sm, st);
-    else if (x_dtype == SAEM_OUT_BF16) e = vec ? launch_rotary_typed<SAEM_OUT_BF16, true, APPEND>(a, n_sm, st) : launch_rotary_typed<SAEM_OUT_BF16, false, APPEND>(a, n_sm, st);
-    else e = vec ? launch_rotary_typed<SAEM_OUT_F16, true, APPEND>(a, n_sm, st) : launch_rotary_typed<SAEM_OUT_F16, false, APPEND>(a, n_sm, st);
+    const cudaError_t e = x_dtype == SAEM_OUT_F32    ? launch_rotary_form<SAEM_OUT_F32, APPEND>(a, aligned, n_sm, st)
+                          : x_dtype == SAEM_OUT_BF16 ? launch_rotary_form<SAEM_OUT_BF16, APPEND>(a, aligned, n_sm, st)
+                                                     : launch_rotary_form<SAEM_OUT_F16, APPEND>(a, aligned, n_sm, st);
     return e == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }
-// Whether runs of four elements of these heads are aligned to their size; *ok: elements to theirs.
-static bool runs_aligned(const void* p, int dtype, int64_t tokens, int64_t heads, int64_t ts, int64_t hs, bool* ok) {
+// The most elements (1, 4 or 8; at most `aligned`) that the heads' addresses are multiples of; *ok: they are aligned to their elements.
+static int heads_aligned(const void* p, int dtype, int64_t tokens, int64_t heads, int64_t ts, int64_t hs, int aligned, bool* ok) {
     const int e = head_elem(dtype);
     *ok = *ok && (uintptr_t)p % e == 0;
-    return (uintptr_t)p % (4 * e) == 0 && (tokens <= 1 || ts % 4 == 0) && (heads <= 1 || hs % 4 == 0);
+    // 16 bytes at a time at most
+    while (aligned > 1 && ((uintptr_t)p % (aligned * e > 16 ? 16 : aligned * e) || (tokens > 1 && ts % aligned) || (heads > 1 && hs % aligned))) aligned = aligned == 8 ? 4 : 1;
+    return aligned;
 }
 
 }  // namespace saem
@@ -295,18 +305,20 @@ extern "C" int saem_rotate(const saem_rotate_config* c, const void* x, const voi
     if (c->x_token_stride < 0 || c->x_head_stride < 0 ||
         !heads_apart(c->tokens, c->heads, c->rotary.head_dim, c->out_token_stride, c->out_head_stride)) return SAEM_ERR_SHAPE;
     bool ok = (uintptr_t)positions % 4 == 0 && (uintptr_t)turns % 8 == 0 && (uintptr_t)w % head_elem(c->w_dtype) == 0;
-    bool vec = runs_aligned(x, c->x_dtype, c->tokens, c->heads, c->x_token_stride, c->x_head_stride, &ok);
-    vec &= runs_aligned(out, c->out_dtype, c->tokens, c->heads, c->out_token_stride, c->out_head_stride, &ok);
+    int aligned = heads_aligned(x, c->x_dtype, c->tokens, c->heads, c->x_token_stride, c->x_head_stride, 8, &ok);
+    aligned = heads_aligned(out, c->out_dtype, c->tokens, c->heads, c->out_token_stride, c->out_head_stride, aligned, &ok);
     if (!ok) return SAEM_ERR_ALIGNMENT;
     RotArgs a = {};
     a.dim = c->rotary.head_dim; a.rot = c->rotary.rotary_dim; a.interleaved = c->rotary.interleaved;
     a.eps = c->rotary.eps; a.amplitude = c->rotary.amplitude;
     a.w_bf16 = c->w_dtype == SAEM_OUT_BF16;
     a.turns = turns; a.positions = positions; a.tokens = c->tokens;
-    a.x[0] = {static_cast<const uint8_t*>(x), c->x_token_stride, c->x_head_stride};
-    a.w[0] = w; a.heads[0] = c->heads;
-    a.out = static_cast<uint8_t*>(out); a.out_ts = c->out_token_stride; a.out_hs = c->out_head_stride; a.out_dtype = c->out_dtype;
-    return launch_rotary<false>(a, c->x_dtype, vec, (cudaStream_t)stream);
+    const int e = head_elem(c->x_dtype), oe = head_elem(c->out_dtype);
+    a.inv_dim = 1.f / (float)a.dim;
+    a.x[0] = {static_cast<const uint8_t*>(x), c->x_token_stride * e, c->x_head_stride * e, c->heads, 0};
+    a.w[0] = w;
+    a.out = static_cast<uint8_t*>(out); a.out_ts = c->out_token_stride * oe; a.out_hs = c->out_head_stride * oe; a.out_dtype = c->out_dtype;
+    return launch_rotary<false>(a, c->x_dtype, aligned, (cudaStream_t)stream);
 }
 
 extern "C" int saem_kv_append(const saem_append_config* c, const saem_kv_cache* cache, const saem_batch* b, const void* q, const void* k,
@@ -330,11 +342,11 @@ extern "C" int saem_kv_append(const saem_append_config* c, const saem_kv_cache* 
         return SAEM_ERR_SHAPE;
     const int we = head_elem(c->w_dtype);
     bool ok = (uintptr_t)positions % 4 == 0 && (uintptr_t)turns % 8 == 0 && (uintptr_t)w_q % we == 0 && (uintptr_t)w_k % we == 0 && (uintptr_t)status % 4 == 0;
-    bool vec = runs_aligned(k, c->x_dtype, b->tokens, cache->kv_heads, c->k_token_stride, c->k_head_stride, &ok);
-    vec &= runs_aligned(v, c->x_dtype, b->tokens, cache->kv_heads, c->v_token_stride, c->v_head_stride, &ok);
+    int aligned = heads_aligned(k, c->x_dtype, b->tokens, cache->kv_heads, c->k_token_stride, c->k_head_stride, 8, &ok);
+    aligned = heads_aligned(v, c->x_dtype, b->tokens, cache->kv_heads, c->v_token_stride, c->v_head_stride, aligned, &ok);
     if (q) {
-        vec &= runs_aligned(q, c->x_dtype, b->tokens, q_heads, c->q_token_stride, c->q_head_stride, &ok);
-        vec &= runs_aligned(q_out, cache->dtype, b->tokens, q_heads, c->out_token_stride, c->out_head_stride, &ok);
+        aligned = heads_aligned(q, c->x_dtype, b->tokens, q_heads, c->q_token_stride, c->q_head_stride, aligned, &ok);
+        aligned = heads_aligned(q_out, cache->dtype, b->tokens, q_heads, c->out_token_stride, c->out_head_stride, aligned, &ok);
     }
     if (!ok) return SAEM_ERR_ALIGNMENT;
     RotArgs a = {};
@@ -342,12 +354,13 @@ extern "C" int saem_kv_append(const saem_append_config* c, const saem_kv_cache* 
     a.eps = c->rotary.eps; a.amplitude = c->rotary.amplitude;
     a.w_bf16 = c->w_dtype == SAEM_OUT_BF16;
     a.turns = turns; a.positions = positions; a.tokens = b->tokens;
-    a.x[0] = {static_cast<const uint8_t*>(q), c->q_token_stride, c->q_head_stride};
-    a.x[1] = {static_cast<const uint8_t*>(k), c->k_token_stride, c->k_head_stride};
-    a.x[2] = {static_cast<const uint8_t*>(v), c->v_token_stride, c->v_head_stride};
+    const int e = head_elem(c->x_dtype);
+    a.inv_dim = 1.f / (float)dim;
+    a.x[0] = {static_cast<const uint8_t*>(q), c->q_token_stride * e, c->q_head_stride * e, q_heads, 0};
+    a.x[1] = {static_cast<const uint8_t*>(k), c->k_token_stride * e, c->k_head_stride * e, cache->kv_heads, 0};
+    a.x[2] = {static_cast<const uint8_t*>(v), c->v_token_stride * e, c->v_head_stride * e, cache->kv_heads, 0};
     a.w[0] = w_q; a.w[1] = w_k;
-    a.heads[0] = q_heads; a.heads[1] = a.heads[2] = cache->kv_heads;
-    a.out = static_cast<uint8_t*>(q_out); a.out_ts = c->out_token_stride; a.out_hs = c->out_head_stride; a.out_dtype = cache->dtype;
+    a.out = static_cast<uint8_t*>(q_out); a.out_ts = c->out_token_stride * 2; a.out_hs = c->out_head_stride * 2; a.out_dtype = cache->dtype;
     a.cache = *cache; a.batch = *b; a.status = status;
-    return launch_rotary<true>(a, c->x_dtype, vec, (cudaStream_t)stream);
+    return launch_rotary<true>(a, c->x_dtype, aligned, (cudaStream_t)stream);
 }

@@ -47,7 +47,42 @@ inline int batch_status(const saem_batch& b) {
     return ((uintptr_t)b.offsets | (uintptr_t)b.lengths | (uintptr_t)b.table) % 4 ? SAEM_ERR_ALIGNMENT : SAEM_OK;
 }
 
+// n / d for 0 <= n < 2^31 by a multiplication: with 2^s >= d, mul = ceil(2^(31 + s) / d) is off by less than 2^s / 2^31 of a quotient.
+struct Divisor {
+    uint32_t d, mul, shift;
+};
+inline Divisor divisor_of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), 31 + s};
+}
+
 #ifdef __CUDACC__
+__device__ __forceinline__ int quotient(int n, const Divisor& d) { return (int)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
+// Two fp32 values in a register pair: one instruction for both.
+__device__ __forceinline__ uint64_t pack_b32x2(uint32_t lo, uint32_t hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+    return d;
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) { return pack_b32x2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ float low_f32(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float high_f32(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // Two fp32 values to a word of two 16-bit ones, the first in the low half.
 template <bool F16>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {

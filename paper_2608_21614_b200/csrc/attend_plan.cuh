@@ -16,16 +16,6 @@ namespace saem {
 
 constexpr int kAttendMaxCtas = 640;         // SMs x CTAs per SM at most
 
-// n / d for 0 <= n < 2^31 by a multiplication: with 2^s >= d, mul = ceil(2^(31 + s) / d) is off by less than 2^s / 2^31 of a quotient.
-struct Divisor {
-    uint32_t d, mul, shift;
-};
-inline Divisor divisor_of(uint32_t d) {
-    uint32_t s = 0;
-    while ((1ull << s) < d) ++s;
-    return {d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), 31 + s};
-}
-__device__ __forceinline__ int quotient(int n, const Divisor& d) { return (int)((uint64_t)(uint32_t)n * d.mul >> d.shift); }
 __device__ __forceinline__ float fast_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

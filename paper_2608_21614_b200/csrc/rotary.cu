@@ -8,14 +8,15 @@
 // bound is DRAM for many tokens; for one it is the launch and a chain of loads.
 //
 // The angle in turns is position * turns[i] mod 2^64 in integers, exact but for the frequency's own rounding (2^-65 turns
-// a position); its upper 32 bits, signed, times 2^-31 are the argument of sincospi in [-1, 1).
+// a position).  Its upper 32 bits give the quarter turn and, signed, the rest r of at most an eighth of a turn, whose sine and cosine come
+// from polynomials (turn2 below): sincospi, with its range checks, took half of the instructions of a group of eight heads.
 #include "attend_common.cuh"
 
 namespace saem {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotMost = 8;                 // heads of a group at most
-constexpr int kRotAhead = 4;                // heads whose loads are under way
+constexpr int kRotAhead = 2;                // heads whose loads are under way
 
 struct HeadsIn {
     const uint8_t* p;
@@ -30,6 +31,8 @@ struct RotArgs {
     const int32_t* positions;
     long long tokens;
     int per_group;                          // heads of a group
+    Divisor by_slices, by_page;
+    int w_runs;                             // the weights are aligned to runs of four
     HeadsIn x[3];                           // q, k, v; rotate: the first alone
     const void* w[2];
     uint8_t* out;                           // q's
@@ -70,35 +73,33 @@ struct Eight {
             w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
         }
     }
-    __device__ __forceinline__ void widen(float (&v)[8]) const {
+    // as four pairs, in the order of the elements
+    __device__ __forceinline__ void widen(uint64_t (&v)[4]) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if constexpr (E == 4) {
-                v[2 * i] = __uint_as_float(w[2 * i]);
-                v[2 * i + 1] = __uint_as_float(w[2 * i + 1]);
-            } else {
+            if constexpr (E == 4) v[i] = pack_b32x2(w[2 * i], w[2 * i + 1]);
+            else {
                 const float2 x = unpack2<DT == SAEM_OUT_F16>(w[i]);
-                v[2 * i] = x.x;
-                v[2 * i + 1] = x.y;
+                v[i] = pack_f32x2(x.x, x.y);
             }
         }
     }
 };
 template <int FORM>
-__device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int dtype, const float (&v)[8]) {
+__device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int dtype, const uint64_t (&v)[4]) {
     if (dtype == SAEM_OUT_F32) {
         if constexpr (FORM == kSingle) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<float*>(i < 4 ? p0 + i * 4 : p1 + (i - 4) * 4) = v[i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<float*>(i < 4 ? p0 + i * 4 : p1 + (i - 4) * 4) = i & 1 ? high_f32(v[i / 2]) : low_f32(v[i / 2]);
         } else {
-            *reinterpret_cast<float4*>(p0) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(p1) = make_float4(v[4], v[5], v[6], v[7]);
+            *reinterpret_cast<float4*>(p0) = make_float4(low_f32(v[0]), high_f32(v[0]), low_f32(v[1]), high_f32(v[1]));
+            *reinterpret_cast<float4*>(p1) = make_float4(low_f32(v[2]), high_f32(v[2]), low_f32(v[3]), high_f32(v[3]));
         }
         return;
     }
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = dtype == SAEM_OUT_F16 ? pack2<true>(v[2 * i], v[2 * i + 1]) : pack2<false>(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) w[i] = dtype == SAEM_OUT_F16 ? pack2<true>(low_f32(v[i]), high_f32(v[i])) : pack2<false>(low_f32(v[i]), high_f32(v[i]));
     if constexpr (FORM == kSingle) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) *reinterpret_cast<uint16_t*>(i < 4 ? p0 + i * 2 : p1 + (i - 4) * 2) = (uint16_t)(w[i / 2] >> (i & 1) * 16);
@@ -125,18 +126,38 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int seqs, int
     return lo;
 }
 
+// Sines and cosines of two angles, given as fractions of a turn in units of 2^-64.  With r in half turns, |r| <= 1/4, and z = r^2:
+// sin(pi r) = r s(z), s of degree 3 with the least largest relative error (2^-28), cos(pi r) = 1 + z c(z), c of degree 3 with the least
+// largest absolute error (2^-34), both by Lawson's iteration in 64 bits; in fp32 both are within 2^-23.4 of the values in 64 bits.
+__device__ __forceinline__ void turn2(uint64_t u0, uint64_t u1, float (&sn)[2], float (&cs)[2]) {
+    const uint32_t h0 = (uint32_t)(u0 >> 32), h1 = (uint32_t)(u1 >> 32), q0 = (h0 + 0x20000000u) >> 30, q1 = (h1 + 0x20000000u) >> 30;
+    const uint64_t r = pack_f32x2((float)(int32_t)(h0 - (q0 << 30)) * 0x1p-31f, (float)(int32_t)(h1 - (q1 << 30)) * 0x1p-31f), z = mul_f32x2(r, r);
+    auto two = [](float v) { return pack_f32x2(v, v); };
+    uint64_t s = fma_f32x2(z, two(-0.5890122056007385f), two(2.5497610569000244f));
+    uint64_t c = fma_f32x2(z, two(0.2314295470714569f), two(-1.3350584506988525f));
+    s = fma_f32x2(z, s, two(-5.167707920074463f));
+    c = fma_f32x2(z, c, two(4.0587077140808105f));
+    s = mul_f32x2(fma_f32x2(z, s, two(3.1415927410125732f)), r);
+    c = fma_f32x2(z, fma_f32x2(z, c, two(-4.934802055358887f)), two(1.f));
+    auto place = [](uint32_t q, float s, float c, float& sn, float& cs) {
+        sn = __uint_as_float(__float_as_uint(q & 1 ? c : s) ^ (q & 2) << 30);
+        cs = __uint_as_float(__float_as_uint(q & 1 ? s : c) ^ (q + 1 & 2) << 30);
+    };
+    place(q0, low_f32(s), low_f32(c), sn[0], cs[0]);
+    place(q1, high_f32(s), high_f32(c), sn[1], cs[1]);
+}
+
 template <int DT, int LANES, int FORM, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, 4)
 rotary_kernel(const __grid_constant__ RotArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % LANES;
     const int group_shift = (threadIdx.x & 31) / LANES * LANES;
     const uint32_t group_mask = (uint32_t)((1ull << LANES) - 1) << group_shift;
-    const int slices = APPEND ? a.x[0].slices + a.x[1].slices + a.x[2].slices : a.x[0].slices;
-    const long long group = (long long)blockIdx.x * (kRotThreads / LANES) + threadIdx.x / LANES;
-    const long long t = group / slices;
-    int slice = (int)(group - t * slices), kind = 0;
+    const int group = blockIdx.x * (kRotThreads / LANES) + threadIdx.x / LANES;
+    const long long t = quotient(group, a.by_slices);
+    int slice = group - (int)t * a.by_slices.d, kind = 0;
     if (t >= a.tokens) return;
     if (APPEND)
         while (slice >= a.x[kind].slices) slice -= a.x[kind++].slices;
@@ -170,7 +191,7 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
             step = a.out_hs;
         } else {
             if (place < 0) return;
-            const int entry = place / a.cache.page_size;
+            const int entry = quotient(place, a.by_page);
             const int page = entry < a.batch.max_pages ? a.batch.table[s * a.batch.table_stride + entry] : -1;
             if (page < 0 || page >= a.cache.pages) {
                 if (a.status && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
@@ -178,7 +199,7 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
             }
             step = (long long)a.cache.page_size * a.dim * 2;
             to = static_cast<uint8_t*>(kind == 1 ? a.cache.k : a.cache.v) +
-                 (((long long)page * a.cache.kv_heads + first) * a.cache.page_size + place % a.cache.page_size) * a.dim * 2;
+                 (((long long)page * a.cache.kv_heads + first) * a.cache.page_size + place - entry * a.cache.page_size) * a.dim * 2;
         }
     } else {
         position = a.positions[t];
@@ -186,23 +207,59 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
         step = a.out_hs;
         out_elem = a.out_dtype == SAEM_OUT_F32 ? 4 : 2;
     }
-    float sn[4], cs[4];
-    if (turn) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint64_t u = a.turns[4 * lane + i] * (uint64_t)(long long)position;
-            sincospif((float)(int32_t)(u >> 32) * 0x1p-31f, &sn[i], &cs[i]);
-            sn[i] *= a.amplitude;
-            cs[i] *= a.amplitude;
-        }
-    }
     const void* const weight = kind == 0 ? a.w[0] : kind == 1 ? a.w[1] : nullptr;
     float w[8];
-    if (weight && here) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = i < 4 ? at0 + i : at1 + i - 4;
-            w[i] = a.w_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(weight)[at] << 16) : static_cast<const float*>(weight)[at];
+    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    if (weight && here) {
+        const uint8_t* p = static_cast<const uint8_t*>(weight);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = i ? at1 : at0;
+            if (a.w_bf16) {
+                uint2 x;
+                if (a.w_runs) x = *reinterpret_cast<const uint2*>(p + at * 2);
+                else {
+                    const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + at;
+                    x = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+                }
+                const float2 lo = unpack2<false>(x.x), hi = unpack2<false>(x.y);
+                w[4 * i] = lo.x; w[4 * i + 1] = lo.y; w[4 * i + 2] = hi.x; w[4 * i + 3] = hi.y;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[4 * i + e] = reinterpret_cast<const float*>(p)[at + e];
+            }
+        }
+    }
+    // y = x * k1 + (the pair's other element) * k2, weights and amplitude in the factors, for four pairs of elements
+    uint64_t k1[4], k2[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k1[i] = pack_f32x2(w[2 * i], w[2 * i + 1]);
+    if (turn) {
+        float sn[4], cs[4];
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const uint64_t at = (uint64_t)(long long)position;
+            float s2[2], c2[2];
+            turn2(a.turns[4 * lane + i] * at, a.turns[4 * lane + i + 1] * at, s2, c2);
+            sn[i] = s2[0]; sn[i + 1] = s2[1]; cs[i] = c2[0]; cs[i + 1] = c2[1];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] *= a.amplitude;
+        if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                k1[i] = pack_f32x2(w[2 * i] * cs[i], w[2 * i + 1] * cs[i]);
+                k2[i] = pack_f32x2(-w[2 * i + 1] * sn[i], w[2 * i] * sn[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                k1[i] = pack_f32x2(w[2 * i] * cs[2 * i], w[2 * i + 1] * cs[2 * i + 1]);
+                k2[i] = pack_f32x2(-w[2 * i + 4] * sn[2 * i], -w[2 * i + 5] * sn[2 * i + 1]);
+                k1[i + 2] = pack_f32x2(w[2 * i + 4] * cs[2 * i], w[2 * i + 5] * cs[2 * i + 1]);
+                k2[i + 2] = pack_f32x2(w[2 * i] * sn[2 * i], w[2 * i + 1] * sn[2 * i + 1]);
+            }
         }
     }
     uint8_t *to0 = to + at0 * out_elem, *to1 = to + at1 * out_elem;
@@ -210,38 +267,33 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
 #pragma unroll
         for (int i = 0; i < kRotAhead; ++i) {
             if (h0 + i >= count) break;
-            float v[8] = {};
+            uint64_t v[4] = {};
             if (here) {
                 raw[i].widen(v);
                 if (h0 + i + kRotAhead < count) raw[i].load(src + at0 * E, src + at1 * E);
             }
             src += x.hs;
             if (weight) {
-                float s = 0.f;
+                uint64_t sq = mul_f32x2(v[0], v[0]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
+                for (int e = 1; e < 4; ++e) sq = fma_f32x2(v[e], v[e], sq);
+                float s = low_f32(sq) + high_f32(sq);
 #pragma unroll
                 for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(group_mask, s, o);
                 const float r = rsqrtf(fmaf(s, a.inv_dim, a.eps));
+                const uint64_t r2 = pack_f32x2(r, r);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= r * w[e];
+                for (int e = 0; e < 4; ++e) v[e] = mul_f32x2(v[e], r2);
             }
             if (turn) {
-                if (a.interleaved) {
+                uint64_t o[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = v[2 * e], q = v[2 * e + 1];
-                        v[2 * e] = fmaf(p, cs[e], -q * sn[e]);
-                        v[2 * e + 1] = fmaf(q, cs[e], p * sn[e]);
-                    }
-                } else {
+                for (int e = 0; e < 4; ++e) o[e] = mul_f32x2(a.interleaved ? pack_f32x2(high_f32(v[e]), low_f32(v[e])) : v[e ^ 2], k2[e]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = v[e], q = v[e + 4];
-                        v[e] = fmaf(p, cs[e], -q * sn[e]);
-                        v[e + 4] = fmaf(q, cs[e], p * sn[e]);
-                    }
-                }
+                for (int e = 0; e < 4; ++e) v[e] = fma_f32x2(v[e], k1[e], o[e]);
+            } else if (weight) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = mul_f32x2(v[e], k1[e]);
             }
             if (here) store8<FORM>(to0, to1, a.out_dtype, v);
             to0 += step;
@@ -261,6 +313,7 @@ static cudaError_t launch_rotary_typed(RotArgs a, int n_sm, cudaStream_t st) {
         for (int i = 0; i < kinds; ++i) slices += a.x[i].slices = (a.x[i].heads + a.per_group - 1) / a.per_group;
         if (a.per_group == 1 || a.tokens * slices >= want) break;
     }
+    a.by_slices = divisor_of((uint32_t)slices);
     const long long per = kRotThreads / lanes, grid = (a.tokens * slices + per - 1) / per;
     if (lanes == 8) return launch_pdl(rotary_kernel<DT, 8, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
     return launch_pdl(rotary_kernel<DT, 16, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
@@ -315,6 +368,7 @@ extern "C" int saem_rotate(const saem_rotate_config* c, const void* x, const voi
     a.turns = turns; a.positions = positions; a.tokens = c->tokens;
     const int e = head_elem(c->x_dtype), oe = head_elem(c->out_dtype);
     a.inv_dim = 1.f / (float)a.dim;
+    a.w_runs = (uintptr_t)w % (4 * head_elem(c->w_dtype)) == 0;
     a.x[0] = {static_cast<const uint8_t*>(x), c->x_token_stride * e, c->x_head_stride * e, c->heads, 0};
     a.w[0] = w;
     a.out = static_cast<uint8_t*>(out); a.out_ts = c->out_token_stride * oe; a.out_hs = c->out_head_stride * oe; a.out_dtype = c->out_dtype;
@@ -356,6 +410,8 @@ extern "C" int saem_kv_append(const saem_append_config* c, const saem_kv_cache* 
     a.turns = turns; a.positions = positions; a.tokens = b->tokens;
     const int e = head_elem(c->x_dtype);
     a.inv_dim = 1.f / (float)dim;
+    a.w_runs = ((uintptr_t)w_q | (uintptr_t)w_k) % (4 * head_elem(c->w_dtype)) == 0;
+    a.by_page = divisor_of(cache->page_size);
     a.x[0] = {static_cast<const uint8_t*>(q), c->q_token_stride * e, c->q_head_stride * e, q_heads, 0};
     a.x[1] = {static_cast<const uint8_t*>(k), c->k_token_stride * e, c->k_head_stride * e, cache->kv_heads, 0};
     a.x[2] = {static_cast<const uint8_t*>(v), c->v_token_stride * e, c->v_head_stride * e, cache->kv_heads, 0};

@@ -68,10 +68,12 @@ class Attention:
     `append` norms (weights `w_q`, `w_k` [head_dim], float32 or bfloat16, where they are given) and rotates (`rotary`) new queries
     and keys; `attend` takes each token's softmax over the places up to its own (`causal`), of these the last `window` (0: all).
     Calls of one Attention must be ordered on the GPU (they share its workspace), and after the stream that was current when it was
-    made."""
+    made; so must those of several with one workspace (`share`: the Attention whose workspace this one uses too, over a cache of the
+    same head_dim at least)."""
 
     def __init__(self, q_heads: int, cache: PagedCache, rotary: Optional[Rotary] = None, w_q: Optional[torch.Tensor] = None,
-                 w_k: Optional[torch.Tensor] = None, eps: float = 1e-6, scale: Optional[float] = None, causal: bool = True, window: int = 0):
+                 w_k: Optional[torch.Tensor] = None, eps: float = 1e-6, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                 share: Optional["Attention"] = None):
         pages, kv_heads, page, dim = cache.k.shape
         if q_heads < 1 or q_heads % kv_heads or q_heads // kv_heads > 128 or window < 0 or window > 2 ** 31 - 1:
             raise B.SaemError(B.SAEM_ERR_SHAPE, "Attention: %d query heads, %d key heads, window %d" % (q_heads, kv_heads, window))
@@ -89,6 +91,11 @@ class Attention:
             size = B.saem_attend_workspace_bytes(B.saem_kv_cache(cache.k.data_ptr(), cache.v.data_ptr(), pages, page, kv_heads, dim, _DTYPE[cache.k.dtype]))
             if not size:
                 raise B.SaemError(B.SAEM_ERR_CUDA, "Attention")
+            if share is not None:
+                if share.workspace.device != cache.k.device or share.workspace.numel() < size:
+                    raise B.SaemError(B.SAEM_ERR_WORKSPACE, "Attention: the shared workspace is of another GPU or too small")
+                self.workspace, self._status = share.workspace, share._status
+                return
             raw = torch.empty(size + 1024, dtype=torch.uint8, device=cache.k.device)
             self.workspace = raw[-raw.data_ptr() % 1024:][:size]
             self.workspace[:B.SAEM_ATTEND_HEAD_BYTES].zero_()

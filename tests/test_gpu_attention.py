@@ -295,3 +295,100 @@ def test_empty_calls():
                            torch.zeros(0, 4, dtype=torch.int32, device="cuda"))
     att.attend(rows, none, out=out)
     assert bool((out == 2).all())
+
+
+def test_refusals_of_tensors():
+    """What a kernel could not read is refused before it is launched: types, shapes, devices, strides, alignment."""
+    from paper_2608_21614_b200 import attention, binding as B
+    q, cache, batch, _ = build([(2, 30), (1, 20)], 4, 2, 64, 16, torch.bfloat16)
+    att = attention.Attention(4, cache)
+
+    def code(f):
+        with pytest.raises(B.SaemError) as e:
+            f()
+        return e.value.code
+    wide = torch.zeros(3, 4, 136, dtype=torch.bfloat16, device="cuda")
+    flat = torch.zeros(3 * 4 * 64 + 8, dtype=torch.bfloat16, device="cuda")
+    assert code(lambda: att.attend(q.half(), batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.attend(q.float(), batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.attend(q[:, :2], batch)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: att.attend(q[..., :32], batch)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: att.attend(q.flatten(1), batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.attend(q.cpu(), batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.attend(wide[..., ::2][..., :64], batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.attend(wide[..., 4:68], batch)) == B.SAEM_ERR_ALIGNMENT
+    assert code(lambda: att.attend(flat[1:769].view(3, 4, 64), batch)) == B.SAEM_ERR_ALIGNMENT
+    assert code(lambda: att.attend(q, batch, out=q[:2])) == B.SAEM_ERR_SHAPE
+    assert code(lambda: att.attend(q, batch, out=torch.empty_like(q[:1]).expand(3, 4, 64))) == B.SAEM_ERR_SHAPE
+    assert code(lambda: att.attend(q, batch, out=torch.empty_like(q, dtype=torch.float32))) == B.SAEM_ERR_INVALID_ARG
+    for lse in (torch.empty(3, 4, device="cuda").half(), torch.empty(3, 4), torch.empty(4, 3, device="cuda").T):
+        assert code(lambda: att.attend(q, batch, lse=lse)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.attend(q, batch, lse=torch.empty(12, device="cuda"))) == B.SAEM_ERR_SHAPE
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    assert code(lambda: att.append(q, k[:2], k, batch)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: att.append(q, k, k.float(), batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.append(q.float(), k, k, batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.append(q, k, k, batch, q_out=torch.empty_like(q, dtype=torch.float16))) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: att.append(None, k, k, batch, positions=torch.zeros(2, dtype=torch.int32, device="cuda"))) == B.SAEM_ERR_SHAPE
+    assert code(lambda: att.append(None, k, k, batch, positions=torch.zeros(3, dtype=torch.int64, device="cuda"))) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: attention.Attention(3, cache)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.Attention(512, cache)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.Attention(4, cache, window=-1)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.Attention(4, cache, scale=0.0).attend(q, batch)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: attention.PagedCache(cache.k, cache.v.half())) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.PagedCache(cache.k.float(), cache.v.float())) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: attention.PagedCache(cache.k[:, :, :8].contiguous(), cache.v[:, :, :8].contiguous())) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.PagedCache(cache.k.transpose(1, 2), cache.v.transpose(1, 2))) == B.SAEM_ERR_INVALID_ARG
+    i = batch.lengths
+    assert code(lambda: attention.Batch(batch.offsets, i.long(), batch.table)) == B.SAEM_ERR_INVALID_ARG
+    assert code(lambda: attention.Batch(batch.offsets[:2], i, batch.table)) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.Batch(batch.offsets, i, batch.table[:1])) == B.SAEM_ERR_SHAPE
+    assert code(lambda: attention.Batch(batch.offsets, i, batch.table.T.contiguous().T)) == B.SAEM_ERR_INVALID_ARG
+    small = attention.Attention(4, cache)
+    small.workspace = small.workspace[:8192]
+    assert code(lambda: small.attend(q, batch)) == B.SAEM_ERR_WORKSPACE
+    att.attend(q, batch)                                                        # and the handle still works
+    assert att.device_status() == 0
+
+
+@pytest.mark.parametrize("named_by", ["stream", "handle"])
+def test_results_of_a_named_stream_keep_clear_of_the_current_one(named_by):
+    from paper_2608_21614_b200 import attention, rotary
+    seqs = [(64, 300), (1, 40)]
+    q, cache, batch, _ = build(seqs, 8, 2, 64, 16, torch.bfloat16, garbage=0.0)
+    k = torch.randn(65, 2, 64, device="cuda").bfloat16()
+    turn = rotary.Rotary(64)
+    att = attention.Attention(8, cache, rotary=turn)
+    p = torch.arange(65, dtype=torch.int32, device="cuda")
+    calls = {"append": lambda st: att.append(q, k, k, batch, stream=st), "attend": lambda st: att.attend(q, batch, stream=st), "rotate": lambda st: turn.rotate(q, p, stream=st)}
+    for name, call in calls.items():
+        want = call(None)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        torch.cuda.empty_cache()
+        buf = torch.empty(q.shape, dtype=q.dtype, device="cuda")                # given back while the current stream will still write to it
+        torch.cuda._sleep(40_000_000)
+        buf.fill_(1)
+        del buf
+        got = call(side if named_by == "stream" else side.cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), name
+
+
+def test_two_handles_on_two_streams_at_once():
+    """Each with its own workspace: both as alone."""
+    from paper_2608_21614_b200 import attention
+    runs = []
+    for seed, max_new in ((1, 1), (2, 1000)):
+        q, cache, batch, _ = build([(3, 5000), (200, 2000), (1, 300)], 8, 2, 128, 64, torch.bfloat16, seed=seed)
+        batch.max_new = max_new
+        att = attention.Attention(8, cache)
+        want = att.attend(q, batch)
+        runs.append((att, q, batch, want, torch.empty_like(q), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for att, q, batch, _, out, st in runs:
+            att.attend(q, batch, out=out, stream=st)
+    torch.cuda.synchronize()
+    for att, _, _, want, out, _ in runs:
+        assert torch.equal(out, want) and att.device_status() == 0

@@ -644,14 +644,19 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     if (n_q[g]) ok = ok && mbar_wait_warp(smem_u32(&bar_free[g]), (n_q[g] - 1) & 1, abort_p, a.status);
                     if (!ok) break;
                     ++n_q[g];
-                    constexpr int kPieces = DK / 8;
-                    const int skip = both ? 0 : g * 128, c = lane % kPieces;
-                    const uint32_t to = base + g * kTile + c / 8 * kAtKeys * 128;
-#pragma unroll 8
-                    for (int r = lane / kPieces; r < 128; r += 32 / kPieces) {
-                        const bool in = skip + r < p.rows && c * 8 < a.dim;
-                        const int row = p.r * kAtR + skip + (in ? r : 0), t = quotient(row, a.by_group), head = p.h * a.group + row - t * a.group;
-                        cp_async16(to + r * 128 + ((c % 8 ^ (r & 7)) << 4), a.q + ((p.e.first + t) * a.q_ts + head * a.q_hs + (in ? c * 8 : 0)) * 2, in ? 16 : 0);
+                    // eight rows at a time, four lanes to a row; rows beyond the item's are left as they are, nobody reads what comes of them
+                    const int skip = both ? 0 : g * 128, n_rows = min(128, p.rows - skip);
+#pragma unroll 2
+                    for (int r = lane >> 2; r < n_rows; r += 8) {
+                        const int row = p.r * kAtR + skip + r, t = quotient(row, a.by_group), head = p.h * a.group + row - t * a.group;
+                        const uint8_t* q = a.q + ((p.e.first + t) * a.q_ts + head * a.q_hs) * 2;
+                        const uint32_t to = base + g * kTile + r * 128;
+#pragma unroll
+                        for (int j = 0; j < DK / 32; ++j) {
+                            const int c = j * 4 + (lane & 3);
+                            const bool in = c * 8 < a.dim;
+                            cp_async16(to + c / 8 * kAtKeys * 128 + ((c % 8 ^ (r & 7)) << 4), q + (in ? c * 16 : 0), in ? 16 : 0);
+                        }
                     }
                     cp_async_commit();
                     cp_async_wait<0>();

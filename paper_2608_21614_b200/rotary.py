@@ -62,13 +62,16 @@ def frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[dict] 
     return result
 
 
+_PER_RADIAN = (10 ** 50 << 320) // (2 * 314159265358979323846264338327950288419716939937510)    # 2^320 / (2 pi)
+
+
 def turns(radians: List[float]) -> List[int]:
     """Frequencies as fractions of a turn per position in units of 2^-64, as the kernels read them (signed 64-bit words)."""
-    from fractions import Fraction
-    two_pi = 2 * Fraction(314159265358979323846264338327950288419716939937510, 10 ** 50)
     out = []
     for f in radians:
-        u = round(Fraction(f) / two_pi * 2 ** 64) % 2 ** 64
+        n, d = f.as_integer_ratio()             # d is a power of two
+        shift = 256 + d.bit_length() - 1
+        u = (n * _PER_RADIAN + (1 << (shift - 1)) >> shift) % 2 ** 64
         out.append(u - 2 ** 64 if u >= 2 ** 63 else u)
     return out
 

@@ -5,7 +5,7 @@
 // for what an item costs by itself (queries, first bytes, the result).  All units of a call, in the order sequence, key head, row
 // tile, are cut into as many equal ranges as there are CTAs: long and short sequences, few and many rows load the SMs alike.  A cut
 // within an item's first HEAD units moves to its beginning, and one within SNAP units (or a third of a range, if that is less) of either end of an
-// item moves there, because a cut costs about as much.  An item that is still cut leaves sums of its parts in the workspace, and the CTA
+// item moves there, because a cut costs about as much; an item of up to 2 HEAD units is not cut at all.  An item that is still cut leaves sums of its parts in the workspace, and the CTA
 // that arrives last adds them up in the order of the parts, so that two runs give the same bits.
 #ifndef SAEM_ATTEND_PLAN_CUH_
 #define SAEM_ATTEND_PLAN_CUH_
@@ -230,7 +230,7 @@ struct AttendWalk {
             key_tiles<KEYS>(a, e, row0, row1, b, t);
             const int units = HEAD + max(1, t - b);
             // its parts begin with the item and at the cuts between item + low and item + units - snap
-            const int first = (int)((item + min(low, units - 1)) / per), last = max(first, (int)((item + units - snap - 1) / per));
+            const int first = (int)((item + min(low, units - 1)) / per), last = units <= 2 * HEAD ? first : max(first, (int)((item + units - snap - 1) / per));
             if (first > me) return false;
             const bool mine = me <= last;
             if (mine) {

@@ -325,10 +325,12 @@ static size_t partials_bytes(int dim, int n_sm) {
     const size_t rows = (size_t)2 * kRowsPerSm * n_sm * RowsShape<kHeadDimMax>::kSlot * 4, tiles = attend_tiles_partials(dim, n_sm);
     return rows > tiles ? rows : tiles;
 }
-// Which form, by the most rows of a sequence and key head (times in us, 8 key heads of 128 elements; few, many).  One tile of 16: few.  Two
-// tiles read the cache twice, from L2 where there is one sequence: 20 rows over 500 places 13.0, 17.0, over 4000 21.4, 27.6, over 16000
-// 33.5, 35.5; of 8 sequences 20.3, 20.1 and 47.9, 43.3 and 175, 98; 64 rows of one sequence over 16000 44.7, 37.3.
-static bool rows_are_few(long long rows, int seqs) { return rows <= 16 || (rows <= 32 && seqs == 1); }
+// Which form, by the most rows of a sequence and key head and by the rows of all heads together (times in us: few, many).  Up to 16 rows read
+// the cache once either way: 64 sequences of 2000 places 94, 110.  More read it once per 16 rows, from L2, but there are more items to
+// share out, which is what counts while there are few in all: 60 tokens of 8 heads over 700 places 14.4, 24.0, 10 of 32 heads in each
+// of 2 sequences of 1000 16.6, 20.3 (of 200 13.5, 11.1), 16 of 32 heads over 4000 22.7, 25.9 (over 16000 44.7, 35.4); and
+// beyond: 5 of 32 heads in each of 8 sequences of 500 19.1, 15.3, of 16000 175, 98.
+static bool rows_are_few(long long rows, long long all_rows) { return rows <= 16 || all_rows <= 768; }
 
 template <bool F16, int DK>
 static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t st) {
@@ -392,7 +394,7 @@ extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cac
     a.status = reinterpret_cast<int*>(ws);
     a.counters = reinterpret_cast<int*>(ws + kAttendCounters);
     a.partials = reinterpret_cast<float*>(ws + SAEM_ATTEND_HEAD_BYTES);
-    const bool f16 = cache->dtype == SAEM_OUT_F16, few = rows_are_few((long long)b->max_new * a.group, b->seqs);
+    const bool f16 = cache->dtype == SAEM_OUT_F16, few = rows_are_few((long long)b->max_new * a.group, (long long)b->tokens * c->q_heads);
     const cudaError_t e = few ? launch_rows(a, f16, n_sm, (cudaStream_t)stream) : launch_attend_tiles(a, f16, n_sm, (cudaStream_t)stream);
     return e == cudaSuccess ? SAEM_OK : SAEM_ERR_CUDA;
 }

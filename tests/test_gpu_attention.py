@@ -18,8 +18,9 @@ def gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
 
-def build(seqs, q_heads, kv_heads, dim, page, dtype, seed=0, garbage=float("nan"), spare_pages=3, spare_rows=0, table_extra=2):
-    """seqs: (new, length) each.  A cache whose every place outside the sequences is `garbage`."""
+def build(seqs, q_heads, kv_heads, dim, page, dtype, seed=0, garbage=float("nan"), spare_pages=3, spare_rows=None, table_extra=2):
+    """seqs: (new, length) each.  A cache whose every place outside the sequences is `garbage`, and rows behind the last sequence: so many, unless
+    said otherwise, that a call is none of few rows in all, and max_new alone chooses the form (1: few rows per key head, 1000: many)."""
     from paper_2608_21614_b200 import attention
     g = gen(seed)
     need = [-(-n // page) for _, n in seqs]
@@ -38,7 +39,7 @@ def build(seqs, q_heads, kv_heads, dim, page, dtype, seed=0, garbage=float("nan"
     offsets = [0]
     for m, _ in seqs:
         offsets.append(offsets[-1] + m)
-    rows = offsets[-1] + spare_rows
+    rows = offsets[-1] + (800 // q_heads + 1 if spare_rows is None else spare_rows)
     q = (torch.randn(rows, q_heads, dim, generator=g, device="cuda") * 1.5).to(dtype)
     batch = attention.Batch(torch.tensor(offsets, dtype=torch.int32, device="cuda"), torch.tensor([n for _, n in seqs], dtype=torch.int32, device="cuda"),
                             table, max_new=max([m for m, _ in seqs] + [0]))
@@ -89,6 +90,13 @@ def run(seqs, q_heads=8, kv_heads=2, dim=128, page=64, dtype=torch.bfloat16, cau
     return out
 
 
+def test_few_rows_in_all():
+    """As a program calls it, without rows to spare: up to 768 rows go to the form for few, one more to the other."""
+    for new in (47, 48, 49):
+        run([(new, 200), (48, 100)], q_heads=8, kv_heads=2, spare_rows=0)
+    run([(300, 700)], q_heads=2, kv_heads=1, spare_rows=0)
+
+
 # one new token, or a few
 @pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 500, 1000, 4097])
 def test_one_token(length):
@@ -130,7 +138,7 @@ SHAPES = {
 @pytest.mark.parametrize("max_new", [1, 1000])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 100), (False, 33), (True, 1)])
 def test_shapes_and_masks(shape, max_new, causal, window):
-    run(SHAPES[shape], causal=causal, window=window, max_new=max_new, spare_rows=5)
+    run(SHAPES[shape], causal=causal, window=window, max_new=max_new)
 
 
 @pytest.mark.parametrize("max_new", [1, 1000])
@@ -156,10 +164,10 @@ def test_what_a_row_does_not_see(max_new, value, where):
         q, cache, batch, offsets = build(seqs, 8, 2, 64, 32, torch.bfloat16)
         batch.max_new = max_new
         att = attention.Attention(8, cache, window=window)
-        before = att.attend(q, batch)
+        before = att.attend(q, batch)[:151]
         c = getattr(cache, where)
         c[batch.table[0, 300 // 32].long(), 1, 300 % 32, 5] = value
-        after = att.attend(q, batch)
+        after = att.attend(q, batch)[:151]
         place = 250 + torch.arange(150, device="cuda")
         sees = (place >= 300) & ((place - 300 < window) if window else True)
         unseen = torch.cat((~sees, torch.ones(1, dtype=torch.bool, device="cuda")))
@@ -193,9 +201,9 @@ def test_twice_the_same_bits_and_shared_workspace(max_new):
     q, cache, batch, _ = build([(5, 3000), (1, 200), (300, 2000)], 8, 2, 128, 64, torch.bfloat16)
     batch.max_new = max_new
     att = attention.Attention(8, cache)
-    first = att.attend(q, batch)
+    first = att.attend(q, batch)[:306]
     for _ in range(3):
-        assert torch.equal(att.attend(q, batch), first)
+        assert torch.equal(att.attend(q, batch)[:306], first)
 
 
 @pytest.mark.parametrize("max_new", [1, 1000])
@@ -206,10 +214,10 @@ def test_pages_outside_the_cache(max_new):
     q, cache, batch, offsets = build(seqs, 4, 2, 64, 32, torch.bfloat16)
     batch.max_new = max_new
     att = attention.Attention(4, cache)
-    want = att.attend(q, batch)
+    want = att.attend(q, batch)[:32]
     for bad in (-1, cache.k.shape[0], 2 ** 31 - 1):
         batch.table[0, 1] = bad
-        got = att.attend(q, batch)
+        got = att.attend(q, batch)[:32]
         assert att.device_status() == B.SAEM_ERR_INVALID_ARG
         assert torch.equal(got[2:], want[2:]) and bool(torch.isfinite(got[:2]).all())
 
@@ -220,9 +228,16 @@ def test_offsets_beyond_the_call_are_cut():
     q, cache, batch, _ = build([(4, 50), (9, 60)], 4, 2, 64, 32, torch.bfloat16)
     for max_new in (1, 1000):
         batch.max_new = max_new
-        out = torch.full((13, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
-        attention.Attention(4, cache).attend(q[:6], batch, out=out[:6])
-        assert bool((out[6:] == 3).all()) and bool(torch.isfinite(out[:6]).all())
+        for rows in (6, 12):
+            out = torch.full((13, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+            attention.Attention(4, cache).attend(q[:rows], batch, out=out[:rows])
+            assert bool((out[rows:] == 3).all()) and bool(torch.isfinite(out[:rows]).all())
+    many, _, _, _ = build([(4, 50), (9, 60)], 64, 2, 64, 32, torch.bfloat16)
+    out = torch.full((14, 64, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    attention.Attention(64, cache).attend(many[:13], batch, out=out[:13])                       # 832 rows: the form for many
+    batch.offsets.copy_(torch.tensor([0, 20, 13], dtype=torch.int32))                           # and not ascending
+    attention.Attention(64, cache).attend(many[:13], batch, out=out[:13])
+    assert bool((out[13:] == 3).all()) and bool(torch.isfinite(out[:13]).all())
 
 
 @pytest.mark.parametrize("max_new", [1, 1000])
@@ -230,10 +245,9 @@ def test_lengths_beyond_the_table_are_cut(max_new):
     from paper_2608_21614_b200 import attention
     seqs = [(3, 64)]
     q, cache, batch, offsets = build(seqs, 4, 2, 64, 32, torch.bfloat16, table_extra=0)
-    want = attention.Attention(4, cache).attend(q, batch)
     batch.max_new = max_new
     batch.lengths.fill_(2 ** 31 - 1)
-    out = attention.Attention(4, cache, causal=False).attend(q, batch)
+    out = attention.Attention(4, cache, causal=False).attend(q, batch)[:3]
     want = torch.stack([ref.attend(q[t:t + 1], *(ref.gather(c, batch.table[0], 64, 32) for c in (cache.k, cache.v)), 1, False, 0, 0.125)[0][0] for t in range(3)])
     assert bool(((out.double() - want).abs() < 0.05).all())
 
@@ -245,7 +259,7 @@ def test_more_places_than_32_bits_of_bytes():
     cache = attention.PagedCache.empty(pages, heads, page, dim)
     for c in (cache.k, cache.v):
         c[-4:] = torch.randn(4, heads, page, dim, generator=gen(4), device="cuda").bfloat16()
-    q = torch.randn(33, 16, dim, generator=gen(5), device="cuda").bfloat16()
+    q = torch.randn(60, 16, dim, generator=gen(5), device="cuda").bfloat16()                    # 27 rows behind the last sequence
     for max_new in (1, 1000):
         batch = attention.Batch(torch.tensor([0, 1, 33], dtype=torch.int32, device="cuda"), torch.tensor([300, 140], dtype=torch.int32, device="cuda"),
                                 torch.tensor([[pages - 1, pages - 3, pages - 2], [pages - 2, pages - 4, 0]], dtype=torch.int32, device="cuda"), max_new)
@@ -300,7 +314,7 @@ def test_empty_calls():
 def test_refusals_of_tensors():
     """What a kernel could not read is refused before it is launched: types, shapes, devices, strides, alignment."""
     from paper_2608_21614_b200 import attention, binding as B
-    q, cache, batch, _ = build([(2, 30), (1, 20)], 4, 2, 64, 16, torch.bfloat16)
+    q, cache, batch, _ = build([(2, 30), (1, 20)], 4, 2, 64, 16, torch.bfloat16, spare_rows=0)
     att = attention.Attention(4, cache)
 
     def code(f):
@@ -355,7 +369,7 @@ def test_refusals_of_tensors():
 def test_results_of_a_named_stream_keep_clear_of_the_current_one(named_by):
     from paper_2608_21614_b200 import attention, rotary
     seqs = [(64, 300), (1, 40)]
-    q, cache, batch, _ = build(seqs, 8, 2, 64, 16, torch.bfloat16, garbage=0.0)
+    q, cache, batch, _ = build(seqs, 8, 2, 64, 16, torch.bfloat16, garbage=0.0, spare_rows=0)
     k = torch.randn(65, 2, 64, device="cuda").bfloat16()
     turn = rotary.Rotary(64)
     att = attention.Attention(8, cache, rotary=turn)
@@ -380,7 +394,7 @@ def test_two_handles_on_two_streams_at_once():
     from paper_2608_21614_b200 import attention
     runs = []
     for seed, max_new in ((1, 1), (2, 1000)):
-        q, cache, batch, _ = build([(3, 5000), (200, 2000), (1, 300)], 8, 2, 128, 64, torch.bfloat16, seed=seed)
+        q, cache, batch, _ = build([(3, 5000), (200, 2000), (1, 300)], 8, 2, 128, 64, torch.bfloat16, seed=seed, spare_rows=0)
         batch.max_new = max_new
         att = attention.Attention(8, cache)
         want = att.attend(q, batch)

@@ -402,44 +402,51 @@ int saem_block_norm(const saem_norm_config* cfg, const void* x, const void* y, c
                     const void* w_pre, void* x_out, void* n_out, void* stream);
 
 /*
- * The attention half of a decoder layer (no counterpart in the paper: what stands beside the expert step).  Three calls: the norm
- * of each head with the rotation of its position, the same on the way of new queries, keys and values with the keys and values
- * appended to a paged cache, and attention of the new tokens over that cache.
+ * The attention half of a decoder layer (no counterpart in the paper: what stands beside the expert step).  Three calls: the
+ * norm of each head with the rotation of its position, the same on the way of new queries, keys and values with the keys and
+ * values appended to a paged cache, and attention of the new tokens over that cache.
  *
- * Heads are tensors [tokens, heads, head_dim] whose head_dim elements are consecutive; token and head strides are in elements.
- * head_dim is a multiple of 8, at most 128.  Types are SAEM_OUT_*; arithmetic is fp32 and results are rounded once.
+ * Heads are tensors [tokens, heads, head_dim] whose head_dim elements are consecutive; token and head strides are in
+ * elements. head_dim is a multiple of 8, at most 128.  Types are SAEM_OUT_*; arithmetic is fp32 and results are rounded
+ * once.
  *
- * Rotation (saem_rotary_config): a head x becomes y = x / sqrt(mean(x^2) + eps) * w (y = x where there is no w), and of its first
- * rotary_dim elements (a multiple of 8, 0 to head_dim) each pair (a, b) becomes amplitude * (a cos - b sin, b cos + a sin).  Pair i
- * is elements (2i, 2i + 1) if interleaved, else (i, i + rotary_dim / 2), and its angle is position * turns[i] / 2^64 turns:
- * turns (dev, rotary_dim / 2 entries, may be NULL if rotary_dim is 0) holds its frequency in turns per position as a fraction of
- * 2^64, so that the angle's whole turns drop out of the integer product and far positions are as exact as near ones.
+ * Rotation (saem_rotary_config): a head x becomes y = x / sqrt(mean(x^2) + eps) * w (y = x where there is no w), and of its
+ * first rotary_dim elements (a multiple of 8, 0 to head_dim) each pair (a, b) becomes amplitude * (a cos - b sin, b cos + a
+ * sin).  Pair i is elements (2i, 2i + 1) if interleaved, else (i, i + rotary_dim / 2), and its angle is position * turns[i]
+ * / 2^64 turns: turns (dev, rotary_dim / 2 entries, may be NULL if rotary_dim is 0) holds its frequency in turns per
+ * position as a fraction of 2^64, so that the angle's whole turns drop out of the integer product and far positions are as
+ * exact as near ones.
  *
- * saem_rotate: x[tokens, heads, head_dim] (any type) to out (any type); positions[tokens] int32 (dev); w (dev) [head_dim] or NULL.
- * out may be x (same type and strides).
+ * saem_rotate: x[tokens, heads, head_dim] (any type) to out (any type); positions[tokens] int32 (dev); w (dev) [head_dim] or
+ * NULL. out may be x (same type and strides).
  *
- * Cache (saem_kv_cache): k and v (dev, 16-byte aligned) [pages, kv_heads, page_size, head_dim], BF16 or F16; page_size a multiple of 16.
- * Batch (saem_batch, all dev): sequence s has the rows offsets[s] .. offsets[s + 1] - 1 of the call's tokens (offsets ascending from
- * 0; rows from offsets[seqs] on belong to no sequence and what is written for tokens leaves them as they were), which are the last of its
- * lengths[s] places, and place p lies in page table[s * table_stride + p / page_size] (max_pages entries a row).  max_new (host): the
- * most new tokens of a sequence, a hint that chooses a kernel form and never changes which rows are computed.  Nothing of a batch is read on the
- * host, so that a captured graph serves growing lengths.
+ * Cache (saem_kv_cache): k and v (dev, 16-byte aligned) [pages, kv_heads, page_size, head_dim], BF16 or F16; page_size a
+ * multiple of 16. Batch (saem_batch, all dev): sequence s has the rows offsets[s] .. offsets[s + 1] - 1 of the call's tokens
+ * (offsets ascending from 0; rows from offsets[seqs] on belong to no sequence and what is written for tokens leaves them as
+ * they were), which are the last of its lengths[s] places, and place p lies in page table[s * table_stride + p / page_size]
+ * (max_pages entries a row).  max_new (host): the most new tokens of a sequence, a hint that chooses a kernel form and never
+ * changes which rows are computed.  Nothing of a batch is read on the host, so that a captured graph serves growing lengths.
  *
- * saem_kv_append: q[tokens, q_heads, head_dim] (may be NULL, as q_out then) is normed (w_q) and rotated into q_out (the cache's type), k with w_k
- * into the cache, v as it is.  positions NULL: a token's place in its sequence.  A token whose place is negative
- * (fewer places than new tokens) or not in the table is not stored.  A place beyond the table or a page outside [0, pages) that a
- * token needs sets *status (dev int32, may be NULL) to SAEM_ERR_INVALID_ARG.  Places are written without order: no two tokens of a
- * batch may share one.
+ * saem_kv_append: q[tokens, q_heads, head_dim] (may be NULL, as q_out then) is normed (w_q) and rotated into q_out (the
+ * cache's type), k with w_k into the cache, v as it is.  q_out may be q (same type and strides).  positions NULL: a token's
+ * place in its sequence.  A token whose place is negative (fewer places than new tokens) or not in the table is not stored.
+ * A place beyond the table or a page outside [0, pages) that a token needs sets *status (dev int32, may be NULL) to
+ * SAEM_ERR_INVALID_ARG.  Places are written without order: no two tokens of a batch may share one.
  *
- * saem_attend: out[t, h] = sum_j p_j v_j, p = softmax_j(scale * q[t, h] . k_j), over the places j of t's sequence, with causal != 0 those up
- * to t's own, with window > 0 those after t's own less window.  q, out and the cache have one type.  q_heads is a multiple of kv_heads;
- * q_heads / kv_heads (at most 128) neighbouring query heads share a key head.  A row that sees nothing is 0 (lse -inf).  lse (dev fp32
- * [tokens, q_heads], may be NULL): log sum_j exp(scale * q . k_j).  What lies in places that a row does not see has no effect on it, whatever it
- * is; of a page outside [0, pages) the places count as zeros, and the status word becomes SAEM_ERR_INVALID_ARG.  q and out: 16-byte aligned, strides
- * multiples of 8 elements.  workspace (dev, 1024-byte aligned, saem_attend_workspace_bytes): its first 4 bytes are the status word;
- * zero its first SAEM_ATTEND_HEAD_BYTES once (again after SAEM_ERR_TIMEOUT).  Calls that share it must be ordered.  Two runs give the same bits.
+ * saem_attend: out[t, h] = sum_j p_j v_j, p = softmax_j(scale * q[t, h] . k_j), over the places j of t's sequence, with
+ * causal != 0 those up to t's own, with window > 0 those after t's own less window.  q, out and the cache have one type.
+ * q_heads is a multiple of kv_heads; q_heads / kv_heads (at most 128) neighbouring query heads share a key head.  A row that
+ * sees nothing is 0 (lse -inf).  lse (dev fp32 [tokens, q_heads], may be NULL): log sum_j exp(scale * q . k_j).  What lies
+ * in places that a row does not see has no effect on it, whatever it is (a result that comes out NaN is summed again from
+ * what its row sees alone); of a page outside [0, pages) the places count as zeros, and the status word becomes
+ * SAEM_ERR_INVALID_ARG.  q and out: 16-byte aligned, strides multiples of 8 elements, apart from each other and the cache.
+ * workspace (dev, 1024-byte aligned, saem_attend_workspace_bytes): its first 4 bytes are the status word; zero its first
+ * SAEM_ATTEND_HEAD_BYTES once (again after SAEM_ERR_TIMEOUT).  Calls that share it must be ordered.  Two runs give the same
+ * bits.
  *
- * Sizes: tokens * max(heads) and pages * kv_heads * page_size below 2^31, seqs <= 65536, page_size <= 65536.  tokens == 0 or seqs == 0 is a no-op.
+ * Sizes: tokens * max(heads) and pages * kv_heads * page_size below 2^31, seqs <= 65536, page_size <= 65536, places of a
+ * sequence below 2^31 - 2^16 (what lies beyond them, or beyond its table, is not seen).  tokens == 0 or seqs == 0 is a
+ * no-op.
  * Errors: INVALID_ARG (null, type, eps, scale), SHAPE, ALIGNMENT, WORKSPACE, CUDA.
  */
 enum { SAEM_ATTEND_HEAD_BYTES = 8192 };

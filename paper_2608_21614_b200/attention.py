@@ -118,7 +118,7 @@ class Attention:
     def attend(self, q: torch.Tensor, batch: Batch, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
         """q [tokens, q_heads, head_dim] (the cache's type) over the cache; lse [tokens, q_heads] float32, if given, becomes the logarithm of each
-        row's sum of exponentials.  Rows behind the batch's last are left as they were."""
+        row's sum of exponentials.  Rows behind the batch's last are left as they were; out must not be q."""
         if out is None:
             with _allocated_on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -129,6 +129,11 @@ class Attention:
         return out
 
     def device_status(self) -> int:
-        """The status word of the calls so far, whatever their streams (synchronises the device)."""
+        """The status word of the calls so far, whatever their streams (synchronises the device): 0, SAEM_ERR_INVALID_ARG after a page
+        outside the cache or a place outside the table, SAEM_ERR_TIMEOUT if a device-side wait ran out.  Clears it."""
         torch.cuda.synchronize(self.workspace.device)
-        return int(self._status.item())
+        code = int(self._status.item())
+        if code:                            # with the counters of a call that did not end
+            self.workspace[:B.SAEM_ATTEND_HEAD_BYTES].zero_()
+            torch.cuda.synchronize(self.workspace.device)
+        return code

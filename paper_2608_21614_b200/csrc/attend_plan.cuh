@@ -284,22 +284,48 @@ __device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExte
         v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
     };
     if (here) four(a.q, token * a.q_ts + head * a.q_hs + at, q);
-    for (int j = lo; j <= hi; ++j) {
-        const int page = a.table[s * a.table_stride + j / a.page_size];
-        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (here && page >= 0 && page < a.pages) {
-            const long long i = (((long long)page * a.kv_heads + h) * a.page_size + j % a.page_size) * a.dim + at;
-            four(a.k, i, k);
-            four(a.v, i, v);
+    constexpr int kAhead = 4;               // places at a time
+    for (int j0 = lo; j0 <= hi; j0 += kAhead) {
+        float k[kAhead][4] = {}, v[kAhead][4] = {}, d[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int j = min(j0 + i, hi), entry = quotient(j, a.by_page), page = a.table[s * a.table_stride + entry];
+            if (here && page >= 0 && page < a.pages) {
+                const long long from = (((long long)page * a.kv_heads + h) * a.page_size + j - entry * a.page_size) * a.dim + at;
+                four(a.k, from, k[i]);
+                four(a.v, from, v[i]);
+            }
         }
-        float d = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
-        d *= a.scale_log2;
-        const float mn = fmaxf(m, d), base = mn == -INFINITY ? 0.f : mn, was = fast_exp2(m - base), p = fast_exp2(d - base);
+        for (int i = 0; i < kAhead; ++i) {
+            d[i] = q[0] * k[i][0] + q[1] * k[i][1] + q[2] * k[i][2] + q[3] * k[i][3];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(p, v[i], o[i] * was);
-        l = l * was + p;
+            for (int x = 16; x > 0; x >>= 1) d[i] += __shfl_xor_sync(0xffffffffu, d[i], x);
+            d[i] = j0 + i <= hi ? d[i] * a.scale_log2 : -INFINITY;
+        }
+        float mn = m;
+        bool nan = false;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            mn = fmaxf(mn, d[i]);
+            nan |= d[i] != d[i] || d[i] == INFINITY;
+        }
+        if (nan) {                          // so is the whole row
+            l = NAN;
+            break;
+        }
+        const float base = mn == -INFINITY ? 0.f : mn, was = fast_exp2(m - base);
+        l *= was;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= was;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (j0 + i > hi) break;         // what is there may not be seen
+            const float p = fast_exp2(d[i] - base);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(p, v[i][e], o[e]);
+            l += p;
+        }
         m = mn;
     }
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;

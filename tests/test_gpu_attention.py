@@ -179,6 +179,25 @@ def test_what_a_row_does_not_see(max_new, value, where):
 
 
 @pytest.mark.parametrize("max_new", [1, 1000])
+def test_rows_that_are_nan_throughout(max_new):
+    """Queries, keys or values of NaN from some place on: rows that see them are NaN, where the formula says so, the others as it says."""
+    from paper_2608_21614_b200 import attention
+    seqs = [(300, 700), (2, 90)]
+    q, cache, batch, offsets = build(seqs, 8, 2, 64, 32, torch.bfloat16)
+    batch.max_new = max_new
+    att = attention.Attention(8, cache)
+    q[40, 3] = math.nan
+    q[41, 2, 7] = math.inf
+    out = att.attend(q, batch)
+    assert bool(torch.isnan(out[40, 3]).all()) and bool(torch.isnan(out[41, 2]).all())
+    assert int(torch.isnan(out[:302]).any(-1).sum()) == 2
+    q[40:42] = 1.0
+    cache.v[batch.table[0, 500 // 32:(680 // 32) + 1].long(), :, :, :9] = math.nan
+    out = att.attend(q, batch)
+    check(out, None, q, cache, batch, seqs, offsets, True, 0, 0.125)
+
+
+@pytest.mark.parametrize("max_new", [1, 1000])
 def test_strides(max_new):
     """Queries as a part of a wider projection, results with heads before tokens."""
     from paper_2608_21614_b200 import attention
@@ -218,7 +237,7 @@ def test_pages_outside_the_cache(max_new):
     for bad in (-1, cache.k.shape[0], 2 ** 31 - 1):
         batch.table[0, 1] = bad
         got = att.attend(q, batch)[:32]
-        assert att.device_status() == B.SAEM_ERR_INVALID_ARG
+        assert att.device_status() == B.SAEM_ERR_INVALID_ARG and att.device_status() == 0       # read and cleared
         assert torch.equal(got[2:], want[2:]) and bool(torch.isfinite(got[:2]).all())
 
 

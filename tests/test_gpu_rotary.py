@@ -242,3 +242,23 @@ def test_captured_append_and_attend_on_a_named_stream():
         graph.replay()
         assert torch.equal(out, want[i])
         batch.lengths += 1
+
+
+def test_append_in_place():
+    """q_out may be q itself; the cache gets what it gets otherwise."""
+    from paper_2608_21614_b200 import attention, rotary
+    g = gen(3)
+    for interleaved in (False, True):
+        batch, _ = batch_of([(9, 40), (1, 16), (30, 30)], 16, 9)
+        qkv = torch.randn(40, 20, 80, generator=g, device="cuda").bfloat16()
+        w = (1 + 0.1 * torch.randn(80, generator=g, device="cuda")).bfloat16()
+        results = []
+        for in_place in (False, True):
+            cache = attention.PagedCache(*(torch.zeros(9, 2, 16, 80, device="cuda").bfloat16() for _ in range(2)))
+            att = attention.Attention(16, cache, rotary=rotary.Rotary(80, 64, interleaved=interleaved), w_q=w, w_k=w)
+            x = qkv.clone()
+            q, k, v = x.split([16, 2, 2], 1)
+            out = att.append(q, k, v, batch, q_out=q if in_place else None)
+            results.append((out.clone(), cache.k, cache.v))
+            assert torch.equal(x[:, 16:], qkv[:, 16:])
+        assert all(torch.equal(a, b) for a, b in zip(*results))

@@ -4,8 +4,8 @@
 // A head is eight elements for each of 8 or 16 neighbouring lanes: two runs of four, which are the two halves of four pairs (half
 // layout) or four pairs next to each other (interleaved), so that a rotation stays within a lane and only the norm's sum crosses
 // them.  A group of lanes takes some neighbouring heads of one token, all queries, all keys or all values, and keeps the token's sines and
-// cosines for them: they cost more instructions than the rest of a head.  Four heads are under way ahead of the one at hand.  The
-// bound is DRAM for many tokens; for one it is the launch and a chain of loads.
+// cosines for them; a warp's groups take the same heads of neighbouring tokens, so that its branches are uniform.  The bound is DRAM for many
+// tokens; for one it is the launch and a chain of loads.
 //
 // The angle in turns is position * turns[i] mod 2^64 in integers, exact but for the frequency's own rounding (2^-65 turns
 // a position).  Its upper 32 bits give the quarter turn and, signed, the rest r of at most an eighth of a turn, whose sine and cosine come
@@ -14,14 +14,14 @@
 
 namespace saem {
 
-constexpr int kRotThreads = 256;
+constexpr int kRotThreads = 128;
 constexpr int kRotMost = 8;                 // heads of a group at most
 constexpr int kRotAhead = 2;                // heads whose loads are under way
 
 struct HeadsIn {
     const uint8_t* p;
     long long ts, hs;                       // strides in bytes
-    int heads, slices;                      // groups of lanes that share a token's heads
+    int heads, slices;                      // groups of lanes that share a token's heads (of one kind)
 };
 struct RotArgs {
     int dim, rot, interleaved;
@@ -113,12 +113,13 @@ __device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int dtype, cons
 
 // The sequence that token t belongs to: the last one whose offset is at most t (offsets[0] = 0).  LANES probes a round.
 template <int LANES>
-__device__ __forceinline__ int sequence_of(const int32_t* offsets, int seqs, int t, int lane, uint32_t group_mask, int group_shift) {
+__device__ __forceinline__ int sequence_of(const int32_t* offsets, int seqs, int t, int lane, int sub) {
+    const uint32_t mask = (uint32_t)((1ull << LANES) - 1) << sub * LANES;       // groups may take different numbers of rounds
     int lo = 0, n = seqs;
     while (n > 1) {
         const int step = (n + LANES - 1) / LANES, at = lane * step;
         const bool below = at < n && offsets[lo + at] <= t;
-        const uint32_t votes = (__ballot_sync(group_mask, below) >> group_shift) & (uint32_t)((1ull << LANES) - 1);
+        const uint32_t votes = __ballot_sync(mask, below) & mask;
         const int last = max(0, __popc(votes) - 1) * step;
         lo += last;
         n = min(step, n - last);
@@ -148,17 +149,17 @@ __device__ __forceinline__ void turn2(uint64_t u0, uint64_t u1, float (&sn)[2], 
 }
 
 template <int DT, int LANES, int FORM, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads, 4)
+__global__ void __launch_bounds__(kRotThreads, 8)
 rotary_kernel(const __grid_constant__ RotArgs a) {
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x % LANES;
-    const int group_shift = (threadIdx.x & 31) / LANES * LANES;
-    const uint32_t group_mask = (uint32_t)((1ull << LANES) - 1) << group_shift;
-    const int group = blockIdx.x * (kRotThreads / LANES) + threadIdx.x / LANES;
-    const long long t = quotient(group, a.by_slices);
-    int slice = group - (int)t * a.by_slices.d, kind = 0;
-    if (t >= a.tokens) return;
+    constexpr int kTokens = 32 / LANES;     // of a warp
+    const int lane = threadIdx.x % LANES, sub = (threadIdx.x & 31) / LANES;
+    const int warp = blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5), many = quotient(warp, a.by_slices);
+    int slice = warp - many * (int)a.by_slices.d, kind = 0;
+    bool there = (long long)many * kTokens + sub < a.tokens;
+    if ((long long)many * kTokens >= a.tokens) return;
+    const long long t = there ? (long long)many * kTokens + sub : a.tokens - 1;     // groups without a token do what another does, but write nothing
     if (APPEND)
         while (slice >= a.x[kind].slices) slice -= a.x[kind++].slices;
     const HeadsIn& x = a.x[kind];
@@ -181,25 +182,24 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
     long long step;
     int out_elem = 2;
     if (APPEND) {
-        const int seqs = a.batch.seqs;
-        if (t >= a.batch.offsets[seqs]) return;
-        const int s = sequence_of<LANES>(a.batch.offsets, seqs, (int)t, lane, group_mask, group_shift);
+        const int seqs = a.batch.seqs, s = sequence_of<LANES>(a.batch.offsets, seqs, (int)t, lane, sub);
+        there = there && t < a.batch.offsets[seqs];
         const int place = a.batch.lengths[s] - (a.batch.offsets[s + 1] - (int)t);
         position = a.positions ? a.positions[t] : place;
         if (kind == 0) {
             to = a.out + t * a.out_ts + first * a.out_hs;
             step = a.out_hs;
         } else {
-            if (place < 0) return;
-            const int entry = quotient(place, a.by_page);
-            const int page = entry < a.batch.max_pages ? a.batch.table[s * a.batch.table_stride + entry] : -1;
+            const int entry = place >= 0 ? quotient(place, a.by_page) : 0;
+            int page = place >= 0 && entry < a.batch.max_pages ? a.batch.table[s * a.batch.table_stride + entry] : -1;
             if (page < 0 || page >= a.cache.pages) {
-                if (a.status && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
-                return;
+                if (there && place >= 0 && a.status && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
+                there = false;
+                page = 0;
             }
             step = (long long)a.cache.page_size * a.dim * 2;
             to = static_cast<uint8_t*>(kind == 1 ? a.cache.k : a.cache.v) +
-                 (((long long)page * a.cache.kv_heads + first) * a.cache.page_size + place - entry * a.cache.page_size) * a.dim * 2;
+                 (((long long)page * a.cache.kv_heads + first) * a.cache.page_size + (there ? place - entry * a.cache.page_size : 0)) * a.dim * 2;
         }
     } else {
         position = a.positions[t];
@@ -279,7 +279,7 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
                 for (int e = 1; e < 4; ++e) sq = fma_f32x2(v[e], v[e], sq);
                 float s = low_f32(sq) + high_f32(sq);
 #pragma unroll
-                for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(group_mask, s, o);
+                for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                 const float r = rsqrtf(fmaf(s, a.inv_dim, a.eps));
                 const uint64_t r2 = pack_f32x2(r, r);
 #pragma unroll
@@ -295,7 +295,7 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = mul_f32x2(v[e], k1[e]);
             }
-            if (here) store8<FORM>(to0, to1, a.out_dtype, v);
+            if (here && there) store8<FORM>(to0, to1, a.out_dtype, v);
             to0 += step;
             to1 += step;
         }
@@ -314,7 +314,7 @@ static cudaError_t launch_rotary_typed(RotArgs a, int n_sm, cudaStream_t st) {
         if (a.per_group == 1 || a.tokens * slices >= want) break;
     }
     a.by_slices = divisor_of((uint32_t)slices);
-    const long long per = kRotThreads / lanes, grid = (a.tokens * slices + per - 1) / per;
+    const long long tokens = 32 / lanes, warps = (a.tokens + tokens - 1) / tokens * slices, grid = (warps + kRotThreads / 32 - 1) / (kRotThreads / 32);
     if (lanes == 8) return launch_pdl(rotary_kernel<DT, 8, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
     return launch_pdl(rotary_kernel<DT, 16, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
 }

@@ -16,7 +16,10 @@ namespace saem {
 
 constexpr int kRotThreads = 128;
 constexpr int kRotMost = 8;                 // heads of a group at most
-constexpr int kRotAhead = 2;                // heads whose loads are under way
+// Heads whose loads are under way, and CTAs per SM, which bound the registers: 8192 tokens of 40 heads rotated 29.5 us with 3 and 6, 38.5 us
+// with 2 and 8, 31.5 us with 4 and 6; 8192 tokens of 32 + 8 + 8 heads appended 54.8, 40.7 and 43.7 us.
+constexpr int rot_ahead(bool append) { return append ? 2 : 3; }
+constexpr int rot_ctas(bool append) { return append ? 8 : 6; }
 
 struct HeadsIn {
     const uint8_t* p;
@@ -43,8 +46,8 @@ struct RotArgs {
     int32_t* status;
 };
 
-// How a lane's eight elements lie: two runs of four anywhere (RUNS), one of eight (WHOLE), or at addresses that are aligned to their
-// elements only (SINGLE).
+// How a lane's eight elements lie: two runs of four (RUNS, the half layout), one of eight (WHOLE, the interleaved one, or no rotation), or
+// either at addresses that are aligned to their elements only (SINGLE).
 enum { kRuns = 0, kWhole = 1, kSingle = 2 };
 constexpr int elem_of(int dtype) { return dtype == SAEM_OUT_F32 ? 4 : 2; }
 template <int DT, int FORM>
@@ -85,9 +88,11 @@ struct Eight {
         }
     }
 };
-template <int FORM>
-__device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int dtype, const uint64_t (&v)[4]) {
-    if (dtype == SAEM_OUT_F32) {
+constexpr int kAnyType = -1;                // the type is told at run time
+template <int FORM, int OT>
+__device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int any_dtype, const uint64_t (&v)[4]) {
+    const bool f32 = OT == kAnyType ? any_dtype == SAEM_OUT_F32 : OT == SAEM_OUT_F32, f16 = OT == kAnyType ? any_dtype == SAEM_OUT_F16 : OT == SAEM_OUT_F16;
+    if (f32) {
         if constexpr (FORM == kSingle) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) *reinterpret_cast<float*>(i < 4 ? p0 + i * 4 : p1 + (i - 4) * 4) = i & 1 ? high_f32(v[i / 2]) : low_f32(v[i / 2]);
@@ -95,19 +100,19 @@ __device__ __forceinline__ void store8(uint8_t* p0, uint8_t* p1, int dtype, cons
             *reinterpret_cast<float4*>(p0) = make_float4(low_f32(v[0]), high_f32(v[0]), low_f32(v[1]), high_f32(v[1]));
             *reinterpret_cast<float4*>(p1) = make_float4(low_f32(v[2]), high_f32(v[2]), low_f32(v[3]), high_f32(v[3]));
         }
-        return;
-    }
-    uint32_t w[4];
+    } else if constexpr (OT != SAEM_OUT_F32) {
+        uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = dtype == SAEM_OUT_F16 ? pack2<true>(low_f32(v[i]), high_f32(v[i])) : pack2<false>(low_f32(v[i]), high_f32(v[i]));
-    if constexpr (FORM == kSingle) {
+        for (int i = 0; i < 4; ++i) w[i] = f16 ? pack2<true>(low_f32(v[i]), high_f32(v[i])) : pack2<false>(low_f32(v[i]), high_f32(v[i]));
+        if constexpr (FORM == kSingle) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint16_t*>(i < 4 ? p0 + i * 2 : p1 + (i - 4) * 2) = (uint16_t)(w[i / 2] >> (i & 1) * 16);
-    } else if constexpr (FORM == kWhole) {
-        *reinterpret_cast<uint4*>(p0) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-        *reinterpret_cast<uint2*>(p0) = make_uint2(w[0], w[1]);
-        *reinterpret_cast<uint2*>(p1) = make_uint2(w[2], w[3]);
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint16_t*>(i < 4 ? p0 + i * 2 : p1 + (i - 4) * 2) = (uint16_t)(w[i / 2] >> (i & 1) * 16);
+        } else if constexpr (FORM == kWhole) {
+            *reinterpret_cast<uint4*>(p0) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            *reinterpret_cast<uint2*>(p0) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2*>(p1) = make_uint2(w[2], w[3]);
+        }
     }
 }
 
@@ -148,12 +153,13 @@ __device__ __forceinline__ void turn2(uint64_t u0, uint64_t u1, float (&sn)[2], 
     place(q1, high_f32(s), high_f32(c), sn[1], cs[1]);
 }
 
-template <int DT, int LANES, int FORM, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads, 8)
+template <int DT, int OT, int LANES, int FORM, bool APPEND>
+__global__ void __launch_bounds__(kRotThreads, rot_ctas(APPEND))
 rotary_kernel(const __grid_constant__ RotArgs a) {
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int kTokens = 32 / LANES;     // of a warp
+    constexpr int kAhead = rot_ahead(APPEND), kTokens = 32 / LANES;             // tokens of a warp
+    const bool interleaved = FORM == kSingle ? a.interleaved : FORM == kWhole;
     const int lane = threadIdx.x % LANES, sub = (threadIdx.x & 31) / LANES;
     const int warp = blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5), many = quotient(warp, a.by_slices);
     int slice = warp - many * (int)a.by_slices.d, kind = 0;
@@ -167,15 +173,15 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
     // where the lane's two runs of four lie in a head, and whether they turn
     const int half = a.rot / 2;
     const bool here = lane * 8 < a.dim, turn = lane * 8 < a.rot && kind < 2;
-    const bool across = lane * 8 < a.rot && !a.interleaved;
+    const bool across = lane * 8 < a.rot && !interleaved;
     const int at0 = across ? 4 * lane : 8 * lane, at1 = across ? half + 4 * lane : 8 * lane + 4;
     constexpr int E = elem_of(DT);
     const uint8_t* src = x.p + t * x.ts + first * x.hs;
-    Eight<DT, FORM> raw[kRotAhead];
+    Eight<DT, FORM> raw[kAhead];
 #pragma unroll
-    for (int i = 0; i < kRotAhead; ++i)     // on their way while the token's place is looked up
+    for (int i = 0; i < kAhead; ++i)     // on their way while the token's place is looked up
         if (here && i < count) raw[i].load(src + i * x.hs + at0 * E, src + i * x.hs + at1 * E);
-    src += kRotAhead * x.hs;
+    src += kAhead * x.hs;
 
     int position;
     uint8_t* to;
@@ -246,7 +252,7 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] *= a.amplitude;
-        if (a.interleaved) {
+        if (interleaved) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 k1[i] = pack_f32x2(w[2 * i] * cs[i], w[2 * i + 1] * cs[i]);
@@ -263,14 +269,14 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
         }
     }
     uint8_t *to0 = to + at0 * out_elem, *to1 = to + at1 * out_elem;
-    for (int h0 = 0; h0 < count; h0 += kRotAhead) {
+    for (int h0 = 0; h0 < count; h0 += kAhead) {
 #pragma unroll
-        for (int i = 0; i < kRotAhead; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
             if (h0 + i >= count) break;
             uint64_t v[4] = {};
             if (here) {
                 raw[i].widen(v);
-                if (h0 + i + kRotAhead < count) raw[i].load(src + at0 * E, src + at1 * E);
+                if (h0 + i + kAhead < count) raw[i].load(src + at0 * E, src + at1 * E);
             }
             src += x.hs;
             if (weight) {
@@ -288,21 +294,21 @@ rotary_kernel(const __grid_constant__ RotArgs a) {
             if (turn) {
                 uint64_t o[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = mul_f32x2(a.interleaved ? pack_f32x2(high_f32(v[e]), low_f32(v[e])) : v[e ^ 2], k2[e]);
+                for (int e = 0; e < 4; ++e) o[e] = mul_f32x2(interleaved ? pack_f32x2(high_f32(v[e]), low_f32(v[e])) : v[e ^ 2], k2[e]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = fma_f32x2(v[e], k1[e], o[e]);
             } else if (weight) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = mul_f32x2(v[e], k1[e]);
             }
-            if (here && there) store8<FORM>(to0, to1, a.out_dtype, v);
+            if (here && there) store8<FORM, OT>(to0, to1, a.out_dtype, v);
             to0 += step;
             to1 += step;
         }
     }
 }
 
-template <int DT, int FORM, bool APPEND>
+template <int DT, int OT, int FORM, bool APPEND>
 static cudaError_t launch_rotary_typed(RotArgs a, int n_sm, cudaStream_t st) {
     const int lanes = a.dim <= 64 ? 8 : 16, kinds = APPEND ? 3 : 1;
     // as many heads to a group as leave groups for the SMs' threads
@@ -315,13 +321,24 @@ static cudaError_t launch_rotary_typed(RotArgs a, int n_sm, cudaStream_t st) {
     }
     a.by_slices = divisor_of((uint32_t)slices);
     const long long tokens = 32 / lanes, warps = (a.tokens + tokens - 1) / tokens * slices, grid = (warps + kRotThreads / 32 - 1) / (kRotThreads / 32);
-    if (lanes == 8) return launch_pdl(rotary_kernel<DT, 8, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
-    return launch_pdl(rotary_kernel<DT, 16, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
+    if (lanes == 8) return launch_pdl(rotary_kernel<DT, OT, 8, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
+    return launch_pdl(rotary_kernel<DT, OT, 16, FORM, APPEND>, dim3((unsigned)grid), dim3(kRotThreads), 0, st, a);
+}
+template <int DT, int FORM, bool APPEND>
+static cudaError_t launch_rotary_out(const RotArgs& a, int n_sm, cudaStream_t st) {
+    if constexpr (FORM == kSingle) {
+        return launch_rotary_typed<DT, kAnyType, kSingle, APPEND>(a, n_sm, st);
+    } else {
+        if (a.out_dtype == SAEM_OUT_BF16) return launch_rotary_typed<DT, SAEM_OUT_BF16, FORM, APPEND>(a, n_sm, st);
+        if (APPEND || a.out_dtype == SAEM_OUT_F16) return launch_rotary_typed<DT, SAEM_OUT_F16, FORM, APPEND>(a, n_sm, st);
+        return launch_rotary_typed<DT, APPEND ? SAEM_OUT_F16 : SAEM_OUT_F32, FORM, APPEND>(a, n_sm, st);
+    }
 }
 template <int DT, bool APPEND>
 static cudaError_t launch_rotary_form(const RotArgs& a, int aligned, int n_sm, cudaStream_t st) {
-    if (aligned >= 8 && (a.interleaved || a.rot == 0)) return launch_rotary_typed<DT, kWhole, APPEND>(a, n_sm, st);
-    return aligned >= 4 ? launch_rotary_typed<DT, kRuns, APPEND>(a, n_sm, st) : launch_rotary_typed<DT, kSingle, APPEND>(a, n_sm, st);
+    const bool whole = a.interleaved || a.rot == 0;
+    if (aligned >= 8 && whole) return launch_rotary_out<DT, kWhole, APPEND>(a, n_sm, st);
+    return aligned >= 4 && !whole ? launch_rotary_out<DT, kRuns, APPEND>(a, n_sm, st) : launch_rotary_out<DT, kSingle, APPEND>(a, n_sm, st);
 }
 // aligned: the elements to which every head's address is a multiple (1, 4 or 8)
 template <bool APPEND>

@@ -57,9 +57,13 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsLeast, kRowsWarps>(a, plan);
     AttendWalk<kRowsR, kRowsKeys, kRowsHead, kRowsSnap> walk;
-    walk.begin(a, plan);
+    if (a.seqs <= kPlanWarpSeqs) {
+        walk.begin_alone<kRowsLeast>(a);
+    } else {
+        make_plan<kRowsR, kRowsKeys, kRowsHead, kRowsLeast, kRowsWarps>(a, plan);
+        walk.begin(a, plan);
+    }
     const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStage;
     float* const meet = reinterpret_cast<float*>(smem + Shape::kRing);          // [warp][kMeet]
     const int quad = lane >> 2, two = (lane & 3) * 2;
@@ -333,12 +337,13 @@ static size_t partials_bytes(int dim, int n_sm) {
 static bool rows_are_few(long long rows, long long all_rows) { return rows <= 16 || all_rows <= 768; }
 
 template <bool F16, int DK>
-static cudaError_t launch_rows_typed(const AttendArgs& a, int n_sm, cudaStream_t st) {
+static cudaError_t launch_rows_typed(AttendArgs a, int n_sm, cudaStream_t st) {
     static DeviceOnce once;
     const cudaError_t e = once_on_device(once, [] {
         return cudaFuncSetAttribute(attend_rows_kernel<F16, DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsShape<DK>::kSmem);
     });
     if (e != cudaSuccess) return e;
+    a.by_ctas = divisor_of((uint32_t)(kRowsPerSm * n_sm));
     return launch_pdl(attend_rows_kernel<F16, DK>, dim3(kRowsPerSm * n_sm), dim3(kRowsThreads), RowsShape<DK>::kSmem, st, a);
 }
 static cudaError_t launch_rows(const AttendArgs& a, bool f16, int n_sm, cudaStream_t st) {

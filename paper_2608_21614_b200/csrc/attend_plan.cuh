@@ -31,7 +31,7 @@ struct AttendArgs {
     const uint8_t* v;
     long long pages;
     int page_size, kv_heads, dim, group;
-    Divisor by_page, by_group;
+    Divisor by_page, by_group, by_ctas;     // by_ctas: the grid's
     const int32_t* offsets;
     const int32_t* lengths;
     const int32_t* table;
@@ -83,68 +83,75 @@ __device__ __forceinline__ int item_units(const AttendArgs& a, const SeqExtent& 
     return HEAD + max(1, t - b);
 }
 
+// x / d where the quotient is below 2^20: an estimate in fp32, off by one at most, and a look at the rest.
+__device__ __forceinline__ int small_quotient(long long x, long long d) {
+    int q = (int)__fdividef((float)x, (float)d);
+    const long long rest = x - q * d;
+    return rest < 0 ? q - 1 : rest >= d ? q + 1 : q;
+}
+// The units of a range, LEAST at least.
+template <int LEAST>
+__device__ __forceinline__ long long range_units(const AttendArgs& a, long long total) {
+    const long long per = total < 0x7FFF0000 ? (long long)quotient((int)total + a.by_ctas.d - 1, a.by_ctas) : (total + gridDim.x - 1) / gridDim.x;
+    return max(per, (long long)LEAST);
+}
+// Units of one key head of the sequence that the lane holds (all lanes of a warp; the row tiles of a sequence with more than one are shared
+// out over the warp).
+template <int R, int KEYS, int HEAD>
+__device__ __forceinline__ long long head_units(const AttendArgs& a, const SeqExtent& e, int lane) {
+    const int tiles = row_tiles<R>(a, e);
+    long long u = tiles == 1 ? item_units<R, KEYS, HEAD>(a, e, 0) : 0;
+    for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 1); many; many &= many - 1) {
+        const int src = __ffs(many) - 1;
+        const SeqExtent o = {0, __shfl_sync(0xffffffffu, e.n, src), __shfl_sync(0xffffffffu, e.len, src)};
+        const int t = __shfl_sync(0xffffffffu, tiles, src);
+        long long sum = 0;
+        for (int r = lane; r < t; r += 32) sum += item_units<R, KEYS, HEAD>(a, o, r);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == src) u = sum;
+    }
+    return u;
+}
+template <class T>
+__device__ __forceinline__ T inclusive_sum(T v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const T o = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+constexpr int kPlanWarpSeqs = 32;           // so many sequences are planned by each warp for itself (AttendWalk::begin_alone)
 struct AttendPlan {                         // in shared memory
     long long per;                          // units of a range
-    long long begin, seq_begin;             // first unit of this CTA's range, and of the sequence s that it lies in
+    long long begin, seq_begin, per_head;   // first unit of this CTA's range, that of the sequence s that it lies in, units of one of its heads
     int s;                                  // seqs: the CTA has no range
     long long scan[12];                     // a warp each
 };
 
-// All threads of the CTA (WARPS whole warps); a range has LEAST units at least.
+// For more sequences than that: all threads of the CTA (WARPS whole warps).
 template <int R, int KEYS, int HEAD, int LEAST, int WARPS>
 __device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p) {
     static_assert(WARPS <= 12, "");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kStep = WARPS * 32;
-    auto units_of = [&](int s) -> long long {
-        // a lane per sequence; the row tiles of a sequence with more than one are shared out over the warp
-        const SeqExtent e = s < a.seqs ? seq_extent(a, s) : SeqExtent{0, 0, 0};
-        const int tiles = row_tiles<R>(a, e);
-        long long u = tiles == 1 ? item_units<R, KEYS, HEAD>(a, e, 0) : 0;
-        for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 1); many; many &= many - 1) {
-            const int src = __ffs(many) - 1;
-            const SeqExtent o = {0, __shfl_sync(0xffffffffu, e.n, src), __shfl_sync(0xffffffffu, e.len, src)};
-            const int t = __shfl_sync(0xffffffffu, tiles, src);
-            long long sum = 0;
-            for (int r = lane; r < t; r += 32) sum += item_units<R, KEYS, HEAD>(a, o, r);
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if (lane == src) u = sum;
-        }
-        return u * a.kv_heads;
-    };
-    auto inclusive = [&](long long v) {
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long o = __shfl_up_sync(0xffffffffu, v, d);
-            if (lane >= d) v += o;
-        }
-        return v;
-    };
-    auto range_of = [&](long long total) { return max((total + gridDim.x - 1) / gridDim.x, (long long)LEAST); };
+    auto units_of = [&](int s) { return head_units<R, KEYS, HEAD>(a, s < a.seqs ? seq_extent(a, s) : SeqExtent{0, 0, 0}, lane) * a.kv_heads; };
     if (threadIdx.x == 0) p.s = a.seqs;
-    if (a.seqs <= 32) {                     // one warp's work
-        if (warp == 0) {
-            const long long mine = units_of(lane), incl = inclusive(mine), per = range_of(__shfl_sync(0xffffffffu, incl, 31)), begin = per * blockIdx.x;
-            __syncwarp();
-            if (incl - mine <= begin && begin < incl) { p.per = per; p.begin = begin; p.seq_begin = incl - mine; p.s = lane; }
-        }
-        __syncthreads();
-        return;
-    }
-    long long mine = units_of(warp * 32 + lane), incl = inclusive(mine), sum = __shfl_sync(0xffffffffu, incl, 31);
-    for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += __shfl_sync(0xffffffffu, inclusive(units_of(s + lane)), 31);
+    long long mine = units_of(warp * 32 + lane), incl = inclusive_sum(mine, lane), sum = __shfl_sync(0xffffffffu, incl, 31);
+    for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += __shfl_sync(0xffffffffu, inclusive_sum(units_of(s + lane), lane), 31);
     if (lane == 0) p.scan[warp] = sum;
     __syncthreads();
     long long total = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) total += p.scan[w];
-    const long long per = range_of(total), begin = per * blockIdx.x;
+    const long long per = range_units<LEAST>(a, total), begin = per * blockIdx.x;
     if (begin >= total) return;
     long long before = 0;
     for (int s0 = 0; before <= begin; s0 += kStep) {
         if (a.seqs > kStep) {               // the sums are not those of this step's sequences
-            if (s0) incl = inclusive(mine = units_of(s0 + warp * 32 + lane));
+            if (s0) incl = inclusive_sum(mine = units_of(s0 + warp * 32 + lane), lane);
             __syncthreads();
             if (lane == 31) p.scan[warp] = incl;
             __syncthreads();
@@ -155,7 +162,7 @@ __device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p) {
             if (w < warp) base += p.scan[w];
             before += p.scan[w];
         }
-        if (base + incl - mine <= begin && begin < base + incl) { p.per = per; p.begin = begin; p.seq_begin = base + incl - mine; p.s = s0 + warp * 32 + lane; }
+        if (base + incl - mine <= begin && begin < base + incl) { p.per = per; p.begin = begin; p.seq_begin = base + incl - mine; p.per_head = mine / a.kv_heads; p.s = s0 + warp * 32 + lane; }
     }
     __syncthreads();
 }
@@ -183,35 +190,41 @@ struct AttendWalk {
         s = p.s;
         if (s >= a.seqs) return;
         per = p.per;
-        snap = (int)min(per / 3, (long long)SNAP);
-        low = max(HEAD, snap);
-        const long long at = p.begin;
         e = seq_extent(a, s);
-        tiles = row_tiles<R>(a, e);
-        item = p.seq_begin;
-        r = 0;
-        if (tiles == 1) {
-            const int units = item_units<R, KEYS, HEAD>(a, e, 0);
-            h = (int)((at - item) / units);
-            item += (long long)h * units;
-            return;
-        }
-        // the item that holds the range's first unit: the head by division, the row tile by a warp's scan
+        find(a, p.begin, p.seq_begin, p.per_head);
+    }
+    // Up to kPlanWarpSeqs sequences, a lane each: the plan without shared memory or barriers (it is what a short call waits for first).
+    template <int LEAST>
+    __device__ __forceinline__ void begin_alone(const AttendArgs& a) {
         const int lane = threadIdx.x & 31;
-        long long per_head = 0;
-        for (int t = lane; t < tiles; t += 32) per_head += item_units<R, KEYS, HEAD>(a, e, t);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) per_head += __shfl_xor_sync(0xffffffffu, per_head, d);
-        h = (int)((at - item) / per_head);
-        item += h * per_head;
+        const SeqExtent mine = lane < a.seqs ? seq_extent(a, lane) : SeqExtent{0, 0, 0};
+        const long long per_head = head_units<R, KEYS, HEAD>(a, mine, lane), units = per_head * a.kv_heads;
+        // sums of 32 of them fit into 32 bits, but for uncommon calls
+        const long long incl = __any_sync(0xffffffffu, units >> 26) ? inclusive_sum(units, lane) : (long long)inclusive_sum((uint32_t)units, lane);
+        const long long total = __shfl_sync(0xffffffffu, incl, 31);
+        per = range_units<LEAST>(a, total);
+        const long long at = per * blockIdx.x;
+        const uint32_t past = __ballot_sync(0xffffffffu, incl > at);
+        s = a.seqs;
+        if (!past) return;
+        s = __ffs(past) - 1;
+        e.first = __shfl_sync(0xffffffffu, mine.first, s);
+        e.n = __shfl_sync(0xffffffffu, mine.n, s);
+        e.len = __shfl_sync(0xffffffffu, mine.len, s);
+        find(a, at, __shfl_sync(0xffffffffu, incl - units, s), __shfl_sync(0xffffffffu, per_head, s));
+    }
+    // The item of sequence s that holds unit `at`: the head by division, the row tile by a warp's scan.
+    __device__ __forceinline__ void find(const AttendArgs& a, long long at, long long seq_begin, long long per_head) {
+        snap = per < 3 * SNAP ? (int)per / 3 : SNAP;
+        low = max(HEAD, snap);
+        tiles = row_tiles<R>(a, e);
+        r = 0;
+        h = small_quotient(at - seq_begin, per_head);
+        item = seq_begin + h * per_head;
+        if (tiles == 1) return;
+        const int lane = threadIdx.x & 31;
         for (int t0 = 0; t0 < tiles; t0 += 32) {
-            const int u = t0 + lane < tiles ? item_units<R, KEYS, HEAD>(a, e, t0 + lane) : 0;
-            int incl = u;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += o;
-            }
+            const int u = t0 + lane < tiles ? item_units<R, KEYS, HEAD>(a, e, t0 + lane) : 0, incl = inclusive_sum(u, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, item + incl > at);
             if (past) {
                 const int l = __ffs(past) - 1;
@@ -230,7 +243,7 @@ struct AttendWalk {
             key_tiles<KEYS>(a, e, row0, row1, b, t);
             const int units = HEAD + max(1, t - b);
             // its parts begin with the item and at the cuts between item + low and item + units - snap
-            const int first = (int)((item + min(low, units - 1)) / per), last = units <= 2 * HEAD ? first : max(first, (int)((item + units - snap - 1) / per));
+            const int first = small_quotient(item + min(low, units - 1), per), last = units <= 2 * HEAD ? first : max(first, small_quotient(item + units - snap - 1, per));
             if (first > me) return false;
             const bool mine = me <= last;
             if (mine) {

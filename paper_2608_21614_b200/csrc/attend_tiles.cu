@@ -143,7 +143,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
     pdl_wait();
     pdl_launch_dependents();
-    make_plan<kAtR, kAtKeys, kAtHead, kAtHead + 1, kAtThreads / 32>(a, plan);
+    if (a.seqs > kPlanWarpSeqs) make_plan<kAtR, kAtKeys, kAtHead, kAtHead + 1, kAtThreads / 32>(a, plan);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -620,7 +620,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         } else if (warp == 2) {
             // ---------------------------------------------------------------- items
             AttendWalk<kAtR, kAtKeys, kAtHead, kAtSnap> walk;
-            walk.begin(a, plan);
+            if (a.seqs > kPlanWarpSeqs) walk.begin(a, plan);
+            else walk.begin_alone<kAtHead + 1>(a);
             for (bool more = true; more; ++turn) {
                 const int at = turn % kAtParts;
                 if (turn >= kAtParts && !mbar_wait_warp(smem_u32(&bar_done[at]), (turn / kAtParts - 1) & 1, abort_p, a.status)) break;
@@ -716,6 +717,7 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, bool f16, int n_sm, cudaStr
     if (e != cudaSuccess) return e;
     TilesArgs t = {a, 128, (int)(a.pages * a.kv_heads * a.page_size)};
     while (a.page_size % t.box) t.box /= 2;
+    t.a.by_ctas = divisor_of((uint32_t)n_sm);
     alignas(64) CUtensorMap map_k, map_v;
     if (!make_cache_map(&map_k, a.k, f16, a.dim, t.rows_total, t.box) || !make_cache_map(&map_v, a.v, f16, a.dim, t.rows_total, t.box)) return cudaErrorInvalidValue;
     const dim3 grid(n_sm), block(kAtThreads);

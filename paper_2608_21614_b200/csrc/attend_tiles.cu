@@ -296,20 +296,24 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             float* const slot = a.partials + (size_t)e.slot * Shape::kSlot;
             const uint32_t stage = base + (2 + kStages) * kTile + (warp - 4) * kAtStage;
             // 32 of the row's columns; two calls are 64, which leave in whole rows of 128 bytes: a thread's own stores would touch a row each
-            auto finish = [&](const float* v, int c, float inv) {
-                float any = 0.f;                                    // NaN if one of them is, or an infinity (which comes out the same again)
+            auto finish = [&](const uint32_t* v, int c, float inv) {
+                const uint64_t by = pack_f32x2(inv, inv);
+                uint64_t any = 0;                                   // NaN if one of them is, or where infinities meet (which comes out the same again)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t w[4];
+                    uint64_t sum = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float x = v[8 * e + 2 * i] * inv, y = v[8 * e + 2 * i + 1] * inv;
-                        if (c * 32 + e * 8 < a.dim) any = fmaf(y, 0.f, fmaf(x, 0.f, any));
-                        w[i] = pack2<F16>(x, y);
+                        const uint64_t x = mul_f32x2(pack_b32x2(v[8 * e + 2 * i], v[8 * e + 2 * i + 1]), by);
+                        sum = add_f32x2(sum, x);
+                        w[i] = pack2<F16>(low_f32(x), high_f32(x));
                     }
+                    if (c * 32 + e * 8 < a.dim) any = add_f32x2(any, sum);
                     st_shared_v4(stage + lane * 128 + ((((c & 1) * 4 + e) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
                 }
-                if (any != any && in) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
+                const float all = low_f32(any) + high_f32(any);
+                if (all != all && in) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
                 if (c & 1) {
                     __syncwarp();
                     const int col = (c >> 1) * 64 + (lane & 7) * 8;
@@ -337,23 +341,26 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 #pragma unroll 1
                 for (int c = 0; c < DK / 32; ++c) {
                     uint32_t o[32];
-                    float v[32];
                     if (n > 0) tc_ld32_now(t_o + c * 32, o);
+                    else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = n > 0 ? __uint_as_float(o[i]) * w_own : 0.f;
+                        for (int i = 0; i < 32; ++i) o[i] = 0;
+                    }
                     if (add) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const float4 x = *reinterpret_cast<const float4*>(meet + ((c * 8 + i) * 128 + own) * 4);
-                            v[4 * i] = fmaf(x.x, w_other, v[4 * i]); v[4 * i + 1] = fmaf(x.y, w_other, v[4 * i + 1]);
-                            v[4 * i + 2] = fmaf(x.z, w_other, v[4 * i + 2]); v[4 * i + 3] = fmaf(x.w, w_other, v[4 * i + 3]);
+                            o[4 * i] = __float_as_uint(fmaf(x.x, w_other, __uint_as_float(o[4 * i]) * w_own));
+                            o[4 * i + 1] = __float_as_uint(fmaf(x.y, w_other, __uint_as_float(o[4 * i + 1]) * w_own));
+                            o[4 * i + 2] = __float_as_uint(fmaf(x.z, w_other, __uint_as_float(o[4 * i + 2]) * w_own));
+                            o[4 * i + 3] = __float_as_uint(fmaf(x.w, w_other, __uint_as_float(o[4 * i + 3]) * w_own));
                         }
                     }
-                    if (e.whole) finish(v, c, inv);
+                    if (e.whole) finish(o, c, inv);
                     else if (in) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            __stcg(reinterpret_cast<float4*>(slot + 2 * kAtR + ((c * 8 + i) * kAtR + tile_row) * 4), make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+                            __stcg(reinterpret_cast<uint4*>(slot + 2 * kAtR + ((c * 8 + i) * kAtR + tile_row) * 4), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
                     }
                 }
                 if (writes) {
@@ -447,7 +454,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                                     v[4 * i + 2] = fmaf(x[i].z, w, v[4 * i + 2]); v[4 * i + 3] = fmaf(x[i].w, w, v[4 * i + 3]);
                                 }
                             }
-                            finish(v, c, inv);
+                            finish(reinterpret_cast<const uint32_t*>(v), c, inv);
                         }
                         if (in) finish_lse(mx, sum);
                     }

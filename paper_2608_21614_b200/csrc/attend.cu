@@ -2,8 +2,8 @@
 //
 // attend_rows_kernel: tiles of 16 rows (a decoding sequence's query heads that share a key head; further tokens are further rows) by
 // mma.sync m16n8k16.  With so few rows every key and value is used for little arithmetic and the bound is the cache's bytes, so that what
-// counts is how many of them are under way: each of a CTA's 8 warps takes every eighth chunk of 16 places through a ring of
-// its own in shared memory (cp.async, no barrier between warps), with its own running maximum, sum and output; they meet at
+// counts is how many of them are under way: each of a CTA's 4 warps (two CTAs per SM) takes every fourth chunk of 16 places through a
+// ring of its own in shared memory (cp.async, no barrier between warps), with its own running maximum, sum and output; they meet at
 // the end of an item.  tcgen05 takes 128 rows at least, of which a decoding sequence fills 4 or 8, and its results would have to
 // cross tensor memory twice for each tile.
 #include "attend_plan.cuh"
@@ -395,7 +395,7 @@ extern "C" int saem_attend(const saem_attend_config* c, const saem_kv_cache* cac
     a.by_page = divisor_of(cache->page_size); a.by_group = divisor_of(a.group);
     a.offsets = b->offsets; a.lengths = b->lengths; a.table = b->table; a.table_stride = b->table_stride;
     a.seqs = b->seqs; a.tokens = b->tokens; a.max_pages = b->max_pages;
-    a.causal = c->causal != 0; a.window = c->window; a.scale = c->scale; a.scale_log2 = c->scale * 1.4426950408889634f;
+    a.causal = c->causal != 0; a.window = c->window; a.scale_log2 = c->scale * 1.4426950408889634f;
     a.status = reinterpret_cast<int*>(ws);
     a.counters = reinterpret_cast<int*>(ws + kAttendCounters);
     a.partials = reinterpret_cast<float*>(ws + SAEM_ATTEND_HEAD_BYTES);

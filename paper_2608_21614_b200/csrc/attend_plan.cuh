@@ -4,9 +4,10 @@
 // tiles of KEYS places that any of its rows may see, one at least, so that rows that see nothing are written too, behind HEAD units
 // for what an item costs by itself (queries, first bytes, the result).  All units of a call, in the order sequence, key head, row
 // tile, are cut into as many equal ranges as there are CTAs: long and short sequences, few and many rows load the SMs alike.  A cut
-// within an item's first HEAD units moves to its beginning, and one within SNAP units (or a third of a range, if that is less) of either end of an
-// item moves there, because a cut costs about as much; an item of up to 2 HEAD units is not cut at all.  An item that is still cut leaves sums of its parts in the workspace, and the CTA
-// that arrives last adds them up in the order of the parts, so that two runs give the same bits.
+// within an item's first HEAD units moves to its beginning, and one within SNAP units (or a third of a range, if that is less) of either
+// end of an item moves there, because a cut costs about as much; an item of up to 2 HEAD units is not cut at all.  An item that is still
+// cut leaves sums of its parts in the workspace, and the CTA that arrives last adds them up in the order of the parts, so that two runs
+// give the same bits.
 #ifndef SAEM_ATTEND_PLAN_CUH_
 #define SAEM_ATTEND_PLAN_CUH_
 
@@ -38,7 +39,7 @@ struct AttendArgs {
     long long table_stride;
     int seqs, tokens, max_pages;
     int causal, window;
-    float scale, scale_log2;                // scale * log2(e)
+    float scale_log2;                       // scale * log2(e)
     int* status;
     int* counters;                          // [kAttendMaxCtas], zero between calls
     float* partials;                        // two slots per CTA
@@ -224,7 +225,8 @@ struct AttendWalk {
         if (tiles == 1) return;
         const int lane = threadIdx.x & 31;
         for (int t0 = 0; t0 < tiles; t0 += 32) {
-            const int u = t0 + lane < tiles ? item_units<R, KEYS, HEAD>(a, e, t0 + lane) : 0, incl = inclusive_sum(u, lane);
+            // 32 tiles of 16 rows over 2^31 - 2^16 places have fewer than 2^32 units
+            const uint32_t u = t0 + lane < tiles ? item_units<R, KEYS, HEAD>(a, e, t0 + lane) : 0, incl = inclusive_sum(u, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, item + incl > at);
             if (past) {
                 const int l = __ffs(past) - 1;

@@ -1,10 +1,11 @@
 // Attention of many rows per key head over a paged cache, on tcgen05: tiles of 2 x 128 rows against tiles of 128 places.
 //
-// One persistent CTA per SM: a warp that walks through the CTA's range of the plan and hands its items on, a warp that copies key and value tiles (TMA, a box per page or part of one) into a ring, a warp that
-// issues the products, and two groups of four warps, a thread per row, that turn scores into weights.  Scores S = Q K^T come to
-// tensor memory, a thread reads its row, and writes the weights back over it as the 16-bit A operand of O += P V; O stays in
-// tensor memory.  While one group works on its scores the tensor cores work for the other.  Values are used as they lie in the
-// cache (places along the rows, the MN-major form of B), so nothing is transposed.
+// One persistent CTA per SM: a warp that walks through the CTA's range of the plan and hands its items on, a warp that copies key and
+// value tiles (TMA, a box per page or part of one) into a ring, one that copies queries, one that issues the products, and two groups of
+// four warps, a thread per row, that turn scores into weights.  Scores S = Q K^T come to tensor memory, a thread reads its row, and writes
+// the weights back over it as the 16-bit A operand of O += P V; O stays in tensor memory.  While one group works on its scores the
+// tensor cores work for the other.  Values are used as they lie in the cache (places along the rows, the MN-major form of B), so
+// nothing is transposed.
 //
 // The maximum that a row's weights refer to is only moved, and O multiplied, where it has grown by more than 2^8: the result is the same but
 // for rounding, 16-bit floats have the range, and it is rare after a row's first tiles.

@@ -287,6 +287,32 @@ def test_more_places_than_32_bits_of_bytes():
         check(out, None, q, cache, batch, [(1, 300), (32, 140)], [0, 1, 33], True, 0, dim ** -0.5)
 
 
+@pytest.mark.parametrize("tokens, max_new", [(528, 1), (800, 1000)])
+def test_the_most_places(tokens, max_new):
+    """2^31 - 2^16 places, of which every row's units alone nearly fill 32 bits with its neighbours': one page over and over, whose weights
+    vanish beside those of another, which comes twice.  A chain of fp32 sums has at most 2^12 terms that count."""
+    from paper_2608_21614_b200 import attention
+    page, dim, entries = 65536, 8, 32767
+    cache = attention.PagedCache.empty(2, 1, page, dim)
+    for c in (cache.k, cache.v):
+        c.copy_(torch.randn(c.shape, generator=gen(6), device="cuda"))
+    cache.k[0] = -64.0                                              # scores below -180, and weights below 2^-200
+    q = (torch.rand(tokens, 1, dim, generator=gen(7), device="cuda") + 1).bfloat16()
+    table = torch.zeros(1, entries, dtype=torch.int32, device="cuda")
+    table[0, [5000, 20000]] = 1
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    att = attention.Attention(1, cache)
+    lse = torch.empty(tokens, 1, device="cuda")
+    out = att.attend(q, attention.Batch(i32(0, tokens), i32(entries * page), table, max_new), lse=lse)
+    assert att.device_status() == 0
+    want, size, want_lse, spread = ref.attend(q, cache.k[1], cache.v[1], tokens, False, 0, dim ** -0.5)
+    delta = spread * ((dim + 8) * 2.0 ** -24 + 2.0 ** -22)
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2 * delta[..., None] + 2.0 ** -11) * size
+    assert float(((out.double() - want).abs() - bound).max()) <= 0
+    want_lse += math.log(2)
+    assert float(((lse.double() - want_lse).abs() - (2 * delta + 2.0 ** -11 + 2.0 ** -22 * want_lse.abs())).max()) <= 0
+
+
 @pytest.mark.parametrize("max_new", [1, 1000])
 def test_captured_and_replayed_while_lengths_grow(max_new):
     from paper_2608_21614_b200 import attention

@@ -98,6 +98,9 @@ __device__ __forceinline__ uint32_t idesc_attend(int n, bool b_mn) {
     return (1u << 4) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
+// The limit of a wait that lasts as long as an item: a tile of places takes at most 2 us.
+__device__ __forceinline__ unsigned long long item_limit_ns(const AttendPart& p) { return kWaitLimitNs + 20000ull * (unsigned)max(0, p.key_end - p.key_begin); }
+
 template <bool F16, int DK>
 __global__ void __launch_bounds__(kAtThreads, 1)
 attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TilesArgs args) {
@@ -151,8 +154,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const uint32_t tmem = warp_uniform(tmem_s);
     bool ok = true;
     int turn = 0;                                                   // items so far
-    auto next = [&]() -> bool {                                     // false at the end, or when a wait has run out
-        ok = ok && mbar_wait_warp(smem_u32(&bar_part[turn % kAtParts]), (turn / kAtParts) & 1, abort_p, a.status);
+    auto next = [&](unsigned long long limit = kWaitLimitNs) -> bool {                                     // false at the end, or when a wait has run out
+        ok = ok && mbar_wait_warp(smem_u32(&bar_part[turn % kAtParts]), (turn / kAtParts) & 1, abort_p, a.status, limit);
         return ok && (int)warp_uniform(parts[turn % kAtParts].rows) > 0;
     };
     auto finished = [&] {
@@ -632,7 +635,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             else walk.begin_alone<kAtHead + 1>(a);
             for (bool more = true; more; ++turn) {
                 const int at = turn % kAtParts;
-                if (turn >= kAtParts && !mbar_wait_warp(smem_u32(&bar_done[at]), (turn / kAtParts - 1) & 1, abort_p, a.status)) break;
+                if (turn >= kAtParts && !mbar_wait_warp(smem_u32(&bar_done[at]), (turn / kAtParts - 1) & 1, abort_p, a.status, item_limit_ns(parts[at]))) break;
                 AttendPart p;
                 more = walk.next(a, p);
                 if (!more) p.rows = 0;
@@ -645,12 +648,13 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         } else {
             // ---------------------------------------------------------------- queries, in the 128-byte swizzle
             int n_q[2] = {0, 0};
-            for (; next(); finished()) {
+            unsigned long long limit = kWaitLimitNs;                    // of the longest item so far: it may be under way still
+            for (; next(limit); finished()) {
                 const AttendPart p = parts[turn % kAtParts];
                 const bool both = p.rows <= 128;
                 for (int g = 0; g < 2; ++g) {
                     if (p.key_end - p.key_begin <= (both ? g : 0)) continue;                     // the group has no tiles
-                    if (n_q[g]) ok = ok && mbar_wait_warp(smem_u32(&bar_free[g]), (n_q[g] - 1) & 1, abort_p, a.status);
+                    if (n_q[g]) ok = ok && mbar_wait_warp(smem_u32(&bar_free[g]), (n_q[g] - 1) & 1, abort_p, a.status, limit);
                     if (!ok) break;
                     ++n_q[g];
                     // eight rows at a time, four lanes to a row; rows beyond the item's are left as they are, nobody reads what comes of them
@@ -673,6 +677,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&bar_q[g]));
                 }
+                limit = max(limit, item_limit_ns(p));
             }
         }
     }

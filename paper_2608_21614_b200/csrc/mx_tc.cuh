@@ -17,8 +17,9 @@ __device__ __forceinline__ uint64_t smem_desc_scales(uint32_t addr) {
 // compiler must take for different in every lane, each operand has to be moved to a uniform register first, and an MMA or
 // a copy took 80 to 120 cycles to issue (an MMA of 128 x 48 x 64 takes 44, a scale copy 8).
 __device__ __forceinline__ uint32_t warp_uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status,
+                                               unsigned long long limit_ns = kWaitLimitNs) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, limit_ns));
 }
 // At the end of the warps that issue copies and MMAs: whatever is under way lands before the CTA gives its shared and tensor
 // memory back, also where another warp has given up meanwhile.  Bounded as every wait; without an abort the barriers have

@@ -48,6 +48,8 @@ class MxAttention:
         self.heads, self.d, self.max_tokens = (q_heads, kv_heads, dim), w_out.shape[0], max_tokens
         if w_qkv.shape != ((q_heads + 2 * kv_heads) * dim, self.d) or w_out.shape != (self.d, q_heads * dim):
             raise B.SaemError(B.SAEM_ERR_SHAPE, "MxAttention: projections")
+        if cache.k.dtype != torch.bfloat16:                                         # the projection behind it takes no other 16-bit type
+            raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "MxAttention: a cache in bfloat16 is wanted")
         if share is not None and (share.heads, share.d, share.max_tokens) != (self.heads, self.d, max_tokens):
             raise B.SaemError(B.SAEM_ERR_SHAPE, "MxAttention: buffers of another layer shape")
         self.qkv, self.out = mx.Linear(mx.quantize(w_qkv), max_tokens), mx.Linear(mx.quantize(w_out), max_tokens)

@@ -143,7 +143,7 @@ def test_stack_with_attention_as_a_graph_while_lengths_grow():
 
 def test_layers_share_workspaces_and_refuse_other_shapes():
     from paper_2608_21614_b200 import attention, binding as B
-    from paper_2608_21614_b200.mx_block import MxMoEStack
+    from paper_2608_21614_b200.mx_block import MxAttention, MxMoEStack
     s = stack(3, 4, 4, 16)
     a = s.attention
     assert a[0].attention.workspace.data_ptr() == a[2].attention.workspace.data_ptr() and a[0].rotated.data_ptr() == a[1].rotated.data_ptr()
@@ -157,6 +157,10 @@ def test_layers_share_workspaces_and_refuse_other_shapes():
         kw.update(bad)
         with pytest.raises(B.SaemError):
             layer(w, share=a[0], **kw)
+    half = attention.PagedCache.empty(2, 2, 16, 64, dtype=torch.float16)
+    with pytest.raises(B.SaemError) as e:
+        MxAttention(w["w_qkv"], w["w_out"], w["post"], w["pre"], half, 8, 4)
+    assert e.value.code == B.SAEM_ERR_INVALID_ARG
     wide = attention.PagedCache.empty(2, 2, 16, 128)
     narrow = attention.Attention(8, attention.PagedCache.empty(2, 2, 16, 64))
     with pytest.raises(B.SaemError) as e:

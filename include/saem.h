@@ -438,8 +438,8 @@ int saem_block_norm(const saem_norm_config* cfg, const void* x, const void* y, c
  * q_heads is a multiple of kv_heads; q_heads / kv_heads (at most 128) neighbouring query heads share a key head.  A row that
  * sees nothing is 0 (lse -inf).  lse (dev fp32 [tokens, q_heads], may be NULL): log sum_j exp(scale * q . k_j).  What lies
  * in places that a row does not see has no effect on it, whatever it is (a result that comes out NaN is summed again from
- * what its row sees alone); of a page outside [0, pages) the places count as zeros, and the status word becomes
- * SAEM_ERR_INVALID_ARG.  q and out: 16-byte aligned, strides multiples of 8 elements, apart from each other and the cache.
+ * what its row sees alone); of a page outside [0, pages) the places count as zeros, places beyond the table are not seen, and
+ * either sets the status word to SAEM_ERR_INVALID_ARG where a token needs them.  q and out: 16-byte aligned, strides multiples of 8 elements, apart from each other and the cache.
  * workspace (dev, 1024-byte aligned, saem_attend_workspace_bytes): its first 4 bytes are the status word; zero its first
  * SAEM_ATTEND_HEAD_BYTES once (again after SAEM_ERR_TIMEOUT).  Calls that share it must be ordered.  Two runs give the same
  * bits.

@@ -106,6 +106,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     };
     auto begin_part = [&]() -> bool {
         if (!walk.next(a, p)) return false;
+        bad |= p.e.cut();
         n_chunk = max(0, (p.key_end - p.key_begin - warp + kRowsWarps - 1) / kRowsWarps);
         table = a.table + p.s * a.table_stride;
         look_up(lane);

@@ -58,19 +58,20 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 struct SeqExtent {
-    int first, n, len;                      // first row of the call's tokens, new tokens, places
+    int first, n;                           // first row of the call's tokens, new tokens
+    int len, before;                        // places that can be read, which the table cuts; place of the first new token (may be negative), which it does not
+    __device__ __forceinline__ bool cut() const { return before + n > len; }                // a token's own place is not in the table
 };
 __device__ __forceinline__ SeqExtent seq_extent(const AttendArgs& a, int s) {
-    const int lo = min(max(a.offsets[s], 0), a.tokens), hi = min(max(a.offsets[s + 1], lo), a.tokens);
+    const int end = a.offsets[s + 1], lo = min(max(a.offsets[s], 0), a.tokens), hi = min(max(end, lo), a.tokens), length = max(a.lengths[s], 0);
     const long long most = min((long long)a.max_pages * a.page_size, 0x7FFF0000ll);      // sums of places stay within 32 bits
-    return {lo, hi - lo, (int)min((long long)max(a.lengths[s], 0), most)};
+    return {lo, hi - lo, (int)min((long long)length, most), hi > lo ? length - (end - lo) : 0};
 }
 // The places that rows [row0, row1] may see, in tiles of KEYS.
 template <int KEYS>
 __device__ __forceinline__ void key_tiles(const AttendArgs& a, const SeqExtent& e, int row0, int row1, int& begin, int& end) {
-    const int before = e.len - e.n;         // may be negative
-    const int stop = a.causal ? before + quotient(row1, a.by_group) + 1 : e.len;
-    const int first = before + quotient(row0, a.by_group) + 1, start = a.window && first > a.window ? first - a.window : 0;
+    const int stop = a.causal ? min(e.before + quotient(row1, a.by_group) + 1, e.len) : e.len;
+    const int first = e.before + quotient(row0, a.by_group) + 1, start = a.window && first > a.window ? first - a.window : 0;
     begin = start / KEYS;
     end = stop > start ? (stop - 1) / KEYS + 1 : begin;
 }
@@ -104,7 +105,7 @@ __device__ __forceinline__ long long head_units(const AttendArgs& a, const SeqEx
     long long u = tiles == 1 ? item_units<R, KEYS, HEAD>(a, e, 0) : 0;
     for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 1); many; many &= many - 1) {
         const int src = __ffs(many) - 1;
-        const SeqExtent o = {0, __shfl_sync(0xffffffffu, e.n, src), __shfl_sync(0xffffffffu, e.len, src)};
+        const SeqExtent o = {0, __shfl_sync(0xffffffffu, e.n, src), __shfl_sync(0xffffffffu, e.len, src), __shfl_sync(0xffffffffu, e.before, src)};
         const int t = __shfl_sync(0xffffffffu, tiles, src);
         long long sum = 0;
         for (int r = lane; r < t; r += 32) sum += item_units<R, KEYS, HEAD>(a, o, r);
@@ -138,7 +139,7 @@ __device__ __forceinline__ void make_plan(const AttendArgs& a, AttendPlan& p) {
     static_assert(WARPS <= 12, "");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kStep = WARPS * 32;
-    auto units_of = [&](int s) { return head_units<R, KEYS, HEAD>(a, s < a.seqs ? seq_extent(a, s) : SeqExtent{0, 0, 0}, lane) * a.kv_heads; };
+    auto units_of = [&](int s) { return head_units<R, KEYS, HEAD>(a, s < a.seqs ? seq_extent(a, s) : SeqExtent{}, lane) * a.kv_heads; };
     if (threadIdx.x == 0) p.s = a.seqs;
     long long mine = units_of(warp * 32 + lane), incl = inclusive_sum(mine, lane), sum = __shfl_sync(0xffffffffu, incl, 31);
     for (int s = kStep + warp * 32; s < a.seqs; s += kStep) sum += __shfl_sync(0xffffffffu, inclusive_sum(units_of(s + lane), lane), 31);
@@ -198,7 +199,7 @@ struct AttendWalk {
     template <int LEAST>
     __device__ __forceinline__ void begin_alone(const AttendArgs& a) {
         const int lane = threadIdx.x & 31;
-        const SeqExtent mine = lane < a.seqs ? seq_extent(a, lane) : SeqExtent{0, 0, 0};
+        const SeqExtent mine = lane < a.seqs ? seq_extent(a, lane) : SeqExtent{};
         const long long per_head = head_units<R, KEYS, HEAD>(a, mine, lane), units = per_head * a.kv_heads;
         // sums of 32 of them fit into 32 bits, but for uncommon calls
         const long long incl = __any_sync(0xffffffffu, units >> 26) ? inclusive_sum(units, lane) : (long long)inclusive_sum((uint32_t)units, lane);
@@ -212,6 +213,7 @@ struct AttendWalk {
         e.first = __shfl_sync(0xffffffffu, mine.first, s);
         e.n = __shfl_sync(0xffffffffu, mine.n, s);
         e.len = __shfl_sync(0xffffffffu, mine.len, s);
+        e.before = __shfl_sync(0xffffffffu, mine.before, s);
         find(a, at, __shfl_sync(0xffffffffu, incl - units, s), __shfl_sync(0xffffffffu, per_head, s));
     }
     // The item of sequence s that holds unit `at`: the head by division, the row tile by a warp's scan.
@@ -277,8 +279,8 @@ struct AttendWalk {
 
 // The rows' bounds: row (of the item) sees places lo .. hi.
 __device__ __forceinline__ void row_bounds(const AttendArgs& a, const SeqExtent& e, int row, bool in, int& lo, int& hi) {
-    const int place = e.len - e.n + quotient(row, a.by_group);
-    hi = !in ? -1 : a.causal ? place : e.len - 1;
+    const int place = e.before + quotient(row, a.by_group);
+    hi = !in ? -1 : a.causal ? min(place, e.len - 1) : e.len - 1;
     lo = a.window && place + 1 > a.window ? place + 1 - a.window : 0;
 }
 

@@ -191,7 +191,6 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             if (!both) free_queries();
             int lo = 0, hi = INT_MAX;                               // rows that are none see everything: nobody reads them
             if (in) row_bounds(a, p.e, row0 + own, true, lo, hi);
-            hi = min(hi, in ? p.e.len - 1 : INT_MAX);
             const int lo_most = __reduce_max_sync(0xffffffffu, lo), hi_least = __reduce_min_sync(0xffffffffu, hi);
             float m = -INFINITY, l = 0.f;                           // m: what the weights refer to, in scores
             for (int i = 0; i < n; ++i) {
@@ -639,6 +638,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 AttendPart p;
                 more = walk.next(a, p);
                 if (!more) p.rows = 0;
+                else if (p.e.cut() && lane == 0) atomicExch(a.status, SAEM_ERR_INVALID_ARG);
                 if (lane == 0) {
                     parts[at] = p;
                     mbar_arrive(smem_u32(&bar_part[at]));

@@ -53,7 +53,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ AttendPlan plan;
     __shared__ int last_s;
-    __shared__ uint32_t nan_s;
+    __shared__ int nan_s;                   // a row of the item has a NaN
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -226,7 +226,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             const long long token = ext.first + i;
             const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
             v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-            if (v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w) atomicOr(&nan_s, 1u << row);
+            if (v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w) nan_s = 1;
             if (col < a.dim) *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + col) * 2) = make_uint2(pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w));
             if (a.lse && col == 0) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
         };
@@ -313,11 +313,9 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                 __syncthreads();
             }
         }
-        // rows with a NaN once more; the barriers above order this after their first results, and the next one before more are noted
+        // the barriers above order this after the first results, and its own the next item's after it
         if (nan_s) {
-            for (int row = warp; row < rows; row += kRowsWarps)
-                if (nan_s >> row & 1) attend_row_again<F16>(a, ext, s_now, h_now, row0 + row);
-            __syncthreads();
+            attend_again<F16, kRowsKeys, kRowsWarps, 0>(a, ext, s_now, h_now, row0, rows, reinterpret_cast<int*>(meet), warp);
             if (threadIdx.x == 0) nan_s = 0;
             __syncthreads();
         }

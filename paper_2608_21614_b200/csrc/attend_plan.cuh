@@ -11,6 +11,8 @@
 #ifndef SAEM_ATTEND_PLAN_CUH_
 #define SAEM_ATTEND_PLAN_CUH_
 
+#include <limits.h>
+
 #include "attend_common.cuh"
 
 namespace saem {
@@ -284,10 +286,28 @@ __device__ __forceinline__ void row_bounds(const AttendArgs& a, const SeqExtent&
     lo = a.window && place + 1 > a.window ? place + 1 - a.window : 0;
 }
 
-// One row over again, by one warp, out of the cache and the places that it sees alone: for rows whose result is NaN.  In a product of
-// tiles a weight of 0 meets what other rows see, and 0 times an infinity or NaN there is NaN.
+// Rows with a NaN, once more.  In a product of tiles a weight of 0 meets what other rows see, and 0 times an infinity or NaN there is NaN; so it
+// is with float16 weights where a row sees an infinity itself and its weight rounds to 0.  The first comes of the few places of an item's tiles that
+// some of its rows do not see, the second of any; a NaN that a row sees is one of its result and needs no second sum.  One token over 131072
+// places, one with a NaN: 99 us as without (bfloat16), 1.9 ms (float16, where all values are looked at); a row that is summed again takes 1.5 us for 16 places.
+constexpr int kAgain = 16;                  // places at a time: of one page, as they are multiples of 16
+constexpr int kAgainMarks = 4 * kHeadDimMax;
+__device__ __forceinline__ int again_page(const AttendArgs& a, int s, int j0) { return a.table[s * a.table_stride + quotient(j0, a.by_page)]; }
+// The lane's four columns of kAgain places from j0 on (zeros of a page outside the cache): all of a page may be read, whatever it holds.
+__device__ __forceinline__ void again_load(const AttendArgs& a, const uint8_t* cache, int page, int h, int j0, int at, uint2 (&w)[kAgain]) {
+#pragma unroll
+    for (int i = 0; i < kAgain; ++i) w[i] = make_uint2(0, 0);
+    if (at < a.dim && page >= 0 && page < a.pages) {
+        const uint8_t* p = cache + ((((long long)page * a.kv_heads + h) * a.page_size + j0 - quotient(j0, a.by_page) * a.page_size) * a.dim + at) * 2;
+#pragma unroll
+        for (int i = 0; i < kAgain; ++i) w[i] = *reinterpret_cast<const uint2*>(p + i * a.dim * 2);
+    }
+}
+
+// One row, by one warp, out of the cache and the places that it sees alone; of its results those are written whose bit is set in `need` (of the
+// lane's four columns).
 template <bool F16>
-__device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExtent& e, int s, int h, int row) {
+__device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExtent& e, int s, int h, int row, uint32_t need) {
     const int lane = threadIdx.x & 31, at = lane * 4;
     const bool here = at < a.dim;
     int lo, hi;
@@ -295,61 +315,137 @@ __device__ __noinline__ void attend_row_again(const AttendArgs& a, const SeqExte
     const long long token = e.first + row / a.group;
     const int head = h * a.group + row % a.group;
     float q[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-    auto four = [&](const uint8_t* p, long long i, float* v) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p + i * 2);
+    auto four = [&](uint2 w, float* v) {
         const float2 x = unpack2<F16>(w.x), y = unpack2<F16>(w.y);
         v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
     };
-    if (here) four(a.q, token * a.q_ts + head * a.q_hs + at, q);
-    constexpr int kAhead = 4;               // places at a time
-    for (int j0 = lo; j0 <= hi; j0 += kAhead) {
-        float k[kAhead][4] = {}, v[kAhead][4] = {}, d[kAhead];
+    if (here) four(*reinterpret_cast<const uint2*>(a.q + (token * a.q_ts + head * a.q_hs + at) * 2), q);
+    int j0 = lo & ~(kAgain - 1), page = j0 <= hi ? again_page(a, s, j0) : -1;
+    for (; j0 <= hi; j0 += kAgain) {
+        uint2 kw[kAgain], vw[kAgain];
+        float d[kAgain];
+        again_load(a, a.k, page, h, j0, at, kw);
+        again_load(a, a.v, page, h, j0, at, vw);
+        if (j0 + kAgain <= hi) page = again_page(a, s, j0 + kAgain);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int j = min(j0 + i, hi), entry = quotient(j, a.by_page), page = a.table[s * a.table_stride + entry];
-            if (here && page >= 0 && page < a.pages) {
-                const long long from = (((long long)page * a.kv_heads + h) * a.page_size + j - entry * a.page_size) * a.dim + at;
-                four(a.k, from, k[i]);
-                four(a.v, from, v[i]);
+        for (int i = 0; i < kAgain; ++i)    // what the row does not see is anything
+            if (j0 + i < lo || j0 + i > hi) vw[i] = make_uint2(0, 0);
+#pragma unroll
+        for (int i = 0; i < kAgain; ++i) {
+            float x[4];
+            four(kw[i], x);
+            d[i] = q[0] * x[0] + q[1] * x[1] + q[2] * x[2] + q[3] * x[3];
+        }
+        // sums over the warp, halving the places that a lane has: lanes 2i and 2i + 1 end with place i's
+#pragma unroll
+        for (int n = kAgain / 2; n > 0; n /= 2) {
+            const bool upper = lane & 2 * n;
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const float give = upper ? d[i] : d[i + n];
+                d[i] = (upper ? d[i + n] : d[i]) + __shfl_xor_sync(0xffffffffu, give, 2 * n);
             }
         }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            d[i] = q[0] * k[i][0] + q[1] * k[i][1] + q[2] * k[i][2] + q[3] * k[i][3];
-#pragma unroll
-            for (int x = 16; x > 0; x >>= 1) d[i] += __shfl_xor_sync(0xffffffffu, d[i], x);
-            d[i] = j0 + i <= hi ? d[i] * a.scale_log2 : -INFINITY;
-        }
-        float mn = m;
-        bool nan = false;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            mn = fmaxf(mn, d[i]);
-            nan |= d[i] != d[i] || d[i] == INFINITY;
-        }
-        if (nan) {                          // so is the whole row
+        d[0] += __shfl_xor_sync(0xffffffffu, d[0], 1);
+        const int mine = j0 + (lane >> 1);
+        const float x = mine >= lo && mine <= hi ? d[0] * a.scale_log2 : -INFINITY;
+        if (__any_sync(0xffffffffu, x != x || x == INFINITY)) {                 // so is the whole row
             l = NAN;
             break;
         }
-        const float base = mn == -INFINITY ? 0.f : mn, was = fast_exp2(m - base);
-        l *= was;
+        float top = fmaxf(m, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] *= was;
+        for (int d = 2; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float base = top == -INFINITY ? 0.f : top, was = fast_exp2(m - base), p = fast_exp2(x - base);
+        m = top;
+        l = l * was + (lane & 1 ? 0.f : p);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (j0 + i > hi) break;         // what is there may not be seen
-            const float p = fast_exp2(d[i] - base);
+        for (int c = 0; c < 4; ++c) o[c] *= was;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(p, v[i][e], o[e]);
-            l += p;
+        for (int i = 0; i < kAgain; ++i) {
+            const float w = __shfl_sync(0xffffffffu, p, 2 * i);
+            float x[4];
+            four(vw[i], x);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = fmaf(w, x[c], o[c]);
         }
-        m = mn;
+        bool open = false;                  // columns that are not NaN for good
+#pragma unroll
+        for (int c = 0; c < 4; ++c) open |= (need >> c & 1) && o[c] == o[c];
+        if (!__any_sync(0xffffffffu, open)) break;
     }
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    if (here) {
-        const uint2 w = make_uint2(pack2<F16>(o[0] * inv, o[1] * inv), pack2<F16>(o[2] * inv, o[3] * inv));
-        *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + at) * 2) = w;
+    uint16_t* const to = reinterpret_cast<uint16_t*>(a.out) + token * a.out_ts + head * a.out_hs + at;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (need >> c & 1) to[c] = (uint16_t)pack2<F16>(o[c] * inv, 0.f);
+}
+
+// The rows row0 .. row0 + rows - 1 of an item whose results are written, by WARPS warps that meet at the barrier BAR; marks: kAgainMarks ints in
+// shared memory, free for it.
+template <bool F16, int KEYS, int WARPS, int BAR>
+__device__ __noinline__ void attend_again(const AttendArgs& a, const SeqExtent& e, int s, int h, int row0, int rows, int* marks, int warp) {
+    constexpr int kThreads = WARPS * 32;
+    const int lane = threadIdx.x & 31, at = lane * 4;
+    int* const nan_first = marks, *const nan_last = marks + kHeadDimMax, *const inf_first = marks + 2 * kHeadDimMax, *const inf_last = marks + 3 * kHeadDimMax;
+    for (int i = warp * 32 + lane; i < kAgainMarks; i += kThreads) marks[i] = i & kHeadDimMax ? -1 : INT_MAX;
+    named_sync(BAR, kThreads);
+    // ---- of each column, the first and the last place with a NaN and with an infinity
+    constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u, kUnit = F16 ? 0x0400u : 0x0080u;
+    int b, t, lo, hi, lo_last, hi_first;
+    key_tiles<KEYS>(a, e, row0, row0 + rows - 1, b, t);
+    row_bounds(a, e, row0, true, lo, hi_first);
+    row_bounds(a, e, row0 + rows - 1, true, lo_last, hi);
+    const int begin = b * KEYS, end = min(t * KEYS, e.len);
+    auto look = [&](int from, int to) {
+        int j0 = (from & ~(kAgain - 1)) + warp * kAgain, page = j0 < to ? again_page(a, s, j0) : -1;
+        for (; j0 < to; j0 += WARPS * kAgain) {
+            uint2 w[kAgain];
+            uint32_t found = 0;
+            again_load(a, a.v, page, h, j0, at, w);
+            if (j0 + WARPS * kAgain < to) page = again_page(a, s, j0 + WARPS * kAgain);
+#pragma unroll
+            for (int i = 0; i < kAgain; ++i) found |= ((w[i].x & kExp * 0x10001u) + kUnit * 0x10001u) | ((w[i].y & kExp * 0x10001u) + kUnit * 0x10001u);
+            if (!(found & 0x80008000u)) continue;
+#pragma unroll
+            for (int i = 0; i < kAgain; ++i) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t y = (c < 2 ? w[i].x : w[i].y) >> (c & 1) * 16 & 0x7FFFu;
+                    if (y >= kExp && j0 + i < end) {
+                        atomicMin((y > kExp ? nan_first : inf_first) + at + c, j0 + i);
+                        atomicMax((y > kExp ? nan_last : inf_last) + at + c, j0 + i);
+                    }
+                }
+            }
+        }
+    };
+    if (F16) look(begin, end);
+    else {                                  // all rows see the places lo_last .. hi_first
+        look(begin, min(lo_last, end));
+        look(max(hi_first + 1, begin), end);
     }
+    named_sync(BAR, kThreads);
+    for (int r = warp; r < rows; r += WARPS) {
+        row_bounds(a, e, row0 + r, true, lo, hi);
+        const int i = quotient(row0 + r, a.by_group), head = h * a.group + row0 + r - i * a.group;
+        uint2 x = make_uint2(0, 0);
+        if (at < a.dim) x = *reinterpret_cast<const uint2*>(a.out + ((e.first + i) * a.out_ts + head * a.out_hs + at) * 2);
+        uint32_t need = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t y = (c < 2 ? x.x : x.y) >> (c & 1) * 16 & 0x7FFFu;
+            if (y <= kExp) continue;
+            const int n0 = nan_first[at + c], n1 = nan_last[at + c], i0 = inf_first[at + c], i1 = inf_last[at + c];
+            const bool unseen = min(n0, i0) < lo || max(n1, i1) > hi, lost = F16 && i0 <= hi && i1 >= lo;
+            const bool own = (n0 >= lo && n0 <= hi) || (n1 >= lo && n1 <= hi);
+            if ((unseen || lost) && !own) need |= 1u << c;
+        }
+        if (__any_sync(0xffffffffu, need != 0)) attend_row_again<F16>(a, e, s, h, row0 + r, need);
+    }
+    named_sync(BAR, kThreads);
 }
 
 }  // namespace saem

@@ -12,8 +12,6 @@
 //
 // An item of at most 128 rows (a short chunk, decoding sequences beside a prompt) is worked on by both groups, even tiles of places
 // and odd ones, whose results are added up at its end.
-#include <limits.h>
-
 #include "attend_plan.cuh"
 #include "mx_tc.cuh"
 
@@ -98,8 +96,18 @@ __device__ __forceinline__ uint32_t idesc_attend(int n, bool b_mn) {
     return (1u << 4) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-// The limit of a wait that lasts as long as an item: a tile of places takes at most 2 us.
+// The limit of a wait that lasts as long as an item: a tile of places takes at most 2 us (rows with a NaN are summed again behind the last item).
 __device__ __forceinline__ unsigned long long item_limit_ns(const AttendPart& p) { return kWaitLimitNs + 20000ull * (unsigned)max(0, p.key_end - p.key_begin); }
+
+// The items that the CTA has ended, for their rows with a NaN: the walk once more, by the eight warps with rows.
+template <bool F16>
+__device__ __noinline__ void attend_items_again(const AttendArgs& a, const AttendPlan& plan, const int* ended, int* marks, int warp) {
+    AttendWalk<kAtR, kAtKeys, kAtHead, kAtSnap> walk;
+    if (a.seqs > kPlanWarpSeqs) walk.begin(a, plan);
+    else walk.begin_alone<kAtHead + 1>(a);
+    for (AttendPart p; walk.next(a, p);)
+        if (p.whole || ended[p.slot & 1]) attend_again<F16, kAtKeys, 8, kAtBarAll>(a, p.e, p.s, p.h, p.r * kAtR, p.rows, marks, warp);
+}
 
 template <bool F16, int DK>
 __global__ void __launch_bounds__(kAtThreads, 1)
@@ -110,8 +118,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_tail, bar_end, bar_q[2], bar_free[2], bar_s[2], bar_p[2][2], bar_o[2], bar_part[kAtParts], bar_done[kAtParts];
     __shared__ AttendPart parts[kAtParts];  // the items at hand; one without rows ends the range
     __shared__ AttendPlan plan;
-    __shared__ uint32_t tmem_s, nan_s[2][8];     // rows with a NaN, of this item and the next
-    __shared__ int abort_flag, last_s;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_flag, last_s, nan_s, ended_s[2];          // some row has a NaN; cut items (by the parity of the part's place) that this CTA has ended
     __shared__ float other_s[2][128];       // the second group's maxima and sums, where both worked on the same rows
     const AttendArgs& a = args.a;
     const uint32_t base = warp_uniform((smem_u32(smem_raw) + 1023u) & ~1023u), ring = base + 2 * kTile;
@@ -137,8 +145,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             mbar_init(smem_u32(&bar_part[i]), 1);
             mbar_init(smem_u32(&bar_done[i]), 11);
         }
-        abort_flag = 0;
-        for (int i = 0; i < 8; ++i) nan_s[0][i] = 0;
+        abort_flag = nan_s = ended_s[0] = ended_s[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -316,7 +323,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     st_shared_v4(stage + lane * 128 + ((((c & 1) * 4 + e) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
                 }
                 const float all = low_f32(any) + high_f32(any);
-                if (all != all && in) atomicOr(&nan_s[turn & 1][tile_row >> 5], 1u << (tile_row & 31));
+                if (all != all && in) nan_s = 1;
                 if (c & 1) {
                     __syncwarp();
                     const int col = (c >> 1) * 64 + (lane & 7) * 8;
@@ -338,7 +345,6 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             auto finish_lse = [&](float mx, float sum) {
                 if (a.lse) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
             };
-            bool done = e.whole;
             if (warp_writes) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll 1
@@ -385,12 +391,14 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     __threadfence();                                // what the barrier has ordered before it, too
                     // a CTA that gave up leaves the item open
                     last_s = !*abort_p && atomicAdd(a.counters + e.first_cta, 1) == e.n_parts - 1;
-                    if (last_s) a.counters[e.first_cta] = 0;
+                    if (last_s) {
+                        a.counters[e.first_cta] = 0;
+                        ended_s[e.slot & 1] = 1;
+                    }
                 }
                 named_sync(kAtBarAll, 256);
                 if (last_s) {
                     __threadfence();
-                    done = true;
                     auto part = [&](int j) { return a.partials + (size_t)part_slot(e.first_cta, j) * Shape::kSlot; };
                     if (e.rows <= 64) {
                         // few rows, and often many parts: the columns are shared out over the warps, and four parts are under way at once
@@ -428,7 +436,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                                     *reinterpret_cast<uint4*>(a.out + (tok * a.out_ts + hd * a.out_hs + c * 4) * 2) = w;
                                 }
                             }
-                            if (any != any) atomicOr(&nan_s[turn & 1][row >> 5], 1u << (row & 31));
+                            if (any != any) nan_s = 1;
                             if (a.lse && at0 == 0) a.lse[tok * a.group * a.kv_heads + hd] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
                         }
                     } else if (warp_writes) {
@@ -463,17 +471,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
                 }
             }
-            named_sync(kAtBarAll, 256);
-            if (threadIdx.x == 128)
-                for (int i = 0; i < 8; ++i) nan_s[~turn & 1][i] = 0;
-            const uint32_t again = done && ok && lane < 8 ? nan_s[turn & 1][lane] : 0u;
-            for (uint32_t words = __ballot_sync(0xffffffffu, again != 0); words; words &= words - 1) {
-                const int w = __ffs(words) - 1;
-                const uint32_t bits = __shfl_sync(0xffffffffu, again, w);
-                for (int r = warp - 4; r < 32; r += 8)
-                    if (bits >> r & 1) attend_row_again<F16>(a, e.e, e.s, e.h, e.r * kAtR + w * 32 + r);
-            }
+            named_sync(kAtBarAll, 256);                             // the groups go on together: 1 % slower if they drift apart
         }
+        // no wait is left that this, which is long, could outlast
+        if (ok && nan_s) attend_items_again<F16>(a, plan, ended_s, reinterpret_cast<int*>(meet), warp - 4);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtRegsFew));
         if (warp == 0) {

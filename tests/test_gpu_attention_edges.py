@@ -1,4 +1,4 @@
-"""Attention at the edges of what a call may hold: lengths that the table cuts.
+"""Attention at the edges of what a call may hold: lengths that the table cuts, values that are not finite.
 
 Bounds as in test_gpu_attention.py: a weight's rounding u and the result's u, 2 delta for the scores, 2^-18 for exponentials and sums."""
 import math
@@ -71,3 +71,92 @@ def test_a_sequence_without_new_tokens_may_have_any_length():
     for max_new in (1, 1000):
         att.attend(q, attention.Batch(i32(0, 0, 2, 2), i32(1000, 20, 2 ** 31 - 1), i32(0, 1, 2, 3, 0, 0).view(3, 2), max_new))
         assert att.device_status() == 0
+
+
+@pytest.mark.parametrize("max_new", [1, 1000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 60), (False, 0), (False, 60)])
+@pytest.mark.parametrize("extra_seqs", [0, 40])
+def test_values_that_are_not_finite_here_and_there(max_new, dtype, causal, window, extra_seqs):
+    """NaN and infinities of both signs, a few in every column of some pages and many in some columns: each result is NaN, infinite or finite as the
+    formula says, whatever else its tile holds."""
+    from paper_2608_21614_b200 import attention
+    seqs = [(150, 400), (1, 90), (300, 2000), (2, 700)] + [(1, 40)] * extra_seqs
+    q, cache, batch, offsets = base.build(seqs, 8, 2, 80, 32, dtype, seed=5)
+    batch.max_new = max_new
+    g = base.gen(6)
+    odd = torch.tensor([math.nan, math.inf, -math.inf], device="cuda").to(dtype)
+    for s, (n, length) in enumerate(seqs):
+        many = 12 if s < 4 else 1
+        r = lambda top, k: torch.randint(0, top, (k,), generator=g, device="cuda")                              # noqa: E731
+        place = torch.cat((r(length, many), length - 1 - r(min(n, length), many)))              # anywhere, and where some of the tokens are
+        column = torch.cat((r(80, many), r(4, many)))
+        cache.v[batch.table[s, place // 32].long(), r(2, 2 * many), place % 32, column] = odd[r(3, 2 * many)]
+    att = attention.Attention(8, cache, causal=causal, window=window)
+    out = att.attend(q, batch)
+    assert att.device_status() == 0
+    base.check(out, None, q, cache, batch, seqs, offsets, causal, window, 80 ** -0.5)
+
+
+@pytest.mark.parametrize("max_new", [1, 1000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_value_that_is_not_finite_at_the_end_of_half_a_million_places(max_new, dtype):
+    """The last token of the first sequence alone sees it; summing the others again takes longer than a wait within the kernel may, and the sequences
+    behind have to be there all the same.  At most 3 pages of 256 places have weights that count: 2^-14 for the sums of so many."""
+    from paper_2608_21614_b200 import attention
+    page, dim, hq, hk, n, entries = 256, 64, 8, 2, 20, 2048
+    g = base.gen(8)
+    cache = attention.PagedCache(*(torch.randn(5, hk, page, dim, generator=g, device="cuda").to(dtype) for _ in range(2)))
+    cache.k[0] = -16.0                                              # scores below -128 and below all others by far more than 100
+    cache.k[1:] *= 0.1
+    q = (torch.rand(8 * n + 20, hq, dim, generator=g, device="cuda") + 1).to(dtype)
+    table = torch.zeros(8, entries, dtype=torch.int32, device="cuda")
+    table[:, 700], table[:, 1500], table[:, -1], table[0, -1] = 1, 2, 3, 4
+    cache.v[4, :, -1, 5], cache.v[4, 1, -1, 6] = math.nan, math.inf
+    att = attention.Attention(hq, cache)
+    out = att.attend(q, attention.Batch(i32(*range(0, 8 * n + 1, n)), i32(*[entries * page] * 8), table, max_new))
+    assert att.device_status() == 0
+    u = torch.finfo(dtype).eps / 2
+    for s in range(8):
+        k, v = (c[[1, 2, 4 if s == 0 else 3]].transpose(0, 1).flatten(1, 2) for c in (cache.k, cache.v))
+        seen = torch.arange(3 * page, device="cuda") <= 3 * page - n + torch.arange(n, device="cuda")[:, None]
+        want, size, delta = formula(q[s * n:(s + 1) * n], k, torch.nan_to_num(v, 0.0, 0.0, 0.0), seen, dim ** -0.5)
+        got = out[s * n:(s + 1) * n]
+        if s == 0:
+            assert bool(torch.isnan(got[-1, :, 5]).all()) and bool((got[-1, 4:, 6] == math.inf).all())
+            got = got.clone()
+            got[-1, :, 5], got[-1, 4:, 6] = want[-1, :, 5].to(dtype), want[-1, 4:, 6].to(dtype)
+        assert bool(((got.double() - want).abs() <= u * want.abs() + (u + 2 * delta[..., None] + 2.0 ** -14) * size).all()), s
+
+
+@pytest.mark.parametrize("dtype,new,length", [(torch.bfloat16, 1, 131072), (torch.bfloat16, 2048, 2048), (torch.float16, 1, 131072), (torch.float16, 2048, 2048)])
+def test_a_nan_that_is_seen_does_not_make_a_call_slow(dtype, new, length):
+    """Such a result is NaN and needs no second sum: of the rows' own places at most one more look at the values is paid for.  At the last place of
+    2048 tokens, the 63 tokens x 4 heads before it in their item do not see it and are summed again: 32 rows a warp, 128 steps of 16 places,
+    each below 2 us, which are 8.2 ms."""
+    from paper_2608_21614_b200 import attention
+    cache = attention.PagedCache(*(torch.randn(length // 64, 8, 64, 128, generator=base.gen(s), device="cuda").to(dtype) for s in (1, 2)))
+    q = torch.randn(new, 32, 128, generator=base.gen(3), device="cuda").to(dtype)
+    batch = attention.Batch(i32(0, new), i32(length), torch.arange(length // 64, dtype=torch.int32, device="cuda")[None], new)
+    att, out = attention.Attention(32, cache), torch.empty_like(q)
+
+    def best():
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            att.attend(q, batch, out=out)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    plain = best()
+    for place in (0, length // 2, length - 1):
+        kept = cache.v[place // 64, :, place % 64, 3].clone()
+        cache.v[place // 64, :, place % 64, 3] = math.nan
+        slow = best()
+        assert bool(torch.isnan(out[-1, :, 3]).all()) and bool(torch.isfinite(out[-1, :, 4:]).all())
+        cache.v[place // 64, :, place % 64, 3] = kept
+        print("%s %d over %d, NaN at %d: %.3f ms, without %.3f ms" % (dtype, new, length, place, slow, plain))
+        again = 32 * 128 * 2e-3 if new > 1 and place == length - 1 else 0.0
+        assert slow < 30 * plain + again                            # summing all again took 400 to 900 times as long

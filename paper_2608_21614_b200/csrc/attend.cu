@@ -49,7 +49,7 @@ template <bool F16, int DK>
 __global__ void __launch_bounds__(kRowsThreads, kRowsPerSm)
 attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     using Shape = RowsShape<DK>;
-    constexpr int kStages = Shape::kStages;
+    constexpr int kStages = Shape::kStages, kLift = F16 ? 15 : 0;   // weights are at most 1
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ AttendPlan plan;
     __shared__ int last_s;
@@ -184,7 +184,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[t][e] = fast_exp2(sc[t][e] - base[e >> 1]);
+                    sc[t][e] = fast_exp2(sc[t][e] - (base[e >> 1] - kLift));
                     l[e >> 1] += sc[t][e];
                 }
             if (__any_sync(0xffffffffu, was[0] != 1.f || was[1] != 1.f)) {
@@ -228,7 +228,7 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
             if (v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w) nan_s = 1;
             if (col < a.dim) *reinterpret_cast<uint2*>(a.out + (token * a.out_ts + head * a.out_hs + col) * 2) = make_uint2(pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w));
-            if (a.lse && col == 0) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
+            if (a.lse && col == 0) a.lse[token * a.group * a.kv_heads + head] = log_sum_exp<kLift>(mx, sum);
         };
 #pragma unroll
         for (int b = 0; b < 2; ++b) {

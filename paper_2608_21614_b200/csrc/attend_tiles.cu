@@ -113,7 +113,7 @@ template <bool F16, int DK>
 __global__ void __launch_bounds__(kAtThreads, 1)
 attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TilesArgs args) {
     using Shape = TilesShape<DK>;
-    constexpr int kStages = Shape::kStages, kTile = Shape::kTile;
+    constexpr int kStages = Shape::kStages, kTile = Shape::kTile, kLift = F16 ? 7 : 0;          // weights are at most 2^8
     extern __shared__ uint8_t smem_raw[];
     __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_tail, bar_end, bar_q[2], bar_free[2], bar_s[2], bar_p[2][2], bar_o[2], bar_part[kAtParts], bar_done[kAtParts];
     __shared__ AttendPart parts[kAtParts];  // the items at hand; one without rows ends the range
@@ -241,7 +241,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : m * a.scale_log2;
-                    const uint64_t by = pack_f32x2(a.scale_log2, a.scale_log2), less = pack_f32x2(-ref, -ref);
+                    const uint64_t by = pack_f32x2(a.scale_log2, a.scale_log2), less = pack_f32x2(kLift - ref, kLift - ref);
                     uint64_t sum[2] = {0, 0};                                   // two sums each: zeros
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {                               // half of the places at a time: its products need not wait for the rest
@@ -343,7 +343,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 }
             };
             auto finish_lse = [&](float mx, float sum) {
-                if (a.lse) a.lse[token * a.group * a.kv_heads + head] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
+                if (a.lse) a.lse[token * a.group * a.kv_heads + head] = log_sum_exp<kLift>(mx, sum);
             };
             if (warp_writes) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
@@ -437,7 +437,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                                 }
                             }
                             if (any != any) nan_s = 1;
-                            if (a.lse && at0 == 0) a.lse[tok * a.group * a.kv_heads + hd] = mx == -INFINITY ? -INFINITY : mx * 0.69314718056f + logf(sum);
+                            if (a.lse && at0 == 0) a.lse[tok * a.group * a.kv_heads + hd] = log_sum_exp<kLift>(mx, sum);
                         }
                     } else if (warp_writes) {
                         float mx = -INFINITY, sum = 0.f;

@@ -1,4 +1,5 @@
-"""Attention at the edges of what a call may hold: lengths that the table cuts, values that are not finite.
+"""Attention at the edges of what a call may hold: lengths that the table cuts, values that are not finite, weights
+that are small beside another.
 
 Bounds as in test_gpu_attention.py: a weight's rounding u and the result's u, 2 delta for the scores, 2^-18 for exponentials and sums."""
 import math
@@ -160,3 +161,36 @@ def test_a_nan_that_is_seen_does_not_make_a_call_slow(dtype, new, length):
         print("%s %d over %d, NaN at %d: %.3f ms, without %.3f ms" % (dtype, new, length, place, slow, plain))
         again = 32 * 128 * 2e-3 if new > 1 and place == length - 1 else 0.0
         assert slow < 30 * plain + again                            # summing all again took 400 to 900 times as long
+
+
+@pytest.mark.parametrize("max_new,new", [(1, 1), (1, 4), (1000, 200)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("bits", [14.3, 18.4, 20.6, 21.7])
+def test_many_small_weights_beside_a_large_one(max_new, new, dtype, bits):
+    """A million places whose weights are 2^-bits of the first one's: together they count as much.  A float16 weight's last bit is 2^-24 of at
+    least 2^7 times the largest weight: 2^-32 for each place, 2^-12 for all; sums of at most 2^11 terms or products in a row, 2^-23 of
+    them lost in each: 2^-12."""
+    from paper_2608_21614_b200 import attention
+    page, dim, entries = 256, 64, 4096
+    g = base.gen(9)
+    k, v = torch.zeros(8, 1, page, dim, device="cuda"), torch.rand(8, 1, page, dim, generator=g, device="cuda") + 0.5
+    k[0, 0, 0, 0] = bits * math.log(2)
+    v[0, 0, 0] = -v[0, 0, 0]
+    cache = attention.PagedCache(k.to(dtype), v.to(dtype))
+    q = torch.zeros(new, 4, dim, device="cuda")
+    q[..., 0] = 8.0                                                 # scores: the keys' first elements
+    q = torch.cat((q, torch.zeros(200, 4, dim, device="cuda"))).to(dtype)
+    table = 1 + torch.arange(entries, dtype=torch.int32, device="cuda")[None] % 7
+    table[0, 0] = 0
+    att = attention.Attention(4, cache, causal=False)
+    lse = torch.empty(new + 200, 4, device="cuda")
+    out = att.attend(q, attention.Batch(i32(0, new), i32(entries * page), table, max_new), lse=lse)
+    times = torch.bincount(table[0], minlength=8).double().repeat_interleave(page)
+    score = cache.k[:, 0].flatten(0, 1)[:, 0].double()
+    p = torch.softmax(score + times.log(), 0)
+    values = cache.v[:, 0].flatten(0, 1).double()
+    want, size = p @ values, p @ values.abs()
+    u = torch.finfo(dtype).eps / 2
+    assert att.device_status() == 0
+    assert bool(((out[:new].double() - want).abs() <= u * want.abs() + (u + 2.0 ** -11) * size).all())
+    assert bool(((lse[:new].double() - torch.logsumexp(score + times.log(), 0)).abs() <= 2.0 ** -12 + 2.0 ** -18).all())

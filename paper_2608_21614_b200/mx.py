@@ -135,6 +135,10 @@ class Linear:
 
     def device_status(self) -> int:
         """The status word of the calls so far, whatever their streams (synchronises the device); 0 unless a device-side wait ran
-        out."""
+        out.  Clears it."""
         torch.cuda.synchronize(self.workspace.device)
-        return int(self.workspace[:4].view(torch.int32).item())
+        code = int(self.workspace[:4].view(torch.int32).item())
+        if code:
+            self.workspace[:4].zero_()
+            torch.cuda.synchronize(self.workspace.device)
+        return code

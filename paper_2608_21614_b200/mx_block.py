@@ -34,6 +34,11 @@ from .norms import BlockNorm
 from .rotary import Rotary
 
 
+def _first_status(parts) -> int:
+    """The first status that is set, all of them read and cleared."""
+    return next(filter(None, [p.device_status() for p in parts]), 0)
+
+
 class MxAttention:
     """The attention half of a layer, its projections in 4 bits.
 
@@ -74,7 +79,7 @@ class MxAttention:
         self.norm.leave(x, y, x_out=x, n_out=n)
 
     def device_status(self) -> int:
-        return self.qkv.device_status() or self.attention.device_status() or self.out.device_status()
+        return _first_status((self.qkv, self.attention, self.out))
 
 
 class MxMoEStack:
@@ -152,10 +157,7 @@ class MxMoEStack:
         return graph
 
     def device_status(self) -> int:
-        status = self.layer.device_status() or self.head.device_status()
-        for a in self.attention or ():
-            status = status or a.device_status()
-        return status
+        return _first_status((self.layer, self.head, *(self.attention or ())))
 
     def close(self):
         self.layer.close()

@@ -44,7 +44,10 @@ class MxAttention:
 
     `w_qkv` [(q_heads + 2 kv_heads) * head_dim, d] (queries, keys, values) and `w_out` [d, q_heads * head_dim] bf16 on the GPU; `post` and `pre` [d]
     the norms behind it (post may be None); the other arguments are Attention's.  `share`: another layer's MxAttention, whose
-    workspaces and buffers this one uses too (layers run one after the other)."""
+    attention workspace and buffers this one uses too (layers run one after the other).
+
+    Rows behind the batch's last sequence (spare ones of a captured step) are not attended: what the buffers held there, zeros or an
+    earlier call's, is projected and added to them, so that their x and n have no meaning.  No other row depends on them, whatever they hold."""
 
     def __init__(self, w_qkv: torch.Tensor, w_out: torch.Tensor, post: Optional[torch.Tensor], pre: torch.Tensor, cache: PagedCache, q_heads: int,
                  max_tokens: int, rotary: Optional[Rotary] = None, w_q: Optional[torch.Tensor] = None, w_k: Optional[torch.Tensor] = None,
@@ -64,8 +67,8 @@ class MxAttention:
             self.projected, self.rotated, self.weighted, self.y = share.projected, share.rotated, share.weighted, share.y
             return
         dev = cache.k.device
-        self.projected = torch.empty(max_tokens, q_heads + 2 * kv_heads, dim, dtype=torch.bfloat16, device=dev)
-        self.rotated, self.weighted = (torch.empty(max_tokens, q_heads, dim, dtype=cache.k.dtype, device=dev) for _ in range(2))
+        self.projected = torch.zeros(max_tokens, q_heads + 2 * kv_heads, dim, dtype=torch.bfloat16, device=dev)
+        self.rotated, self.weighted = (torch.zeros(max_tokens, q_heads, dim, dtype=cache.k.dtype, device=dev) for _ in range(2))
         self.y = torch.empty(max_tokens, self.d, dtype=torch.float32, device=dev)
 
     def __call__(self, x: torch.Tensor, n: torch.Tensor, batch: Batch) -> None:
@@ -86,7 +89,7 @@ class MxMoEStack:
     """`n_layers` MoE layers over 4-bit experts with the norms between them, and a 4-bit head.
 
     `attention`: an MxAttention for each layer, run before its experts (`pres[l]` are then the norms before attention, and a step
-    takes the Batch of its tokens).
+    takes the Batch of its tokens; results of rows behind the batch's last sequence have no meaning).
 
     Weights are given per layer: `experts[l]` a sequence of (gate, up, down) bf16 matrices on the GPU, `routers[l]`
     [E, d], `posts[l]`, `pres[l]` [d] (pres has one more entry, for the head's input), `head` [vocabulary, d]; all bf16."""

@@ -26,7 +26,7 @@ __device__ __forceinline__ float fast_exp2(float x) {
 }
 
 // Weights are multiplied by 2^LIFT before they are rounded to float16, and so is their sum: the largest is then close to 65504 and the last bit
-// of a small one is 2^-24 of that, not of 1.  Without it a long context of small weights beside a large one lost them (2^20 places of 2^-20.6: 4 %).
+// of a small one is 2^-24 of that, not of 1.  Without it small weights beside a large one of the same CTA came out 4 % off (2^-20.6) or not at all (2^-25.2).
 template <int LIFT>
 __device__ __forceinline__ float log_sum_exp(float top, float sum) {           // top in powers of two
     return top == -INFINITY ? -INFINITY : top * 0.69314718056f + logf(sum * (1.f / (1 << LIFT)));

@@ -33,6 +33,17 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Two weights as 16-bit ones and what they lose.  A bfloat16 is cut, and its rest above 0 where the weight is, so that both parts' products with an
+// infinity are that infinity (0 times it, or a sum of both signs, is NaN; float16 has no exponents for that, see attend_again).
+template <bool F16>
+__device__ __forceinline__ uint32_t cut2(float a, float b, float2& rest) {
+    const uint32_t w = F16 ? pack2<true>(a, b) : __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    const float2 got = unpack2<F16>(w);
+    rest = make_float2(a - got.x, b - got.y);
+    if (!F16) rest = make_float2(fmaxf(rest.x, fminf(a, 0x1p-126f)), fmaxf(rest.y, fminf(b, 0x1p-126f)));
+    return w;
+}
+
 // DK: head_dim rounded up to 64 or 128.
 template <int DK>
 struct RowsShape {
@@ -135,6 +146,9 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                 for (int c = 0; c < 2; ++c)
                     qf[k][b + 2 * c] = in && k * 16 + c * 8 < a.dim ? *reinterpret_cast<const uint32_t*>(q + (k * 16 + c * 8) * 2) : 0u;
         }
+        // An item of at most 8 rows leaves half of a tile's rows free: they take what the weights lose to 16 bits, and are added at the end (1 % of a
+        // call).  An item of more rows has its weights in 16 bits: a second product for what they lose took 4 to 8 %.
+        const bool half = rows <= 8;
         float o[DK / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < DK / 8; ++d)
@@ -187,13 +201,21 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                     sc[t][e] = fast_exp2(sc[t][e] - (base[e >> 1] - kLift));
                     l[e >> 1] += sc[t][e];
                 }
+            if (half) was[1] = was[0];
             if (__any_sync(0xffffffffu, was[0] != 1.f || was[1] != 1.f)) {
 #pragma unroll
                 for (int d = 0; d < DK / 8; ++d)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[d][e] *= was[e >> 1];
             }
-            const uint32_t w[4] = {pack2<F16>(sc[0][0], sc[0][1]), pack2<F16>(sc[0][2], sc[0][3]), pack2<F16>(sc[1][0], sc[1][1]), pack2<F16>(sc[1][2], sc[1][3])};
+            uint32_t w[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float2 rest;
+                const uint32_t most = cut2<F16>(sc[t][0], sc[t][1], rest);
+                w[2 * t] = half ? most : pack2<F16>(sc[t][0], sc[t][1]);
+                w[2 * t + 1] = pack2<F16>(half ? rest.x : sc[t][2], half ? rest.y : sc[t][3]);
+            }
 #pragma unroll
             for (int k = 0; k < DK / 16; ++k) {
                 if (k < n_k) {
@@ -208,6 +230,13 @@ attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         }
         cp_async_wait<0>();
         __syncwarp();
+        if (half) {
+#pragma unroll
+            for (int d = 0; d < DK / 8; ++d) {
+                o[d][0] += o[d][2];
+                o[d][1] += o[d][3];
+            }
+        }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             l[b] += __shfl_xor_sync(0xffffffffu, l[b], 1);

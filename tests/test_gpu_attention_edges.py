@@ -1,5 +1,5 @@
-"""Attention at the edges of what a call may hold: lengths that the table cuts, values that are not finite, weights
-that are small beside another.
+"""Attention at the edges of what a call may hold: lengths that the table cuts, values that are not finite, weights that are small beside
+another, and what weights lose to 16 bits.
 
 Bounds as in test_gpu_attention.py: a weight's rounding u and the result's u, 2 delta for the scores, 2^-18 for exponentials and sums."""
 import math
@@ -191,3 +191,40 @@ def test_many_small_weights_beside_a_large_one(max_new, dtype, bits):
     assert att.device_status() == 0
     assert float((out.double() / want - 1).abs().max()) <= 2 * u + sums + (2.0 ** (bits - 32) if dtype == torch.float16 else 0.0)
     assert float((lse.double() - torch.logsumexp(score + times.log(), 0)).abs().max()) <= sums
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("q_heads,kv_heads,dim", [(8, 1, 128), (16, 4, 64), (3, 3, 96)])
+@pytest.mark.parametrize("length", [3, 40, 700, 20000])
+def test_weights_of_up_to_eight_rows_lose_little_to_16_bits(dtype, q_heads, kv_heads, dim, length):
+    """A weight is the sum of two 16-bit ones, of which the first is below it by 2^-7 of it at most and the second off by 2^-9 of itself: 2^-16."""
+    from paper_2608_21614_b200 import attention
+    seqs = [(1, length)] * 3 + [(8 // (q_heads // kv_heads), length)]
+    q, cache, batch, offsets = base.build(seqs, q_heads, kv_heads, dim, 32, dtype, seed=12, spare_rows=0)
+    out = attention.Attention(q_heads, cache).attend(q, batch)
+    u = torch.finfo(dtype).eps / 2
+    for s, (n, _) in enumerate(seqs):
+        t = slice(offsets[s], offsets[s + 1])
+        k, v = (base.ref.gather(c, batch.table[s], length, 32) for c in (cache.k, cache.v))
+        want, size, _, spread = base.ref.attend(q[t], k, v, n, True, 0, dim ** -0.5)
+        delta = spread * ((dim + 8) * 2.0 ** -24 + 2.0 ** -22)
+        off = (out[t].double() - want).abs() - u * want.abs() - (2.0 ** -16 + 2 * delta[..., None] + 2.0 ** -18) * size
+        assert float(off.max()) <= torch.finfo(dtype).tiny * 2
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_infinities_that_few_rows_see(dtype, value):
+    """Times a weight and times what the weight lost to 16 bits: the infinity, also where a weight is exact or very small."""
+    from paper_2608_21614_b200 import attention
+    k, v = (torch.zeros(40, 1, 32, 64, device="cuda", dtype=dtype) for _ in range(2))
+    q = torch.zeros(3, 2, 64, device="cuda", dtype=dtype)
+    q[:, :, 0] = 8.0
+    k[:, :, :, 0] = -torch.randint(0, 30, (40, 1, 32), generator=base.gen(1), device="cuda").to(dtype) / 2              # weights from 1 to e^-14.5
+    v[7, 0, 3, 5], v[20, 0, 31, 6], v[39, 0, 31, 7] = value, value, value
+    k[7, 0, 3, 0], k[20, 0, 31, 0] = 0.0, -60.0
+    batch = attention.Batch(i32(0, 1, 3), i32(1280, 1280), torch.arange(40, dtype=torch.int32, device="cuda").repeat(2, 1))
+    out = attention.Attention(2, attention.PagedCache(k, v)).attend(q, batch).float()
+    want = torch.zeros(3, 2, 64, device="cuda")
+    want[:, :, 5:7], want[[0, 2], :, 7] = value, value                       # the last place is the last token's
+    assert torch.equal(torch.nan_to_num(out, 3.0, 1.0, 2.0), torch.nan_to_num(want, 3.0, 1.0, 2.0))

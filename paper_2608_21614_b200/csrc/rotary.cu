@@ -134,7 +134,8 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int seqs, int
 
 // Sines and cosines of two angles, given as fractions of a turn in units of 2^-64.  With r in half turns, |r| <= 1/4, and z = r^2:
 // sin(pi r) = r s(z), s of degree 3 with the least largest relative error (2^-28), cos(pi r) = 1 + z c(z), c of degree 3 with the least
-// largest absolute error (2^-34), both by Lawson's iteration in 64 bits; in fp32 both are within 2^-23.4 of the values in 64 bits.
+// largest absolute error (2^-34), both by Lawson's iteration in 64 bits; in fp32, r's own rounding included, the sine is within 2^-23.2 and the
+// cosine within 2^-23.6 of the angle's in 64 bits (over 24 million angles).
 __device__ __forceinline__ void turn2(uint64_t u0, uint64_t u1, float (&sn)[2], float (&cs)[2]) {
     const uint32_t h0 = (uint32_t)(u0 >> 32), h1 = (uint32_t)(u1 >> 32), q0 = (h0 + 0x20000000u) >> 30, q1 = (h1 + 0x20000000u) >> 30;
     const uint64_t r = pack_f32x2((float)(int32_t)(h0 - (q0 << 30)) * 0x1p-31f, (float)(int32_t)(h1 - (q1 << 30)) * 0x1p-31f), z = mul_f32x2(r, r);

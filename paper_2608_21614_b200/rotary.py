@@ -35,6 +35,8 @@ def frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[dict] 
             result = [f / factor for f in plain], 1.0
         elif kind == "base":
             wider = base * factor ** (rotary_dim / (rotary_dim - 2)) if rotary_dim > 2 else base
+            if not math.isfinite(wider):
+                raise ValueError("base %r, factor %r" % (base, factor))
             result = [wider ** (-2.0 * i / rotary_dim) for i in range(n)], 1.0
         elif kind == "bands":
             original, low, high = float(s.pop("original")), float(s.pop("low")), float(s.pop("high"))
@@ -57,7 +59,7 @@ def frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[dict] 
             raise ValueError("kind %r" % (kind,))
         if s:
             raise ValueError("unknown %s" % ", ".join(sorted(s)))
-    except (KeyError, TypeError, ValueError) as e:
+    except (KeyError, TypeError, ValueError, OverflowError) as e:
         raise B.SaemError(B.SAEM_ERR_INVALID_ARG, "frequencies: scaling: %s" % (e,)) from None
     return result
 

@@ -10,6 +10,9 @@
 // The maximum that a row's weights refer to is only moved, and O multiplied, where it has grown by more than 2^8: the result is the same but
 // for rounding, 16-bit floats have the range, and it is rare after a row's first tiles.
 //
+// The weights are rounded to 16 bits, half a step each, because that is the width of the operand beside 16-bit values; their sum is of the unrounded
+// ones.  A second product for what they lose would add 1024 cycles of the tensor cores, and as many conversions again, to a tile's 3300 cycles.
+//
 // An item of at most 128 rows (a short chunk, decoding sequences beside a prompt) is worked on by both groups, even tiles of places
 // and odd ones, whose results are added up at its end.
 #include "attend_plan.cuh"

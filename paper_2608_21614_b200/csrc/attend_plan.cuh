@@ -296,7 +296,7 @@ __device__ __forceinline__ void row_bounds(const AttendArgs& a, const SeqExtent&
 // Rows with a NaN, once more.  In a product of tiles a weight of 0 meets what other rows see, and 0 times an infinity or NaN there is NaN; so it
 // is with float16 weights where a row sees an infinity itself and its weight rounds to 0.  The first comes of the few places of an item's tiles that
 // some of its rows do not see, the second of any; a NaN that a row sees is one of its result and needs no second sum.  One token over 131072
-// places, one with a NaN: 99 us as without (bfloat16), 1.9 ms (float16, where all values are looked at); a row that is summed again takes 1.5 us for 16 places.
+// places, one with a NaN: 99 us as without (bfloat16), 1.5 ms (float16, where all values are looked at); a row that is summed again takes 1.5 us for 16 places.
 constexpr int kAgain = 16;                  // places at a time: of one page, as they are multiples of 16
 constexpr int kAgainMarks = 4 * kHeadDimMax;
 __device__ __forceinline__ int again_page(const AttendArgs& a, int s, int j0) { return a.table[s * a.table_stride + quotient(j0, a.by_page)]; }
@@ -407,23 +407,30 @@ __device__ __noinline__ void attend_again(const AttendArgs& a, const SeqExtent& 
     row_bounds(a, e, row0 + rows - 1, true, lo_last, hi);
     const int begin = b * KEYS, end = min(t * KEYS, e.len);
     auto look = [&](int from, int to) {
-        int j0 = (from & ~(kAgain - 1)) + warp * kAgain, page = j0 < to ? again_page(a, s, j0) : -1;
-        for (; j0 < to; j0 += WARPS * kAgain) {
-            uint2 w[kAgain];
+        constexpr int kGroups = 4, kStep = WARPS * kAgain;          // groups of places whose loads are under way
+        int pages = -1;                     // lane l: of the l-th of 32 groups
+        for (int j0 = (from & ~(kAgain - 1)) + warp * kAgain, n = 0; j0 < to; j0 += kGroups * kStep, n += kGroups) {
+            uint2 w[kGroups][kAgain];
             uint32_t found = 0;
-            again_load(a, a.v, page, h, j0, at, w);
-            if (j0 + WARPS * kAgain < to) page = again_page(a, s, j0 + WARPS * kAgain);
+            if (n % 32 == 0) pages = (long long)j0 + lane * kStep < to ? again_page(a, s, j0 + lane * kStep) : -1;
 #pragma unroll
-            for (int i = 0; i < kAgain; ++i) found |= ((w[i].x & kExp * 0x10001u) + kUnit * 0x10001u) | ((w[i].y & kExp * 0x10001u) + kUnit * 0x10001u);
+            for (int g = 0; g < kGroups; ++g) again_load(a, a.v, __shfl_sync(0xffffffffu, pages, (n + g) % 32), h, j0 + g * kStep, at, w[g]);
+#pragma unroll
+            for (int i = 0; i < kGroups * kAgain; ++i) {
+                const uint2 x = w[i / kAgain][i % kAgain];
+                found |= ((x.x & kExp * 0x10001u) + kUnit * 0x10001u) | ((x.y & kExp * 0x10001u) + kUnit * 0x10001u);
+            }
             if (!(found & 0x80008000u)) continue;
 #pragma unroll
-            for (int i = 0; i < kAgain; ++i) {
+            for (int i = 0; i < kGroups * kAgain; ++i) {
+                const uint2 x = w[i / kAgain][i % kAgain];
+                const int j = j0 + i / kAgain * kStep + i % kAgain;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const uint32_t y = (c < 2 ? w[i].x : w[i].y) >> (c & 1) * 16 & 0x7FFFu;
-                    if (y >= kExp && j0 + i < end) {
-                        atomicMin((y > kExp ? nan_first : inf_first) + at + c, j0 + i);
-                        atomicMax((y > kExp ? nan_last : inf_last) + at + c, j0 + i);
+                    const uint32_t y = (c < 2 ? x.x : x.y) >> (c & 1) * 16 & 0x7FFFu;
+                    if (y >= kExp && j < end) {
+                        atomicMin((y > kExp ? nan_first : inf_first) + at + c, j);
+                        atomicMax((y > kExp ? nan_last : inf_last) + at + c, j);
                     }
                 }
             }
